@@ -63,6 +63,20 @@ enum {
 typedef enum { SPX_BF16 = 0, SPX_F32 = 1 } spx_dtype_t;
 
 /*
+ * What the K and V pools hold.
+ *   SPX_CACHE_KV_DTYPE: elements of kv_dtype.
+ *   SPX_CACHE_E4M3: one byte per element, an 8-bit float of 4 exponent and 3 mantissa bits (largest
+ *     value 448, 0x7f and 0xff NaN, no infinities), and one float32 scale for each block of
+ *     scale_block consecutive token slots of a page and kv head:
+ *       value(page, g, slot, d) = code(page, g, slot, d) * scales[(page * num_kv_heads + g) *
+ *                                 (page_size / scale_block) + slot / scale_block]
+ *     scale_block is a power of two, 1 <= scale_block <= page_size.  The pools' strides count
+ *     elements, that is bytes.  kv_dtype remains the type of everything else (queries, outputs, new
+ *     rows).
+ */
+typedef enum { SPX_CACHE_KV_DTYPE = 0, SPX_CACHE_E4M3 = 1 } spx_cache_format_t;
+
+/*
  * Attention half.  For request r with m_r = q_indptr[r+1]-q_indptr[r] = k_r+1 query rows and
  * L_r = seq_lens[r] cached tokens (the m_r new positions INCLUDED, their K/V already written),
  * query j (0 <= j < m_r), q-head h, kv-head g = h / (num_q_heads/num_kv_heads):
@@ -79,6 +93,12 @@ typedef enum { SPX_BF16 = 0, SPX_F32 = 1 } spx_dtype_t;
  * (num_q_heads/num_kv_heads)*max_q_len <= SPX_MAX_PACKED_ROWS; page_size a power of two in
  * 1..128; kv_dtype BF16 (tensor-core path; pools and strides 16-byte aligned) or F32 (true fp32
  * arithmetic).  Accumulation is fp32 in both.
+ *
+ * The pools may hold 8-bit floats with a scale per block of tokens and kv head instead
+ * (cache_format = SPX_CACHE_E4M3, see spx_cache_format_t; every combination of the above is
+ * supported).  K and V are then the scaled values, and a NaN in the V of a position reaches only the
+ * queries that see that position.  Scales are finite and not negative; those of blocks past L_r are
+ * never read.
  */
 typedef struct {
   int32_t batch;             /* B >= 0                                                        */
@@ -98,6 +118,10 @@ typedef struct {
   const int32_t *q_indptr;    /* [B+1], q_indptr[0] = 0, non-decreasing                       */
   void *out;                  /* [TQ, num_q_heads, head_dim], written                         */
   float *lse;                 /* [TQ, num_q_heads], written; may be NULL                      */
+  /* 8-bit pools; all zero: the pools hold kv_dtype                                             */
+  spx_cache_format_t cache_format;
+  int32_t scale_block;        /* E4M3: tokens per scale                                         */
+  const float *k_scales, *v_scales; /* E4M3: [num_pages, num_kv_heads, page_size/scale_block]   */
 } spx_attn_args_t;
 
 /*
@@ -211,6 +235,24 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
  * element size to be a multiple of 16 bytes and head_dim <= 512 (SPX_ERR_UNSUPPORTED otherwise); a negative, NaN or
  * infinite rope_base is SPX_ERR_INVALID_ARG.
  *
+ * q_out (optional, like q_rows; it may be q_rows itself) receives the rotated rows instead, and q_rows is then left as it is.
+ *
+ * Pools of 8-bit floats (cache_format = SPX_CACHE_E4M3, see spx_cache_format_t): a request may bring
+ * ANY number m_r >= 1 of new rows (a prompt as well as a step), in place of at most SPX_MAX_K + 1.
+ * With y the new rows' values in binary32 (K after the rotation, whose only rounding is the one from
+ * float64), every scale block that receives one of them is stored anew, the older tokens of its
+ * request in it included:
+ *   amax  = the largest finite magnitude among the block's values: the older tokens' code * scale
+ *           as they were, and the new y (slots past L_r do not count);
+ *   scale = 2^e with the smallest e for which amax <= 448 * 2^e (-126 <= e), 1 when amax is 0;
+ *   code  = the value / scale, rounded to the nearest 8-bit float (ties to even).
+ * Powers of two make the older tokens' change of scale exact, except where a larger scale pushes
+ * their last bits below the smallest subnormal.  NaNs and infinities are stored as NaN.  No slot or
+ * scale outside those blocks is touched, and slots past L_r keep their codes.  A request some of
+ * whose new positions lie on a page id out of range is skipped as a whole.  Two requests of one call
+ * may share pages, but no block that either of them writes.  Supported: head_dim 64 or 128, page_size
+ * a power of two in 1..128; kv_dtype (BF16 or F32) is the type of new_k, new_v, q_rows and q_out.
+ *
  * spx_kv_rollback computes, AFTER sampling, the lengths that drop the rejected drafts:
  * new_seq_lens[r] = seq_lens[r] - (k_r - accepted_len[r]) (position 0 and the accepted drafts
  * stay; the emitted token is the next step's position 0 and is not cached yet).  An accepted
@@ -229,12 +271,58 @@ typedef struct {
   float rope_base;                    /* 0: plain copy; > 0: rotary base (e.g. 10000, 500000) */
   int32_t num_q_heads;                /* heads of q_rows (ignored when q_rows is NULL)        */
   void *q_rows;                       /* optional, rotated in place; NULL: none               */
+  void *q_out;                        /* optional: receives the rotated q_rows instead        */
+  /* 8-bit pools; all zero: the pools hold kv_dtype                                           */
+  spx_cache_format_t cache_format;
+  int32_t scale_block;                /* E4M3: tokens per scale                               */
+  float *k_scales, *v_scales;         /* E4M3: [num_pages, num_kv_heads, page_size/scale_block], written */
 } spx_kv_append_args_t;
 
 spx_status_t spx_kv_append(const spx_kv_append_args_t *args, int32_t *dev_status, void *cuda_stream);
 spx_status_t spx_kv_rollback(int32_t batch, const int32_t *seq_lens, const int32_t *q_indptr,
                              const int32_t *accepted_len, int32_t *new_seq_lens, int32_t *dev_status,
                              void *cuda_stream);
+
+/*
+ * Log-probabilities: what a server reports beside the tokens it emits.  For every row i < rows of
+ * logits, with x_v the logits as stored, lse = log sum_v exp(x_v) and p_v = exp(x_v - lse), v < vocab:
+ *   logprobs[i]        = x_t - lse for t = token_ids[i];
+ *   entropy[i]         = -sum_v p_v log p_v (tokens of p = 0 add nothing);
+ *   top_ids[i][j], top_logprobs[i][j], j < top_n: the top_n tokens by logit, the largest first and the
+ *                        lowest id first among equal logits, and x - lse of each; with
+ *                        top_n > vocab the places past vocab hold -1 and NaN.
+ * token_ids[i] = -1 marks a row without a token (the slots of spx_rejection_sample's out_tokens
+ * behind a request's last one, whose logits rows pair with them): the row is not read and its
+ * outputs are NaN, and -1 in top_ids.  Any other id outside [0, vocab) does the same and sets
+ * SPX_DEV_BAD_TOKEN.  token_ids may be NULL (then logprobs is too, and every row counts).  Every output is optional, top_n
+ * = 0 without top_ids and top_logprobs; those two may be given singly.
+ * Rows may hold -inf (p = 0, x - lse = -inf).  A row with a NaN or a +inf, or of nothing but -inf, has
+ * NaN for its log-probabilities and its entropy; top_ids still holds the order, NaN above +inf.
+ * fp32 exponentials and in-segment sums, float64 across segments; the largest logit's own
+ * exponential, which is exactly 1, is kept out of the sums, so that a log-probability or an entropy
+ * next to 0 keeps its relative accuracy.
+ *
+ * Supported: vocab 1 .. 2^24, top_n 0 .. SPX_MAX_TOP_N; logits_row_stride >= vocab and a multiple of
+ * 8 (BF16) or 4 (F32) elements; logits 16-byte aligned.  Columns past vocab are never looked at.
+ * Workspace from spx_token_logprobs_workspace (0 = invalid arguments), 256-byte aligned, caller-owned.
+ */
+#define SPX_MAX_TOP_N 32
+typedef struct {
+  int32_t rows, vocab;
+  int64_t logits_row_stride;         /* elements                                                */
+  spx_dtype_t logits_dtype;
+  int32_t top_n;
+  const void *logits;                /* [rows, logits_row_stride]                               */
+  const int32_t *token_ids;          /* [rows]; may be NULL when logprobs is NULL               */
+  float *logprobs;                   /* optional [rows], written                                */
+  float *entropy;                    /* optional [rows], written                                */
+  int32_t *top_ids;                  /* optional [rows, top_n], written                         */
+  float *top_logprobs;               /* optional [rows, top_n], written                         */
+} spx_logprob_args_t;
+
+size_t spx_token_logprobs_workspace(const spx_logprob_args_t *args);
+spx_status_t spx_token_logprobs(const spx_logprob_args_t *args, void *workspace, size_t workspace_bytes,
+                                int32_t *dev_status, void *cuda_stream);
 
 /*
  * Selective speculation support (the paper's Section 5.1: drafted tokens are ranked by the
@@ -337,7 +425,8 @@ spx_status_t spx_lm_head(const spx_lm_head_args_t *args, int32_t *dev_status, vo
  * spx_host_step_arena_size).  Copies inputs host->device, runs spx_verify_step, copies
  * out/lse/accepted_len/out_tokens and the status word back, all on `cuda_stream`, and returns
  * after enqueueing; *dev_status_host is valid after the stream is synchronised.  `kv_pool_elems`
- * is the number of elements of each KV pool to copy.
+ * is the number of elements of each KV pool to copy (8-bit pools: bytes; their scales, which are
+ * num_pages * num_kv_heads * page_size / scale_block floats each, are copied with them).
  */
 size_t spx_host_step_arena_size(const spx_attn_args_t *attn, const spx_sample_args_t *sample,
                                 int64_t kv_pool_elems);

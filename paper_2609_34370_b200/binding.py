@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Tuple
@@ -13,13 +14,15 @@ from .build import LIB_PATH
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA = 0, 1, 2, 3, 4
 DEV_BAD_PAGE, DEV_BAD_TOKEN, DEV_BAD_LEN, DEV_TIMEOUT, DEV_DEGENERATE, DEV_BAD_PARAM = 1, 2, 4, 8, 16, 32
 BF16, F32 = 0, 1
+CACHE_KV_DTYPE, CACHE_E4M3 = 0, 1
+MAX_TOP_N = 32
 
 EXPORTS = ("spx_workspace_size", "spx_verify_attention", "spx_rejection_sample", "spx_verify_step",
            "spx_host_step_arena_size", "spx_verify_step_host", "spx_status_string", "spx_last_launch_count",
            "spx_set_timing_events", "spx_plan_layout", "spx_debug_timeline", "spx_debug_wait_expiry", "spx_rejection_sample_static", "spx_kv_append", "spx_kv_rollback",
            "spx_draft_confidence_workspace", "spx_draft_confidence", "spx_select_speculation",
            "spx_lookahead_memory", "spx_sp_effective_batch", "spx_selective_batch", "spx_selective_effective_batch",
-           "spx_delay_gain", "spx_lm_head")
+           "spx_delay_gain", "spx_lm_head", "spx_token_logprobs_workspace", "spx_token_logprobs")
 
 
 class AttnArgs(C.Structure):
@@ -32,6 +35,7 @@ class AttnArgs(C.Structure):
         ("kv_stride_page", C.c_int64), ("kv_stride_head", C.c_int64), ("kv_stride_token", C.c_int64),
         ("block_table", C.c_void_p), ("seq_lens", C.c_void_p), ("q_indptr", C.c_void_p),
         ("out", C.c_void_p), ("lse", C.c_void_p),
+        ("cache_format", C.c_int), ("scale_block", C.c_int32), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
     ]
 
 
@@ -54,7 +58,16 @@ class KvAppendArgs(C.Structure):
         ("new_k", C.c_void_p), ("new_v", C.c_void_p), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
         ("kv_stride_page", C.c_int64), ("kv_stride_head", C.c_int64), ("kv_stride_token", C.c_int64),
         ("block_table", C.c_void_p), ("seq_lens", C.c_void_p), ("q_indptr", C.c_void_p),
-        ("rope_base", C.c_float), ("num_q_heads", C.c_int32), ("q_rows", C.c_void_p),
+        ("rope_base", C.c_float), ("num_q_heads", C.c_int32), ("q_rows", C.c_void_p), ("q_out", C.c_void_p),
+        ("cache_format", C.c_int), ("scale_block", C.c_int32), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+    ]
+
+
+class LogprobArgs(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int32), ("vocab", C.c_int32), ("logits_row_stride", C.c_int64), ("logits_dtype", C.c_int),
+        ("top_n", C.c_int32), ("logits", C.c_void_p), ("token_ids", C.c_void_p),
+        ("logprobs", C.c_void_p), ("entropy", C.c_void_p), ("top_ids", C.c_void_p), ("top_logprobs", C.c_void_p),
     ]
 
 
@@ -143,6 +156,10 @@ def load_library():
         lib.spx_delay_gain.argtypes = [C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double)]
         lib.spx_lm_head.restype = C.c_int
         lib.spx_lm_head.argtypes = [C.POINTER(LmHeadArgs), C.c_void_p, C.c_void_p]
+        lib.spx_token_logprobs_workspace.restype = C.c_size_t
+        lib.spx_token_logprobs_workspace.argtypes = [C.POINTER(LogprobArgs)]
+        lib.spx_token_logprobs.restype = C.c_int
+        lib.spx_token_logprobs.argtypes = [C.POINTER(LogprobArgs), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         lib.spx_set_timing_events.restype = None
         lib.spx_set_timing_events.argtypes = [C.c_void_p, C.c_void_p]
         _lib = lib
@@ -180,8 +197,42 @@ def _require_cuda(*tensors):
             raise SpxError(ERR_INVALID_ARG, "device tensors required (there is no CPU path)")
 
 
+def _on_device_of(fn):
+    """The library launches on the current device: the call is made with its first tensor's device current."""
+    @functools.wraps(fn)
+    def call(first, *args, **kw):
+        if not isinstance(first, torch.Tensor) or first.device.type != "cuda" or first.device.index == torch.cuda.current_device():
+            return fn(first, *args, **kw)
+        with torch.cuda.device(first.device):
+            return fn(first, *args, **kw)
+    return call
+
+
+def _set_cache_scales(a, k_cache, v_cache, num_kv_heads, page_size, num_pages, k_scales, v_scales):
+    """The fields of an argument struct that describe 8-bit pools; k_scales None: the pools hold kv_dtype."""
+    if k_scales is None and v_scales is None:
+        if k_cache.element_size() == 1 or v_cache.element_size() == 1:
+            raise SpxError(ERR_INVALID_ARG, "8-bit pools need k_scales and v_scales")
+        return
+    if k_scales is None or v_scales is None:
+        raise SpxError(ERR_INVALID_ARG, "k_scales and v_scales come together")
+    for pool in (k_cache, v_cache):
+        if pool.dtype not in (torch.float8_e4m3fn, torch.uint8):
+            raise TypeError(f"pools with scales hold float8_e4m3fn (or its bytes as uint8), got {pool.dtype}")
+    per_page = k_scales.shape[-1] if k_scales.dim() == 3 else 0
+    for t in (k_scales, v_scales):
+        if t.dtype != torch.float32 or tuple(t.shape) != (num_pages, num_kv_heads, per_page) or not t.is_contiguous():
+            raise SpxError(ERR_INVALID_ARG, "scales must be contiguous float32 [num_pages, num_kv_heads, page_size / scale_block]")
+    if per_page < 1 or page_size % per_page:
+        raise SpxError(ERR_INVALID_ARG, "the scales of a page must divide its tokens")
+    a.cache_format, a.scale_block = CACHE_E4M3, page_size // per_page
+    a.k_scales, a.v_scales = _ptr(k_scales), _ptr(v_scales)
+
+
 def make_attn_args(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, num_kv_heads, page_size,
-                   num_pages, out, lse=None, sm_scale=0.0, max_q_len=0) -> AttnArgs:
+                   num_pages, out, lse=None, sm_scale=0.0, max_q_len=0, k_scales=None, v_scales=None) -> AttnArgs:
+    """``k_scales`` / ``v_scales`` ([num_pages, num_kv_heads, page_size / scale_block] float32): the pools hold
+    float8_e4m3fn, one scale per block of tokens and kv head; everything else keeps the type of ``q``."""
     TQ, Hq, D = q.shape
     a = AttnArgs()
     a.batch = seq_lens.numel()
@@ -196,6 +247,7 @@ def make_attn_args(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_ind
     a.kv_stride_page, a.kv_stride_head, a.kv_stride_token = (int(x) for x in kv_strides)
     a.block_table, a.seq_lens, a.q_indptr = _ptr(block_table), _ptr(seq_lens), q_indptr.data_ptr()
     a.out, a.lse = _ptr(out), _ptr(lse)
+    _set_cache_scales(a, k_cache, v_cache, num_kv_heads, page_size, num_pages, k_scales, v_scales)
     return a
 
 
@@ -242,18 +294,19 @@ class Workspace:
             self.buf = torch.empty(nbytes, dtype=torch.uint8, device=self.buf.device)
 
 
+@_on_device_of
 def verify_attention(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, num_kv_heads, page_size,
                      num_pages, out=None, lse=None, sm_scale=0.0, max_q_len=0, ws: Optional[Workspace] = None,
-                     want_lse=True):
-    """spx_verify_attention on the current stream.  Returns (out, lse, ws)."""
-    _require_cuda(q, k_cache, v_cache, block_table, seq_lens, q_indptr)
+                     want_lse=True, k_scales=None, v_scales=None):
+    """spx_verify_attention on the current stream.  Returns (out, lse, ws).  8-bit pools: see make_attn_args."""
+    _require_cuda(q, k_cache, v_cache, block_table, seq_lens, q_indptr, k_scales, v_scales)
     lib = load_library()
     if out is None:
         out = torch.empty_like(q)
     if lse is None and want_lse:
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
     a = make_attn_args(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, num_kv_heads, page_size,
-                       num_pages, out, lse, sm_scale, max_q_len)
+                       num_pages, out, lse, sm_scale, max_q_len, k_scales, v_scales)
     need = workspace_size(a, None)
     if ws is None:
         ws = Workspace.allocate(need, q.device)
@@ -378,11 +431,16 @@ def rejection_sample_static(target_logits, draft_logits, draft_ids, q_indptr, u_
     return accepted, tokens, status
 
 
+@_on_device_of
 def kv_append(new_k, new_v, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, page_size, num_pages,
-              status: Optional[torch.Tensor] = None, rope_base: float = 0.0, q_rows: Optional[torch.Tensor] = None):
+              status: Optional[torch.Tensor] = None, rope_base: float = 0.0, q_rows: Optional[torch.Tensor] = None,
+              k_scales=None, v_scales=None, q_out: Optional[torch.Tensor] = None):
     """spx_kv_append on the current stream: the new positions' K/V go into their pages, in place.
-    rope_base > 0: the K rows (and q_rows [TQ, Hq, D], in place) are rotated to their positions."""
-    _require_cuda(new_k, new_v, k_cache, v_cache, block_table, seq_lens, q_indptr)
+    rope_base > 0: the K rows (and q_rows [TQ, Hq, D], in place or into ``q_out``) are rotated to their positions.
+    With ``k_scales`` / ``v_scales`` ([num_pages, Hkv, page_size / scale_block] float32) the pools hold
+    float8_e4m3fn: rows are quantised on the way, the touched blocks' scales are written, and a request may
+    bring any number of rows."""
+    _require_cuda(new_k, new_v, k_cache, v_cache, block_table, seq_lens, q_indptr, k_scales, v_scales)
     lib = load_library()
     dev = new_k.device
     if status is None:
@@ -401,6 +459,17 @@ def kv_append(new_k, new_v, k_cache, v_cache, kv_strides, block_table, seq_lens,
         if q_rows.dtype != new_k.dtype or not q_rows.is_contiguous():
             raise SpxError(ERR_INVALID_ARG, "q_rows must be contiguous and of the cache's dtype")
         a.num_q_heads, a.q_rows = q_rows.shape[1], _ptr(q_rows)
+        if q_out is not None:
+            _require_cuda(q_out)
+            if q_out.dtype != q_rows.dtype or q_out.shape != q_rows.shape or not q_out.is_contiguous():
+                raise SpxError(ERR_INVALID_ARG, "q_out must be contiguous and like q_rows")
+            a.q_out = _ptr(q_out)
+    elif q_out is not None:
+        raise SpxError(ERR_INVALID_ARG, "q_out needs q_rows")
+    _set_cache_scales(a, k_cache, v_cache, new_k.shape[1], page_size, num_pages, k_scales, v_scales)
+    if a.cache_format == CACHE_E4M3 and (new_v.dtype != new_k.dtype or new_v.shape != new_k.shape or
+                                         not new_k.is_contiguous() or not new_v.is_contiguous()):
+        raise SpxError(ERR_INVALID_ARG, "new_k and new_v must be contiguous and alike")
     _check(lib.spx_kv_append(C.byref(a), status.data_ptr(), _stream(dev)))
     return status
 
@@ -445,6 +514,68 @@ def draft_confidence(draft_logits, draft_ids, q_indptr, vocab=None, want_token_c
     ws.ensure(need)
     _check(lib.spx_draft_confidence(C.byref(a), ws.buf.data_ptr(), ws.buf.numel(), ws.status.data_ptr(), _stream(dev)))
     return conf_max, conf_tok, req_conf, ws
+
+
+def _check_output(t, shape, dtype, what):
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise SpxError(ERR_INVALID_ARG, f"{what} must be contiguous {dtype} {list(shape)}")
+    _require_cuda(t)
+
+
+@_on_device_of
+def token_logprobs(logits, token_ids=None, top_n: int = 0, vocab=None, want_entropy=True, logprobs=None, entropy=None,
+                   top_ids=None, top_logprobs=None, ws: Optional[Workspace] = None):
+    """spx_token_logprobs on the current stream: log-probabilities of ``token_ids`` ([rows] int32, -1 = no token),
+    the rows' entropies and the ``top_n`` alternatives.  Returns (logprobs or None, entropy or None, top_ids or None,
+    top_logprobs or None, ws); outputs the caller brings are written in place."""
+    _require_cuda(logits, token_ids)
+    lib = load_library()
+    dev = logits.device
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise SpxError(ERR_INVALID_ARG, "logits must be two-dimensional with contiguous rows")
+    rows = logits.shape[0]
+    a = LogprobArgs()
+    a.rows, a.vocab, a.top_n = rows, int(vocab if vocab is not None else logits.shape[1]), int(top_n)
+    if a.vocab > logits.shape[1]:
+        raise SpxError(ERR_INVALID_ARG, "vocab exceeds the logits' columns")
+    a.logits_row_stride = logits.stride(0) if rows > 1 else -(-a.vocab // 8) * 8
+    a.logits_dtype, a.logits = _dtype_code(logits), _ptr(logits)
+    if token_ids is not None:
+        if token_ids.dtype != torch.int32 or token_ids.numel() != rows or not token_ids.is_contiguous():
+            raise SpxError(ERR_INVALID_ARG, "token_ids must be contiguous int32 [rows]")
+        a.token_ids = _ptr(token_ids)
+        if logprobs is None:
+            logprobs = torch.empty(rows, dtype=torch.float32, device=dev)
+    elif logprobs is not None:
+        raise SpxError(ERR_INVALID_ARG, "logprobs needs token_ids")
+    if entropy is None and want_entropy:
+        entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    if not 0 <= a.top_n <= MAX_TOP_N:
+        raise SpxError(ERR_UNSUPPORTED, f"top_n must be in 0..{MAX_TOP_N}")
+    if a.top_n > 0:
+        if top_ids is None:
+            top_ids = torch.empty((rows, a.top_n), dtype=torch.int32, device=dev)
+        if top_logprobs is None:
+            top_logprobs = torch.empty((rows, a.top_n), dtype=torch.float32, device=dev)
+        _check_output(top_ids, (rows, a.top_n), torch.int32, "top_ids")
+        _check_output(top_logprobs, (rows, a.top_n), torch.float32, "top_logprobs")
+        a.top_ids, a.top_logprobs = _ptr(top_ids), _ptr(top_logprobs)
+    elif top_ids is not None or top_logprobs is not None:
+        raise SpxError(ERR_INVALID_ARG, "top_ids and top_logprobs need top_n > 0")
+    if logprobs is not None:
+        _check_output(logprobs, (rows,), torch.float32, "logprobs")
+        a.logprobs = _ptr(logprobs)
+    if entropy is not None:
+        _check_output(entropy, (rows,), torch.float32, "entropy")
+        a.entropy = _ptr(entropy)
+    need = int(lib.spx_token_logprobs_workspace(C.byref(a)))
+    if need == 0:
+        raise SpxError(ERR_INVALID_ARG, "invalid arguments for workspace sizing")
+    if ws is None:
+        ws = Workspace.allocate(need, dev)
+    ws.ensure(need)
+    _check(lib.spx_token_logprobs(C.byref(a), ws.buf.data_ptr(), ws.buf.numel(), ws.status.data_ptr(), _stream(dev)))
+    return logprobs, entropy, top_ids, top_logprobs, ws
 
 
 def select_speculation(confidence, k_in, alpha: float, out: Optional[torch.Tensor] = None,

@@ -1,6 +1,7 @@
 // Shared device helpers for the verify-step kernels (sm_100a).
 #pragma once
 #include <cuda_bf16.h>
+#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -59,6 +60,11 @@ __device__ __forceinline__ float ld_as_float(const __nv_bfloat16 *p, int64_t i) 
 
 __device__ __forceinline__ void st_from_float(float *p, int64_t i, float v) { p[i] = v; }
 __device__ __forceinline__ void st_from_float(__nv_bfloat16 *p, int64_t i, float v) { p[i] = __float2bfloat16_rn(v); }
+
+// The value of one 8-bit float (4 exponent bits, 3 mantissa bits): exact.
+__device__ __forceinline__ float e4m3_to_float(unsigned char c) {
+  return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3)));
+}
 
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;
@@ -153,6 +159,9 @@ struct AttnParams {
   float2 *part_ml;         // [slot][rows_cap]  (m in log2 domain, l)
   int32_t rows_cap;        // G * max_q_len
   int32_t q_box_rows;      // query positions one Q box of the tensor-core kernel fetches (<= max_q_len)
+  // 8-bit pools: tokens per scale = 1 << log2SB, scales [page, head, P >> log2SB]
+  const float *k_scales, *v_scales;
+  int32_t log2SB;
   int32_t *dev_status;
   long long *prof;         // optional per-CTA cycle counters (profiling builds only), else NULL
 };

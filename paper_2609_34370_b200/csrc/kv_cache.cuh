@@ -15,7 +15,8 @@ struct KvAppendParams {
   const int32_t *block_table, *seq_lens, *q_indptr;
   int32_t *dev_status;
   double rope_base;        // 0: plain copy; > 0: K rows (and q_rows) are rotated to their positions
-  unsigned char *q_rows;   // optional [TQ, Hq, D], rotated in place
+  unsigned char *q_rows;   // optional [TQ, Hq, D], rotated into q_out (in place when the two are one)
+  unsigned char *q_out;
   int32_t Hq;
 };
 
@@ -108,14 +109,16 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendParams p) {
       for (int i = threadIdx.x; i < n_q; i += blockDim.x) {
         const int v = i % half_vecs, jh = i / half_vecs, h = jh % p.Hq, j = jh / p.Hq;
         const int t = L - m + j;
-        unsigned char *row = p.q_rows + (((int64_t)(q0 + j) * p.Hq + h) * p.D) * p.elem_size + (int64_t)v * 16;
+        const int64_t at = (((int64_t)(q0 + j) * p.Hq + h) * p.D) * p.elem_size + (int64_t)v * 16;
+        const unsigned char *row = p.q_rows + at;
+        unsigned char *dst = p.q_out + at;
         const int64_t half_bytes = (int64_t)(p.D >> 1) * p.elem_size;
         uint4 lo = *reinterpret_cast<const uint4 *>(row);
         uint4 hi = *reinterpret_cast<const uint4 *>(row + half_bytes);
         if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(lo, hi, v * elems_per_vec, t, s_inv_freq);
         else rope_vectors<float>(lo, hi, v * elems_per_vec, t, s_inv_freq);
-        *reinterpret_cast<uint4 *>(row) = lo;
-        *reinterpret_cast<uint4 *>(row + half_bytes) = hi;
+        *reinterpret_cast<uint4 *>(dst) = lo;
+        *reinterpret_cast<uint4 *>(dst + half_bytes) = hi;
       }
     }
     return;

@@ -12,6 +12,8 @@
 #include "attn_tc4.cuh"
 #include "common.cuh"
 #include "kv_cache.cuh"
+#include "kv_cache_e4m3.cuh"
+#include "logprob.cuh"
 #include "select.cuh"
 #include "lookahead.cuh"
 #include "lm_head.cuh"
@@ -96,6 +98,26 @@ struct AttnWs {
   int32_t max_work, max_part_slots, rows_cap;
 };
 
+static int cache_elem_size(const spx_attn_args_t *a) {
+  return a->cache_format == SPX_CACHE_E4M3 ? 1 : a->kv_dtype == SPX_BF16 ? 2 : 4;
+}
+
+// The fields that describe 8-bit pools, shared by the attention and the append.
+static spx_status_t check_cache_format(spx_cache_format_t format, int32_t scale_block, int32_t page_size) {
+  if (format == SPX_CACHE_KV_DTYPE) return SPX_OK;
+  if (format != SPX_CACHE_E4M3 || scale_block <= 0) return SPX_ERR_INVALID_ARG;
+  if ((scale_block & (scale_block - 1)) != 0 || scale_block > page_size) return SPX_ERR_UNSUPPORTED;
+  return SPX_OK;
+}
+static bool scales_ok(const float *k_scales, const float *v_scales) {
+  return k_scales && v_scales && (((uintptr_t)k_scales | (uintptr_t)v_scales) & 3) == 0;
+}
+static int log2_of(int x) {
+  int n = 0;
+  while ((1 << n) < x) ++n;
+  return n;
+}
+
 static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs) {
   if (!a) return SPX_ERR_INVALID_ARG;
   if (a->batch < 0 || a->total_q < a->batch || a->num_q_heads <= 0 || a->num_kv_heads <= 0 || a->head_dim <= 0 ||
@@ -110,10 +132,13 @@ static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs) {
   if (max_q > SPX_MAX_K + 1) return SPX_ERR_UNSUPPORTED;
   if ((a->num_q_heads / a->num_kv_heads) * max_q > SPX_MAX_PACKED_ROWS) return SPX_ERR_UNSUPPORTED;
   if (a->kv_stride_page < 0 || a->kv_stride_head < 0 || a->kv_stride_token < a->head_dim) return SPX_ERR_INVALID_ARG;
+  const spx_status_t cf = check_cache_format(a->cache_format, a->scale_block, a->page_size);
+  if (cf != SPX_OK) return cf;
   if (need_ptrs && a->batch > 0) {
     if (!a->q || !a->k_cache || !a->v_cache || !a->block_table || !a->seq_lens || !a->q_indptr || !a->out)
       return SPX_ERR_INVALID_ARG;
-    const int es = a->kv_dtype == SPX_BF16 ? 2 : 4;
+    if (a->cache_format == SPX_CACHE_E4M3 && !scales_ok(a->k_scales, a->v_scales)) return SPX_ERR_INVALID_ARG;
+    const int es = cache_elem_size(a);
     if (((uintptr_t)a->q | (uintptr_t)a->k_cache | (uintptr_t)a->v_cache | (uintptr_t)a->out) & 15) return SPX_ERR_INVALID_ARG;
     if (((a->kv_stride_page * es) | (a->kv_stride_head * es) | (a->kv_stride_token * es)) & 15) return SPX_ERR_INVALID_ARG;
   }
@@ -253,7 +278,7 @@ static bool make_q_map(CUtensorMap *map, const spx_attn_args_t *a, int rows) {
 
 // The tensor-core kernel handles bf16 pools whose pages hold at least one 8-row swizzle atom.
 static bool use_tensor_core_path(const spx_attn_args_t *a) {
-  return a->kv_dtype == SPX_BF16 && a->page_size >= 8 && a->num_pages > 0 && a->kv_stride_page > 0 &&
+  return a->kv_dtype == SPX_BF16 && a->cache_format == SPX_CACHE_KV_DTYPE && a->page_size >= 8 && a->num_pages > 0 && a->kv_stride_page > 0 &&
          a->kv_stride_head > 0;
 }
 
@@ -341,6 +366,10 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
   p.part_ml = reinterpret_cast<float2 *>(ws + w.part_ml);
   p.part_o = reinterpret_cast<float *>(ws + w.part_o);
   p.rows_cap = w.rows_cap;
+  if (a->cache_format == SPX_CACHE_E4M3) {
+    p.k_scales = a->k_scales; p.v_scales = a->v_scales;
+    p.log2SB = log2_of(a->scale_block);
+  }
   p.dev_status = dev_status;
   p.prof = t_prof;
 
@@ -386,7 +415,12 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
       ++t_launches;
       return cudaGetLastError();
     };
-    if (a->kv_dtype == SPX_F32)
+    if (a->cache_format == SPX_CACHE_E4M3) {
+      if (a->kv_dtype == SPX_F32)
+        e = p.D == 64 ? launch_simt(attn_simt_kernel<float, 64, true>) : launch_simt(attn_simt_kernel<float, 128, true>);
+      else
+        e = p.D == 64 ? launch_simt(attn_simt_kernel<__nv_bfloat16, 64, true>) : launch_simt(attn_simt_kernel<__nv_bfloat16, 128, true>);
+    } else if (a->kv_dtype == SPX_F32)
       e = p.D == 64 ? launch_simt(attn_simt_kernel<float, 64>) : launch_simt(attn_simt_kernel<float, 128>);
     else
       e = p.D == 64 ? launch_simt(attn_simt_kernel<__nv_bfloat16, 64>) : launch_simt(attn_simt_kernel<__nv_bfloat16, 128>);
@@ -620,15 +654,16 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
 // ---- host-buffer convenience ---------------------------------------------------------------
 namespace {
 struct HostStepLayout {
-  size_t q, k, v, bt, sl, qi, out, lse, tl, dl, ids, ua, us, tau, topk, topp, acc, tok, status, ws, total;
-  size_t q_bytes, kv_bytes, bt_bytes, out_bytes, lse_bytes, tl_bytes, dl_bytes, ws_bytes;
+  size_t q, k, v, ks, vs, bt, sl, qi, out, lse, tl, dl, ids, ua, us, tau, topk, topp, acc, tok, status, ws, total;
+  size_t q_bytes, kv_bytes, scale_bytes, bt_bytes, out_bytes, lse_bytes, tl_bytes, dl_bytes, ws_bytes;
 };
 HostStepLayout host_layout(const spx_attn_args_t *a, const spx_sample_args_t *s, int64_t kv_pool_elems) {
   HostStepLayout L{};
   const size_t es = a->kv_dtype == SPX_BF16 ? 2 : 4, ls = s->logits_dtype == SPX_BF16 ? 2 : 4;
   const size_t B = a->batch, TQ = a->total_q, TD = TQ - B;
   L.q_bytes = TQ * a->num_q_heads * a->head_dim * es;
-  L.kv_bytes = (size_t)kv_pool_elems * es;
+  L.kv_bytes = (size_t)kv_pool_elems * cache_elem_size(a);
+  L.scale_bytes = a->cache_format == SPX_CACHE_E4M3 ? (size_t)a->num_pages * a->num_kv_heads * (a->page_size / a->scale_block) * 4 : 0;
   L.bt_bytes = B * (size_t)a->max_pages_per_req * 4;
   L.out_bytes = L.q_bytes;
   L.lse_bytes = TQ * a->num_q_heads * 4;
@@ -637,7 +672,8 @@ HostStepLayout host_layout(const spx_attn_args_t *a, const spx_sample_args_t *s,
   L.ws_bytes = spx_workspace_size(a, s);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
-  L.q = take(L.q_bytes); L.k = take(L.kv_bytes); L.v = take(L.kv_bytes); L.bt = take(L.bt_bytes);
+  L.q = take(L.q_bytes); L.k = take(L.kv_bytes); L.v = take(L.kv_bytes);
+  L.ks = take(L.scale_bytes); L.vs = take(L.scale_bytes); L.bt = take(L.bt_bytes);
   L.sl = take(B * 4); L.qi = take((B + 1) * 4); L.out = take(L.out_bytes); L.lse = take(L.lse_bytes);
   L.tl = take(L.tl_bytes); L.dl = take(L.dl_bytes); L.ids = take(TD * 4); L.ua = take(TD * 4); L.us = take(B * 4);
   L.tau = take(s->temperature ? B * 4 : 0); L.topk = take(s->top_k ? B * 4 : 0); L.topp = take(s->top_p ? B * 4 : 0);
@@ -672,6 +708,7 @@ spx_status_t spx_verify_step_host(const spx_attn_args_t *attn, const spx_sample_
     if (bytes && dst) ok = ok && cudaMemcpyAsync(dst, d + off, bytes, cudaMemcpyDeviceToHost, stream) == cudaSuccess;
   };
   h2d(L.q, attn->q, L.q_bytes); h2d(L.k, attn->k_cache, L.kv_bytes); h2d(L.v, attn->v_cache, L.kv_bytes);
+  h2d(L.ks, attn->k_scales, L.scale_bytes); h2d(L.vs, attn->v_scales, L.scale_bytes);
   h2d(L.bt, attn->block_table, L.bt_bytes); h2d(L.sl, attn->seq_lens, B * 4); h2d(L.qi, attn->q_indptr, (B + 1) * 4);
   h2d(L.tl, sample->target_logits, L.tl_bytes); h2d(L.dl, sample->draft_logits, L.dl_bytes);
   h2d(L.ids, sample->draft_token_ids, TD * 4); h2d(L.ua, sample->u_accept, TD * 4); h2d(L.us, sample->u_sample, B * 4);
@@ -681,6 +718,8 @@ spx_status_t spx_verify_step_host(const spx_attn_args_t *attn, const spx_sample_
   spx_attn_args_t a = *attn;
   spx_sample_args_t s = *sample;
   a.q = d + L.q; a.k_cache = d + L.k; a.v_cache = d + L.v;
+  a.k_scales = attn->k_scales ? reinterpret_cast<float *>(d + L.ks) : nullptr;
+  a.v_scales = attn->v_scales ? reinterpret_cast<float *>(d + L.vs) : nullptr;
   a.block_table = reinterpret_cast<int32_t *>(d + L.bt); a.seq_lens = reinterpret_cast<int32_t *>(d + L.sl);
   a.q_indptr = reinterpret_cast<int32_t *>(d + L.qi); a.out = d + L.out;
   a.lse = attn->lse ? reinterpret_cast<float *>(d + L.lse) : nullptr;
@@ -700,6 +739,45 @@ spx_status_t spx_verify_step_host(const spx_attn_args_t *attn, const spx_sample_
 }
 
 // ---- cache maintenance ------------------------------------------------------------------------
+static spx_status_t launch_append_e4m3(const spx_kv_append_args_t *a, int32_t *dev_status, cudaStream_t stream) {
+  if (!scales_ok(a->k_scales, a->v_scales)) return SPX_ERR_INVALID_ARG;
+  DeviceInfo dev;
+  if (!get_device_info(&dev)) return SPX_ERR_CUDA;
+  KvQuantParams p{};
+  p.batch = a->batch; p.total_q = a->total_q; p.Hkv = a->num_kv_heads; p.Hq = a->num_q_heads;
+  p.log2P = log2_of(a->page_size); p.log2SB = log2_of(a->scale_block);
+  p.num_pages = a->num_pages; p.max_pages_per_req = a->max_pages_per_req;
+  p.new_k = a->new_k; p.new_v = a->new_v; p.k_cache = static_cast<unsigned char *>(a->k_cache); p.v_cache = static_cast<unsigned char *>(a->v_cache);
+  p.stride_page = a->kv_stride_page; p.stride_head = a->kv_stride_head; p.stride_token = a->kv_stride_token;
+  p.k_scales = a->k_scales; p.v_scales = a->v_scales;
+  p.block_table = a->block_table; p.seq_lens = a->seq_lens; p.q_indptr = a->q_indptr; p.dev_status = dev_status;
+  p.rope = a->rope_base > 0.f;
+  p.q_in = p.rope ? a->q_rows : nullptr;
+  p.q_out = a->q_out ? a->q_out : a->q_rows;
+  if (p.rope)
+    for (int i = 0; i < a->head_dim / 2; ++i) p.inv_freq[i] = std::pow((double)a->rope_base, -2.0 * i / a->head_dim);
+  const int warp_tokens = a->head_dim == 128 ? QuantShape<128>::kWarpTokens : QuantShape<64>::kWarpTokens;
+  p.task_warps = a->head_dim == 128 ? QuantShape<128>::task_warps(a->scale_block) : QuantShape<64>::task_warps(a->scale_block);
+  const int tile = warp_tokens * p.task_warps;
+  p.log2_tile = log2_of(tile);
+  const int64_t tiles = (int64_t)a->total_q / tile + 2 * (int64_t)a->batch;
+  if (tiles > 0x7fffffff) return SPX_ERR_UNSUPPORTED;
+  // the tasks of a tile are split over blocks until there are about four blocks per SM
+  const int slots = kQuantWarps / p.task_warps, tasks = 2 * p.Hkv + (p.q_in ? p.Hq : 0);
+  int64_t splits = (4 * (int64_t)dev.num_sms + tiles - 1) / tiles;
+  if (splits > (tasks + slots - 1) / slots) splits = (tasks + slots - 1) / slots;
+  const int smem = p.rope ? tile * (a->head_dim / 2) * (int)sizeof(double2) : 0;
+  auto launch = [&](auto kernel) -> spx_status_t {
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPX_ERR_CUDA;
+    kernel<<<dim3((unsigned)tiles, (unsigned)splits), kQuantThreads, smem, stream>>>(p);
+    ++t_launches;
+    return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
+  };
+  if (a->kv_dtype == SPX_F32)
+    return a->head_dim == 64 ? launch(kv_append_e4m3_kernel<float, 64>) : launch(kv_append_e4m3_kernel<float, 128>);
+  return a->head_dim == 64 ? launch(kv_append_e4m3_kernel<__nv_bfloat16, 64>) : launch(kv_append_e4m3_kernel<__nv_bfloat16, 128>);
+}
+
 spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, void *cuda_stream) {
   t_launches = 0;
   if (!a || !dev_status) return SPX_ERR_INVALID_ARG;
@@ -708,19 +786,24 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
     return SPX_ERR_INVALID_ARG;
   if (a->kv_dtype != SPX_BF16 && a->kv_dtype != SPX_F32) return SPX_ERR_INVALID_ARG;
   if ((a->page_size & (a->page_size - 1)) != 0) return SPX_ERR_UNSUPPORTED;
-  const int es = a->kv_dtype == SPX_BF16 ? 2 : 4;
+  const spx_status_t cf = check_cache_format(a->cache_format, a->scale_block, a->page_size);
+  if (cf != SPX_OK) return cf;
+  const bool e4m3 = a->cache_format == SPX_CACHE_E4M3;
+  const int es = a->kv_dtype == SPX_BF16 ? 2 : 4, cache_es = e4m3 ? 1 : es;   // rows, pools
   if ((a->head_dim * es) % 16 != 0) return SPX_ERR_UNSUPPORTED;
   if (a->kv_stride_page < 0 || a->kv_stride_head < 0 || a->kv_stride_token < a->head_dim) return SPX_ERR_INVALID_ARG;
   if (!(a->rope_base >= 0.f) || std::isinf(a->rope_base)) return SPX_ERR_INVALID_ARG;
   const bool rope = a->rope_base > 0.f;
   if (rope && ((a->head_dim & 1) || ((a->head_dim / 2) * es) % 16 != 0 || a->head_dim > kRopeMaxHeadDim)) return SPX_ERR_UNSUPPORTED;
   if (rope && a->q_rows && a->num_q_heads <= 0) return SPX_ERR_INVALID_ARG;
+  if (e4m3 && (a->page_size > 128 || (a->head_dim != 64 && a->head_dim != 128))) return SPX_ERR_UNSUPPORTED;
   if (a->batch == 0) return SPX_OK;
   if (!a->new_k || !a->new_v || !a->k_cache || !a->v_cache || !a->block_table || !a->seq_lens || !a->q_indptr)
     return SPX_ERR_INVALID_ARG;
   if (((uintptr_t)a->new_k | (uintptr_t)a->new_v | (uintptr_t)a->k_cache | (uintptr_t)a->v_cache) & 15) return SPX_ERR_INVALID_ARG;
-  if (rope && ((uintptr_t)a->q_rows & 15)) return SPX_ERR_INVALID_ARG;
-  if (((a->kv_stride_page * es) | (a->kv_stride_head * es) | (a->kv_stride_token * es)) & 15) return SPX_ERR_INVALID_ARG;
+  if (rope && (((uintptr_t)a->q_rows | (uintptr_t)a->q_out) & 15)) return SPX_ERR_INVALID_ARG;
+  if (((a->kv_stride_page * cache_es) | (a->kv_stride_head * cache_es) | (a->kv_stride_token * cache_es)) & 15) return SPX_ERR_INVALID_ARG;
+  if (e4m3) return launch_append_e4m3(a, dev_status, static_cast<cudaStream_t>(cuda_stream));
   KvAppendParams p{};
   p.batch = a->batch; p.total_q = a->total_q; p.Hkv = a->num_kv_heads; p.D = a->head_dim; p.P = a->page_size;
   while ((1 << p.log2P) < p.P) ++p.log2P;
@@ -731,6 +814,7 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
   p.block_table = a->block_table; p.seq_lens = a->seq_lens; p.q_indptr = a->q_indptr; p.dev_status = dev_status;
   p.rope_base = rope ? (double)a->rope_base : 0.0;
   p.q_rows = rope ? static_cast<unsigned char *>(a->q_rows) : nullptr;
+  p.q_out = a->q_out ? static_cast<unsigned char *>(a->q_out) : p.q_rows;
   p.Hq = a->num_q_heads;
   kv_append_kernel<<<a->batch, 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
   ++t_launches;
@@ -745,6 +829,46 @@ spx_status_t spx_kv_rollback(int32_t batch, const int32_t *seq_lens, const int32
   if (!seq_lens || !q_indptr || !accepted_len || !new_seq_lens) return SPX_ERR_INVALID_ARG;
   kv_rollback_kernel<<<(batch + 127) / 128, 128, 0, static_cast<cudaStream_t>(cuda_stream)>>>(batch, seq_lens, q_indptr,
                                                                                                accepted_len, new_seq_lens, dev_status);
+  ++t_launches;
+  return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
+}
+
+// ---- log-probabilities --------------------------------------------------------------------------
+static spx_status_t check_logprobs(const spx_logprob_args_t *a, bool need_ptrs) {
+  if (!a) return SPX_ERR_INVALID_ARG;
+  if (a->rows < 0 || a->vocab <= 0 || a->logits_row_stride < a->vocab || a->top_n < 0) return SPX_ERR_INVALID_ARG;
+  if (a->logits_dtype != SPX_BF16 && a->logits_dtype != SPX_F32) return SPX_ERR_INVALID_ARG;
+  if (a->logits_row_stride % (a->logits_dtype == SPX_BF16 ? 8 : 4) != 0) return SPX_ERR_INVALID_ARG;
+  if (a->vocab > (1 << 24) || a->top_n > SPX_MAX_TOP_N) return SPX_ERR_UNSUPPORTED;
+  if (need_ptrs && a->rows > 0) {
+    if (!a->logits || ((uintptr_t)a->logits & 15)) return SPX_ERR_INVALID_ARG;
+    if (a->logprobs && !a->token_ids) return SPX_ERR_INVALID_ARG;
+    if (a->top_n == 0 && (a->top_ids || a->top_logprobs)) return SPX_ERR_INVALID_ARG;
+  }
+  return SPX_OK;
+}
+
+size_t spx_token_logprobs_workspace(const spx_logprob_args_t *a) {
+  if (check_logprobs(a, false) != SPX_OK) return 0;
+  return 256;
+}
+
+spx_status_t spx_token_logprobs(const spx_logprob_args_t *a, void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                void *cuda_stream) {
+  t_launches = 0;
+  const spx_status_t st = check_logprobs(a, true);
+  if (st != SPX_OK) return st;
+  if (!dev_status) return SPX_ERR_INVALID_ARG;
+  if (a->rows == 0) return SPX_OK;
+  const size_t need = spx_token_logprobs_workspace(a);
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPX_ERR_WORKSPACE;
+  LogprobParams p{};
+  p.rows = a->rows; p.vocab = a->vocab; p.top_n = a->top_n; p.row_stride = a->logits_row_stride;
+  p.logits = a->logits; p.token_ids = a->token_ids;
+  p.logprobs = a->logprobs; p.entropy = a->entropy; p.top_ids = a->top_ids; p.top_logprobs = a->top_logprobs;
+  p.dev_status = dev_status;
+  if (a->logits_dtype == SPX_BF16) logprob_kernel<__nv_bfloat16><<<a->rows, kLogprobThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+  else logprob_kernel<float><<<a->rows, kLogprobThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
   ++t_launches;
   return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
 }
