@@ -7,6 +7,7 @@
 #include <mutex>
 #include <type_traits>
 
+#include "attn_e4m3.cuh"
 #include "attn_simt.cuh"
 #include "attn_tc.cuh"
 #include "attn_tc4.cuh"
@@ -261,6 +262,21 @@ static bool make_pool_map(CUtensorMap *map, const void *pool, const spx_attn_arg
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 4-D byte view of an 8-bit pool, dims ordered as above; one box = one page x one kv-head, rows of
+// head_dim bytes swizzled over their own length.
+static bool make_pool_map_e4m3(CUtensorMap *map, const void *pool, const spx_attn_args_t *a, bool head_inner) {
+  EncodeTiledFn encode = get_encode_fn();
+  if (!encode) return false;
+  const cuuint64_t D = a->head_dim, P = a->page_size, H = a->num_kv_heads, N = a->num_pages;
+  const cuuint64_t st = a->kv_stride_token, sh = a->kv_stride_head, sp = a->kv_stride_page;
+  const cuuint64_t dims[4] = {D, head_inner ? H : P, head_inner ? P : H, N};
+  const cuuint64_t strides[3] = {head_inner ? sh : st, head_inner ? st : sh, sp};
+  const cuuint32_t box[4] = {(cuuint32_t)D, head_inner ? 1 : (cuuint32_t)P, head_inner ? (cuuint32_t)P : 1, 1}, estr[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // 3-D bf16 view of the query rows [TQ, Hq, D]: one box = 64 columns x the G heads of one kv-head x
 // `rows` consecutive query positions, which lands in shared memory as the packed rows j*G + h of a
 // work entry, 128 bytes each, 128-byte swizzle: the K-major A operand of the score MMA.
@@ -276,9 +292,9 @@ static bool make_q_map(CUtensorMap *map, const spx_attn_args_t *a, int rows) {
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The tensor-core kernel handles bf16 pools whose pages hold at least one 8-row swizzle atom.
+// The tensor-core kernels handle bf16 queries over pools whose pages hold at least one 8-row swizzle atom.
 static bool use_tensor_core_path(const spx_attn_args_t *a) {
-  return a->kv_dtype == SPX_BF16 && a->cache_format == SPX_CACHE_KV_DTYPE && a->page_size >= 8 && a->num_pages > 0 && a->kv_stride_page > 0 &&
+  return a->kv_dtype == SPX_BF16 && a->page_size >= 8 && a->num_pages > 0 && a->kv_stride_page > 0 &&
          a->kv_stride_head > 0;
 }
 
@@ -323,6 +339,19 @@ static cudaError_t launch_tc(const CUtensorMap &kmap, const CUtensorMap &vmap, c
   // CTAs only take registers away from the sampling kernels that run beside them.)
   if (t_ev_start) cudaEventRecord(t_ev_start, stream);
   kernel<<<num_sms, kTcThreads, Cfg::kSmemBytes, stream>>>(kmap, vmap, p);
+  if (t_ev_stop) cudaEventRecord(t_ev_stop, stream);
+  ++t_launches;
+  return cudaGetLastError();
+}
+
+template <int D, int MROWS>
+static cudaError_t launch_e4m3(const CUtensorMap &kmap, const CUtensorMap &vmap, const AttnParams &p, int num_sms, cudaStream_t stream) {
+  using Cfg = E8Cfg<D, MROWS>;
+  auto kernel = attn_e4m3_kernel<D, MROWS>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  if (t_ev_start) cudaEventRecord(t_ev_start, stream);
+  kernel<<<num_sms, kE8Threads, Cfg::kSmemBytes, stream>>>(kmap, vmap, p);
   if (t_ev_stop) cudaEventRecord(t_ev_stop, stream);
   ++t_launches;
   return cudaGetLastError();
@@ -386,9 +415,17 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
   if (use_tensor_core_path(a)) {
     p.head_inner = a->kv_stride_head < a->kv_stride_token ? 1 : 0;
     CUtensorMap kmap, vmap;
-    if (!make_pool_map(&kmap, a->k_cache, a, p.head_inner) || !make_pool_map(&vmap, a->v_cache, a, p.head_inner))
+    if (a->cache_format == SPX_CACHE_E4M3) {
+      if (!make_pool_map_e4m3(&kmap, a->k_cache, a, p.head_inner) || !make_pool_map_e4m3(&vmap, a->v_cache, a, p.head_inner)) return SPX_ERR_CUDA;
+      if (p.rows_cap <= 32)
+        e = p.D == 128 ? launch_e4m3<128, 32>(kmap, vmap, p, sms, stream) : launch_e4m3<64, 32>(kmap, vmap, p, sms, stream);
+      else if (p.rows_cap <= 64)
+        e = p.D == 128 ? launch_e4m3<128, 64>(kmap, vmap, p, sms, stream) : launch_e4m3<64, 64>(kmap, vmap, p, sms, stream);
+      else
+        e = p.D == 128 ? launch_e4m3<128, 128>(kmap, vmap, p, sms, stream) : launch_e4m3<64, 128>(kmap, vmap, p, sms, stream);
+    } else if (!make_pool_map(&kmap, a->k_cache, a, p.head_inner) || !make_pool_map(&vmap, a->v_cache, a, p.head_inner))
       return SPX_ERR_CUDA;
-    if (p.rows_cap <= 64) {
+    else if (p.rows_cap <= 64) {
       // the packed query rows of a work entry arrive by one box pair of a 3-D map over Q
       CUtensorMap qmap;
       p.q_box_rows = p.max_q_len < p.total_q ? p.max_q_len : p.total_q;

@@ -102,6 +102,11 @@ class Cache:
         s = out[0].stride()
         return (*out, (s[0], s[1], s[2]), self.table.to(device), self.k_scales.clone().to(device), self.v_scales.clone().to(device))
 
+    def token_scales(self, which, r, n):
+        """The scales of the first n tokens of request r: [n, hkv] in 64 bits."""
+        pages = self.table[r, : -(-n // self.page)].long()
+        return np.repeat(getattr(self, which + "_scales")[pages].double().numpy(), self.sb, axis=2).transpose(0, 2, 1).reshape(-1, self.hkv)[:n]
+
     def values(self, which, r, n):
         """The first n tokens of request r: [n, hkv, d] in 64 bits."""
         codes, scales = getattr(self, which), getattr(self, which + "_scales")
@@ -112,7 +117,14 @@ class Cache:
 
 def attention(c: Cache, q: torch.Tensor, lens, m, sm_scale=0.0):
     """(out, lse, spread, reach) in 64 bits; spread = sum_t p_t |v_t| and reach = max_t sum_d |q_d k_td| sm_scale, for
-    the bounds on rounding errors."""
+    the bounds on rounding errors.
+
+    For 16-bit types spread also holds what lies below the range the kernel keeps for a row.  A weight times its
+    token's V scale is held in binary16 pieces with a least step of 2^-16 under a reference that puts the largest of
+    the row at 2^13 - 2^4 at least (the reference is a bound, up to a factor of 16 above it): half a step is 2^-26 of
+    the largest, and a token's value is its code times that.  Divided by the 2^-7 that attention_bounds multiplies
+    spread with for these types it is added here: 2^-19 max_t(p_t scale_t) sum_t |code_t|.
+    """
     hq, d = q.shape[1], q.shape[2]
     g = hq // c.hkv
     scale = sm_scale or 1 / math.sqrt(d)
@@ -130,8 +142,13 @@ def attention(c: Cache, q: torch.Tensor, lens, m, sm_scale=0.0):
             z = e.sum(-1, keepdims=True)
             p = e / z
             outs.append(np.einsum("ght,tgd->ghd", p, vv).reshape(hq, d))
+            below = 0.0
+            if q.dtype == torch.bfloat16:
+                sc = c.token_scales("v", r, seen)
+                codes = np.abs(vv) / np.where(sc > 0, sc, 1.0)[..., None]
+                below = (2.0 ** -19 * (p * sc.T[:, None]).max(-1)[..., None] * codes.sum(0)[:, None]).reshape(hq, d)
             lses.append((top + np.log(z)).reshape(hq))
-            spreads.append(np.einsum("ght,tgd->ghd", p, np.abs(vv)).reshape(hq, d))
+            spreads.append(np.einsum("ght,tgd->ghd", p, np.abs(vv)).reshape(hq, d) + below)
             reaches.append((np.einsum("ghd,tgd->ght", np.abs(x[j]), np.abs(kk)).max(-1) * scale).reshape(hq))
         q0 += k
     return tuple(np.stack(v) if v else np.zeros((0,)) for v in (outs, lses, spreads, reaches))
