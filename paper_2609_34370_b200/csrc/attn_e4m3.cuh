@@ -75,26 +75,40 @@ namespace e8 {
 
 using namespace tc;
 
-__device__ __forceinline__ bool bounded_wait(uint64_t *b, uint32_t parity, E8Barriers *bars, int32_t *dev_status) {
-  if (mbar_try_wait(b, parity)) return true;
+// Bounded wait of a converged warp; the outcome is shared, so that a warp never diverges around the
+// .sync.aligned instructions.  What does not find the barrier completed goes on out of line: with the
+// polling loops in line in some twenty places the kernel was 180 KB of code, and its warps waited for
+// instructions more than for anything else.
+__device__ __noinline__ bool wait_slow(uint64_t *b, uint32_t parity, E8Barriers *bars, int32_t *dev_status) {
   const long long t0 = clock64();
+#pragma unroll 1
   for (;;) {
+#pragma unroll 1
     for (int i = 0; i < 64; ++i)
-      if (mbar_try_wait(b, parity)) return true;
-    if (bars->abort) return false;
-    if (clock64() - t0 > kWaitLimitCycles) {
+      if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
+    if (__any_sync(0xffffffffu, bars->abort)) return false;
+    if (__any_sync(0xffffffffu, clock64() - t0 > kWaitLimitCycles)) {
       bars->abort = 1;
       atomicOr(dev_status, SPX_DEV_TIMEOUT);
       return false;
     }
   }
 }
+__device__ __forceinline__ bool warp_wait(uint64_t *b, uint32_t parity, E8Barriers *bars, int32_t *dev_status) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
+  return wait_slow(b, parity, bars, dev_status);
+}
 
 // Weight-stationary MMA, A e5m2, B e4m3; three of them in a row multiply one B tile, which the first
-// leaves in collector buffer kBuf.  One elected lane of the converged warp issues.
-#define SPX_E8_MMA(OP)                                                                                                        \
-  asm volatile("{ .reg .pred p, q; elect.sync _|q, 0xffffffff; setp.ne.b32 p, %4, 0; @q tcgen05.mma.ws.cta_group::1.kind::f8f6f4" OP \
-               " [%0], %1, %2, %3, p; }" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc) : "memory")
+// leaves in collector buffer kBuf.  One elected lane issues.
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t r;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
+  return r != 0;
+}
+#define SPX_E8_MMA(OP)                                                                                                      \
+  asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.ws.cta_group::1.kind::f8f6f4" OP " [%0], %1, %2, %3, p; }" \
+               ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc) : "memory")
 template <int kBuf, int kPieceIdx>
 __device__ __forceinline__ void mma_piece(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
   if constexpr (kBuf == 0) {
@@ -108,10 +122,6 @@ __device__ __forceinline__ void mma_piece(uint32_t d_tmem, uint64_t adesc, uint6
   }
 }
 #undef SPX_E8_MMA
-__device__ __forceinline__ void commit_elected(uint64_t *bar) {
-  asm volatile("{ .reg .pred q; elect.sync _|q, 0xffffffff; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }"
-               ::"r"(smem_u32(bar)) : "memory");
-}
 // D fp32, A e5m2 K-major, B e4m3
 __host__ __device__ constexpr uint32_t idesc_f8(uint32_t m, uint32_t n, bool b_mn_major) {
   return (1u << 4) | (1u << 7) | (b_mn_major ? (1u << 16) : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
@@ -189,8 +199,11 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
+#pragma unroll 1
     for (int s = 0; s < 4; ++s) { mbar_init(&bars->k_full[s], 1); mbar_init(&bars->v_full[s], 1); mbar_init(&bars->k_empty[s], 1); mbar_init(&bars->v_empty[s], 1); }
+#pragma unroll 1
     for (int s = 0; s < kE8ScaleSlots; ++s) { mbar_init(&bars->sc_full[s], 1); mbar_init(&bars->sc_empty[s], kE8SoftmaxWarps); }
+#pragma unroll 1
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->s_full[b], 1); mbar_init(&bars->p_full[b], kE8SoftmaxWarps); mbar_init(&bars->q_full[b], 1); mbar_init(&bars->q_empty[b], 1);
       mbar_init(&bars->pv_done[b], 1); mbar_init(&bars->o_free[b], kE8SoftmaxWarps);
@@ -200,6 +213,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     for (int i = 0; i < kE8NanSlots; ++i) bars->nan_any[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+#pragma unroll 1
   for (int i = tid; i < kE8NanSlots * 128; i += kE8Threads) sNan[i] = 0;
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "n"(Cfg::kTmemCols) : "memory");
@@ -216,10 +230,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   const int item_end = planned ? p.cta_off[blockIdx.x + 1] : 0;
   auto item_index = [&](int it) -> int { return item_begin + it < item_end ? item_begin + it : -1; };
   const int pages_per_tile = kTileTokens >> p.log2P;
-  // the outcome is shared so that a warp never diverges around the .sync.aligned instructions
-  auto warp_wait = [&](uint64_t *bar, uint32_t parity) -> bool {
-    return __all_sync(0xffffffffu, bounded_wait(bar, parity, bars, p.dev_status));
-  };
+  auto warp_wait = [&](uint64_t *bar, uint32_t parity) -> bool { return e8::warp_wait(bar, parity, bars, p.dev_status); };
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
@@ -317,6 +328,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       fence_after();
       const uint64_t qa = smem_desc(smem_u32(sQ + qb * 3 * Cfg::kPiece), 16, 1024), ka = kv_desc<D>(smem_u32(sK + slot * Cfg::kTileBytes));
       const uint32_t ts = tmem + Cfg::kColS + (t & 1) * Cfg::kSCols;
+      if (elect_lane()) {
 #pragma unroll
       for (int k = 0; k < D / 32; k += 2) {   // descriptors count 16-byte units: 32 columns are 2
         mma_piece<0, 0>(ts, qa + k * 2, ka + k * 2, kIdescQK, k > 0);
@@ -326,9 +338,11 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         mma_piece<1, 1>(ts, qa + k * 2 + 2 + (Cfg::kPiece >> 4), ka + k * 2 + 2, kIdescQK, 1);
         mma_piece<1, 2>(ts, qa + k * 2 + 2 + 2 * (Cfg::kPiece >> 4), ka + k * 2 + 2, kIdescQK, 1);
       }
-      commit_elected(&bars->s_full[t & 1]);
-      commit_elected(&bars->k_empty[slot]);
-      if (qk.i + 1 >= qk.n_tiles) commit_elected(&bars->q_empty[qb]);  // last score MMA of the entry
+      mma_commit(&bars->s_full[t & 1]);
+      mma_commit(&bars->k_empty[slot]);
+      if (qk.i + 1 >= qk.n_tiles) mma_commit(&bars->q_empty[qb]);  // last score MMA of the entry
+      }
+      __syncwarp();
       advance(qk);
       return true;
     };
@@ -346,6 +360,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       fence_after();
       const uint64_t pa = smem_desc(smem_u32(sP + (Cfg::kPBufs == 2 ? (t & 1) : 0) * 3 * Cfg::kPiece), 16, 1024), va = kv_desc<D>(smem_u32(sV + slot * Cfg::kTileBytes));
       const uint32_t to = tmem + Cfg::kColO + (pv.it & 1) * Cfg::kOCols;
+      if (elect_lane()) {
 #pragma unroll
       for (int k = 0; k < kTileTokens / 32; k += 2) {   // 32 tokens are 32 * D bytes of V, 32 bytes of P
         constexpr int kStep = 32 * D >> 4;
@@ -356,8 +371,10 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         mma_piece<1, 1>(to, pa + k * 2 + 2 + (Cfg::kPiece >> 4), va + (k + 1) * kStep, kIdescPV, 1);
         mma_piece<1, 2>(to, pa + k * 2 + 2 + 2 * (Cfg::kPiece >> 4), va + (k + 1) * kStep, kIdescPV, 1);
       }
-      commit_elected(&bars->v_empty[slot]);
-      commit_elected(&bars->pv_done[t & 1]);
+      mma_commit(&bars->v_empty[slot]);
+      mma_commit(&bars->pv_done[t & 1]);
+      }
+      __syncwarp();
       advance(pv);
     }
   } else if (warp == 2) {
@@ -425,7 +442,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         if (b != 0) lo = min(lo, b);
       }
       const float v_max = __uint_as_float(__reduce_max_sync(0xffffffffu, hi)), v_min = __uint_as_float(__reduce_min_sync(0xffffffffu, lo));
-      if (lane == 0) sVr[slot] = make_float2(fmaxf(log2f(v_max), kE8MinLog2), v_max == 0.f || v_max * 0.0625f <= v_min ? 1.f : 0.f);
+      if (lane == 0) sVr[slot] = make_float2(fmaxf(__log2f(v_max), kE8MinLog2), v_max == 0.f || v_max * 0.0625f <= v_min ? 1.f : 0.f);
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->sc_full[slot]);
       valid = valid_next;
@@ -627,7 +644,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           float mx2 = -INFINITY;
           const float *vs1 = reinterpret_cast<const float *>(vs4);
 #pragma unroll
-          for (int i = 0; i < TPT; ++i) mx2 = fmaxf(mx2, fmaf(__uint_as_float(r[i]), row_f, fmaxf(log2f(vs1[i]), kE8MinLog2)));
+          for (int i = 0; i < TPT; ++i) mx2 = fmaxf(mx2, fmaf(__uint_as_float(r[i]), row_f, fmaxf(__log2f(vs1[i]), kE8MinLog2)));
           sMx2[(b * kParts + part) * MROWS + row] = mx2;
         }
         ok = softmax_sync();
@@ -710,8 +727,10 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           ok = warp_wait(&bars->v_full[slot], (tc_ / Cfg::kStages) & 1);
           if (!ok) break;
           unsigned char *vt = sV + slot * Cfg::kTileBytes;
+#pragma unroll 1
           for (int i = sm_tid; i < (kTileTokens - ntok) * (D / 16); i += 256)
             *reinterpret_cast<uint4 *>(vt + ntok * D + i * 16) = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
           for (int i = sm_tid; i < (ntok - hidden) * (D / 16); i += 256) {
             const int tok = hidden + i / (D / 16), ch = i % (D / 16);
             uint4 *at = reinterpret_cast<uint4 *>(vt + tok * D + ch * 16);
@@ -724,6 +743,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
               // logical columns of this chunk under the swizzle
               const int col = (D == 128 ? ch ^ (tok & 7) : ch ^ ((tok >> 1) & 3)) * 16;
               const uint32_t bit = 1u << (tile * kTileTokens + tok - (e.L - e.m + 1));   // rows j > this position's index see it
+#pragma unroll 1
               for (int k = 0; k < 16; ++k)
                 if (((w[k >> 2] >> (8 * (k & 3))) & 0x7f) == 0x7f) {
                   w[k >> 2] &= ~(0xffu << (8 * (k & 3)));
@@ -755,6 +775,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   // ---------------------------------------------------------------------- teardown
   __syncwarp();
   if (bars->abort) {
+#pragma unroll 1
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   }
   fence_before();
