@@ -16,58 +16,67 @@
 // one thread instead of by elect.sync in a converged warp.  24 of them take 650 of the 1,420 cycles a tile's
 // 32 KB need from memory: the kernel stays bound by HBM.
 //
-// binary16 has no exponents to spare for V's scales, so a row keeps two references: m for the sum of
-// the weights, and m' for x, the running maximum of s_t + log2 v_t: x_t = 2^13 * 2^(s_t + log2 v_t - m').
-// Within a tile whose scales lie within a factor of 16 of each other the bound max s + max log2 v
-// stands for the maximum; other tiles take it element by element.  m' moves when it is passed by a
-// factor of 4, which rescales O.  The least weight with a byte left is then 2^-29 of the largest.
+// binary16 has no exponents to spare for V's scales, so a row's reference m' is the running maximum of
+// s_t + log2 v_t instead of s_t: y_t = 2^(11 + s_t - m') goes into the row's sum and x_t = y_t v_t into
+// P, both under the one reference.  Within a tile whose scales lie within a factor of 16 of each
+// other the bound max s + max log2 v stands for the maximum; other tiles take it element by element.
+// m' moves when it is passed by a factor of 16, which rescales O.  The least x with a bit left is then 2^-27
+// of the largest, or better.
 //
 // Roles of the 384 threads: warp 0 TMA producer, warp 1 MMA issuer, warp 2 scales of the next tiles,
-// warp 3 query pieces of the next entry, warps 4-11 softmax: a lane quadrant belongs to two warps, each
-// with half of the quadrant's tokens.  The plan, its work entries, partial results and bounded waits
-// are those of the 16-bit kernels.
+// warp 3 query pieces of the next entry, warps 4-7 and 8-11 two softmax groups that take the tiles in
+// turn, each with its own reference, sum and O, merged in the entry's epilogue: a tile's chain (scores,
+// maximum, weights, pieces) is some 2,000 cycles long, and two tiles in it at a time keep up with
+// memory.  (Eight warps on one tile: 118 us on the Llama-3-8B layer shape.)  The plan, its work entries,
+// partial results and bounded waits are those of the 16-bit kernels.
 #pragma once
+#include <cstddef>
+
 #include "attn_tc4.cuh"
 
 namespace spx {
 
-constexpr int kE8Threads = 384;
-constexpr int kE8SoftmaxWarps = 8;
+constexpr int kE8Threads = 512;
+constexpr int kE8QueryWarps = 4;   // 3, 13, 14, 15
+constexpr int kE8GroupWarps = 4;   // softmax warps of a group
 constexpr int kE8ScaleSlots = 4;   // tiles whose scales are staged
 constexpr int kE8RowSlots = 8;     // entries whose row factors are kept: the query warp is at most four entries ahead of the softmax
-constexpr int kE8NanSlots = 4;
-constexpr float kE8Shift = 13.f;   // x <= 2^(13 + 2) stays below binary16's 65504
-constexpr float kE8Rescale = 2.f;
-constexpr float kE8MinLog2 = -110.f;  // smaller V scales count as this in m', so that 2^(13 + m - m') stays finite
+constexpr int kE8NanSlots = 8;
+constexpr float kE8Shift = 11.f;   // x <= 2^(11 + 4) stays below binary16's 65504
+constexpr float kE8Rescale = 4.f;
+constexpr float kE8MinLog2 = -90.f;  // smaller V scales count as this in m', so that no sum of y overflows
 
 template <int D, int MROWS>
 struct E8Cfg {
-  static constexpr int kSplit = 128 / MROWS;                       // token blocks of a tile (the accumulator layout of the M = MROWS MMA)
-  static constexpr int kParts = 2 * kSplit;                        // softmax warps that share a row
-  static constexpr int kTokPerThread = kTileTokens / kParts;       // 16, 32, 64
+  static constexpr int kSplit = 128 / MROWS;                       // token blocks of a tile (the accumulator layout of the M = MROWS MMA): warps that share a row
+  static constexpr int kTokPerThread = kTileTokens / kSplit;       // 32, 64, 128
   static constexpr int kTileBytes = kTileTokens * D;
   static constexpr int kPiece = MROWS * 128;                       // one piece of Q (D <= 128 columns) or of P (128 tokens), 128-byte rows
-  static constexpr int kQBufs = MROWS == 128 ? 1 : 2, kPBufs = MROWS == 128 ? 1 : 2;
+  static constexpr int kQBufs = MROWS == 128 ? 1 : 2, kPBufs = MROWS == 128 ? 1 : 2, kOBufs = MROWS == 128 && D == 128 ? 1 : 2;
   static constexpr int kStages = MROWS == 32 ? 4 : 3;
-  static constexpr int kColBlock = D / kSplit / 2;                 // columns of O a thread holds
+  static constexpr int kColBlock = D / kSplit / 2;                 // columns of O a thread finishes
   static constexpr int kSCols = kTileTokens / kSplit, kOCols = D / kSplit;
-  static constexpr int kColS = 0, kColO = 2 * kSCols;
-  static constexpr int kTmemCols = kColO + 2 * kOCols <= 128 ? 128 : kColO + 2 * kOCols <= 256 ? 256 : 512;
+  static constexpr int kColS = 0, kColO = 2 * kSCols;              // two score buffers, kOBufs pairs of O (one of each group)
+  static constexpr int kTmemNeed = kColO + 2 * kOBufs * kOCols;
+  static constexpr int kTmemCols = kTmemNeed <= 128 ? 128 : kTmemNeed <= 256 ? 256 : 512;
+  static_assert(kTmemNeed <= 512, "tensor memory");
   // byte offsets into shared memory, after rounding its base up to 1024
-  static constexpr int kOffK = 0, kOffV = kOffK + kStages * kTileBytes, kOffQ = kOffV + kStages * kTileBytes, kOffP = kOffQ + kQBufs * 3 * kPiece;
+  static constexpr int kOffK = 0, kOffV = kOffK + kStages * kTileBytes, kOffQ = kOffV + kStages * kTileBytes, kOffP = kOffQ + kQBufs * 2 * kPiece;
   static constexpr int kOffKs = kOffP + kPBufs * 3 * kPiece, kOffVs = kOffKs + kE8ScaleSlots * 512, kOffVr = kOffVs + kE8ScaleSlots * 512;
-  static constexpr int kOffMx = kOffVr + kE8ScaleSlots * 16, kOffMx2 = kOffMx + 2 * 1024, kOffL = kOffMx2 + 2 * 1024;
-  static constexpr int kOffRow = kOffL + 2 * 1024, kOffNan = kOffRow + kE8RowSlots * MROWS * 4, kOffBar = kOffNan + kE8NanSlots * 128 * 4;
+  static constexpr int kOffMx = kOffVr + kE8ScaleSlots * 16, kOffL = kOffMx + 2 * 1024;
+  static constexpr int kOffRef = kOffL + 2 * 1024, kOffRow = kOffRef + 2 * 2 * MROWS * 4, kOffNan = kOffRow + kE8RowSlots * MROWS * 4;
+  static constexpr int kOffBar = kOffNan + kE8NanSlots * 128 * 4;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
   static_assert(kSmemBytes <= 232448, "shared memory");
 };
 
 struct E8Barriers {
   uint64_t k_full[4], v_full[4], k_empty[4], v_empty[4], sc_full[kE8ScaleSlots], sc_empty[kE8ScaleSlots];
-  uint64_t s_full[2], p_full[2], q_full[2], q_empty[2], pv_done[2], o_free[2], e_bar;
+  uint64_t s_full[2], p_full[2], q_full[2], q_empty[2], pv_done[2], o_full[2], o_free[2], item_done[2], e_bar[2];
   uint32_t tmem_base;
   volatile int32_t abort;
   int32_t nan_any[kE8NanSlots];
+  int32_t *dev_status;
 };
 static_assert(sizeof(E8Barriers) <= 512, "barrier area");
 
@@ -75,56 +84,65 @@ namespace e8 {
 
 using namespace tc;
 
-// Bounded wait of a converged warp; the outcome is shared, so that a warp never diverges around the
-// .sync.aligned instructions.  What does not find the barrier completed goes on out of line: with the
-// polling loops in line in some twenty places the kernel was 180 KB of code, and its warps waited for
-// instructions more than for anything else.
-__device__ __noinline__ bool wait_slow(uint64_t *b, uint32_t parity, E8Barriers *bars, int32_t *dev_status) {
+// Bounded wait of a converged warp.  What does not find the barrier completed goes on out of line: with
+// the polling loops in line in some twenty places the kernel was 180 KB of code, and its warps waited for
+// instructions more than for anything else.  For the same reason the outcome is not handed back: when
+// a wait gives up it raises SPX_DEV_TIMEOUT and the CTA's abort flag, which ends every other wait as well, and
+// every role's loop looks at the flag once a tile.
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, E8Barriers *bars) {
   const long long t0 = clock64();
 #pragma unroll 1
   for (;;) {
 #pragma unroll 1
     for (int i = 0; i < 64; ++i)
-      if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
-    if (__any_sync(0xffffffffu, bars->abort)) return false;
+      if (__all_sync(0xffffffffu, try_wait(bar, parity))) return;
+    if (__any_sync(0xffffffffu, bars->abort)) return;
     if (__any_sync(0xffffffffu, clock64() - t0 > kWaitLimitCycles)) {
       bars->abort = 1;
-      atomicOr(dev_status, SPX_DEV_TIMEOUT);
-      return false;
+      atomicOr(bars->dev_status, SPX_DEV_TIMEOUT);
+      return;
     }
   }
 }
-__device__ __forceinline__ bool warp_wait(uint64_t *b, uint32_t parity, E8Barriers *bars, int32_t *dev_status) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
-  return wait_slow(b, parity, bars, dev_status);
+__device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t parity, E8Barriers *bars) {
+  if (!__all_sync(0xffffffffu, try_wait(bar, parity))) wait_slow(bar, parity, bars);
 }
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
-// Weight-stationary MMA, A e5m2, B e4m3; three of them in a row multiply one B tile, which the first
-// leaves in collector buffer kBuf.  One elected lane issues.
 __device__ __forceinline__ bool elect_lane() {
   uint32_t r;
   asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
   return r != 0;
 }
+// Weight-stationary MMAs; those in a row that multiply one B tile share it through collector buffer kBuf:
+// kUse 0 fills it, 1 uses it, 2 is the last to.
 #define SPX_E8_MMA(OP)                                                                                                      \
   asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.ws.cta_group::1.kind::f8f6f4" OP " [%0], %1, %2, %3, p; }" \
                ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc) : "memory")
-template <int kBuf, int kPieceIdx>
+template <int kBuf, int kUse>
 __device__ __forceinline__ void mma_piece(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
   if constexpr (kBuf == 0) {
-    if constexpr (kPieceIdx == 0) SPX_E8_MMA(".collector::b0::fill");
-    else if constexpr (kPieceIdx == 1) SPX_E8_MMA(".collector::b0::use");
+    if constexpr (kUse == 0) SPX_E8_MMA(".collector::b0::fill");
+    else if constexpr (kUse == 1) SPX_E8_MMA(".collector::b0::use");
     else SPX_E8_MMA(".collector::b0::lastuse");
   } else {
-    if constexpr (kPieceIdx == 0) SPX_E8_MMA(".collector::b1::fill");
-    else if constexpr (kPieceIdx == 1) SPX_E8_MMA(".collector::b1::use");
+    if constexpr (kUse == 0) SPX_E8_MMA(".collector::b1::fill");
+    else if constexpr (kUse == 1) SPX_E8_MMA(".collector::b1::use");
     else SPX_E8_MMA(".collector::b1::lastuse");
   }
 }
 #undef SPX_E8_MMA
-// D fp32, A e5m2 K-major, B e4m3
-__host__ __device__ constexpr uint32_t idesc_f8(uint32_t m, uint32_t n, bool b_mn_major) {
-  return (1u << 4) | (1u << 7) | (b_mn_major ? (1u << 16) : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// D fp32, A e4m3 or e5m2 K-major, B e4m3
+__host__ __device__ constexpr uint32_t idesc_f8(uint32_t m, uint32_t n, bool a_e5m2, bool b_mn_major) {
+  return (1u << 4) | (a_e5m2 ? 1u << 7 : 0u) | (b_mn_major ? (1u << 16) : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 // rows of D bytes: 128-byte swizzle for 128 columns, 64-byte swizzle for 64
 template <int D>
@@ -161,6 +179,43 @@ __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
   asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+// two fp32 operations in one instruction
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+// Four values, as two binary16 pairs, as the sums of an e4m3 and an e5m2 value, each rounded to nearest.
+__device__ __forceinline__ void cut2(uint32_t h01, uint32_t h23, uint32_t &w1, uint32_t &w2) {
+  uint16_t a, b;
+  uint32_t u, v;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(a) : "r"(h01));
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(b) : "r"(h23));
+  w1 = (uint32_t)a | ((uint32_t)b << 16);
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(u) : "h"(a));
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"(b));
+  u = sub_f16x2(h01, u);
+  v = sub_f16x2(h23, v);
+  asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(a) : "r"(u));
+  asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(b) : "r"(v));
+  w2 = (uint32_t)a | ((uint32_t)b << 16);
+}
 // Four values, as two binary16 pairs, cut into three e5m2 pieces of four bytes each.
 __device__ __forceinline__ void cut3(uint32_t h01, uint32_t h23, uint32_t &w1, uint32_t &w2, uint32_t &w3) {
   w1 = __byte_perm(h01, h23, 0x7531);
@@ -185,14 +240,15 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   using Cfg = E8Cfg<D, MROWS>;
   using namespace e8;
-  constexpr int kSplit = Cfg::kSplit, kParts = Cfg::kParts, TPT = Cfg::kTokPerThread, CB = Cfg::kColBlock;
+  constexpr int kSplit = Cfg::kSplit, TPT = Cfg::kTokPerThread, CB = Cfg::kColBlock;
   extern __shared__ __align__(1024) unsigned char smem_dyn[];
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
   unsigned char *sK = smem + Cfg::kOffK, *sV = smem + Cfg::kOffV, *sQ = smem + Cfg::kOffQ, *sP = smem + Cfg::kOffP;
   float *sKs = reinterpret_cast<float *>(smem + Cfg::kOffKs), *sVs = reinterpret_cast<float *>(smem + Cfg::kOffVs);
   float2 *sVr = reinterpret_cast<float2 *>(smem + Cfg::kOffVr);    // per tile: (log2 of the largest V scale, 1 if all are within a factor of 16)
-  float *sMx = reinterpret_cast<float *>(smem + Cfg::kOffMx), *sMx2 = reinterpret_cast<float *>(smem + Cfg::kOffMx2);   // [2 tiles][kParts][MROWS]
-  float *sL = reinterpret_cast<float *>(smem + Cfg::kOffL);        // [2 entries][kParts][MROWS]
+  float *sMx = reinterpret_cast<float *>(smem + Cfg::kOffMx);   // [2 tiles][group][kSplit][MROWS]
+  float *sL = reinterpret_cast<float *>(smem + Cfg::kOffL);        // [2 entries][group][kSplit][MROWS]
+  float *sRef = reinterpret_cast<float *>(smem + Cfg::kOffRef);    // [2 entries][group][MROWS]
   float *sRow = reinterpret_cast<float *>(smem + Cfg::kOffRow);    // [kE8RowSlots][MROWS]
   uint32_t *sNan = reinterpret_cast<uint32_t *>(smem + Cfg::kOffNan);  // [kE8NanSlots][128]
   E8Barriers *bars = reinterpret_cast<E8Barriers *>(smem + Cfg::kOffBar);
@@ -202,14 +258,15 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
 #pragma unroll 1
     for (int s = 0; s < 4; ++s) { mbar_init(&bars->k_full[s], 1); mbar_init(&bars->v_full[s], 1); mbar_init(&bars->k_empty[s], 1); mbar_init(&bars->v_empty[s], 1); }
 #pragma unroll 1
-    for (int s = 0; s < kE8ScaleSlots; ++s) { mbar_init(&bars->sc_full[s], 1); mbar_init(&bars->sc_empty[s], kE8SoftmaxWarps); }
+    for (int s = 0; s < kE8ScaleSlots; ++s) { mbar_init(&bars->sc_full[s], 1); mbar_init(&bars->sc_empty[s], kE8GroupWarps); }
 #pragma unroll 1
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&bars->s_full[b], 1); mbar_init(&bars->p_full[b], kE8SoftmaxWarps); mbar_init(&bars->q_full[b], 1); mbar_init(&bars->q_empty[b], 1);
-      mbar_init(&bars->pv_done[b], 1); mbar_init(&bars->o_free[b], kE8SoftmaxWarps);
+      mbar_init(&bars->s_full[b], 1); mbar_init(&bars->p_full[b], kE8GroupWarps); mbar_init(&bars->q_full[b], kE8QueryWarps); mbar_init(&bars->q_empty[b], 1);
+      mbar_init(&bars->pv_done[b], 1); mbar_init(&bars->o_full[b], 1); mbar_init(&bars->o_free[b], 2 * kE8GroupWarps);
+      mbar_init(&bars->item_done[b], 2 * kE8GroupWarps); mbar_init(&bars->e_bar[b], kE8GroupWarps);
     }
-    mbar_init(&bars->e_bar, kE8SoftmaxWarps);
     bars->abort = 0;
+    bars->dev_status = p.dev_status;
     for (int i = 0; i < kE8NanSlots; ++i) bars->nan_any[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -230,7 +287,9 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   const int item_end = planned ? p.cta_off[blockIdx.x + 1] : 0;
   auto item_index = [&](int it) -> int { return item_begin + it < item_end ? item_begin + it : -1; };
   const int pages_per_tile = kTileTokens >> p.log2P;
-  auto warp_wait = [&](uint64_t *bar, uint32_t parity) -> bool { return e8::warp_wait(bar, parity, bars, p.dev_status); };
+  const uint32_t bar0 = smem_u32(bars);
+  auto warp_wait = [&](uint32_t bar, uint32_t parity) { e8::warp_wait(bar, parity, bars); };
+#define SPX_E8_BAR(member, i) (bar0 + (uint32_t)offsetof(E8Barriers, member) + 8u * (uint32_t)(i))
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
@@ -270,8 +329,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     open(la, 0);
     int page_la = load_page(la);
     uint32_t tc_ = 0;
-    bool ok = true;
-    while (la.valid && ok && !bars->abort) {
+    while (la.valid && !bars->abort) {
       const GCursor cur = la;
       const int page = page_la;
       advance(la);
@@ -284,98 +342,81 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         const int ntok = min(kTileTokens, cur.e.L - tile * kTileTokens);
         const uint32_t bytes = (uint32_t)(((ntok + p.P - 1) >> p.log2P) << p.log2P) * D;
         const bool mine = (my_tile == ti) && page >= 0;
-        ok = warp_wait(&bars->k_empty[slot], ph ^ 1);
-        if (!ok) break;
+        warp_wait(SPX_E8_BAR(k_empty, slot), ph ^ 1);
         if (lane == 0) mbar_expect_tx(&bars->k_full[slot], bytes);
         if (mine) tma_load_4d(smem_u32(sK + slot * Cfg::kTileBytes + my_page * p.P * D), &kmap, &bars->k_full[slot], 0, p.head_inner ? g : 0, p.head_inner ? 0 : g, page);
-        ok = warp_wait(&bars->v_empty[slot], ph ^ 1);
-        if (!ok) break;
+        warp_wait(SPX_E8_BAR(v_empty, slot), ph ^ 1);
         if (lane == 0) mbar_expect_tx(&bars->v_full[slot], bytes);
         if (mine) tma_load_4d(smem_u32(sV + slot * Cfg::kTileBytes + my_page * p.P * D), &vmap, &bars->v_full[slot], 0, p.head_inner ? g : 0, p.head_inner ? 0 : g, page);
       }
     }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer (the whole warp, converged)
-    constexpr uint32_t kIdescQK = idesc_f8(MROWS, kTileTokens, false);
-    constexpr uint32_t kIdescPV = idesc_f8(MROWS, D, true);
-    // two cursors over the CTA's flat tile sequence: the score MMAs run one tile ahead of the value
-    // MMAs, across entries too
-    struct Cursor { int it, n_tiles, n_tiles_next, i; uint32_t t; bool valid; };
-    auto tiles_of = [&](int it) -> int {
-      const int idx = item_index(it);
+  } else if (warp == 1 || warp == 12) {
+    // ------------------------------------------------------------------ MMA issuers: scores (warp 1), values (warp 12)
+    // One warp for both was the kernel's longest chain: a tile's MMAs take the issuing thread some 46 cycles each.
+    const bool scores = warp == 1;
+    int it = 0;
+    auto tiles_of = [&](int i) -> int {
+      const int idx = item_index(i);
       if (idx < 0) return 0;
       return p.work[idx].tile_end - p.work[idx].tile_begin;
     };
-    auto open_item = [&](Cursor &c) {
-      c.valid = item_index(c.it) >= 0;
-      c.i = 0;
-      c.n_tiles_next = tiles_of(c.it + 1);
-    };
-    auto advance = [&](Cursor &c) {
-      ++c.t;
-      if (++c.i >= c.n_tiles) { ++c.it; c.n_tiles = c.n_tiles_next; open_item(c); }
-    };
-    Cursor qk{0, 0, 0, 0, 0, false}, pv{0, 0, 0, 0, 0, false};
-    qk.n_tiles = pv.n_tiles = tiles_of(0);
-    open_item(qk);
-    open_item(pv);
-    bool ok = true;
-    auto issue_qk = [&]() -> bool {
-      const uint32_t t = qk.t, qb = Cfg::kQBufs == 2 ? (qk.it & 1) : 0;
-      if (qk.i == 0 && !warp_wait(&bars->q_full[qb], (Cfg::kQBufs == 2 ? (qk.it >> 1) : qk.it) & 1)) return false;
+    int n_tiles = tiles_of(0), n_next = tiles_of(1), i = 0;
+#pragma unroll 1
+    for (uint32_t t = 0; item_index(it) >= 0 && !bars->abort; ++t) {
       const int slot = t % Cfg::kStages;
-      if (!warp_wait(&bars->k_full[slot], (t / Cfg::kStages) & 1)) return false;
-      fence_after();
-      const uint64_t qa = smem_desc(smem_u32(sQ + qb * 3 * Cfg::kPiece), 16, 1024), ka = kv_desc<D>(smem_u32(sK + slot * Cfg::kTileBytes));
-      const uint32_t ts = tmem + Cfg::kColS + (t & 1) * Cfg::kSCols;
-      if (elect_lane()) {
+      const uint32_t ph = (t / Cfg::kStages) & 1;
+      const bool last = i + 1 >= n_tiles;
+      if (scores) {
+        constexpr uint32_t kIdesc0 = idesc_f8(MROWS, kTileTokens, false, false), kIdesc1 = idesc_f8(MROWS, kTileTokens, true, false);
+        const uint32_t qb = Cfg::kQBufs == 2 ? (it & 1) : 0;
+        if (i == 0) warp_wait(SPX_E8_BAR(q_full, qb), (Cfg::kQBufs == 2 ? (it >> 1) : it) & 1);
+        warp_wait(SPX_E8_BAR(k_full, slot), ph);
+        // the buffer's last scores have been read once they are weights
+        if (t >= 2) warp_wait(SPX_E8_BAR(p_full, t & 1), ((t - 2) >> 1) & 1);
+        fence_after();
+        const uint64_t qa = smem_desc(smem_u32(sQ + qb * 2 * Cfg::kPiece), 16, 1024), ka = kv_desc<D>(smem_u32(sK + slot * Cfg::kTileBytes));
+        const uint32_t ts = tmem + Cfg::kColS + (t & 1) * Cfg::kSCols;
+        if (elect_lane()) {
 #pragma unroll
-      for (int k = 0; k < D / 32; k += 2) {   // descriptors count 16-byte units: 32 columns are 2
-        mma_piece<0, 0>(ts, qa + k * 2, ka + k * 2, kIdescQK, k > 0);
-        mma_piece<0, 1>(ts, qa + k * 2 + (Cfg::kPiece >> 4), ka + k * 2, kIdescQK, 1);
-        mma_piece<0, 2>(ts, qa + k * 2 + 2 * (Cfg::kPiece >> 4), ka + k * 2, kIdescQK, 1);
-        mma_piece<1, 0>(ts, qa + k * 2 + 2, ka + k * 2 + 2, kIdescQK, 1);
-        mma_piece<1, 1>(ts, qa + k * 2 + 2 + (Cfg::kPiece >> 4), ka + k * 2 + 2, kIdescQK, 1);
-        mma_piece<1, 2>(ts, qa + k * 2 + 2 + 2 * (Cfg::kPiece >> 4), ka + k * 2 + 2, kIdescQK, 1);
-      }
-      mma_commit(&bars->s_full[t & 1]);
-      mma_commit(&bars->k_empty[slot]);
-      if (qk.i + 1 >= qk.n_tiles) mma_commit(&bars->q_empty[qb]);  // last score MMA of the entry
+          for (int k = 0; k < D / 32; k += 2) {   // descriptors count 16-byte units: 32 columns are 2
+            mma_piece<0, 0>(ts, qa + k * 2, ka + k * 2, kIdesc0, k > 0);
+            mma_piece<0, 2>(ts, qa + k * 2 + (Cfg::kPiece >> 4), ka + k * 2, kIdesc1, 1);
+            mma_piece<1, 0>(ts, qa + k * 2 + 2, ka + k * 2 + 2, kIdesc0, 1);
+            mma_piece<1, 2>(ts, qa + k * 2 + 2 + (Cfg::kPiece >> 4), ka + k * 2 + 2, kIdesc1, 1);
+          }
+          commit(SPX_E8_BAR(s_full, t & 1));
+          commit(SPX_E8_BAR(k_empty, slot));
+          if (last) commit(SPX_E8_BAR(q_empty, qb));
+        }
+      } else {
+        constexpr uint32_t kIdesc = idesc_f8(MROWS, D, true, true);
+        constexpr int kStep = 32 * D >> 4;   // 32 tokens are 32 * D bytes of V, 32 bytes of P
+        // O's buffers were last used kOBufs entries ago
+        if (i == 0 && it >= Cfg::kOBufs)
+          warp_wait(SPX_E8_BAR(o_free, Cfg::kOBufs == 2 ? (it & 1) : 0), (Cfg::kOBufs == 2 ? (it >> 1) - 1 : it - 1) & 1);
+        warp_wait(SPX_E8_BAR(v_full, slot), ph);
+        warp_wait(SPX_E8_BAR(p_full, t & 1), (t >> 1) & 1);
+        fence_after();
+        const uint64_t pa = smem_desc(smem_u32(sP + (Cfg::kPBufs == 2 ? (t & 1) : 0) * 3 * Cfg::kPiece), 16, 1024), va = kv_desc<D>(smem_u32(sV + slot * Cfg::kTileBytes));
+        const uint32_t to = tmem + Cfg::kColO + ((Cfg::kOBufs == 2 ? (it & 1) * 2 : 0) + (t & 1)) * Cfg::kOCols;
+        if (elect_lane()) {
+#pragma unroll
+          for (int k = 0; k < kTileTokens / 32; k += 2) {
+            mma_piece<0, 0>(to, pa + k * 2, va + k * kStep, kIdesc, (i > 1) || (k > 0));   // an entry's first two tiles begin their group's O
+            mma_piece<0, 1>(to, pa + k * 2 + (Cfg::kPiece >> 4), va + k * kStep, kIdesc, 1);
+            mma_piece<0, 2>(to, pa + k * 2 + 2 * (Cfg::kPiece >> 4), va + k * kStep, kIdesc, 1);
+            mma_piece<1, 0>(to, pa + k * 2 + 2, va + (k + 1) * kStep, kIdesc, 1);
+            mma_piece<1, 1>(to, pa + k * 2 + 2 + (Cfg::kPiece >> 4), va + (k + 1) * kStep, kIdesc, 1);
+            mma_piece<1, 2>(to, pa + k * 2 + 2 + 2 * (Cfg::kPiece >> 4), va + (k + 1) * kStep, kIdesc, 1);
+          }
+          commit(SPX_E8_BAR(v_empty, slot));
+          commit(SPX_E8_BAR(pv_done, t & 1));
+          if (last) commit(SPX_E8_BAR(o_full, it & 1));
+        }
       }
       __syncwarp();
-      advance(qk);
-      return true;
-    };
-    if (qk.valid) ok = issue_qk();
-    while (ok && pv.valid && !bars->abort) {
-      if (qk.valid) ok = issue_qk();
-      if (!ok) break;
-      const uint32_t t = pv.t;
-      ok = warp_wait(&bars->p_full[t & 1], (t >> 1) & 1);
-      // the O buffer of this entry's parity was last used two entries ago
-      if (ok && pv.i == 0 && pv.it >= 2) ok = warp_wait(&bars->o_free[pv.it & 1], ((pv.it >> 1) - 1) & 1);
-      const int slot = t % Cfg::kStages;
-      if (ok) ok = warp_wait(&bars->v_full[slot], (t / Cfg::kStages) & 1);
-      if (!ok) break;
-      fence_after();
-      const uint64_t pa = smem_desc(smem_u32(sP + (Cfg::kPBufs == 2 ? (t & 1) : 0) * 3 * Cfg::kPiece), 16, 1024), va = kv_desc<D>(smem_u32(sV + slot * Cfg::kTileBytes));
-      const uint32_t to = tmem + Cfg::kColO + (pv.it & 1) * Cfg::kOCols;
-      if (elect_lane()) {
-#pragma unroll
-      for (int k = 0; k < kTileTokens / 32; k += 2) {   // 32 tokens are 32 * D bytes of V, 32 bytes of P
-        constexpr int kStep = 32 * D >> 4;
-        mma_piece<0, 0>(to, pa + k * 2, va + k * kStep, kIdescPV, (pv.i > 0) || (k > 0));
-        mma_piece<0, 1>(to, pa + k * 2 + (Cfg::kPiece >> 4), va + k * kStep, kIdescPV, 1);
-        mma_piece<0, 2>(to, pa + k * 2 + 2 * (Cfg::kPiece >> 4), va + k * kStep, kIdescPV, 1);
-        mma_piece<1, 0>(to, pa + k * 2 + 2, va + (k + 1) * kStep, kIdescPV, 1);
-        mma_piece<1, 1>(to, pa + k * 2 + 2 + (Cfg::kPiece >> 4), va + (k + 1) * kStep, kIdescPV, 1);
-        mma_piece<1, 2>(to, pa + k * 2 + 2 + 2 * (Cfg::kPiece >> 4), va + (k + 1) * kStep, kIdescPV, 1);
-      }
-      mma_commit(&bars->v_empty[slot]);
-      mma_commit(&bars->pv_done[t & 1]);
-      }
-      __syncwarp();
-      advance(pv);
+      ++i;
+      if (last) { ++it; i = 0; n_tiles = n_next; n_next = tiles_of(it + 1); }
     }
   } else if (warp == 2) {
     // ------------------------------------------------------------------ scales, one float per token and tile
@@ -403,14 +444,25 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     };
     auto load_scales = [&](const TCursor &c, int page, float (&ks)[4], float (&vs)[4]) {
       const int t = c.tile * kTileTokens + lane * 4;
+      const int left = page >= 0 ? c.e.L - t : 0;   // tokens past the end have scale zero
       const int64_t base = ((int64_t)page * p.Hkv + c.e.g) << (p.log2P - p.log2SB);
+      const int slot = t & (p.P - 1);
+      if (p.log2SB >= 2) {   // one scale for the lane's tokens
+        float k = 0.f, v = 0.f;
+        if (left > 0) {
+          k = __ldg(p.k_scales + base + (slot >> p.log2SB));
+          v = __ldg(p.v_scales + base + (slot >> p.log2SB));
+        }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ks[i] = vs[i] = 0.f;   // tokens past the end
-        if (page >= 0 && t + i < c.e.L) {
-          const int64_t at = base + (((t + i) & (p.P - 1)) >> p.log2SB);
-          ks[i] = __ldg(p.k_scales + at);
-          vs[i] = __ldg(p.v_scales + at);
+        for (int i = 0; i < 4; ++i) { ks[i] = i < left ? k : 0.f; vs[i] = i < left ? v : 0.f; }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ks[i] = vs[i] = 0.f;
+          if (i < left) {
+            ks[i] = __ldg(p.k_scales + base + ((slot + i) >> p.log2SB));
+            vs[i] = __ldg(p.v_scales + base + ((slot + i) >> p.log2SB));
+          }
         }
       }
     };
@@ -430,7 +482,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       advance(next);
       page_next = load_page(next);
       const int slot = t % kE8ScaleSlots;
-      if (t >= kE8ScaleSlots && !warp_wait(&bars->sc_empty[slot], ((t / kE8ScaleSlots) - 1) & 1)) break;
+      if (t >= kE8ScaleSlots) warp_wait(SPX_E8_BAR(sc_empty, slot), ((t / kE8ScaleSlots) - 1) & 1);
       *reinterpret_cast<float4 *>(sKs + slot * 128 + lane * 4) = make_float4(ks[0], ks[1], ks[2], ks[3]);
       *reinterpret_cast<float4 *>(sVs + slot * 128 + lane * 4) = make_float4(vs[0], vs[1], vs[2], vs[3]);
       // positive floats order like their patterns
@@ -444,15 +496,18 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       const float v_max = __uint_as_float(__reduce_max_sync(0xffffffffu, hi)), v_min = __uint_as_float(__reduce_min_sync(0xffffffffu, lo));
       if (lane == 0) sVr[slot] = make_float2(fmaxf(__log2f(v_max), kE8MinLog2), v_max == 0.f || v_max * 0.0625f <= v_min ? 1.f : 0.f);
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->sc_full[slot]);
+      if (lane == 0) arrive(SPX_E8_BAR(sc_full, slot));
       valid = valid_next;
 #pragma unroll
       for (int i = 0; i < 4; ++i) { ks[i] = ks_next[i]; vs[i] = vs_next[i]; }
     }
-  } else if (warp == 3) {
+  } else if (warp == 3 || warp > 12) {
     // ------------------------------------------------------------------ query pieces, an entry ahead
-    // A lane owns 8 columns of a row: a pass covers 2 rows of 128 columns or 4 of 64.
+    // A lane owns 8 columns of a row: a pass of one warp covers 2 rows of 128 columns or 4 of 64.  Four warps,
+    // each with four passes' loads in flight, turn 32 rows in one trip to memory; a single warp took 8,500
+    // cycles an entry of 32 rows, the time of six tiles.
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+    const int q_warp = warp == 3 ? 0 : warp - 12;
     const int c = lane % kLanes;
     const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(p.q);
     WorkEntry e, e_next;
@@ -463,7 +518,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       const int qb = Cfg::kQBufs == 2 ? (it & 1) : 0, uses = Cfg::kQBufs == 2 ? (it >> 1) : it;
       const int R = e.m * p.G;
       float *rows_out = sRow + (it % kE8RowSlots) * MROWS;
-      unsigned char *dst = sQ + qb * 3 * Cfg::kPiece;
+      unsigned char *dst = sQ + qb * 2 * Cfg::kPiece;
       auto load = [&](int row) -> uint4 {
         if (row >= R) return make_uint4(0, 0, 0, 0);
         const int j = row / p.G, hg = row - j * p.G;
@@ -471,13 +526,13 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       };
       constexpr int kAhead = 4;   // passes whose loads are in flight together
       bool waited = false;
-      for (int row0 = 0; row0 < R; row0 += kAhead * kRows) {
+      for (int row0 = q_warp * kAhead * kRows; row0 < R || !waited; row0 += kE8QueryWarps * kAhead * kRows) {
         uint4 v[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) v[u] = load(row0 + u * kRows + lane / kLanes);
         if (!waited) {
           waited = true;
-          if (uses >= 1 && !warp_wait(&bars->q_empty[qb], (uses - 1) & 1)) break;
+          if (uses >= 1) warp_wait(SPX_E8_BAR(q_empty, qb), (uses - 1) & 1);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -489,87 +544,94 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           a = max(a & 0xffffu, a >> 16);
 #pragma unroll
           for (int o = 1; o < kLanes; o <<= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
-          // 2^f puts the row's largest element into [2^14, 2^15); a row that is not finite becomes NaN through its factor
+          // 2^f puts the row's largest element into [2^7, 2^8); a row that is not finite becomes NaN through its factor
           const bool finite = a < 0x7f80u;
-          const int field = a == 0 ? 127 : min(268 - (int)(a >> 7), 253);
+          const int field = a == 0 ? 127 : min(261 - (int)(a >> 7), 253);
           const float mult = finite ? __uint_as_float((uint32_t)field << 23) : 0.f;
           uint32_t h[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) h[i] = finite ? pack_f16(__uint_as_float(w[i] << 16) * mult, __uint_as_float(w[i] & 0xffff0000u) * mult) : 0u;
-          uint2 piece[3];
-          cut3(h[0], h[1], piece[0].x, piece[1].x, piece[2].x);
-          cut3(h[2], h[3], piece[0].y, piece[1].y, piece[2].y);
+          uint2 piece[2];
+          cut2(h[0], h[1], piece[0].x, piece[1].x);
+          cut2(h[2], h[3], piece[0].y, piece[1].y);
           if (row < R) {
             unsigned char *at = dst + (row >> 3) * 1024 + (row & 7) * 128 + (((c >> 1) ^ (row & 7)) << 4) + (c & 1) * 8;
 #pragma unroll
-            for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2 *>(at + i * Cfg::kPiece) = piece[i];
+            for (int i = 0; i < 2; ++i) *reinterpret_cast<uint2 *>(at + i * Cfg::kPiece) = piece[i];
             // (never zero: a hidden score is -inf, and times zero it would be NaN)
             if (c == 0) rows_out[row] = finite ? fmaxf(ldexpf(p.scale_log2, 127 - field), 1.17549435e-38f) : __int_as_float(0x7fc00000);
           }
         }
       }
-      if (bars->abort) break;
       fence_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->q_full[qb]);
+      if (lane == 0) arrive(SPX_E8_BAR(q_full, qb));
       e = e_next;
     }
   } else {
     // ------------------------------------------------------------------ softmax / epilogue
-    const int quad = warp & 3, half = (warp - 4) >> 2;
+    const int quad = warp & 3, grp = (warp - 4) >> 2;
     // the accumulator layouts of the M = 32 / 64 / 128 weight-stationary MMAs: quadrant -> (row group,
-    // token block); the same split applies to the columns of O.  Two warps halve a quadrant's columns.
+    // token block); the same split applies to the columns of O
     const int rgrp = kSplit == 4 ? 0 : kSplit == 2 ? (quad & 1) : quad;
-    const int tblk = kSplit == 4 ? quad : kSplit == 2 ? (quad >> 1) : 0;
+    const int part = kSplit == 4 ? quad : kSplit == 2 ? (quad >> 1) : 0;
     const int row = rgrp * 32 + lane;                       // packed query row
-    const int part = tblk * 2 + half;                       // this warp's share of the row: tokens and output columns
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
-    const int sm_tid = tid - 128;                           // 0 .. 255
+    const int sm_tid = tid - 128, g_tid = sm_tid & 127;
+    const int row_j = row / p.G, row_h = row - row_j * p.G;
     __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(p.out);
 
-    uint32_t tc_ = 0, qc = 0, ec = 0;
-    bool ok = true;
-    // bounded barrier among the softmax warps (a named barrier could not time out)
-    auto softmax_sync = [&]() -> bool {
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->e_bar);
-      const bool r = warp_wait(&bars->e_bar, ec & 1);
-      ++ec;
-      return r;
-    };
-    // The sums of a row's parts are merged through sL (written at the end of the entry's last tile, visible
-    // after the next bounded barrier); each thread then finishes its columns.
-    struct Pending { bool valid; WorkEntry e; float m_ref, x_ref; uint32_t last_tc, qc; } pend;
+    uint32_t ec = 0;
+    // An entry's epilogue needs both groups' sums (item_done) and both O's (o_full); it is deferred behind
+    // the group's next tile, so that neither is waited for.  All eight warps run it once per entry, in
+    // order and before they report the next entry done; each takes half of its quadrant's columns.
+    struct Pending { bool valid; WorkEntry e; uint32_t t_first; int it; } pend;
     pend.valid = false;
-    auto run_epilogue = [&]() -> bool {
+    auto run_epilogue = [&]() {
       const WorkEntry &J = pend.e;
-      const float *sl = sL + (pend.qc & 1) * 256;
-      float l_row = 0.f;
-#pragma unroll
-      for (int i = 0; i < kParts; ++i) l_row += sl[i * MROWS + row];
-      if (!warp_wait(&bars->pv_done[pend.last_tc & 1], (pend.last_tc >> 1) & 1)) return false;
+      const int it = pend.it;
+      warp_wait(SPX_E8_BAR(item_done, it & 1), (it >> 1) & 1);
+      warp_wait(SPX_E8_BAR(o_full, it & 1), (it >> 1) & 1);
       fence_after();
-      uint32_t o[CB];
-      tmem_load<CB>(tmem + Cfg::kColO + (pend.qc & 1) * Cfg::kOCols + half * CB + lane_addr, o);
+      uint32_t o[CB], o2[CB];
+      const uint32_t to = tmem + Cfg::kColO + (Cfg::kOBufs == 2 ? (it & 1) * 2 : 0) * Cfg::kOCols + grp * CB + lane_addr;
+      tmem_load<CB>(to, o);
+      tmem_load<CB>(to + Cfg::kOCols, o2);
       wait_ld();
-      // O has been read: the entry after next may overwrite this buffer
+      // O has been read: a later entry may overwrite the buffers
       fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->o_free[pend.qc & 1]);
-      const int j = row / p.G, hg = row - j * p.G;
-      const int nan_slot = pend.qc % kE8NanSlots;
+      if (lane == 0) arrive(SPX_E8_BAR(o_free, Cfg::kOBufs == 2 ? (it & 1) : 0));
+      float l0 = 0.f, l1 = 0.f;
+      const float *sl = sL + (it & 1) * 256;
+#pragma unroll
+      for (int i = 0; i < kSplit; ++i) { l0 += sl[i * MROWS + row]; l1 += sl[128 + i * MROWS + row]; }
+      const float ref0 = sRef[(it & 1) * 2 * MROWS + row], ref1 = sRef[(it & 1) * 2 * MROWS + MROWS + row];
+      // the groups' tiles: those of parity 0 and 1 among t_first .. t_first + n - 1; an O without one is nobody's
+      const bool one_tile = J.tile_end - J.tile_begin == 1;
+      const bool use0 = !one_tile || (pend.t_first & 1) == 0, use1 = !one_tile || (pend.t_first & 1) == 1;
+      float ref = fmaxf(ref0, ref1);
+      const float w0 = ref0 == -INFINITY ? 0.f : fast_exp2(ref0 - ref), w1 = ref1 == -INFINITY ? 0.f : fast_exp2(ref1 - ref);
+      const float l_row = w0 * l0 + w1 * l1;
+      if (l_row != l_row) ref = 0.f;   // a NaN row stays one where its chunks are merged
+#pragma unroll
+      for (int i = 0; i < CB; ++i) {
+        const float a = use0 ? w0 * __uint_as_float(o[i]) : 0.f;
+        o[i] = __float_as_uint(use1 ? fmaf(w1, __uint_as_float(o2[i]), a) : a);
+      }
+      const int col0 = part * Cfg::kOCols + grp * CB;
+      const int nan_slot = it % kE8NanSlots;
       if (bars->nan_any[nan_slot]) {
         // columns of V with a NaN at a new position: into the rows that see it
 #pragma unroll
         for (int i = 0; i < CB; ++i)
-          if (sNan[nan_slot * 128 + part * CB + i] & ((1u << j) - 1)) o[i] = 0x7fc00000u;
+          if (sNan[nan_slot * 128 + col0 + i] & ((1u << row_j) - 1)) o[i] = 0x7fc00000u;
       }
       if (row < J.m * p.G) {
-        // from x's reference to the weights' (a row with no value above zero so far: its O is zero)
-        const float f = pend.x_ref == -INFINITY ? 0.f : exp2f(pend.x_ref - kE8Shift - pend.m_ref);
         if (J.part_slot < 0) {
-          const float inv = f / l_row;
-          __nv_bfloat16 *dst = out + ((int64_t)(J.q0 + j) * p.Hq + J.g * p.G + hg) * D + part * CB;
+          const float inv = 1.f / l_row;
+          const int64_t at = (int64_t)(J.q0 + row_j) * p.Hq + J.g * p.G + row_h;
+          __nv_bfloat16 *dst = out + at * D + col0;
 #pragma unroll
           for (int v = 0; v < CB / 8; ++v) {
             uint4 u;
@@ -579,144 +641,178 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
             u.w = pack_bf16(__uint_as_float(o[8 * v + 6]) * inv, __uint_as_float(o[8 * v + 7]) * inv);
             *reinterpret_cast<uint4 *>(dst + v * 8) = u;
           }
-          if (part == 0 && p.lse) p.lse[(int64_t)(J.q0 + j) * p.Hq + J.g * p.G + hg] = (pend.m_ref + log2f(l_row)) * kLn2;
+          if (col0 == 0 && p.lse) p.lse[at] = (ref - kE8Shift + log2f(l_row)) * kLn2;
         } else {
           const int64_t slot = (int64_t)J.part_slot * p.rows_cap + row;
-          float *dst = p.part_o + slot * D + part * CB;
+          float *dst = p.part_o + slot * D + col0;
 #pragma unroll
           for (int v = 0; v < CB / 4; ++v)
-            *reinterpret_cast<float4 *>(dst + v * 4) = make_float4(__uint_as_float(o[4 * v]) * f, __uint_as_float(o[4 * v + 1]) * f,
-                                                                  __uint_as_float(o[4 * v + 2]) * f, __uint_as_float(o[4 * v + 3]) * f);
-          if (part == 0) p.part_ml[slot] = make_float2(pend.m_ref, l_row);
+            *reinterpret_cast<uint4 *>(dst + v * 4) = make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
+          if (col0 == 0) p.part_ml[slot] = make_float2(ref - kE8Shift, l_row);
         }
       }
-      // the slot of the entry after next: its last user's epilogue lies at least one barrier back, its
-      // next user's first look at V at least one ahead
-      const int clear = (pend.qc + 2) % kE8NanSlots;
+      // the slot of the fourth entry from here: nobody can be that far ahead, nor still behind its last user
+      const int clear = (it + 4) % kE8NanSlots;
       if (sm_tid < 128) sNan[clear * 128 + sm_tid] = 0;
       if (sm_tid == 128) bars->nan_any[clear] = 0;
       pend.valid = false;
-      return true;
     };
+    // One step of the loop: this group's next tile of the current entry, if it has one, then the epilogue of
+    // the entry before, then, behind the entry's last tile, its sums and the next entry.
     WorkEntry e, e_next;
-    if (item_index(0) >= 0) e = p.work[item_index(0)];
-    for (int it = 0; item_index(it) >= 0 && ok; ++it, ++qc) {
-      if (bars->abort) break;
-      const int idx_next = item_index(it + 1);
-      if (idx_next >= 0) e_next = p.work[idx_next];
-      const bool valid_row = row < e.m * p.G;
-      float m_ref = -INFINITY, x_ref = -INFINITY, l_sum = 0.f, row_f = 0.f;   // the references are the same in all parts of a row
-      const int limit = e.L - e.m + row / p.G;  // last visible token of this row
-      for (int tile = e.tile_begin; tile < e.tile_end && ok; ++tile, ++tc_) {
-        const uint32_t b = tc_ & 1;
+    int it = 0;
+    bool have = item_index(0) >= 0;
+    if (have) e = p.work[item_index(0)];
+    if (item_index(1) >= 0) e_next = p.work[item_index(1)];
+    uint32_t t_first = 0;                          // the entry's first tile in the CTA's sequence
+    int tile = have ? e.tile_begin + grp : 0;
+    float x_ref = -INFINITY, l_sum = 0.f, row_f = 0.f;   // the reference is the same in all parts of a row
+    bool first = true;
+#pragma unroll 1
+    while (!bars->abort) {
+      // with a single pair of O's the entry's first value MMAs wait for the last epilogue, and the other
+      // group's may be what this tile's P waits for: nothing is deferred there
+      if (Cfg::kOBufs == 1 && pend.valid) run_epilogue();
+      if (have && tile < e.tile_end) {
+        const bool valid_row = row < e.m * p.G;
+        const int limit = e.L - e.m + row_j;         // last visible token of this row
+        const uint32_t tc_ = t_first + (uint32_t)(tile - e.tile_begin);
         const int sc_slot = tc_ % kE8ScaleSlots;
         const int t0 = tile * kTileTokens + part * TPT;  // first token of this thread
         const bool mask_tile = tile * kTileTokens + kTileTokens - 1 > e.L - e.m;
-        ok = warp_wait(&bars->sc_full[sc_slot], (tc_ / kE8ScaleSlots) & 1) && warp_wait(&bars->s_full[b], (tc_ >> 1) & 1);
-        if (!ok) break;
+        warp_wait(SPX_E8_BAR(sc_full, sc_slot), (tc_ / kE8ScaleSlots) & 1);
+        warp_wait(SPX_E8_BAR(s_full, grp), (tc_ >> 1) & 1);
         fence_after();
-        if (tile == e.tile_begin) row_f = sRow[(it % kE8RowSlots) * MROWS + row];
-        uint32_t r[TPT];
-        tmem_load<TPT>(tmem + Cfg::kColS + b * Cfg::kSCols + half * TPT + lane_addr, r);
-        wait_ld();
-        const float4 *ks4 = reinterpret_cast<const float4 *>(sKs + sc_slot * 128 + part * TPT);
-        const float4 *vs4 = reinterpret_cast<const float4 *>(sVs + sc_slot * 128 + part * TPT);
+        if (first) row_f = sRow[(it % kE8RowSlots) * MROWS + row];
+        // 32 tokens a thread stay in registers; more are taken in chunks of 32, twice (the scores stay in tensor memory)
+        constexpr int CH = 32, NCH = TPT / CH;
+        uint64_t v[CH / 2];
+        auto load_scores = [&](int ch) {
+          uint32_t r[CH];
+          tmem_load<CH>(tmem + Cfg::kColS + grp * Cfg::kSCols + ch * CH + lane_addr, r);
+          wait_ld();
+#pragma unroll
+          for (int i = 0; i < CH / 2; ++i) v[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+          const ulonglong2 *ks4 = reinterpret_cast<const ulonglong2 *>(sKs + sc_slot * 128 + part * TPT + ch * CH);
+#pragma unroll
+          for (int i = 0; i < CH / 4; ++i) {
+            const ulonglong2 s = ks4[i];
+            v[2 * i] = mul2(v[2 * i], s.x);
+            v[2 * i + 1] = mul2(v[2 * i + 1], s.y);
+          }
+          if (mask_tile) {
+#pragma unroll
+            for (int i = 0; i < CH / 2; ++i) {
+              float a, b;
+              unpair(v[i], a, b);
+              const int t = t0 + ch * CH + 2 * i;
+              v[i] = pair(t <= limit ? a : -INFINITY, t + 1 <= limit ? b : -INFINITY);
+            }
+          }
+        };
         const float2 v_range = sVr[sc_slot];
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < TPT / 4; ++i) {
-          const float4 s = ks4[i];
-          r[4 * i] = __float_as_uint(__uint_as_float(r[4 * i]) * s.x);
-          r[4 * i + 1] = __float_as_uint(__uint_as_float(r[4 * i + 1]) * s.y);
-          r[4 * i + 2] = __float_as_uint(__uint_as_float(r[4 * i + 2]) * s.z);
-          r[4 * i + 3] = __float_as_uint(__uint_as_float(r[4 * i + 3]) * s.w);
-        }
-        if (mask_tile) {
-#pragma unroll
-          for (int i = 0; i < TPT; ++i) r[i] = (t0 + i <= limit) ? r[i] : 0xff800000u;  // -inf
-        }
-#pragma unroll
-        for (int i = 0; i < TPT; ++i) mx = fmaxf(mx, __uint_as_float(r[i]));
-        // agree on the row's maxima over the whole tile
         const bool narrow = v_range.y != 0.f;
-        sMx[(b * kParts + part) * MROWS + row] = mx * row_f;
-        if (!narrow) {
-          float mx2 = -INFINITY;
-          const float *vs1 = reinterpret_cast<const float *>(vs4);
+        float mx = -INFINITY, mx2 = -INFINITY;
+#pragma unroll 1
+        for (int ch = 0; ch < NCH; ++ch) {
+          load_scores(ch);
 #pragma unroll
-          for (int i = 0; i < TPT; ++i) mx2 = fmaxf(mx2, fmaf(__uint_as_float(r[i]), row_f, fmaxf(__log2f(vs1[i]), kE8MinLog2)));
-          sMx2[(b * kParts + part) * MROWS + row] = mx2;
+          for (int i = 0; i < CH / 2; ++i) {
+            float a, b;
+            unpair(v[i], a, b);
+            mx = fmaxf(mx, fmaxf(a, b));
+          }
+          if (!narrow) {
+            const float *vs1 = sVs + sc_slot * 128 + part * TPT + ch * CH;
+#pragma unroll
+            for (int i = 0; i < CH / 2; ++i) {
+              float a, b;
+              unpair(v[i], a, b);
+              mx2 = fmaxf(mx2, fmaxf(fmaf(a, row_f, fmaxf(__log2f(vs1[2 * i]), kE8MinLog2)), fmaf(b, row_f, fmaxf(__log2f(vs1[2 * i + 1]), kE8MinLog2))));
+            }
+          }
         }
-        ok = softmax_sync();
-        if (!ok) break;
-        float m_tile = -INFINITY, x_tile = -INFINITY;
+        float x_tile = narrow ? fmaf(mx, row_f, v_range.x) : mx2;
+        if constexpr (kSplit > 1) {
+          // agree on the row's maximum over the whole tile
+          float *sm = sMx + ((ec & 1) ? 2 * 128 : 0) + grp * 128;
+          sm[part * MROWS + row] = x_tile;
+          __syncwarp();
+          if (lane == 0) arrive(SPX_E8_BAR(e_bar, grp));
+          warp_wait(SPX_E8_BAR(e_bar, grp), ec & 1);
+          ++ec;
+          x_tile = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) m_tile = fmaxf(m_tile, sMx[(b * kParts + i) * MROWS + row]);
-        if (narrow) {
-          x_tile = m_tile + v_range.x;
+          for (int i = 0; i < kSplit; ++i) x_tile = fmaxf(x_tile, sm[i * MROWS + row]);
         } else {
-#pragma unroll
-          for (int i = 0; i < kParts; ++i) x_tile = fmaxf(x_tile, sMx2[(b * kParts + i) * MROWS + row]);
+          x_tile = fmaxf(x_tile, -INFINITY);   // (no NaN)
         }
-        if (m_tile > m_ref) {
-          l_sum *= m_ref == -INFINITY ? 0.f : fast_exp2(m_ref - m_tile);
-          m_ref = m_tile;
-        }
-        // x's reference moves when it is passed by a factor of four; a row without one adopts the
-        // tile's (its O is zero)
+        // the reference moves when it is passed by a factor of sixteen; a row without one adopts the tile's
+        // (its O and its sum are zero)
         float alpha = 1.f;
-        bool need_scale = false;
         if (x_ref == -INFINITY) {
           x_ref = x_tile;
         } else if (x_tile > x_ref + kE8Rescale) {
           alpha = fast_exp2(x_ref - x_tile);
           x_ref = x_tile;
-          need_scale = valid_row;
+          l_sum *= alpha;
         }
-        if (__any_sync(0xffffffffu, need_scale)) {
-          // this warp's columns of O hold earlier tiles: wait for the last value MMA, scale
-          ok = warp_wait(&bars->pv_done[(tc_ - 1) & 1], ((tc_ - 1) >> 1) & 1);
-          if (!ok) break;
+        // this group's last value MMA: its P is rewritten, its O perhaps rescaled
+        if (tc_ >= 2) {
+          warp_wait(SPX_E8_BAR(pv_done, grp), ((tc_ - 2) >> 1) & 1);
+        }
+        if (Cfg::kPBufs == 1 && tc_ >= 1) {   // one P for both groups
+          warp_wait(SPX_E8_BAR(pv_done, grp ^ 1), ((tc_ - 1) >> 1) & 1);
+        }
+        if (__any_sync(0xffffffffu, valid_row && alpha != 1.f)) {
           fence_after();
-          uint32_t o[CB];
-          const uint32_t to = tmem + Cfg::kColO + (qc & 1) * Cfg::kOCols + half * CB + lane_addr;
-          tmem_load<CB>(to, o);
-          wait_ld();
+          const uint32_t to = tmem + Cfg::kColO + ((Cfg::kOBufs == 2 ? (it & 1) * 2 : 0) + grp) * Cfg::kOCols + lane_addr;
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            uint32_t o[CB];
+            tmem_load<CB>(to + h * CB, o);
+            wait_ld();
 #pragma unroll
-          for (int i = 0; i < CB; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-          tmem_store<CB>(to, o);
+            for (int i = 0; i < CB; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+            tmem_store<CB>(to + h * CB, o);
+          }
           wait_st();
         }
-        const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-        const float gain = x_ref == -INFINITY ? 0.f : fast_exp2(kE8Shift + m_use - x_ref);
-        // P's buffer is free once the value MMAs that read it last are done
-        if (tc_ >= (uint32_t)Cfg::kPBufs) {
-          const uint32_t u = tc_ - Cfg::kPBufs;
-          ok = warp_wait(&bars->pv_done[u & 1], (u >> 1) & 1);
-          if (!ok) break;
-        }
-        unsigned char *pr = sP + (Cfg::kPBufs == 2 ? b : 0) * 3 * Cfg::kPiece + (row >> 3) * 1024 + (row & 7) * 128;
-        float sum = 0.f;
+        const float shift = x_ref == -INFINITY ? 0.f : kE8Shift - x_ref;
+        unsigned char *pr = sP + (Cfg::kPBufs == 2 ? grp : 0) * 3 * Cfg::kPiece + (row >> 3) * 1024 + (row & 7) * 128;
+        const uint64_t row_f2 = pair(row_f, row_f), shift2 = pair(shift, shift);
+        uint64_t sum2 = 0;
+#pragma unroll 1
+        for (int ch = 0; ch < NCH; ++ch) {
+          if (NCH > 1) load_scores(ch);
+          const ulonglong2 *vs4 = reinterpret_cast<const ulonglong2 *>(sVs + sc_slot * 128 + part * TPT + ch * CH);
 #pragma unroll
-        for (int c = 0; c < TPT / 16; ++c) {
-          uint32_t w[3][4];
+          for (int c = 0; c < CH / 16; ++c) {
+            uint32_t w[3][4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 s = vs4[4 * c + i];
-            const int at = 16 * c + 4 * i;
-            const float p0 = fast_exp2(fmaf(__uint_as_float(r[at]), row_f, -m_use));
-            const float p1 = fast_exp2(fmaf(__uint_as_float(r[at + 1]), row_f, -m_use));
-            const float p2 = fast_exp2(fmaf(__uint_as_float(r[at + 2]), row_f, -m_use));
-            const float p3 = fast_exp2(fmaf(__uint_as_float(r[at + 3]), row_f, -m_use));
-            sum += (p0 + p1) + (p2 + p3);
-            cut3(pack_f16(p0 * s.x * gain, p1 * s.y * gain), pack_f16(p2 * s.z * gain, p3 * s.w * gain), w[0][i], w[1][i], w[2][i]);
+            for (int i = 0; i < 4; ++i) {
+              const ulonglong2 s = vs4[4 * c + i];
+              uint32_t h[2];
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                float y0, y1;
+                unpair(fma2(v[8 * c + 2 * i + u], row_f2, shift2), y0, y1);
+                const uint64_t y = pair(fast_exp2(y0), fast_exp2(y1));
+                sum2 = add2(sum2, y);
+                unpair(mul2(y, u ? s.y : s.x), y0, y1);
+                h[u] = pack_f16(y0, y1);
+              }
+              cut3(h[0], h[1], w[0][i], w[1][i], w[2][i]);
+            }
+            const int chunk = (part * TPT + ch * CH) / 16 + c;   // 16-byte chunk of the row: 16 tokens
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+              *reinterpret_cast<uint4 *>(pr + i * Cfg::kPiece + ((chunk ^ (row & 7)) << 4)) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
           }
-          const int chunk = part * (TPT / 16) + c;   // 16-byte chunk of the row: 16 tokens
-#pragma unroll
-          for (int i = 0; i < 3; ++i)
-            *reinterpret_cast<uint4 *>(pr + i * Cfg::kPiece + ((chunk ^ (row & 7)) << 4)) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
         }
-        l_sum += sum;
+        float sum_lo, sum_hi;
+        unpair(sum2, sum_lo, sum_hi);
+        l_sum += sum_lo + sum_hi;
         if (mask_tile) {
           // V at the end of the request, as its value MMA must see it: slots past the end are zero (they
           // hold an earlier tile's or nobody's bytes, and 0 * NaN is NaN), and a NaN at a position that some
@@ -724,54 +820,61 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           const int ntok = min(kTileTokens, e.L - tile * kTileTokens);
           const int hidden = max(0, e.L - e.m + 1 - tile * kTileTokens);   // first token of the tile not seen by every row
           const int slot = tc_ % Cfg::kStages;
-          ok = warp_wait(&bars->v_full[slot], (tc_ / Cfg::kStages) & 1);
-          if (!ok) break;
+          warp_wait(SPX_E8_BAR(v_full, slot), (tc_ / Cfg::kStages) & 1);
           unsigned char *vt = sV + slot * Cfg::kTileBytes;
 #pragma unroll 1
-          for (int i = sm_tid; i < (kTileTokens - ntok) * (D / 16); i += 256)
+          for (int i = g_tid; i < (kTileTokens - ntok) * (D / 16); i += 128)
             *reinterpret_cast<uint4 *>(vt + ntok * D + i * 16) = make_uint4(0, 0, 0, 0);
 #pragma unroll 1
-          for (int i = sm_tid; i < (ntok - hidden) * (D / 16); i += 256) {
+          for (int i = g_tid; i < (ntok - hidden) * (D / 16); i += 128) {
             const int tok = hidden + i / (D / 16), ch = i % (D / 16);
             uint4 *at = reinterpret_cast<uint4 *>(vt + tok * D + ch * 16);
-            uint4 v = *at;
-            uint32_t *w = &v.x;
-            uint32_t any = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) any |= __vcmpeq4(w[k] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+            const uint4 v = *at;
+            const uint32_t any = __vcmpeq4(v.x & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v.y & 0x7f7f7f7fu, 0x7f7f7f7fu) |
+                                 __vcmpeq4(v.z & 0x7f7f7f7fu, 0x7f7f7f7fu) | __vcmpeq4(v.w & 0x7f7f7f7fu, 0x7f7f7f7fu);
             if (any) {
               // logical columns of this chunk under the swizzle
               const int col = (D == 128 ? ch ^ (tok & 7) : ch ^ ((tok >> 1) & 3)) * 16;
               const uint32_t bit = 1u << (tile * kTileTokens + tok - (e.L - e.m + 1));   // rows j > this position's index see it
+              unsigned char *bytes = reinterpret_cast<unsigned char *>(at);
 #pragma unroll 1
               for (int k = 0; k < 16; ++k)
-                if (((w[k >> 2] >> (8 * (k & 3))) & 0x7f) == 0x7f) {
-                  w[k >> 2] &= ~(0xffu << (8 * (k & 3)));
-                  atomicOr(&sNan[(qc % kE8NanSlots) * 128 + col + k], bit);
+                if ((bytes[k] & 0x7f) == 0x7f) {
+                  bytes[k] = 0;
+                  atomicOr(&sNan[(it % kE8NanSlots) * 128 + col + k], bit);
                 }
-              *at = v;
-              bars->nan_any[qc % kE8NanSlots] = 1;
+              bars->nan_any[it % kE8NanSlots] = 1;
             }
           }
         }
         fence_async_smem();
         fence_before();
         __syncwarp();
-        if (lane == 0) { mbar_arrive(&bars->p_full[b]); mbar_arrive(&bars->sc_empty[sc_slot]); }
-        if (pend.valid) ok = run_epilogue();  // previous entry (its sL became visible at this tile's barrier)
+        if (lane == 0) { arrive(SPX_E8_BAR(p_full, grp)); arrive(SPX_E8_BAR(sc_empty, sc_slot)); }
+        first = false;
+        tile += 2;
       }
-      if (!ok) break;
-      // the entry's epilogue is deferred: it runs after the first tile of the next one
-      sL[((qc & 1) * kParts + part) * MROWS + row] = l_sum;
-      pend.valid = true; pend.e = e; pend.m_ref = m_ref; pend.x_ref = x_ref; pend.last_tc = tc_ - 1; pend.qc = qc;
-      e = e_next;
-    }
-    if (ok && pend.valid && !bars->abort) {
-      ok = softmax_sync();  // make the last entry's row sums visible
-      if (ok) ok = run_epilogue();
+      if (Cfg::kOBufs == 2 && pend.valid) run_epilogue();
+      if (!have) break;
+      if (tile >= e.tile_end) {
+        sL[(it & 1) * 256 + grp * 128 + part * MROWS + row] = l_sum;
+        if (part == 0) sRef[(it & 1) * 2 * MROWS + grp * MROWS + row] = x_ref;
+        __syncwarp();
+        if (lane == 0) arrive(SPX_E8_BAR(item_done, it & 1));
+        pend.valid = true; pend.e = e; pend.t_first = t_first; pend.it = it;
+        t_first += (uint32_t)(e.tile_end - e.tile_begin);
+        ++it;
+        have = item_index(it) >= 0;
+        e = e_next;
+        if (item_index(it + 1) >= 0) e_next = p.work[item_index(it + 1)];
+        if (have) tile = e.tile_begin + (int)((t_first ^ (uint32_t)grp) & 1);
+        x_ref = -INFINITY; l_sum = 0.f;
+        first = true;
+      }
     }
   }
 
+#undef SPX_E8_BAR
   // ---------------------------------------------------------------------- teardown
   __syncwarp();
   if (bars->abort) {
