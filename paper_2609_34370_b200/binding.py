@@ -538,7 +538,7 @@ def token_logprobs(logits, token_ids=None, top_n: int = 0, vocab=None, want_entr
     a.rows, a.vocab, a.top_n = rows, int(vocab if vocab is not None else logits.shape[1]), int(top_n)
     if a.vocab > logits.shape[1]:
         raise SpxError(ERR_INVALID_ARG, "vocab exceeds the logits' columns")
-    a.logits_row_stride = logits.stride(0) if rows > 1 else -(-a.vocab // 8) * 8
+    a.logits_row_stride = logits.stride(0) if rows else -(-a.vocab // 8) * 8
     a.logits_dtype, a.logits = _dtype_code(logits), _ptr(logits)
     if token_ids is not None:
         if token_ids.dtype != torch.int32 or token_ids.numel() != rows or not token_ids.is_contiguous():

@@ -1,40 +1,270 @@
 // Log-probabilities of given tokens, row entropies and top alternatives.
+//
+// With m the row's largest logit, lse = m + log(1 + rest), rest = sum_v e^(x_v - m) without one of the
+// largest, and the entropy is log(1 + rest) - E[x - m].  The alternatives are the top_n by (logit, -id).
+//
+// One pass over the logits: a bulk-copy ring feeds warps that each reduce 4 KB of a row (a sub-segment:
+// 2048 bf16 or 1024 fp32 logits) to its maximum, sum e^(x - M), sum e^(x - M) (x - M), and to the maxima of
+// its 32 lanes' shares (a group: 64 or 32 logits).  A block per row then merges the sub-segments in 64 bits
+// and finds the alternatives from the group maxima: the n-th largest sub-segment maximum bounds the n-th
+// largest logit from below, so only groups whose maximum reaches it are read again (some 30 of 2016
+// for 20 of 128,256).  Bound by HBM: 16 exponentials a cycle and SM are 72% busy at its full rate on bf16 rows.
 #pragma once
+#include "attn_e4m3.cuh"   // e8::pair and the packed fp32 arithmetic
 #include "common.cuh"
+#include "sampler.cuh"     // ring_wait
 
 namespace spx {
 
+constexpr int kLpSubBytes = 4096;                   // a sub-segment: one warp, 8 16-byte vectors a lane
+constexpr int kLpStageSubs = 8;                     // sub-segments of a full ring stage
+constexpr int kLpStages = 6;
+constexpr int kLpGroups = 2;                        // groups of 8 consumer warps, each takes every second chunk
+constexpr int kLpThreads = (kLpGroups * kLpStageSubs + 1) * 32;
+constexpr int kLpSmemBytes = kLpStages * kLpStageSubs * kLpSubBytes + 1024 + 256;
+constexpr int kLpTailThreads = 128;
+constexpr int kLpMaxCand = 128;                     // groups looked at again in the common case
+constexpr int kLpMaxList = 2048;                    // candidates: at least 31 groups of 64 and 32 more
+
 struct LogprobParams {
   int32_t rows, vocab, top_n;
+  int32_t nsub;             // sub-segments of a row
+  int32_t chunk_subs;       // sub-segments of a ring stage: fewer than 8 when there are few rows
+  int32_t chunks_per_row, n_chunks;
   int64_t row_stride;
   const void *logits;
   const int32_t *token_ids;
   float *logprobs, *entropy, *top_logprobs;
   int32_t *top_ids;
+  float4 *seg;              // [rows][nsub]: maximum, sum, sum of products (log2 units)
+  void *group_max;          // [rows][nsub][32] of the logits' type
   int32_t *dev_status;
 };
 
-constexpr int kLogprobThreads = 256;
-
 // Order of the alternatives, as an unsigned key: larger logits first, equal ones (-0 and +0 too) alike,
-// NaN above +inf.
-__device__ __forceinline__ uint32_t logit_key(float x) {
+// NaN above +inf.  16 bits hold a bf16 logit's.
+__device__ __forceinline__ uint32_t logit_key32(float x) {
   if (x != x) return 0xffffffffu;
   const uint32_t u = __float_as_uint(x + 0.f);   // -0 becomes +0
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
-
-// One block per row.
 template <typename T>
-__global__ void __launch_bounds__(kLogprobThreads) logprob_kernel(LogprobParams p) {
+__device__ __forceinline__ uint32_t logit_key(float x) { return sizeof(T) == 2 ? logit_key32(x) >> 16 : logit_key32(x); }
+
+template <typename T> struct LpVec;
+template <> struct LpVec<__nv_bfloat16> {
+  static constexpr int N = 8;                     // logits of a vector
+  static constexpr int kSub = kLpSubBytes / 2;
+  // the vector with the logits from `valid` on as -inf
+  __device__ static uint4 cut(uint4 v, int valid) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (2 * j >= valid) w[j] = (w[j] & 0xffff0000u) | 0xff80u;
+      if (2 * j + 1 >= valid) w[j] = (w[j] & 0x0000ffffu) | 0xff800000u;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ static uint32_t max_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  __device__ static float lane_max(const uint4 (&v)[8]) {
+    uint32_t m = v[0].x;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) m = max_nan(m, max_nan(max_nan(v[c].x, v[c].y), max_nan(v[c].z, v[c].w)));
+    m = max_nan(m, m >> 16 | m << 16);
+    return __uint_as_float(m << 16);
+  }
+  // pair i of the vector's logits, those below `floor` raised to it
+  __device__ static uint64_t pair_of(const uint4 &v, int i, uint32_t floor2) {
+    const uint32_t w = max_nan(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w, floor2);
+    return e8::pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+  __device__ static uint32_t floor_bits(float f) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(f, f);
+    return *reinterpret_cast<const uint32_t *>(&b);
+  }
+  __device__ static float at(const uint4 &v, int i) {
+    const uint32_t w = (i >> 1) == 0 ? v.x : (i >> 1) == 1 ? v.y : (i >> 1) == 2 ? v.z : v.w;
+    return __uint_as_float((i & 1) ? w & 0xffff0000u : w << 16);
+  }
+};
+template <> struct LpVec<float> {
+  static constexpr int N = 4;
+  static constexpr int kSub = kLpSubBytes / 4;
+  __device__ static uint4 cut(uint4 v, int valid) {
+    return make_uint4(valid > 0 ? v.x : 0xff800000u, valid > 1 ? v.y : 0xff800000u, valid > 2 ? v.z : 0xff800000u, valid > 3 ? v.w : 0xff800000u);
+  }
+  __device__ static float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+  }
+  __device__ static float lane_max(const uint4 (&v)[8]) {
+    float m = __uint_as_float(v[0].x);
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      m = max_nan(m, max_nan(max_nan(__uint_as_float(v[c].x), __uint_as_float(v[c].y)), max_nan(__uint_as_float(v[c].z), __uint_as_float(v[c].w))));
+    return m;
+  }
+  __device__ static uint64_t pair_of(const uint4 &v, int i, uint32_t floor2) {
+    const float f = __uint_as_float(floor2);
+    return i == 0 ? e8::pair(max_nan(__uint_as_float(v.x), f), max_nan(__uint_as_float(v.y), f))
+                  : e8::pair(max_nan(__uint_as_float(v.z), f), max_nan(__uint_as_float(v.w), f));
+  }
+  __device__ static uint32_t floor_bits(float f) { return __float_as_uint(f); }
+  __device__ static float at(const uint4 &v, int i) { return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
+};
+
+// grid: one CTA per SM at most; chunk g of the list (row, share of the row) goes to CTA g % gridDim.x.
+template <typename T>
+__global__ void __launch_bounds__(kLpThreads, 1) logprob_stats_kernel(LogprobParams p) {
+  using V = LpVec<T>;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge kernel's blocks may take their places
+  extern __shared__ __align__(1024) unsigned char lp_smem[];
+  unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(lp_smem) + 1023) & ~uintptr_t(1023));
+  uint64_t *full = reinterpret_cast<uint64_t *>(stages + kLpStages * kLpStageSubs * kLpSubBytes);
+  uint64_t *empty = full + kLpStages;
+  volatile int *abort = reinterpret_cast<volatile int *>(empty + kLpStages);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kLpStages; ++s) {
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&full[s])), "r"(1));
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(&empty[s])), "r"(kLpStageSubs));
+    }
+    *abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  const T *logits = reinterpret_cast<const T *>(p.logits);
+  const int chunk_elems = p.chunk_subs * V::kSub;
+  // rows without a token are not read
+  auto token_of = [&](int g) -> int { return p.token_ids ? p.token_ids[g / p.chunks_per_row] : 0; };
+  auto counts = [&](int tok) -> bool { return tok >= 0 && tok < p.vocab; };
+  if (warp == kLpGroups * kLpStageSubs) {
+    // ---- producer (one thread)
+    if (lane == 0) {
+      int i = 0;
+      int tok_next = (int)blockIdx.x < p.n_chunks ? token_of(blockIdx.x) : 0;
+      for (int g = blockIdx.x; g < p.n_chunks; g += gridDim.x, ++i) {
+        const int tok = tok_next;
+        if (g + (int)gridDim.x < p.n_chunks) tok_next = token_of(g + gridDim.x);   // off the issue path
+        const int s = i % kLpStages;
+        if (i >= kLpStages && !ring_wait(&empty[s], ((i / kLpStages) - 1) & 1, abort, p.dev_status)) break;
+        const int row = g / p.chunks_per_row, e0 = (g % p.chunks_per_row) * chunk_elems;
+        const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&full[s]);
+        if (!counts(tok)) {
+          // handed over empty, the consumers release it at once
+          asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+          continue;
+        }
+        const int elems = min(chunk_elems, p.vocab - e0);
+        const uint32_t bytes = (uint32_t)((elems * (int)sizeof(T) + 15) & ~15);  // stays inside the row: its stride is a multiple of 16 bytes
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     ::"r"((uint32_t)__cvta_generic_to_shared(stages + (size_t)s * kLpStageSubs * kLpSubBytes)),
+                       "l"(logits + (int64_t)row * p.row_stride + e0), "r"(bytes), "r"(bar) : "memory");
+      }
+    }
+  } else {
+    // ---- consumers: group `grp` takes chunks grp, grp + kLpGroups, ...; its warp w reduces sub-segment w
+    const int grp = warp / kLpStageSubs, wsub = warp % kLpStageSubs;
+    int i = grp;
+    for (int g = blockIdx.x + grp * gridDim.x; g < p.n_chunks; g += kLpGroups * gridDim.x, i += kLpGroups) {
+      const int s = i % kLpStages;
+      const int row = g / p.chunks_per_row, sub = (g % p.chunks_per_row) * p.chunk_subs + wsub;
+      const int tok = token_of(g);   // in flight while the stage fills
+      const bool ok = __all_sync(0xffffffffu, ring_wait(&full[s], (i / kLpStages) & 1, abort, p.dev_status));
+      if (!ok) break;
+      const bool mine = wsub < p.chunk_subs && sub < p.nsub && counts(tok);
+      uint4 v[8];
+      if (mine) {
+        const uint4 *src = reinterpret_cast<const uint4 *>(stages + (size_t)(s * kLpStageSubs + wsub) * kLpSubBytes);
+        const int left = p.vocab - sub * V::kSub;   // logits of the row from this sub-segment on
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          v[c] = src[c * 32 + lane];
+          const int at = (c * 32 + lane) * V::N;
+          if (at + V::N > left) v[c] = V::cut(v[c], left - at);   // past the vocabulary: never copied, or the row's padding
+        }
+      }
+      __syncwarp();
+      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"((uint32_t)__cvta_generic_to_shared(&empty[s])) : "memory");
+      if (!mine) continue;
+      const float lm = V::lane_max(v);
+      const int64_t at = (int64_t)row * p.nsub + sub;
+      st_from_float(reinterpret_cast<T *>(p.group_max), at * 32 + lane, lm);
+      const bool nan = __any_sync(0xffffffffu, lm != lm);
+      const float M = warp_max(lm);
+      float S, P;
+      if (nan || M == INFINITY) {
+        S = P = __int_as_float(0x7fc00000);   // the row has no finite sum
+      } else if (M == -INFINITY) {
+        S = P = 0.f;
+      } else if (M < -1e37f) {
+        // a row of the types' lowest values: the floor below has no room under them
+        S = P = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < 8; ++c)
+          for (int k = 0; k < V::N; ++k) {
+            uint4 w = v[0];
+#pragma unroll
+            for (int u = 1; u < 8; ++u) w = c == u ? v[u] : w;
+            const float t = fmaxf((V::at(w, k) - M) * kLog2e, -400.f), e = fast_exp2(t);
+            S += e;
+            P = fmaf(e, t, P);
+          }
+        S = warp_sum(S);
+        P = warp_sum(P);
+      } else {
+        // logits more than 256 below the maximum (-inf among them) add nothing: they are raised to that, so that no
+        // product is 0 * inf
+        const uint32_t floor2 = V::floor_bits(M - fmaxf(256.f, fabsf(M) * 0.015625f));
+        const uint64_t minus_m = e8::pair(-M, -M), log2e = e8::pair(kLog2e, kLog2e);
+        uint64_t sum = 0, prod = 0;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int k = 0; k < V::N / 2; ++k) {
+            const uint64_t t = e8::mul2(e8::add2(V::pair_of(v[c], k, floor2), minus_m), log2e);
+            float a, b;
+            e8::unpair(t, a, b);
+            const uint64_t e = e8::pair(fast_exp2(a), fast_exp2(b));
+            sum = e8::add2(sum, e);
+            prod = e8::fma2(e, t, prod);
+          }
+        float a, b;
+        e8::unpair(sum, a, b);
+        S = warp_sum(a + b);
+        e8::unpair(prod, a, b);
+        P = warp_sum(a + b);
+      }
+      if (lane == 0) p.seg[at] = make_float4(nan ? __int_as_float(0x7fc00000) : M, S, P, 0.f);
+    }
+  }
+}
+
+// One block per row: merge, then the alternatives.
+template <typename T>
+__global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobParams p) {
+  using V = LpVec<T>;
+  constexpr int kThreads = kLpTailThreads, kWarps = kThreads / 32, kKeyBits = sizeof(T) * 8;
+  __shared__ float s_f[kWarps];
+  __shared__ double s_d[2][kWarps];
+  __shared__ int s_i[kWarps];
+  __shared__ int s_cand_n, s_list_n;
+  __shared__ int s_cand[kLpMaxCand];
+  __shared__ uint2 s_list[kLpMaxList];   // (key, ~id)
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  __shared__ float s_max[kLogprobThreads / 32];
-  __shared__ double s_a[kLogprobThreads / 32], s_b[kLogprobThreads / 32];
-  __shared__ int s_n[kLogprobThreads / 32];
-  __shared__ unsigned long long s_k[kLogprobThreads / 32];
   const int tok = p.token_ids ? p.token_ids[row] : 0;
   const float nan = __int_as_float(0x7fc00000);
-  if (tok < 0 || tok >= p.vocab) {
+  const T *x = reinterpret_cast<const T *>(p.logits) + (int64_t)row * p.row_stride;
+  const bool counted = tok >= 0 && tok < p.vocab;
+  const float x_tok = counted ? ld_as_float(x, tok) : 0.f;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // the statistics are read from here on
+  if (!counted) {
     if (tid == 0) {
       if (p.logprobs) p.logprobs[row] = nan;
       if (p.entropy) p.entropy[row] = nan;
@@ -46,52 +276,189 @@ __global__ void __launch_bounds__(kLogprobThreads) logprob_kernel(LogprobParams 
     }
     return;
   }
-  const T *x = reinterpret_cast<const T *>(p.logits) + row * p.row_stride;
-  float m = -INFINITY;
-  for (int v = tid; v < p.vocab; v += kLogprobThreads) m = fmaxf(m, ld_as_float(x, v));
+  const float4 *seg = p.seg + (int64_t)row * p.nsub;
+  const T *gmax = reinterpret_cast<const T *>(p.group_max) + (int64_t)row * p.nsub * 32;
+
+  // ---- the row's maximum, and whether it has finite sums
+  const float4 seg0 = tid < p.nsub ? seg[tid] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  float m = seg0.x;
+  bool bad = seg0.x != seg0.x || seg0.x == INFINITY;
+  for (int i = tid + kThreads; i < p.nsub; i += kThreads) {
+    const float f = seg[i].x;
+    bad |= f != f || f == INFINITY;
+    m = fmaxf(m, f);
+  }
   m = warp_max(m);
-  if (lane == 0) s_max[warp] = m;
-  __syncthreads();
-  for (int w = 0; w < kLogprobThreads / 32; ++w) m = fmaxf(m, s_max[w]);
-  double z = 0.0, s = 0.0;   // sum of e^(x - m) without the m's own ones, sum of e^(x - m) (x - m)
-  int n_max = 0;
-  for (int v = tid; v < p.vocab; v += kLogprobThreads) {
-    const float d = ld_as_float(x, v) - m;
-    if (d == 0.f) { ++n_max; continue; }
-    const float e = expf(d);
-    z += e;
-    if (!(e == 0.f)) s += (double)e * d;
+  if (lane == 0) s_f[warp] = m;
+  bad = __syncthreads_or(bad);
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s_f[w]);
+  bad |= m == -INFINITY;
+  // ---- rest = sum e^(x - m) without one of the largest, and sum e^(x - m) (x - m), in 64 bits.  top: the first
+  // sub-segment that holds the maximum
+  double rest = 0.0, prod = 0.0, top_sum = 0.0;
+  int top = 0x7fffffff;
+  if (!bad) {
+    for (int i = tid; i < p.nsub; i += kThreads) {
+      const float4 f = i == tid ? seg0 : seg[i];
+      if (f.x == -INFINITY) continue;
+      const double d = (double)f.x - m;
+      const double w = d == 0.0 ? 1.0 : (double)expf((float)d);
+      prod += w * ((double)f.z * 0.6931471805599453 + (double)f.y * d);
+      if (d == 0.0 && top == 0x7fffffff) { top = i; top_sum = f.y; }   // (a thread's first)
+      else rest += w * f.y;
+    }
   }
-  n_max = __reduce_add_sync(0xffffffffu, n_max);
-  for (int o = 16; o > 0; o >>= 1) { z += __shfl_xor_sync(0xffffffffu, z, o); s += __shfl_xor_sync(0xffffffffu, s, o); }
-  if (lane == 0) { s_a[warp] = z; s_b[warp] = s; s_n[warp] = n_max; }
+  const int top_mine = top;
+  top = __reduce_min_sync(0xffffffffu, top);
+  if (lane == 0) s_i[warp] = top;
   __syncthreads();
-  z = 0.0; s = 0.0; n_max = -1;   // the largest logit's own 1 is left to log1p
-  for (int w = 0; w < kLogprobThreads / 32; ++w) { z += s_a[w]; s += s_b[w]; n_max += s_n[w]; }
-  z += n_max;
-  const double log_z = log1p(z);
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) top = min(top, s_i[w]);
+  const bool owns = top_mine == top && top != 0x7fffffff;
+  if (top_mine != 0x7fffffff && !owns) rest += top_sum;   // holds the maximum too, but not first
+  auto block_sum2 = [&](double &a, double &b) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); b += __shfl_xor_sync(0xffffffffu, b, o); }
+    __syncthreads();
+    if (lane == 0) { s_d[0][warp] = a; s_d[1][warp] = b; }
+    __syncthreads();
+    a = b = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) { a += s_d[0][w]; b += s_d[1][w]; }
+  };
+  double log_z = 0.0;
+  if (!bad) {
+    double others = rest, unused = owns ? top_sum : 0.0;
+    block_sum2(others, prod);
+    double with_top = unused, none = 0.0;
+    block_sum2(with_top, none);
+    rest = others + with_top - 1.0;
+    if (rest < 0.125) {
+      // near-certain row: the sub-segment's fp32 sum has rounded its share of the rest against the maximum's 1;
+      // add it up again without that
+      double a = 0.0, n_max = 0.0;
+      const int e0 = top * V::kSub;
+      for (int i = tid; i < V::kSub && e0 + i < p.vocab; i += kThreads) {
+        const float d = ld_as_float(x, e0 + i) - m;
+        if (d == 0.f) n_max += 1.0;
+        else a += (double)expf(d);
+      }
+      block_sum2(a, n_max);
+      rest = others + a + (n_max - 1.0);
+    }
+    log_z = log1p(rest);
+  }
   if (tid == 0) {
-    if (p.logprobs) p.logprobs[row] = (float)((double)ld_as_float(x, tok) - m - log_z);
-    if (p.entropy) p.entropy[row] = (float)(log_z - s / (1.0 + z));
+    if (p.logprobs) p.logprobs[row] = bad ? nan : (float)((double)x_tok - m - log_z);
+    if (p.entropy) p.entropy[row] = bad ? nan : (float)(log_z - prod / (1.0 + rest));
   }
-  unsigned long long last = ~0ull;   // (key, ~id) of the alternative before
-  for (int j = 0; j < p.top_n; ++j) {
-    unsigned long long best = 0;
-    for (int v = tid; v < p.vocab; v += kLogprobThreads) {
-      const unsigned long long c = ((unsigned long long)logit_key(ld_as_float(x, v)) << 32) | (uint32_t)~v;
-      if (c < last && c > best) best = c;
+  const int n = p.top_n;
+  if (n == 0) return;
+
+  // ---- the alternatives
+  // the k-th largest of count(i)'s keys, i < total (or a key that exactly k reach): bit by bit from the top
+  auto kth_largest = [&](int total, int k, auto key_of) -> uint32_t {
+    uint32_t thr = 0;
+    for (int bit = kKeyBits - 1; bit >= 0; --bit) {
+      const uint32_t cand = thr | (1u << bit);
+      int count = 0;
+      for (int i0 = 0; i0 < total; i0 += kThreads) count += __syncthreads_count(i0 + tid < total && key_of(i0 + tid) >= cand);
+      if (count >= k) {
+        thr = cand;
+        if (count == k) break;
+      }
     }
-    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    __syncthreads();
-    if (lane == 0) s_k[warp] = best;
-    __syncthreads();
-    for (int w = 0; w < kLogprobThreads / 32; ++w) best = max(best, s_k[w]);
-    last = best;
-    const int id = best ? (int)~(uint32_t)best : -1;
-    if (tid == 0) {
-      if (p.top_ids) p.top_ids[(int64_t)row * p.top_n + j] = id;
-      if (p.top_logprobs) p.top_logprobs[(int64_t)row * p.top_n + j] = id < 0 ? nan : (float)((double)ld_as_float(x, id) - m - log_z);
+    return thr;
+  };
+  if (tid == 0) { s_cand_n = 0; s_list_n = 0; }
+  const int n_groups = p.nsub * 32;
+  const uint32_t key0 = logit_key<T>(seg0.x);
+  auto seg_key = [&](int i) -> uint32_t { return i == tid ? key0 : logit_key<T>(seg[i].x); };
+  auto group_key = [&](int i) -> uint32_t { return logit_key<T>(ld_as_float(gmax, i)); };
+  const uint32_t floor_key = p.nsub >= n ? kth_largest(p.nsub, n, seg_key) : kth_largest(n_groups, n, group_key);
+  __syncthreads();
+  for (int i = tid; i < n_groups; i += kThreads)
+    if (group_key(i) >= floor_key) {
+      const int at = atomicAdd(&s_cand_n, 1);
+      if (at < kLpMaxCand) s_cand[at] = i;
     }
+  __syncthreads();
+  // every logit of the listed groups for which take(key) holds, behind the list's end
+  auto gather = [&](int n_cand, auto take) {
+    for (int i = tid; i < n_cand * 8; i += kThreads) {
+      const int g = s_cand[i >> 3], c = i & 7;
+      const int e0 = (g >> 5) * V::kSub + (c * 32 + (g & 31)) * V::N;
+      if (e0 >= p.vocab) continue;
+      const uint4 v = *reinterpret_cast<const uint4 *>(x + e0);
+#pragma unroll
+      for (int k = 0; k < V::N; ++k) {
+        const uint32_t key = logit_key<T>(V::at(v, k));
+        if (e0 + k < p.vocab && take(key)) {
+          const int at = atomicAdd(&s_list_n, 1);
+          if (at < kLpMaxList) s_list[at] = make_uint2(key, ~(uint32_t)(e0 + k));
+        }
+      }
+    }
+    __syncthreads();
+  };
+  bool listed = s_cand_n <= kLpMaxCand;
+  if (listed) {
+    gather(s_cand_n, [&](uint32_t key) { return key >= floor_key; });
+    listed = s_list_n <= kLpMaxList;
+  }
+  if (!listed) {
+    // ties by the hundred (a masked or constant row): with thr the n-th largest group maximum at most n - 1 groups
+    // lie above it, and all their logits above thr fit the list; the ones equal to it are taken by ascending id
+    const uint32_t thr = kth_largest(n_groups, n, group_key);
+    // (kth_largest may stop at a key that exactly n groups reach: then it is no group's and nothing ties with it)
+    __syncthreads();
+    if (tid == 0) { s_cand_n = 0; s_list_n = 0; }
+    __syncthreads();
+    for (int i = tid; i < n_groups; i += kThreads)
+      if (group_key(i) > thr) {
+        const int at = atomicAdd(&s_cand_n, 1);
+        if (at < kLpMaxCand) s_cand[at] = i;
+      }
+    __syncthreads();
+    gather(min(s_cand_n, kLpMaxCand), [&](uint32_t key) { return key > thr; });
+    int have = s_list_n;
+    for (int e0 = 0; have < n && e0 < p.vocab; e0 += kThreads) {
+      const int e = e0 + tid;
+      const bool tie = e < p.vocab && logit_key<T>(ld_as_float(x, e)) == thr;
+      const uint32_t ballot = __ballot_sync(0xffffffffu, tie);
+      __syncthreads();
+      if (lane == 0) s_i[warp] = __popc(ballot);
+      __syncthreads();
+      int before = have, all = 0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) { before += w < warp ? s_i[w] : 0; all += s_i[w]; }
+      before += __popc(ballot & ((1u << lane) - 1));
+      if (tie && before < n) s_list[before] = make_uint2(thr, ~(uint32_t)e);
+      have += all;
+    }
+    __syncthreads();
+    if (tid == 0) s_list_n = min(have, max(n, s_list_n));
+    __syncthreads();
+  }
+  // ---- rank the candidates
+  const int total = min(s_list_n, kLpMaxList);
+  for (int i = tid; i < total; i += kThreads) {
+    const uint2 me = s_list[i];
+    int rank = 0;
+    for (int j = 0; j < total && rank < n; ++j) {
+      const uint2 o = s_list[j];
+      rank += o.x > me.x || (o.x == me.x && o.y > me.y);
+    }
+    if (rank < n) {
+      const int id = (int)~me.y;
+      if (p.top_ids) p.top_ids[(int64_t)row * n + rank] = id;
+      if (p.top_logprobs) p.top_logprobs[(int64_t)row * n + rank] = bad ? nan : (float)((double)ld_as_float(x, id) - m - log_z);
+    }
+  }
+  if (tid >= total && tid < n) {   // fewer logits than alternatives
+    if (p.top_ids) p.top_ids[(int64_t)row * n + tid] = -1;
+    if (p.top_logprobs) p.top_logprobs[(int64_t)row * n + tid] = nan;
   }
 }
 

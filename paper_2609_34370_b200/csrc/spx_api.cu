@@ -14,12 +14,12 @@
 #include "common.cuh"
 #include "kv_cache.cuh"
 #include "kv_cache_e4m3.cuh"
-#include "logprob.cuh"
 #include "select.cuh"
 #include "lookahead.cuh"
 #include "lm_head.cuh"
 #include "plan.cuh"
 #include "sampler.cuh"
+#include "logprob.cuh"
 #include "spx.h"
 #if SPX_WAIT_TEST
 #include "wait_test.cuh"
@@ -885,9 +885,27 @@ static spx_status_t check_logprobs(const spx_logprob_args_t *a, bool need_ptrs) 
   return SPX_OK;
 }
 
+namespace {
+struct LogprobWs {
+  size_t seg, group_max, total;
+  int32_t nsub;
+};
+LogprobWs logprob_ws_layout(const spx_logprob_args_t *a) {
+  LogprobWs w{};
+  const size_t es = a->logits_dtype == SPX_BF16 ? 2 : 4;
+  w.nsub = (int32_t)((a->vocab * es + kLpSubBytes - 1) / kLpSubBytes);
+  const size_t subs = (size_t)a->rows * w.nsub;
+  size_t off = 0;
+  w.seg = off; off = align_up(off + sizeof(float4) * subs, 256);
+  w.group_max = off; off = align_up(off + es * 32 * subs, 256);
+  w.total = off ? off : 256;
+  return w;
+}
+}  // namespace
+
 size_t spx_token_logprobs_workspace(const spx_logprob_args_t *a) {
   if (check_logprobs(a, false) != SPX_OK) return 0;
-  return 256;
+  return logprob_ws_layout(a).total;
 }
 
 spx_status_t spx_token_logprobs(const spx_logprob_args_t *a, void *workspace, size_t workspace_bytes, int32_t *dev_status,
@@ -897,17 +915,36 @@ spx_status_t spx_token_logprobs(const spx_logprob_args_t *a, void *workspace, si
   if (st != SPX_OK) return st;
   if (!dev_status) return SPX_ERR_INVALID_ARG;
   if (a->rows == 0) return SPX_OK;
-  const size_t need = spx_token_logprobs_workspace(a);
-  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return SPX_ERR_WORKSPACE;
+  const LogprobWs w = logprob_ws_layout(a);
+  if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < w.total) return SPX_ERR_WORKSPACE;
+  DeviceInfo info;
+  if (!get_device_info(&info)) return SPX_ERR_CUDA;
+  unsigned char *ws = static_cast<unsigned char *>(workspace);
   LogprobParams p{};
   p.rows = a->rows; p.vocab = a->vocab; p.top_n = a->top_n; p.row_stride = a->logits_row_stride;
   p.logits = a->logits; p.token_ids = a->token_ids;
   p.logprobs = a->logprobs; p.entropy = a->entropy; p.top_ids = a->top_ids; p.top_logprobs = a->top_logprobs;
+  p.seg = reinterpret_cast<float4 *>(ws + w.seg); p.group_max = ws + w.group_max;
   p.dev_status = dev_status;
-  if (a->logits_dtype == SPX_BF16) logprob_kernel<__nv_bfloat16><<<a->rows, kLogprobThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
-  else logprob_kernel<float><<<a->rows, kLogprobThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
-  ++t_launches;
-  return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
+  p.nsub = w.nsub;
+  // few rows are cut finer, so that they reach every SM
+  auto chunks = [&](int subs) { return (int64_t)a->rows * ((p.nsub + subs - 1) / subs); };
+  p.chunk_subs = kLpStageSubs;
+  while (p.chunk_subs > 1 && chunks(p.chunk_subs) < 2 * info.num_sms) p.chunk_subs /= 2;
+  if (chunks(p.chunk_subs) > 0x7fffffff) return SPX_ERR_UNSUPPORTED;
+  p.chunks_per_row = (p.nsub + p.chunk_subs - 1) / p.chunk_subs;
+  p.n_chunks = (int32_t)chunks(p.chunk_subs);
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  auto launch = [&](auto stats, auto merge) -> spx_status_t {
+    if (cudaFuncSetAttribute(stats, cudaFuncAttributeMaxDynamicSharedMemorySize, kLpSmemBytes) != cudaSuccess) return SPX_ERR_CUDA;
+    stats<<<p.n_chunks < info.num_sms ? p.n_chunks : info.num_sms, kLpThreads, kLpSmemBytes, stream>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return SPX_ERR_CUDA;
+    if (launch_pdl(merge, dim3(a->rows), dim3(kLpTailThreads), 0, stream, p) != cudaSuccess) return SPX_ERR_CUDA;
+    t_launches = 2;
+    return SPX_OK;
+  };
+  return a->logits_dtype == SPX_BF16 ? launch(logprob_stats_kernel<__nv_bfloat16>, logprob_merge_kernel<__nv_bfloat16>)
+                                     : launch(logprob_stats_kernel<float>, logprob_merge_kernel<float>);
 }
 
 // ---- selective speculation support ------------------------------------------------------------
