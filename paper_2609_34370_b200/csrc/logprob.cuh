@@ -19,7 +19,7 @@ namespace spx {
 constexpr int kLpSubBytes = 4096;                   // a sub-segment: one warp, 8 16-byte vectors a lane
 constexpr int kLpStageSubs = 8;                     // sub-segments of a full ring stage
 constexpr int kLpStages = 6;
-constexpr int kLpGroups = 2;                        // groups of 8 consumer warps, each takes every second chunk
+constexpr int kLpGroups = 3;                        // groups of 8 consumer warps, each takes every third chunk
 constexpr int kLpThreads = (kLpGroups * kLpStageSubs + 1) * 32;
 constexpr int kLpSmemBytes = kLpStages * kLpStageSubs * kLpSubBytes + 1024 + 256;
 constexpr int kLpTailThreads = 128;
@@ -246,15 +246,20 @@ __global__ void __launch_bounds__(kLpThreads, 1) logprob_stats_kernel(LogprobPar
   }
 }
 
-// One block per row: merge, then the alternatives.
+// One block per row: merge, then the alternatives.  A chain of dependent reads (statistics -> candidate groups ->
+// their logits) with little between them: what the next step reads is asked for as early as it is known,
+// and the 64-bit sums are done while the candidates' logits are on their way.
 template <typename T>
 __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobParams p) {
   using V = LpVec<T>;
   constexpr int kThreads = kLpTailThreads, kWarps = kThreads / 32, kKeyBits = sizeof(T) * 8;
+  constexpr int kMaxVecs = 2;            // 16-byte vectors of group maxima a thread holds in the common case
   __shared__ float s_f[kWarps];
-  __shared__ double s_d[2][kWarps];
+  __shared__ double s_d[3][kWarps];
   __shared__ int s_i[kWarps];
+  __shared__ uint32_t s_floor;
   __shared__ int s_cand_n, s_list_n;
+  __shared__ __align__(16) uint32_t s_key[kThreads];
   __shared__ int s_cand[kLpMaxCand];
   __shared__ uint2 s_list[kLpMaxList];   // (key, ~id)
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -263,6 +268,7 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
   const T *x = reinterpret_cast<const T *>(p.logits) + (int64_t)row * p.row_stride;
   const bool counted = tok >= 0 && tok < p.vocab;
   const float x_tok = counted ? ld_as_float(x, tok) : 0.f;
+  const int n = p.top_n;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the statistics are read from here on
   if (!counted) {
     if (tid == 0) {
@@ -270,17 +276,25 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
       if (p.entropy) p.entropy[row] = nan;
       if (tok != -1) atomicOr(p.dev_status, SPX_DEV_BAD_TOKEN);
     }
-    if (tid < p.top_n) {
-      if (p.top_ids) p.top_ids[(int64_t)row * p.top_n + tid] = -1;
-      if (p.top_logprobs) p.top_logprobs[(int64_t)row * p.top_n + tid] = nan;
+    if (tid < n) {
+      if (p.top_ids) p.top_ids[(int64_t)row * n + tid] = -1;
+      if (p.top_logprobs) p.top_logprobs[(int64_t)row * n + tid] = nan;
     }
     return;
   }
   const float4 *seg = p.seg + (int64_t)row * p.nsub;
   const T *gmax = reinterpret_cast<const T *>(p.group_max) + (int64_t)row * p.nsub * 32;
+  const int n_groups = p.nsub * 32, n_vecs = n_groups / V::N;
+  const float4 seg0 = tid < p.nsub ? seg[tid] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const uint4 *gvec = reinterpret_cast<const uint4 *>(gmax);
+  uint4 gv[kMaxVecs];
+  if (n > 0) {
+#pragma unroll
+    for (int u = 0; u < kMaxVecs; ++u)
+      if (tid + u * kThreads < n_vecs) gv[u] = gvec[tid + u * kThreads];
+  }
 
   // ---- the row's maximum, and whether it has finite sums
-  const float4 seg0 = tid < p.nsub ? seg[tid] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
   float m = seg0.x;
   bool bad = seg0.x != seg0.x || seg0.x == INFINITY;
   for (int i = tid + kThreads; i < p.nsub; i += kThreads) {
@@ -290,76 +304,30 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
   }
   m = warp_max(m);
   if (lane == 0) s_f[warp] = m;
+  // Keys whose n-th largest bounds the n-th largest logit from below: the sub-segments' maxima, or, of a row
+  // with fewer than n, the maxima of their q equal shares, the least power of two that makes n of them
+  int q = 1;
+  while (p.nsub * q < n) q *= 2;
+  const int n_keys = p.nsub * q;
+  uint32_t my_key = 0;
+  if (n > 0) {
+    if (q == 1) {
+      my_key = logit_key<T>(seg0.x);
+    } else if (tid < n_keys) {
+      for (int i = 0; i < 32 / q; ++i) my_key = max(my_key, logit_key<T>(ld_as_float(gmax, tid * (32 / q) + i)));
+    }
+    s_key[tid] = tid < n_keys ? my_key : 0;
+  }
+  if (tid == 0) { s_cand_n = 0; s_list_n = 0; }
   bad = __syncthreads_or(bad);
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s_f[w]);
   bad |= m == -INFINITY;
-  // ---- rest = sum e^(x - m) without one of the largest, and sum e^(x - m) (x - m), in 64 bits.  top: the first
-  // sub-segment that holds the maximum
-  double rest = 0.0, prod = 0.0, top_sum = 0.0;
-  int top = 0x7fffffff;
-  if (!bad) {
-    for (int i = tid; i < p.nsub; i += kThreads) {
-      const float4 f = i == tid ? seg0 : seg[i];
-      if (f.x == -INFINITY) continue;
-      const double d = (double)f.x - m;
-      const double w = d == 0.0 ? 1.0 : (double)expf((float)d);
-      prod += w * ((double)f.z * 0.6931471805599453 + (double)f.y * d);
-      if (d == 0.0 && top == 0x7fffffff) { top = i; top_sum = f.y; }   // (a thread's first)
-      else rest += w * f.y;
-    }
-  }
-  const int top_mine = top;
-  top = __reduce_min_sync(0xffffffffu, top);
-  if (lane == 0) s_i[warp] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) top = min(top, s_i[w]);
-  const bool owns = top_mine == top && top != 0x7fffffff;
-  if (top_mine != 0x7fffffff && !owns) rest += top_sum;   // holds the maximum too, but not first
-  auto block_sum2 = [&](double &a, double &b) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); b += __shfl_xor_sync(0xffffffffu, b, o); }
-    __syncthreads();
-    if (lane == 0) { s_d[0][warp] = a; s_d[1][warp] = b; }
-    __syncthreads();
-    a = b = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) { a += s_d[0][w]; b += s_d[1][w]; }
-  };
-  double log_z = 0.0;
-  if (!bad) {
-    double others = rest, unused = owns ? top_sum : 0.0;
-    block_sum2(others, prod);
-    double with_top = unused, none = 0.0;
-    block_sum2(with_top, none);
-    rest = others + with_top - 1.0;
-    if (rest < 0.125) {
-      // near-certain row: the sub-segment's fp32 sum has rounded its share of the rest against the maximum's 1;
-      // add it up again without that
-      double a = 0.0, n_max = 0.0;
-      const int e0 = top * V::kSub;
-      for (int i = tid; i < V::kSub && e0 + i < p.vocab; i += kThreads) {
-        const float d = ld_as_float(x, e0 + i) - m;
-        if (d == 0.f) n_max += 1.0;
-        else a += (double)expf(d);
-      }
-      block_sum2(a, n_max);
-      rest = others + a + (n_max - 1.0);
-    }
-    log_z = log1p(rest);
-  }
-  if (tid == 0) {
-    if (p.logprobs) p.logprobs[row] = bad ? nan : (float)((double)x_tok - m - log_z);
-    if (p.entropy) p.entropy[row] = bad ? nan : (float)(log_z - prod / (1.0 + rest));
-  }
-  const int n = p.top_n;
-  if (n == 0) return;
 
-  // ---- the alternatives
-  // the k-th largest of count(i)'s keys, i < total (or a key that exactly k reach): bit by bit from the top
+  // the k-th largest of key_of(i), i < total (or a key that exactly k reach): bit by bit from the top
   auto kth_largest = [&](int total, int k, auto key_of) -> uint32_t {
     uint32_t thr = 0;
+#pragma unroll 1
     for (int bit = kKeyBits - 1; bit >= 0; --bit) {
       const uint32_t cand = thr | (1u << bit);
       int count = 0;
@@ -371,47 +339,150 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
     }
     return thr;
   };
-  if (tid == 0) { s_cand_n = 0; s_list_n = 0; }
-  const int n_groups = p.nsub * 32;
-  const uint32_t key0 = logit_key<T>(seg0.x);
-  auto seg_key = [&](int i) -> uint32_t { return i == tid ? key0 : logit_key<T>(seg[i].x); };
   auto group_key = [&](int i) -> uint32_t { return logit_key<T>(ld_as_float(gmax, i)); };
-  const uint32_t floor_key = p.nsub >= n ? kth_largest(p.nsub, n, seg_key) : kth_largest(n_groups, n, group_key);
-  __syncthreads();
-  for (int i = tid; i < n_groups; i += kThreads)
-    if (group_key(i) >= floor_key) {
-      const int at = atomicAdd(&s_cand_n, 1);
-      if (at < kLpMaxCand) s_cand[at] = i;
-    }
-  __syncthreads();
-  // every logit of the listed groups for which take(key) holds, behind the list's end
-  auto gather = [&](int n_cand, auto take) {
-    for (int i = tid; i < n_cand * 8; i += kThreads) {
-      const int g = s_cand[i >> 3], c = i & 7;
-      const int e0 = (g >> 5) * V::kSub + (c * 32 + (g & 31)) * V::N;
-      if (e0 >= p.vocab) continue;
-      const uint4 v = *reinterpret_cast<const uint4 *>(x + e0);
-#pragma unroll
-      for (int k = 0; k < V::N; ++k) {
-        const uint32_t key = logit_key<T>(V::at(v, k));
-        if (e0 + k < p.vocab && take(key)) {
-          const int at = atomicAdd(&s_list_n, 1);
-          if (at < kLpMaxList) s_list[at] = make_uint2(key, ~(uint32_t)(e0 + k));
+  // the logits of the listed groups, one vector of a group per thread and round
+  auto vec_at = [&](int i) -> int {
+    const int g = s_cand[i >> 3], c = i & 7;
+    return (g >> 5) * V::kSub + (c * 32 + (g & 31)) * V::N;
+  };
+  uint32_t floor_key = 0;
+  int n_cand = 0;
+  uint4 held[kMaxVecs];
+  if (n > 0) {
+    if (n_keys <= kThreads) {
+      // rank by counting: every thread its key against all (they lie behind one another in shared memory)
+      if (tid < n_keys) {
+        int above = 0, level = 0;   // larger keys, equal ones
+        for (int j = 0; j < n_keys; j += 4) {
+          const uint4 k = *reinterpret_cast<const uint4 *>(s_key + j);
+          above += (k.x > my_key) + (k.y > my_key) + (k.z > my_key) + (k.w > my_key);
+          level += (k.x == my_key) + (j + 1 < n_keys && k.y == my_key) + (j + 2 < n_keys && k.z == my_key) + (j + 3 < n_keys && k.w == my_key);
         }
+        if (above < n && above + level >= n) s_floor = my_key;   // (all that write write the same)
       }
+      __syncthreads();
+      floor_key = s_floor;
+    } else {
+      floor_key = kth_largest(n_keys, n, [&](int i) -> uint32_t { return i == tid ? my_key : logit_key<T>(seg[i].x); });
+    }
+    auto list_vec = [&](const uint4 &v, int base) {
+#pragma unroll
+      for (int k = 0; k < V::N; ++k)
+        if (logit_key<T>(V::at(v, k)) >= floor_key) {
+          const int at = atomicAdd(&s_cand_n, 1);
+          if (at < kLpMaxCand) s_cand[at] = base + k;
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < kMaxVecs; ++u)
+      if (tid + u * kThreads < n_vecs) list_vec(gv[u], (tid + u * kThreads) * V::N);
+    for (int i = tid + kMaxVecs * kThreads; i < n_vecs; i += kThreads) list_vec(gvec[i], i * V::N);
+    __syncthreads();
+    n_cand = s_cand_n;
+    if (n_cand <= kLpMaxCand) {
+#pragma unroll
+      for (int u = 0; u < kMaxVecs; ++u)
+        if (tid + u * kThreads < n_cand * 8) {
+          const int e0 = vec_at(tid + u * kThreads);
+          if (e0 < p.vocab) held[u] = *reinterpret_cast<const uint4 *>(x + e0);
+        }
+    }
+  }
+
+  // ---- rest = sum e^(x - m) without one of the largest, and sum e^(x - m) (x - m), in 64 bits.  top: the first
+  // sub-segment that holds the maximum
+  double rest = 0.0, prod = 0.0, log_z = 0.0;
+  if (!bad) {
+    double top_sum = 0.0;
+    int top = 0x7fffffff;
+    for (int i = tid; i < p.nsub; i += kThreads) {
+      const float4 f = i == tid ? seg0 : seg[i];
+      if (f.x == -INFINITY) continue;
+      const float d = f.x - m;   // (a rounded difference is a factor off by 2^-24 |d|)
+      const float w = expf(d);
+      prod += (double)w * fma((double)f.z, 0.6931471805599453, (double)f.y * (double)d);
+      if (d == 0.f && top == 0x7fffffff) { top = i; top_sum = f.y; }   // (a thread's first)
+      else rest += (double)w * (double)f.y;
+    }
+    const int top_mine = top;
+    top = __reduce_min_sync(0xffffffffu, top);
+    if (lane == 0) s_i[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = min(top, s_i[w]);
+    if (top_mine != top) { rest += top_sum; top_sum = 0.0; }   // holds the maximum too, but not first
+    auto block_sum3 = [&](double &a, double &b, double &c) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+        c += __shfl_xor_sync(0xffffffffu, c, o);
+      }
+      if (lane == 0) { s_d[0][warp] = a; s_d[1][warp] = b; s_d[2][warp] = c; }
+      __syncthreads();
+      a = b = c = 0.0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) { a += s_d[0][w]; b += s_d[1][w]; c += s_d[2][w]; }
+    };
+    double others = rest;
+    block_sum3(others, prod, top_sum);
+    rest = others + (top_sum - 1.0);
+    if (rest < 0.125) {
+      // near-certain row: the sub-segment's fp32 sum has rounded its share of the rest against the maximum's 1;
+      // add it up again without that
+      double a = 0.0, n_max = 0.0, none = 0.0;
+      const int e0 = top * V::kSub;
+      for (int i = tid; i < V::kSub && e0 + i < p.vocab; i += kThreads) {
+        const float d = ld_as_float(x, e0 + i) - m;
+        if (d == 0.f) n_max += 1.0;
+        else a += (double)expf(d);
+      }
+      __syncthreads();
+      block_sum3(a, n_max, none);
+      rest = others + a + (n_max - 1.0);
+    }
+    log_z = log1p(rest);
+  }
+  if (tid == 0) {
+    if (p.logprobs) p.logprobs[row] = bad ? nan : (float)((double)x_tok - m - log_z);
+    if (p.entropy) p.entropy[row] = bad ? nan : (float)(log_z - prod / (1.0 + rest));
+  }
+  if (n == 0) return;
+
+  // ---- the alternatives: every logit of the listed groups for which take(key) holds, behind the list's end
+  auto take_vec = [&](const uint4 &v, int e0, auto take) {
+#pragma unroll
+    for (int k = 0; k < V::N; ++k) {
+      const uint32_t key = logit_key<T>(V::at(v, k));
+      if (take(key) && e0 + k < p.vocab) {
+        const int at = atomicAdd(&s_list_n, 1);
+        if (at < kLpMaxList) s_list[at] = make_uint2(key, ~(uint32_t)(e0 + k));
+      }
+    }
+  };
+  auto gather = [&](int i0, int cands, auto take) {
+    for (int i = i0 + tid; i < cands * 8; i += kThreads) {
+      const int e0 = vec_at(i);
+      if (e0 < p.vocab) take_vec(*reinterpret_cast<const uint4 *>(x + e0), e0, take);
     }
     __syncthreads();
   };
-  bool listed = s_cand_n <= kLpMaxCand;
+  bool listed = n_cand <= kLpMaxCand;
   if (listed) {
-    gather(s_cand_n, [&](uint32_t key) { return key >= floor_key; });
+    auto take = [&](uint32_t key) { return key >= floor_key; };
+#pragma unroll
+    for (int u = 0; u < kMaxVecs; ++u)
+      if (tid + u * kThreads < n_cand * 8) {
+        const int e0 = vec_at(tid + u * kThreads);
+        if (e0 < p.vocab) take_vec(held[u], e0, take);
+      }
+    gather(kMaxVecs * kThreads, n_cand, take);
     listed = s_list_n <= kLpMaxList;
   }
   if (!listed) {
-    // ties by the hundred (a masked or constant row): with thr the n-th largest group maximum at most n - 1 groups
-    // lie above it, and all their logits above thr fit the list; the ones equal to it are taken by ascending id
+    // ties by the hundred (a masked or constant row): with thr the n-th largest group maximum at most n groups lie
+    // above it, and all their logits above thr fit the list; the ones equal to it are taken by ascending id
     const uint32_t thr = kth_largest(n_groups, n, group_key);
-    // (kth_largest may stop at a key that exactly n groups reach: then it is no group's and nothing ties with it)
     __syncthreads();
     if (tid == 0) { s_cand_n = 0; s_list_n = 0; }
     __syncthreads();
@@ -421,8 +492,9 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
         if (at < kLpMaxCand) s_cand[at] = i;
       }
     __syncthreads();
-    gather(min(s_cand_n, kLpMaxCand), [&](uint32_t key) { return key > thr; });
-    int have = s_list_n;
+    gather(0, min(s_cand_n, kLpMaxCand), [&](uint32_t key) { return key > thr; });
+    const int above = s_list_n;
+    int have = above;
     for (int e0 = 0; have < n && e0 < p.vocab; e0 += kThreads) {
       const int e = e0 + tid;
       const bool tie = e < p.vocab && logit_key<T>(ld_as_float(x, e)) == thr;
@@ -438,7 +510,7 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
       have += all;
     }
     __syncthreads();
-    if (tid == 0) s_list_n = min(have, max(n, s_list_n));
+    if (tid == 0) s_list_n = min(have, max(n, above));
     __syncthreads();
   }
   // ---- rank the candidates
@@ -446,7 +518,7 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
   for (int i = tid; i < total; i += kThreads) {
     const uint2 me = s_list[i];
     int rank = 0;
-    for (int j = 0; j < total && rank < n; ++j) {
+    for (int j = 0; j < total; ++j) {
       const uint2 o = s_list[j];
       rank += o.x > me.x || (o.x == me.x && o.y > me.y);
     }
