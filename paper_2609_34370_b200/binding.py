@@ -184,16 +184,22 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None or t.numel() == 0 else t.data_ptr()
+    return None if t is None else t.data_ptr()   # (0, that is NULL, for a tensor without elements)
 
 
 def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+    # the raw handle of torch.cuda.current_stream(device), without the Stream object around it
+    index = None if device is None else device.index if isinstance(device, torch.device) else torch.device(device).index
+    return _raw_stream(_current_device() if index is None else index)
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch.cuda.current_device
 
 
 def _require_cuda(*tensors):
     for t in tensors:
-        if t is not None and t.device.type != "cuda":
+        if t is not None and not t.is_cuda:
             raise SpxError(ERR_INVALID_ARG, "device tensors required (there is no CPU path)")
 
 
@@ -201,7 +207,7 @@ def _on_device_of(fn):
     """The library launches on the current device: the call is made with its first tensor's device current."""
     @functools.wraps(fn)
     def call(first, *args, **kw):
-        if not isinstance(first, torch.Tensor) or first.device.type != "cuda" or first.device.index == torch.cuda.current_device():
+        if not getattr(first, "is_cuda", False) or first.get_device() == _current_device():
             return fn(first, *args, **kw)
         with torch.cuda.device(first.device):
             return fn(first, *args, **kw)
@@ -220,8 +226,9 @@ def _set_cache_scales(a, k_cache, v_cache, num_kv_heads, page_size, num_pages, k
         if pool.dtype not in (torch.float8_e4m3fn, torch.uint8):
             raise TypeError(f"pools with scales hold float8_e4m3fn (or its bytes as uint8), got {pool.dtype}")
     per_page = k_scales.shape[-1] if k_scales.dim() == 3 else 0
+    shape = (num_pages, num_kv_heads, per_page)
     for t in (k_scales, v_scales):
-        if t.dtype != torch.float32 or tuple(t.shape) != (num_pages, num_kv_heads, per_page) or not t.is_contiguous():
+        if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
             raise SpxError(ERR_INVALID_ARG, "scales must be contiguous float32 [num_pages, num_kv_heads, page_size / scale_block]")
     if per_page < 1 or page_size % per_page:
         raise SpxError(ERR_INVALID_ARG, "the scales of a page must divide its tokens")
@@ -517,7 +524,7 @@ def draft_confidence(draft_logits, draft_ids, q_indptr, vocab=None, want_token_c
 
 
 def _check_output(t, shape, dtype, what):
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise SpxError(ERR_INVALID_ARG, f"{what} must be contiguous {dtype} {list(shape)}")
     _require_cuda(t)
 

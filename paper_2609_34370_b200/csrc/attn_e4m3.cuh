@@ -281,6 +281,9 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   fence_after();
   const uint32_t tmem = bars->tmem_base;
 
+  // Everything above touched only this CTA's own resources; the plan, and what the caller's kernels before it
+  // wrote, is read from here on.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   // this CTA's range of the plan: entries cta_off[c] .. cta_off[c+1] of the work list, in order
   const bool planned = !p.hdr->overflow && (int)blockIdx.x < p.hdr->n_cta;
   const int item_begin = planned ? p.cta_off[blockIdx.x] : 0;

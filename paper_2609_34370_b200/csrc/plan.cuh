@@ -47,6 +47,8 @@ __device__ __forceinline__ int plan_entry_cost(int tiles) { return tiles <= 2 ? 
 // slots for the pairs a cut crosses and emits each range's work entries in axis order.
 __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   SPX_TL_SCOPE(kTlPlan);
+  // a kernel launched programmatically behind this one may come up now (it waits before it reads the plan)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __shared__ int s_scratch[32];
   __shared__ int s_total;
   __shared__ int s_cut[kPlanMaxCta + 1];     // cut c: first tile (axis position) of range c

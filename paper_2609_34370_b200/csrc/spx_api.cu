@@ -1,6 +1,7 @@
 // libspx: C ABI, argument validation, workspace layout and kernel launches.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -88,6 +89,19 @@ static bool get_device_info(DeviceInfo *info) {
   if (cudaDeviceGetAttribute(&info->max_smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, info->device) != cudaSuccess) return false;
   return true;
 }
+
+// A kernel's limit on dynamic shared memory, raised once per kernel and device.
+struct SmemOnce {
+  std::atomic<uint64_t> done{0};
+  template <typename K>
+  cudaError_t raise(K kernel, int bytes, int device) {
+    const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
+    if (bit && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+  }
+};
 
 constexpr int kPlanSmCount = 148;  // workspace sizing must not depend on a device query
 
@@ -345,16 +359,25 @@ static cudaError_t launch_tc(const CUtensorMap &kmap, const CUtensorMap &vmap, c
 }
 
 template <int D, int MROWS>
-static cudaError_t launch_e4m3(const CUtensorMap &kmap, const CUtensorMap &vmap, const AttnParams &p, int num_sms, cudaStream_t stream) {
+static cudaError_t launch_e4m3(const CUtensorMap &kmap, const CUtensorMap &vmap, const AttnParams &p, int num_sms, int device,
+                               bool behind_plan, cudaStream_t stream) {
   using Cfg = E8Cfg<D, MROWS>;
   auto kernel = attn_e4m3_kernel<D, MROWS>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
+  static SmemOnce smem;
+  cudaError_t e = smem.raise(kernel, Cfg::kSmemBytes, device);
   if (e != cudaSuccess) return e;
   if (t_ev_start) cudaEventRecord(t_ev_start, stream);
-  kernel<<<num_sms, kE8Threads, Cfg::kSmemBytes, stream>>>(kmap, vmap, p);
+  // directly behind the planner the CTAs come up while it plans; in the whole step they would take their SMs from
+  // the sampling kernels that run beside the planner
+  if (behind_plan && !t_ev_start) {
+    e = launch_pdl(kernel, dim3(num_sms), dim3(kE8Threads), Cfg::kSmemBytes, stream, kmap, vmap, p);
+  } else {
+    kernel<<<num_sms, kE8Threads, Cfg::kSmemBytes, stream>>>(kmap, vmap, p);
+    e = cudaGetLastError();
+  }
   if (t_ev_stop) cudaEventRecord(t_ev_stop, stream);
   ++t_launches;
-  return cudaGetLastError();
+  return e;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -418,11 +441,11 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
     if (a->cache_format == SPX_CACHE_E4M3) {
       if (!make_pool_map_e4m3(&kmap, a->k_cache, a, p.head_inner) || !make_pool_map_e4m3(&vmap, a->v_cache, a, p.head_inner)) return SPX_ERR_CUDA;
       if (p.rows_cap <= 32)
-        e = p.D == 128 ? launch_e4m3<128, 32>(kmap, vmap, p, sms, stream) : launch_e4m3<64, 32>(kmap, vmap, p, sms, stream);
+        e = p.D == 128 ? launch_e4m3<128, 32>(kmap, vmap, p, sms, dev.device, phases == kPhaseAll, stream) : launch_e4m3<64, 32>(kmap, vmap, p, sms, dev.device, phases == kPhaseAll, stream);
       else if (p.rows_cap <= 64)
-        e = p.D == 128 ? launch_e4m3<128, 64>(kmap, vmap, p, sms, stream) : launch_e4m3<64, 64>(kmap, vmap, p, sms, stream);
+        e = p.D == 128 ? launch_e4m3<128, 64>(kmap, vmap, p, sms, dev.device, phases == kPhaseAll, stream) : launch_e4m3<64, 64>(kmap, vmap, p, sms, dev.device, phases == kPhaseAll, stream);
       else
-        e = p.D == 128 ? launch_e4m3<128, 128>(kmap, vmap, p, sms, stream) : launch_e4m3<64, 128>(kmap, vmap, p, sms, stream);
+        e = p.D == 128 ? launch_e4m3<128, 128>(kmap, vmap, p, sms, dev.device, phases == kPhaseAll, stream) : launch_e4m3<64, 128>(kmap, vmap, p, sms, dev.device, phases == kPhaseAll, stream);
     } else if (!make_pool_map(&kmap, a->k_cache, a, p.head_inner) || !make_pool_map(&vmap, a->v_cache, a, p.head_inner))
       return SPX_ERR_CUDA;
     else if (p.rows_cap <= 64) {
@@ -936,7 +959,8 @@ spx_status_t spx_token_logprobs(const spx_logprob_args_t *a, void *workspace, si
   p.n_chunks = (int32_t)chunks(p.chunk_subs);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   auto launch = [&](auto stats, auto merge) -> spx_status_t {
-    if (cudaFuncSetAttribute(stats, cudaFuncAttributeMaxDynamicSharedMemorySize, kLpSmemBytes) != cudaSuccess) return SPX_ERR_CUDA;
+    static SmemOnce smem[2];
+    if (smem[a->logits_dtype == SPX_BF16].raise(stats, kLpSmemBytes, info.device) != cudaSuccess) return SPX_ERR_CUDA;
     stats<<<p.n_chunks < info.num_sms ? p.n_chunks : info.num_sms, kLpThreads, kLpSmemBytes, stream>>>(p);
     if (cudaGetLastError() != cudaSuccess) return SPX_ERR_CUDA;
     if (launch_pdl(merge, dim3(a->rows), dim3(kLpTailThreads), 0, stream, p) != cudaSuccess) return SPX_ERR_CUDA;
