@@ -7,6 +7,9 @@
 // token's change of scale rounds only where its last bits fall below the smallest subnormal, and
 // appending the same rows again changes nothing.
 #pragma once
+#include <type_traits>
+
+#include "attn_e4m3.cuh"   // e8::pair and the packed fp32 arithmetic
 #include "common.cuh"
 
 namespace spx {
@@ -39,17 +42,24 @@ struct KvQuantParams {
   double inv_freq[64];     // base^(-2i/D)
 };
 
-// 8 elements of a row as floats
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&x)[8]) {
-  const uint4 v = *reinterpret_cast<const uint4 *>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// Eight elements of a row as they are stored, and as floats.
+template <typename T> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+  uint4 a;
+  __device__ void load(const __nv_bfloat16 *p) { a = __ldg(reinterpret_cast<const uint4 *>(p)); }
+  __device__ void values(float (&x)[8]) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+};
+template <> struct Raw8<float> {
+  float4 a, b;
+  __device__ void load(const float *p) { a = __ldg(reinterpret_cast<const float4 *>(p)); b = __ldg(reinterpret_cast<const float4 *>(p) + 1); }
+  __device__ void values(float (&x)[8]) const {
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&x)[8]) {
   uint32_t w[4];
 #pragma unroll
@@ -63,7 +73,6 @@ __device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
   *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
   *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
 }
-// 8 codes as floats, and back (values within the format's range, or not finite: NaN)
 __device__ __forceinline__ void decode8(uint2 c, float (&x)[8]) {
   const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
@@ -73,21 +82,57 @@ __device__ __forceinline__ void decode8(uint2 c, float (&x)[8]) {
     x[2 * i] = f.x; x[2 * i + 1] = f.y;
   }
 }
+// (the conversion saturates: no value passes 448 but an infinity, which the caller has made a NaN)
 __device__ __forceinline__ uint2 encode8(const float (&x)[8]) {
-  uint32_t w[2] = {0, 0};
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[2 * i], x[2 * i + 1]), __NV_NOSAT, __NV_E4M3) << (16 * (i & 1));
+  for (int i = 0; i < 2; ++i) {
+    uint16_t a, b;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(a) : "f"(x[4 * i + 1]), "f"(x[4 * i]));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(x[4 * i + 3]), "f"(x[4 * i + 2]));
+    w[i] = (uint32_t)a | ((uint32_t)b << 16);
+  }
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ uint32_t finite_amax8(const float (&x)[8], uint32_t m) {
+__device__ __forceinline__ float amax8(const float (&x)[8], float m) {   // NaNs do not count
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
-    m = b < 0x7f800000u && b > m ? b : m;
-  }
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
   return m;
 }
+
+// The rotation.  cos = ch + cl and sin = sh + sl, each as two floats of the float64 value (2^-48 of it left out).
+struct CosSin { uint64_t ch, cl, sh, sl; };   // of two pairs
+__device__ __forceinline__ uint64_t neg2(uint64_t a) { return e8::mul2(a, e8::pair(-1.f, -1.f)); }
+__device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) { return e8::fma2(b, e8::pair(-1.f, -1.f), a); }
+// y0 = x0 cos - x1 sin, y1 = x1 cos + x0 sin.  kExact: products and sum with their rounding errors, one rounding
+// to fp32 at the end of a value good to 2^-46 of |x| (what float64 arithmetic gives but for one in some millions
+// of last bits, at a third of its time: conversions from and to float64 alone are 8 cycles each); what goes into the
+// 8-bit codes and into fp32 rows.  Otherwise the leading errors only: within 2 steps of fp32 of the value, for
+// rows that are rounded to 16 bits.
+template <bool kExact>
+__device__ __forceinline__ void rotate2(uint64_t x0, uint64_t x1, const CosSin &k, uint64_t &y0, uint64_t &y1) {
+  using namespace e8;
+  const uint64_t n0 = neg2(x0), n1 = neg2(x1);
+  if constexpr (kExact) {
+    {
+      const uint64_t p = mul2(x0, k.ch), np = fma2(n0, k.ch, p), q = mul2(x1, k.sh), nq = fma2(n1, k.sh, q);
+      const uint64_t s = sub2(p, q), bb = sub2(s, p);
+      const uint64_t err = sub2(sub2(p, sub2(s, bb)), add2(q, bb));
+      y0 = add2(s, add2(fma2(n1, k.sl, fma2(x0, k.cl, err)), sub2(nq, np)));
+    }
+    {
+      const uint64_t p = mul2(x1, k.ch), np = fma2(n1, k.ch, p), q = mul2(x0, k.sh), nq = fma2(n0, k.sh, q);
+      const uint64_t s = add2(p, q), bb = sub2(s, p);
+      const uint64_t err = add2(sub2(p, sub2(s, bb)), sub2(q, bb));
+      y1 = add2(s, sub2(fma2(x0, k.sl, fma2(x1, k.cl, err)), add2(np, nq)));
+    }
+  } else {
+    const uint64_t w = mul2(x1, k.sh), nw = mul2(n1, k.sh), u = mul2(x0, k.sh), nu = mul2(n0, k.sh);
+    y0 = add2(fma2(x0, k.ch, nw), fma2(n1, k.sl, fma2(x0, k.cl, fma2(n1, k.sh, w))));
+    y1 = add2(fma2(x1, k.ch, u), fma2(x0, k.sl, fma2(x1, k.cl, fma2(x0, k.sh, nu))));
+  }
+}
+
 // The exponent field of 2^e with the smallest e for which amax <= 448 * 2^e = 1.75 * 2^(e+8); amax as
 // its bit pattern.  Subnormal values count as the smallest exponent: their scale is 2^-126 anyway.
 __device__ __forceinline__ uint32_t scale_exponent(uint32_t amax_bits) {
@@ -102,11 +147,12 @@ __device__ __forceinline__ uint32_t scale_exponent(uint32_t amax_bits) {
 // m / tile + 2 aligned tiles, so no prefix sums over the lengths are needed; tiles past a request's
 // last one leave at once.
 template <typename T, int D>
-__global__ void __launch_bounds__(kQuantThreads) kv_append_e4m3_kernel(const __grid_constant__ KvQuantParams p) {
+__global__ void __launch_bounds__(kQuantThreads, 2) kv_append_e4m3_kernel(const __grid_constant__ KvQuantParams p) {
   using S = QuantShape<D>;
-  constexpr int kVecs = S::kVecs;
+  constexpr int kVecs = S::kVecs, kStep = 32 / kVecs;   // tokens between a lane's items
   extern __shared__ __align__(16) unsigned char quant_smem[];
-  double2 *s_cs = reinterpret_cast<double2 *>(quant_smem);   // [tile tokens][8][kVecs] (cos, sin) of the new tokens
+  // (ch, ch', cl, cl'), (sh, sh', sl, sl') of two neighbouring pairs: [tile tokens][4][2][kVecs] of 16 bytes
+  float *s_cs = reinterpret_cast<float *>(quant_smem);
   __shared__ uint32_t s_amax[2][kQuantWarps];
   __shared__ int s_req;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -143,90 +189,158 @@ __global__ void __launch_bounds__(kQuantThreads) kv_append_e4m3_kernel(const __g
   if (i_tile < 0 || tile64 > ((L - 1) >> p.log2_tile)) return;
   const int t0 = (int)tile64 << p.log2_tile;
   const int32_t *table = p.block_table + (int64_t)r * p.max_pages_per_req;
+
+  const int slots = kQuantWarps / p.task_warps;                  // tasks the block works on at a time
+  const int wsub = warp & (p.task_warps - 1);
+  const int first_task = blockIdx.y * slots + warp / p.task_warps, task_step = gridDim.y * slots;
+  const int n_kv = 2 * p.Hkv, n_tasks = n_kv + (p.q_in ? p.Hq : 0);
+  const int t_block = (t_new >> p.log2SB) << p.log2SB;            // first token of the first touched block
+  const int tok0 = (wsub * kQuantItems * 32 + lane) / kVecs, vec = lane % kVecs;
+  int page[kQuantItems];
+#pragma unroll
+  for (int k = 0; k < kQuantItems; ++k) {
+    const int t = t0 + tok0 + k * kStep;
+    page[k] = t >= t_block && t < L ? table[t >> p.log2P] : -1;
+  }
+  // a lane's new rows of a task, fetched before anything else is waited for
+  struct Rows { Raw8<T> lo[kQuantItems], hi[kQuantItems]; } rows;
+  auto fetch = [&](int task) {
+    const bool is_q = task >= n_kv, is_v = !is_q && (task & 1);
+    const int head = is_q ? task - n_kv : task >> 1, heads = is_q ? p.Hq : p.Hkv;
+    const T *src = reinterpret_cast<const T *>(is_q ? p.q_in : is_v ? p.new_v : p.new_k) + head * D + vec * 8;
+#pragma unroll
+    for (int k = 0; k < kQuantItems; ++k) {
+      const int t = t0 + tok0 + k * kStep;
+      if (t >= t_new && t < L) {
+        const T *row = src + (int64_t)(q0 + t - t_new) * heads * D;
+        rows.lo[k].load(row);
+        rows.hi[k].load(row + D / 2);
+      }
+    }
+  };
+  if (first_task < n_tasks) fetch(first_task);
   // a request with a bad page among its new positions is skipped as a whole: every one of its tiles
   // looks at all of these pages
   int bad = 0;
   for (int i = (t_new >> p.log2P) + tid; i <= (L - 1) >> p.log2P; i += kQuantThreads) {
-    const int page = table[i];
-    bad |= page < 0 || page >= p.num_pages;
+    const int pg = table[i];
+    bad |= pg < 0 || pg >= p.num_pages;
+  }
+  if (p.rope) {
+    // angles in float64; a thread takes four tokens of a pair: one sine and cosine, and three turns by the pair's
+    // frequency (each adds 2^-52)
+    const int t_lo = max(t0, t_new), n = min(t0 + tile_tokens, L) - t_lo;   // the tile's new tokens
+    for (int i = tid; i < (n + 3) / 4 * (D / 2); i += kQuantThreads) {
+      const int pair = i % (D / 2), tok = t_lo - t0 + i / (D / 2) * 4;
+      const double f = p.inv_freq[pair];
+      double c, sn, cf, sf;
+      sincos((double)(t0 + tok) * f, &sn, &c);
+      sincos(f, &sf, &cf);
+      float *at = s_cs + ((((tok * 4 + ((pair & 7) >> 1)) * 2) * kVecs + (pair >> 3)) << 2) + (pair & 1);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (tok + u < t_lo - t0 + n) {
+          const float ch = (float)c, sh = (float)sn;
+          at[0] = ch; at[2] = (float)(c - (double)ch);
+          at[4 * kVecs] = sh; at[4 * kVecs + 2] = (float)(sn - (double)sh);
+        }
+        at += 4 * 2 * kVecs * 4;
+        const double c2 = c * cf - sn * sf;
+        sn = sn * cf + c * sf;
+        c = c2;
+      }
+    }
   }
   if (__syncthreads_or(bad)) {
     if (tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
     return;
   }
 
-  const int slots = kQuantWarps / p.task_warps;                  // tasks the block works on at a time
-  const int wsub = warp & (p.task_warps - 1);
-  const int first_task = blockIdx.y * slots + warp / p.task_warps, task_step = gridDim.y * slots;
-  const int n_kv = 2 * p.Hkv, n_tasks = n_kv + (p.q_in ? p.Hq : 0);
-  if (p.rope) {
-    const int n = min(tile_tokens, L - t0);
-    for (int i = tid; i < n * (D / 2); i += kQuantThreads) {
-      const int tok = i / (D / 2), pair = i % (D / 2);
-      const int t = t0 + tok;
-      if (t < t_new) continue;
-      double2 cs;
-      sincos((double)t * p.inv_freq[pair], &cs.y, &cs.x);
-      s_cs[(tok * 8 + (pair & 7)) * kVecs + (pair >> 3)] = cs;
-    }
-    __syncthreads();
-  }
-
-  const int t_block = (t_new >> p.log2SB) << p.log2SB;            // first token of the first touched block
-  const int tok0 = (wsub * kQuantItems * 32 + lane) / kVecs, vec = lane % kVecs;
-  int page[kQuantItems];
+  auto turn = [&](int tok, float (&lo)[8], float (&hi)[8], auto exact) {
 #pragma unroll
-  for (int k = 0; k < kQuantItems; ++k) {
-    const int t = t0 + tok0 + k * (32 / kVecs);
-    page[k] = t >= t_block && t < L ? table[t >> p.log2P] : -1;
-  }
+    for (int u = 0; u < 4; ++u) {
+      const ulonglong2 *at = reinterpret_cast<const ulonglong2 *>(s_cs) + (tok * 4 + u) * 2 * kVecs + vec;
+      const ulonglong2 a = at[0], b = at[kVecs];
+      const CosSin cs{a.x, a.y, b.x, b.y};
+      uint64_t y0, y1;
+      rotate2<decltype(exact)::value>(e8::pair(lo[2 * u], lo[2 * u + 1]), e8::pair(hi[2 * u], hi[2 * u + 1]), cs, y0, y1);
+      e8::unpair(y0, lo[2 * u], lo[2 * u + 1]);
+      e8::unpair(y1, hi[2 * u], hi[2 * u + 1]);
+    }
+  };
   int parity = 0;
   for (int task = first_task; task < n_tasks; task += task_step, parity ^= 1) {
-    const bool is_q = task >= n_kv, is_v = !is_q && (task & 1);
-    const int head = is_q ? task - n_kv : task >> 1;
-    const int heads = is_q ? p.Hq : p.Hkv;
-    const T *src = reinterpret_cast<const T *>(is_q ? p.q_in : is_v ? p.new_v : p.new_k) + head * D + vec * 8;
+    if (task != first_task) fetch(task);
+    if (task >= n_kv) {
+      // ---- query rows
+      const int head = task - n_kv;
+#pragma unroll
+      for (int k = 0; k < kQuantItems; ++k) {
+        const int tok = tok0 + k * kStep, t = t0 + tok;
+        if (t < t_new || t >= L) continue;
+        float lo[8], hi[8];
+        rows.lo[k].values(lo);
+        rows.hi[k].values(hi);
+        turn(tok, lo, hi, std::integral_constant<bool, sizeof(T) == 4>());
+        T *dst = reinterpret_cast<T *>(p.q_out) + ((int64_t)(q0 + t - t_new) * p.Hq + head) * D + vec * 8;
+        store8(dst, lo);
+        store8(dst + D / 2, hi);
+      }
+      continue;
+    }
+    // ---- K or V rows
+    const bool is_v = task & 1;
+    const int head = task >> 1;
     unsigned char *cache = (is_v ? p.v_cache : p.k_cache) + head * p.stride_head + vec * 8;
     float *scales = is_v ? p.v_scales : p.k_scales;
+    auto scale_at = [&](int k, int t) -> float * {
+      return scales + ((((int64_t)page[k] * p.Hkv + head) << (p.log2P - p.log2SB)) + ((t & ((1 << p.log2P) - 1)) >> p.log2SB));
+    };
+    auto cache_at = [&](int k, int t) -> unsigned char * {
+      return cache + (int64_t)page[k] * p.stride_page + (int64_t)(t & ((1 << p.log2P) - 1)) * p.stride_token;
+    };
     float lo[kQuantItems][8], hi[kQuantItems][8];
     uint32_t amax[kQuantItems];
     float old_scale[kQuantItems];
 #pragma unroll
     for (int k = 0; k < kQuantItems; ++k) {
-      const int tok = tok0 + k * (32 / kVecs), t = t0 + tok;
+      const int tok = tok0 + k * kStep, t = t0 + tok;
       amax[k] = 0;
       old_scale[k] = 0.f;
       if (t >= L || t < t_block) continue;
       if (t >= t_new) {
-        const T *row = src + (int64_t)(q0 + t - t_new) * heads * D;
-        load8(row, lo[k]);
-        load8(row + D / 2, hi[k]);
-        if (p.rope && !is_v) {
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const double2 cs = s_cs[(tok * 8 + u) * kVecs + vec];
-            const double x0 = lo[k][u], x1 = hi[k][u];
-            lo[k][u] = __double2float_rn(x0 * cs.x - x1 * cs.y);
-            hi[k][u] = __double2float_rn(x1 * cs.x + x0 * cs.y);
-          }
-        }
-        if (is_q) {
-          T *dst = reinterpret_cast<T *>(p.q_out) + (int64_t)(q0 + t - t_new) * heads * D + head * D + vec * 8;
-          store8(dst, lo[k]);
-          store8(dst + D / 2, hi[k]);
-        }
-      } else if (!is_q) {
-        const unsigned char *at = cache + (int64_t)page[k] * p.stride_page + (int64_t)(t & ((1 << p.log2P) - 1)) * p.stride_token;
-        const float sc = scales[(((int64_t)page[k] * p.Hkv + head) << (p.log2P - p.log2SB)) + ((t & ((1 << p.log2P) - 1)) >> p.log2SB)];
+        rows.lo[k].values(lo[k]);
+        rows.hi[k].values(hi[k]);
+        if (p.rope && !is_v) turn(tok, lo[k], hi[k], std::true_type());
+      } else {
+        const unsigned char *at = cache_at(k, t);
+        const float sc = *scale_at(k, t);
         decode8(*reinterpret_cast<const uint2 *>(at), lo[k]);
         decode8(*reinterpret_cast<const uint2 *>(at + D / 2), hi[k]);
 #pragma unroll
         for (int u = 0; u < 8; ++u) { lo[k][u] *= sc; hi[k][u] *= sc; }
         old_scale[k] = sc;
       }
-      amax[k] = finite_amax8(hi[k], finite_amax8(lo[k], 0));
+      float a = amax8(hi[k], amax8(lo[k], 0.f));
+      if (a == INFINITY) {
+        // infinities become NaN and do not count
+        a = 0.f;
+#pragma unroll 1
+        for (int u = 0; u < 16; ++u) {
+          float v = 0.f;
+#pragma unroll
+          for (int w = 0; w < 8; ++w) v = u == w ? lo[k][w] : u == w + 8 ? hi[k][w] : v;
+          const bool inf = fabsf(v) == INFINITY;
+          if (!inf) a = fmaxf(a, fabsf(v));
+#pragma unroll
+          for (int w = 0; w < 8; ++w) {
+            if (inf && u == w) lo[k][w] = __int_as_float(0x7fc00000);
+            if (inf && u == w + 8) hi[k][w] = __int_as_float(0x7fc00000);
+          }
+        }
+      }
+      amax[k] = __float_as_uint(a);
     }
-    if (is_q) continue;   // no exchange between the warps of a query task
     // amax of the scale block of each item: over the lanes, the items and the warps that share it
     const int share = kVecs << p.log2SB;   // items of a block
     for (int o = 1; o < min(32, share); o <<= 1)
@@ -248,17 +362,15 @@ __global__ void __launch_bounds__(kQuantThreads) kv_append_e4m3_kernel(const __g
     }
 #pragma unroll
     for (int k = 0; k < kQuantItems; ++k) {
-      const int t = t0 + tok0 + k * (32 / kVecs);
+      const int t = t0 + tok0 + k * kStep;
       if (t >= L || t < t_block) continue;
       const uint32_t e = scale_exponent(amax[k]);
       const float scale = __uint_as_float(e << 23), inv = __uint_as_float((254 - e) << 23);   // 2^127 / 2^-126 at most: both normal
-      const int slot = t & ((1 << p.log2P) - 1);
-      if (vec == 0 && (t & ((1 << p.log2SB) - 1)) == 0)
-        scales[(((int64_t)page[k] * p.Hkv + head) << (p.log2P - p.log2SB)) + (slot >> p.log2SB)] = scale;
+      if (vec == 0 && (t & ((1 << p.log2SB) - 1)) == 0) *scale_at(k, t) = scale;
       if (t < t_new && scale == old_scale[k]) continue;
 #pragma unroll
       for (int u = 0; u < 8; ++u) { lo[k][u] *= inv; hi[k][u] *= inv; }
-      unsigned char *at = cache + (int64_t)page[k] * p.stride_page + (int64_t)slot * p.stride_token;
+      unsigned char *at = cache_at(k, t);
       *reinterpret_cast<uint2 *>(at) = encode8(lo[k]);
       *reinterpret_cast<uint2 *>(at + D / 2) = encode8(hi[k]);
     }
