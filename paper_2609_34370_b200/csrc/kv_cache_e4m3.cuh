@@ -46,6 +46,8 @@ struct KvQuantParams {
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
   uint4 a;
+  __device__ void set_codes(uint2 lo, uint2 hi) { a = make_uint4(lo.x, lo.y, hi.x, hi.y); }
+  __device__ void codes(uint2 &lo, uint2 &hi) const { lo = make_uint2(a.x, a.y); hi = make_uint2(a.z, a.w); }
   __device__ void load(const __nv_bfloat16 *p) { a = __ldg(reinterpret_cast<const uint4 *>(p)); }
   __device__ void values(float (&x)[8]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
@@ -55,6 +57,11 @@ template <> struct Raw8<__nv_bfloat16> {
 };
 template <> struct Raw8<float> {
   float4 a, b;
+  __device__ void set_codes(uint2 lo, uint2 hi) { a = make_float4(__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(hi.x), __uint_as_float(hi.y)); }
+  __device__ void codes(uint2 &lo, uint2 &hi) const {
+    lo = make_uint2(__float_as_uint(a.x), __float_as_uint(a.y));
+    hi = make_uint2(__float_as_uint(a.z), __float_as_uint(a.w));
+  }
   __device__ void load(const float *p) { a = __ldg(reinterpret_cast<const float4 *>(p)); b = __ldg(reinterpret_cast<const float4 *>(p) + 1); }
   __device__ void values(float (&x)[8]) const {
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
@@ -299,44 +306,52 @@ __global__ void __launch_bounds__(kQuantThreads, 2) kv_append_e4m3_kernel(const 
     auto cache_at = [&](int k, int t) -> unsigned char * {
       return cache + (int64_t)page[k] * p.stride_page + (int64_t)(t & ((1 << p.log2P) - 1)) * p.stride_token;
     };
-    float lo[kQuantItems][8], hi[kQuantItems][8];
+    // Two passes over the rows as they were fetched, 16 elements at a time: the maxima, then the codes.  (Keeping the
+    // rotated values of the first pass takes 64 registers more and spills; three blocks per SM, 80 registers, do too:
+    // 142 us for 14.6k rows.)
     uint32_t amax[kQuantItems];
     float old_scale[kQuantItems];
+    auto values = [&](int k, float (&lo)[8], float (&hi)[8]) {
+      const int tok = tok0 + k * kStep, t = t0 + tok;
+      if (t >= t_new) {
+        rows.lo[k].values(lo);
+        rows.hi[k].values(hi);
+        if (p.rope && !is_v) turn(tok, lo, hi, std::true_type());
+      } else {
+        uint2 c_lo, c_hi;
+        rows.lo[k].codes(c_lo, c_hi);
+        decode8(c_lo, lo);
+        decode8(c_hi, hi);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) { lo[u] *= old_scale[k]; hi[u] *= old_scale[k]; }
+      }
+    };
 #pragma unroll
     for (int k = 0; k < kQuantItems; ++k) {
-      const int tok = tok0 + k * kStep, t = t0 + tok;
-      amax[k] = 0;
+      const int t = t0 + tok0 + k * kStep;
       old_scale[k] = 0.f;
-      if (t >= L || t < t_block) continue;
-      if (t >= t_new) {
-        rows.lo[k].values(lo[k]);
-        rows.hi[k].values(hi[k]);
-        if (p.rope && !is_v) turn(tok, lo[k], hi[k], std::true_type());
-      } else {
+      if (t < t_new && t >= t_block) {
         const unsigned char *at = cache_at(k, t);
-        const float sc = *scale_at(k, t);
-        decode8(*reinterpret_cast<const uint2 *>(at), lo[k]);
-        decode8(*reinterpret_cast<const uint2 *>(at + D / 2), hi[k]);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) { lo[k][u] *= sc; hi[k][u] *= sc; }
-        old_scale[k] = sc;
+        rows.lo[k].set_codes(*reinterpret_cast<const uint2 *>(at), *reinterpret_cast<const uint2 *>(at + D / 2));
+        old_scale[k] = *scale_at(k, t);
       }
-      float a = amax8(hi[k], amax8(lo[k], 0.f));
-      if (a == INFINITY) {
-        // infinities become NaN and do not count
+    }
+    bool infinite = false;
+#pragma unroll
+    for (int k = 0; k < kQuantItems; ++k) {
+      const int t = t0 + tok0 + k * kStep;
+      amax[k] = 0;
+      if (t >= L || t < t_block) continue;
+      float lo[8], hi[8];
+      values(k, lo, hi);
+      float a = amax8(hi, amax8(lo, 0.f));
+      if (a == INFINITY) {   // infinities do not count
+        infinite = true;
         a = 0.f;
-#pragma unroll 1
-        for (int u = 0; u < 16; ++u) {
-          float v = 0.f;
 #pragma unroll
-          for (int w = 0; w < 8; ++w) v = u == w ? lo[k][w] : u == w + 8 ? hi[k][w] : v;
-          const bool inf = fabsf(v) == INFINITY;
-          if (!inf) a = fmaxf(a, fabsf(v));
-#pragma unroll
-          for (int w = 0; w < 8; ++w) {
-            if (inf && u == w) lo[k][w] = __int_as_float(0x7fc00000);
-            if (inf && u == w + 8) hi[k][w] = __int_as_float(0x7fc00000);
-          }
+        for (int u = 0; u < 8; ++u) {
+          if (fabsf(lo[u]) < INFINITY) a = fmaxf(a, fabsf(lo[u]));
+          if (fabsf(hi[u]) < INFINITY) a = fmaxf(a, fabsf(hi[u]));
         }
       }
       amax[k] = __float_as_uint(a);
@@ -368,11 +383,20 @@ __global__ void __launch_bounds__(kQuantThreads, 2) kv_append_e4m3_kernel(const 
       const float scale = __uint_as_float(e << 23), inv = __uint_as_float((254 - e) << 23);   // 2^127 / 2^-126 at most: both normal
       if (vec == 0 && (t & ((1 << p.log2SB) - 1)) == 0) *scale_at(k, t) = scale;
       if (t < t_new && scale == old_scale[k]) continue;
+      float lo[8], hi[8];
+      values(k, lo, hi);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) { lo[k][u] *= inv; hi[k][u] *= inv; }
+      for (int u = 0; u < 8; ++u) { lo[u] *= inv; hi[u] *= inv; }
+      if (infinite) {   // and become NaN
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          if (fabsf(lo[u]) == INFINITY) lo[u] = __int_as_float(0x7fc00000);
+          if (fabsf(hi[u]) == INFINITY) hi[u] = __int_as_float(0x7fc00000);
+        }
+      }
       unsigned char *at = cache_at(k, t);
-      *reinterpret_cast<uint2 *>(at) = encode8(lo[k]);
-      *reinterpret_cast<uint2 *>(at + D / 2) = encode8(hi[k]);
+      *reinterpret_cast<uint2 *>(at) = encode8(lo);
+      *reinterpret_cast<uint2 *>(at + D / 2) = encode8(hi);
     }
   }
 }
