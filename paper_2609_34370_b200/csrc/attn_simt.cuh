@@ -7,8 +7,6 @@
 // the bf16 tensor-core kernel and also accepts bf16 inputs, which the tests
 // use to cross-check the two kernels.
 #pragma once
-#include <type_traits>
-
 #include "common.cuh"
 
 namespace spx {
@@ -34,10 +32,7 @@ struct SimtSmem {
   }
 };
 
-// kE4m3: the pools hold 8-bit floats, dequantised (code * scale, one fp32 rounding) as they are staged.
-// A masked score is kept apart from a vanishing one there (weight -1), so that a NaN in the V of a
-// position a query does not see cannot reach it as 0 * NaN.
-template <typename T, int D, bool kE4m3 = false>
+template <typename T, int D>
 __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(AttnParams p) {
   SPX_TL_SCOPE(kTlAttention);
   // the combine kernel may take its places now (it reads the planner's list, then waits for this
@@ -57,9 +52,8 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(AttnParams p) {
   int *sPage = reinterpret_cast<int *>(smem_raw + lay.page);
 
   const T *Q = reinterpret_cast<const T *>(p.q);
-  using C = typename std::conditional<kE4m3, unsigned char, T>::type;
-  const C *Kc = reinterpret_cast<const C *>(p.k_cache);
-  const C *Vc = reinterpret_cast<const C *>(p.v_cache);
+  const T *Kc = reinterpret_cast<const T *>(p.k_cache);
+  const T *Vc = reinterpret_cast<const T *>(p.v_cache);
   T *out = reinterpret_cast<T *>(p.out);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int G = p.G;
@@ -114,14 +108,8 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(AttnParams p) {
         if (page >= 0) {
           const int64_t a = (int64_t)page * p.stride_page + (int64_t)g * p.stride_head +
                             (int64_t)((t0 + tt) & (p.P - 1)) * p.stride_token + d;
-          if constexpr (kE4m3) {
-            const int64_t si = (((int64_t)page * p.Hkv + g) << (p.log2P - p.log2SB)) + (((t0 + tt) & (p.P - 1)) >> p.log2SB);
-            kv = e4m3_to_float(Kc[a]) * p.k_scales[si];
-            vv = e4m3_to_float(Vc[a]) * p.v_scales[si];
-          } else {
-            kv = ld_as_float(Kc, a);
-            vv = ld_as_float(Vc, a);
-          }
+          kv = ld_as_float(Kc, a);
+          vv = ld_as_float(Vc, a);
         }
         sK[tt * (D + 1) + d] = kv;
         sV[tt * D + d] = vv;
@@ -141,12 +129,10 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(AttnParams p) {
         // online softmax for this row over the 32 tokens of the step
         const float m_old = sM[row];
         const float m_new = fmaxf(m_old, warp_max(s));
-        // (a NaN score is no maximum: with 8-bit pools a row of nothing else still sums to NaN)
-        const float pexp = kE4m3 ? (vis ? fast_exp2(s - (m_new == -INFINITY ? 0.f : m_new)) : 0.f)
-                                 : (m_new == -INFINITY) ? 0.f : fast_exp2(s - m_new);
+        const float pexp = (m_new == -INFINITY) ? 0.f : fast_exp2(s - m_new);
         const float alpha = (m_new == -INFINITY) ? 1.f : fast_exp2(m_old - m_new);
         const float psum = warp_sum(pexp);
-        sS[row * kSimtSub + lane] = kE4m3 && !vis ? -1.f : pexp;
+        sS[row * kSimtSub + lane] = pexp;
         if (lane == 0) { sM[row] = m_new; sL[row] = sL[row] * alpha + psum; sAlpha[row] = alpha; }
       }
       __syncthreads();
@@ -156,10 +142,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_kernel(AttnParams p) {
         const float *pr = sS + row * kSimtSub;
         float acc = sO[i] * sAlpha[row];
 #pragma unroll 8
-        for (int tt = 0; tt < kSimtSub; ++tt) {
-          if (kE4m3 && pr[tt] < 0.f) continue;
-          acc = fmaf(pr[tt], sV[tt * D + d], acc);
-        }
+        for (int tt = 0; tt < kSimtSub; ++tt) acc = fmaf(pr[tt], sV[tt * D + d], acc);
         sO[i] = acc;
       }
     }

@@ -61,11 +61,6 @@ __device__ __forceinline__ float ld_as_float(const __nv_bfloat16 *p, int64_t i) 
 __device__ __forceinline__ void st_from_float(float *p, int64_t i, float v) { p[i] = v; }
 __device__ __forceinline__ void st_from_float(__nv_bfloat16 *p, int64_t i, float v) { p[i] = __float2bfloat16_rn(v); }
 
-// The value of one 8-bit float (4 exponent bits, 3 mantissa bits): exact.
-__device__ __forceinline__ float e4m3_to_float(unsigned char c) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3)));
-}
-
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -10,6 +10,7 @@
 
 #include "attn_e4m3.cuh"
 #include "attn_simt.cuh"
+#include "attn_simt_e4m3.cuh"
 #include "attn_tc.cuh"
 #include "attn_tc4.cuh"
 #include "common.cuh"
@@ -460,26 +461,39 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
     } else
       e = p.D == 128 ? launch_tc<128, 128>(kmap, vmap, p, sms, stream) : launch_tc<64, 128>(kmap, vmap, p, sms, stream);
   } else {
-    const SimtSmem lay(p.rows_cap, p.D);
-    if (lay.total > dev.max_smem_optin) return SPX_ERR_UNSUPPORTED;
+    const bool e4m3 = a->cache_format == SPX_CACHE_E4M3;
+    const int threads = e4m3 ? kSfThreads : kSimtThreads;
+    const int smem = e4m3 ? SfSmem(p.rows_cap, p.D).total : SimtSmem(p.rows_cap, p.D).total;
+    if (smem > dev.max_smem_optin) return SPX_ERR_UNSUPPORTED;
     auto launch_simt = [&](auto kernel) -> cudaError_t {
-      cudaError_t er = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lay.total);
+      cudaError_t er = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (er != cudaSuccess) return er;
       int per_sm = 0;
-      er = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kSimtThreads, lay.total);
+      er = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
       if (er != cudaSuccess) return er;
       if (per_sm < 1) per_sm = 1;
       if (t_ev_start) cudaEventRecord(t_ev_start, stream);
-      kernel<<<dev.num_sms * per_sm, kSimtThreads, lay.total, stream>>>(p);
+      kernel<<<dev.num_sms * per_sm, threads, smem, stream>>>(p);
       if (t_ev_stop) cudaEventRecord(t_ev_stop, stream);
       ++t_launches;
       return cudaGetLastError();
     };
-    if (a->cache_format == SPX_CACHE_E4M3) {
+    // 8-bit pools: packed rows per warp of the smallest kernel that holds them
+    auto launch_simt_e4m3 = [&](auto type, auto dim) -> cudaError_t {
+      using T = decltype(type);
+      constexpr int D = decltype(dim)::value;
+      if (p.rows_cap <= 16) return launch_simt(attn_simt_e4m3_kernel<T, D, 2>);
+      if (p.rows_cap <= 32) return launch_simt(attn_simt_e4m3_kernel<T, D, 4>);
+      if (p.rows_cap <= 64) return launch_simt(attn_simt_e4m3_kernel<T, D, 8>);
+      return launch_simt(attn_simt_e4m3_kernel<T, D, 16>);
+    };
+    if (e4m3) {
+      using D64 = std::integral_constant<int, 64>;
+      using D128 = std::integral_constant<int, 128>;
       if (a->kv_dtype == SPX_F32)
-        e = p.D == 64 ? launch_simt(attn_simt_kernel<float, 64, true>) : launch_simt(attn_simt_kernel<float, 128, true>);
+        e = p.D == 64 ? launch_simt_e4m3(float(), D64()) : launch_simt_e4m3(float(), D128());
       else
-        e = p.D == 64 ? launch_simt(attn_simt_kernel<__nv_bfloat16, 64, true>) : launch_simt(attn_simt_kernel<__nv_bfloat16, 128, true>);
+        e = p.D == 64 ? launch_simt_e4m3(__nv_bfloat16(), D64()) : launch_simt_e4m3(__nv_bfloat16(), D128());
     } else if (a->kv_dtype == SPX_F32)
       e = p.D == 64 ? launch_simt(attn_simt_kernel<float, 64>) : launch_simt(attn_simt_kernel<float, 128>);
     else
