@@ -16,19 +16,21 @@
 // one thread instead of by elect.sync in a converged warp.  24 of them take 650 of the 1,420 cycles a tile's
 // 32 KB need from memory: the kernel stays bound by HBM.
 //
-// binary16 has no exponents to spare for V's scales, so a row's reference m' is the running maximum of
-// s_t + log2 v_t instead of s_t: y_t = 2^(11 + s_t - m') goes into the row's sum and x_t = y_t v_t into
-// P, both under the one reference.  Within a tile whose scales lie within a factor of 16 of each
-// other the bound max s + max log2 v stands for the maximum; other tiles take it element by element.
-// m' moves when it is passed by a factor of 16, which rescales O.  The least x with a bit left is then 2^-27
-// of the largest, or better.
+// binary16 has no exponents to spare for V's scales, so a row's reference m' is the maximum of s_t + log2 v_t
+// instead of s_t: y_t = 2^(10 + s_t - m') goes into the row's sum and x_t = y_t v_t into P, both under
+// the one reference.  It is taken from an entry's first tile (a bound: max s + max log2 v where the tile's scales
+// lie within a factor of 16 of each other, element by element elsewhere) and kept: the tiles after it need no
+// maximum, and their warps no agreement, before the weights.  They look at the x they make.  One above 2^13 has the
+// group take the next tile's maximum again; one above 2^15 is past what P can hold, and the
+// group takes the maximum and makes the same tile's weights again: scores, scales and V are held until the
+// tile's verdict is read, which the issuers do as well before they go on.  m' moves, and O is rescaled, when a tile's
+// maximum passes it by a factor of 16.  The least x with a bit left is 2^-22 of the row's largest, or better.
 //
-// Roles of the 384 threads: warp 0 TMA producer, warp 1 MMA issuer, warp 2 scales of the next tiles,
-// warp 3 query pieces of the next entry, warps 4-7 and 8-11 two softmax groups that take the tiles in
-// turn, each with its own reference, sum and O, merged in the entry's epilogue: a tile's chain (scores,
-// maximum, weights, pieces) is some 2,000 cycles long, and two tiles in it at a time keep up with
-// memory.  (Eight warps on one tile: 118 us on the Llama-3-8B layer shape.)  The plan, its work entries,
-// partial results and bounded waits are those of the 16-bit kernels.
+// Roles of the 512 threads: warp 0 TMA producer, warp 1 issuer of the score MMAs, warp 12 of the value MMAs,
+// warp 2 scales of the next tiles, warps 3 and 13-15 query pieces of the next entry, warps 4-7 and 8-11 two softmax groups
+// that take the tiles in turn, each with its own reference, sum and O, merged in the entry's epilogue: a tile's
+// chain (scores, weights, pieces) is some 2,000 cycles long, and two tiles in it at a time keep up with memory.
+// The plan, its work entries, partial results and bounded waits are those of the 16-bit kernels.
 #pragma once
 #include <cstddef>
 
@@ -42,8 +44,9 @@ constexpr int kE8GroupWarps = 4;   // softmax warps of a group
 constexpr int kE8ScaleSlots = 4;   // tiles whose scales are staged
 constexpr int kE8RowSlots = 8;     // entries whose row factors are kept: the query warp is at most four entries ahead of the softmax
 constexpr int kE8NanSlots = 8;
-constexpr float kE8Shift = 11.f;   // x <= 2^(11 + 4) stays below binary16's 65504
-constexpr float kE8Rescale = 4.f;
+constexpr float kE8Shift = 10.f;
+constexpr float kE8Rescale = 4.f;   // under a fresh reference x <= 2^(10 + 4)
+constexpr uint32_t kE8Warn = 0x7000u, kE8Redo = 0x7800u;   // 2^13, 2^15 as binary16 (its largest: 65504)
 constexpr float kE8MinLog2 = -90.f;  // smaller V scales count as this in m', so that no sum of y overflows
 
 template <int D, int MROWS>
@@ -72,10 +75,11 @@ struct E8Cfg {
 
 struct E8Barriers {
   uint64_t k_full[4], v_full[4], k_empty[4], v_empty[4], sc_full[kE8ScaleSlots], sc_empty[kE8ScaleSlots];
-  uint64_t s_full[2], p_full[2], q_full[2], q_empty[2], pv_done[2], o_full[2], o_free[2], item_done[2], e_bar[2];
+  uint64_t s_full[2], p_full[2], q_full[2], q_empty[2], pv_done[2], o_full[2], o_free[2], item_done[2], e_bar[2], redo_ack[2];
   uint32_t tmem_base;
   volatile int32_t abort;
   int32_t nan_any[kE8NanSlots];
+  int32_t verdict[2][4];   // of a group's last weights, by phase of p_full: 0 fine, 1 near the end of P's range, 2 past it
   int32_t *dev_status;
 };
 static_assert(sizeof(E8Barriers) <= 512, "barrier area");
@@ -201,6 +205,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 // Four values, as two binary16 pairs, as the sums of an e4m3 and an e5m2 value, each rounded to nearest.
 __device__ __forceinline__ void cut2(uint32_t h01, uint32_t h23, uint32_t &w1, uint32_t &w2) {
   uint16_t a, b;
@@ -264,6 +273,8 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       mbar_init(&bars->s_full[b], 1); mbar_init(&bars->p_full[b], kE8GroupWarps); mbar_init(&bars->q_full[b], kE8QueryWarps); mbar_init(&bars->q_empty[b], 1);
       mbar_init(&bars->pv_done[b], 1); mbar_init(&bars->o_full[b], 1); mbar_init(&bars->o_free[b], 2 * kE8GroupWarps);
       mbar_init(&bars->item_done[b], 2 * kE8GroupWarps); mbar_init(&bars->e_bar[b], kE8GroupWarps);
+      mbar_init(&bars->redo_ack[b], 2);
+      for (int i = 0; i < 4; ++i) bars->verdict[b][i] = 0;
     }
     bars->abort = 0;
     bars->dev_status = p.dev_status;
@@ -364,8 +375,21 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       return p.work[idx].tile_end - p.work[idx].tile_begin;
     };
     int n_tiles = tiles_of(0), n_next = tiles_of(1), i = 0;
+    // the weights of group b's next tile: those the group has not taken back
+    uint32_t phase0 = 0, phase1 = 0;
+    auto wait_weights = [&](uint32_t b) {
 #pragma unroll 1
-    for (uint32_t t = 0; item_index(it) >= 0 && !bars->abort; ++t) {
+      for (;;) {
+        const uint32_t n = b ? phase1++ : phase0++;
+        warp_wait(SPX_E8_BAR(p_full, b), n & 1);
+        if (*reinterpret_cast<volatile int32_t *>(&bars->verdict[b][n & 3]) != 2 || bars->abort) return;
+        __syncwarp();
+        if (lane == 0) arrive(SPX_E8_BAR(redo_ack, b));   // seen: the group may complete another phase
+      }
+    };
+    uint32_t n_issued = 0;
+#pragma unroll 1
+    for (uint32_t t = 0; item_index(it) >= 0 && !bars->abort; ++t, ++n_issued) {
       const int slot = t % Cfg::kStages;
       const uint32_t ph = (t / Cfg::kStages) & 1;
       const bool last = i + 1 >= n_tiles;
@@ -375,7 +399,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         if (i == 0) warp_wait(SPX_E8_BAR(q_full, qb), (Cfg::kQBufs == 2 ? (it >> 1) : it) & 1);
         warp_wait(SPX_E8_BAR(k_full, slot), ph);
         // the buffer's last scores have been read once they are weights
-        if (t >= 2) warp_wait(SPX_E8_BAR(p_full, t & 1), ((t - 2) >> 1) & 1);
+        if (t >= 2) wait_weights(t & 1);
         fence_after();
         const uint64_t qa = smem_desc(smem_u32(sQ + qb * 2 * Cfg::kPiece), 16, 1024), ka = kv_desc<D>(smem_u32(sK + slot * Cfg::kTileBytes));
         const uint32_t ts = tmem + Cfg::kColS + (t & 1) * Cfg::kSCols;
@@ -398,7 +422,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         if (i == 0 && it >= Cfg::kOBufs)
           warp_wait(SPX_E8_BAR(o_free, Cfg::kOBufs == 2 ? (it & 1) : 0), (Cfg::kOBufs == 2 ? (it >> 1) - 1 : it - 1) & 1);
         warp_wait(SPX_E8_BAR(v_full, slot), ph);
-        warp_wait(SPX_E8_BAR(p_full, t & 1), (t >> 1) & 1);
+        wait_weights(t & 1);
         fence_after();
         const uint64_t pa = smem_desc(smem_u32(sP + (Cfg::kPBufs == 2 ? (t & 1) : 0) * 3 * Cfg::kPiece), 16, 1024), va = kv_desc<D>(smem_u32(sV + slot * Cfg::kTileBytes));
         const uint32_t to = tmem + Cfg::kColO + ((Cfg::kOBufs == 2 ? (it & 1) * 2 : 0) + (t & 1)) * Cfg::kOCols;
@@ -421,6 +445,10 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       ++i;
       if (last) { ++it; i = 0; n_tiles = n_next; n_next = tiles_of(it + 1); }
     }
+    // (the score issuer looks at the last two tiles' verdicts too: a group that takes weights back waits for both)
+    if (scores)
+#pragma unroll 1
+      for (uint32_t t = n_issued < 2 ? 0 : n_issued - 2; t < n_issued && !bars->abort; ++t) wait_weights(t & 1);
   } else if (warp == 2) {
     // ------------------------------------------------------------------ scales, one float per token and tile
     // A lane owns four consecutive tokens (of one page: pages hold eight at least).  The chain table ->
@@ -660,8 +688,9 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       if (sm_tid == 128) bars->nan_any[clear] = 0;
       pend.valid = false;
     };
-    // One step of the loop: this group's next tile of the current entry, if it has one, then the epilogue of
-    // the entry before, then, behind the entry's last tile, its sums and the next entry.
+    // One step of the loop: the verdict on the last tile's weights, then this group's next tile of the current entry (or
+    // the last one again), then the epilogue of the entry before; behind the entry's last tile its sums and
+    // the next entry.
     WorkEntry e, e_next;
     int it = 0;
     bool have = item_index(0) >= 0;
@@ -670,13 +699,34 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     uint32_t t_first = 0;                          // the entry's first tile in the CTA's sequence
     int tile = have ? e.tile_begin + grp : 0;
     float x_ref = -INFINITY, l_sum = 0.f, row_f = 0.f;   // the reference is the same in all parts of a row
-    bool first = true;
+    bool first = true, need_max = true, check = false, again = false;
+    uint32_t n_phase = 0, n_redo = 0;                    // p_full phases completed by this group, tiles taken back
+    uint32_t last_slot = 0;
+    float l_before = 0.f;
 #pragma unroll 1
     while (!bars->abort) {
+      if (check) {
+        check = false;
+        warp_wait(SPX_E8_BAR(p_full, grp), (n_phase - 1) & 1);   // (all four warps' verdicts are in)
+        const int verdict = *reinterpret_cast<volatile int32_t *>(&bars->verdict[grp][(n_phase - 1) & 3]);
+        if (verdict == 2) {
+          warp_wait(SPX_E8_BAR(redo_ack, grp), n_redo & 1);
+          ++n_redo;
+          tile -= 2;
+          l_sum = l_before;
+          again = true;   // (once: under a fresh reference nothing passes 2^14 but what is not finite)
+        } else {
+          again = false;
+          __syncwarp();
+          if (lane == 0) arrive(SPX_E8_BAR(sc_empty, last_slot));
+        }
+        need_max |= verdict != 0;
+      }
       // with a single pair of O's the entry's first value MMAs wait for the last epilogue, and the other
       // group's may be what this tile's P waits for: nothing is deferred there
       if (Cfg::kOBufs == 1 && pend.valid) run_epilogue();
-      if (have && tile < e.tile_end) {
+      const bool work = have && tile < e.tile_end;
+      if (work) {
         const bool valid_row = row < e.m * p.G;
         const int limit = e.L - e.m + row_j;         // last visible token of this row
         const uint32_t tc_ = t_first + (uint32_t)(tile - e.tile_begin);
@@ -713,52 +763,57 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
             }
           }
         };
-        const float2 v_range = sVr[sc_slot];
-        const bool narrow = v_range.y != 0.f;
-        float mx = -INFINITY, mx2 = -INFINITY;
+        float alpha = 1.f;
+        if (NCH == 1 || need_max) load_scores(0);
+        if (need_max) {
+          const float2 v_range = sVr[sc_slot];
+          const bool narrow = v_range.y != 0.f;
+          float mx = -INFINITY, mx2 = -INFINITY;
 #pragma unroll 1
-        for (int ch = 0; ch < NCH; ++ch) {
-          load_scores(ch);
-#pragma unroll
-          for (int i = 0; i < CH / 2; ++i) {
-            float a, b;
-            unpair(v[i], a, b);
-            mx = fmaxf(mx, fmaxf(a, b));
-          }
-          if (!narrow) {
-            const float *vs1 = sVs + sc_slot * 128 + part * TPT + ch * CH;
+          for (int ch = 0;;) {
 #pragma unroll
             for (int i = 0; i < CH / 2; ++i) {
               float a, b;
               unpair(v[i], a, b);
-              mx2 = fmaxf(mx2, fmaxf(fmaf(a, row_f, fmaxf(__log2f(vs1[2 * i]), kE8MinLog2)), fmaf(b, row_f, fmaxf(__log2f(vs1[2 * i + 1]), kE8MinLog2))));
+              mx = fmaxf(mx, fmaxf(a, b));
             }
-          }
-        }
-        float x_tile = narrow ? fmaf(mx, row_f, v_range.x) : mx2;
-        if constexpr (kSplit > 1) {
-          // agree on the row's maximum over the whole tile
-          float *sm = sMx + ((ec & 1) ? 2 * 128 : 0) + grp * 128;
-          sm[part * MROWS + row] = x_tile;
-          __syncwarp();
-          if (lane == 0) arrive(SPX_E8_BAR(e_bar, grp));
-          warp_wait(SPX_E8_BAR(e_bar, grp), ec & 1);
-          ++ec;
-          x_tile = -INFINITY;
+            if (!narrow) {
+              const float *vs1 = sVs + sc_slot * 128 + part * TPT + ch * CH;
 #pragma unroll
-          for (int i = 0; i < kSplit; ++i) x_tile = fmaxf(x_tile, sm[i * MROWS + row]);
-        } else {
-          x_tile = fmaxf(x_tile, -INFINITY);   // (no NaN)
-        }
-        // the reference moves when it is passed by a factor of sixteen; a row without one adopts the tile's
-        // (its O and its sum are zero)
-        float alpha = 1.f;
-        if (x_ref == -INFINITY) {
-          x_ref = x_tile;
-        } else if (x_tile > x_ref + kE8Rescale) {
-          alpha = fast_exp2(x_ref - x_tile);
-          x_ref = x_tile;
-          l_sum *= alpha;
+              for (int i = 0; i < CH / 2; ++i) {
+                float a, b;
+                unpair(v[i], a, b);
+                mx2 = fmaxf(mx2, fmaxf(fmaf(a, row_f, fmaxf(__log2f(vs1[2 * i]), kE8MinLog2)), fmaf(b, row_f, fmaxf(__log2f(vs1[2 * i + 1]), kE8MinLog2))));
+              }
+            }
+            if (++ch >= NCH) break;
+            load_scores(ch);
+          }
+          float x_tile = narrow ? fmaf(mx, row_f, v_range.x) : mx2;
+          if constexpr (kSplit > 1) {
+            // agree on the row's maximum over the whole tile
+            float *sm = sMx + ((ec & 1) ? 2 * 128 : 0) + grp * 128;
+            sm[part * MROWS + row] = x_tile;
+            __syncwarp();
+            if (lane == 0) arrive(SPX_E8_BAR(e_bar, grp));
+            warp_wait(SPX_E8_BAR(e_bar, grp), ec & 1);
+            ++ec;
+            x_tile = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kSplit; ++i) x_tile = fmaxf(x_tile, sm[i * MROWS + row]);
+          } else {
+            x_tile = fmaxf(x_tile, -INFINITY);   // (no NaN)
+          }
+          // the reference moves when it is passed by a factor of sixteen; a row without one adopts the tile's
+          // (its O and its sum are zero)
+          if (x_ref == -INFINITY) {
+            x_ref = x_tile;
+          } else if (x_tile > x_ref + kE8Rescale) {
+            alpha = fast_exp2(x_ref - x_tile);
+            x_ref = x_tile;
+            l_sum *= alpha;
+          }
+          need_max = false;
         }
         // this group's last value MMA: its P is rewritten, its O perhaps rescaled
         if (tc_ >= 2) {
@@ -785,6 +840,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         unsigned char *pr = sP + (Cfg::kPBufs == 2 ? grp : 0) * 3 * Cfg::kPiece + (row >> 3) * 1024 + (row & 7) * 128;
         const uint64_t row_f2 = pair(row_f, row_f), shift2 = pair(shift, shift);
         uint64_t sum2 = 0;
+        uint32_t h_max = 0;
 #pragma unroll 1
         for (int ch = 0; ch < NCH; ++ch) {
           if (NCH > 1) load_scores(ch);
@@ -804,6 +860,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
                 sum2 = add2(sum2, y);
                 unpair(mul2(y, u ? s.y : s.x), y0, y1);
                 h[u] = pack_f16(y0, y1);
+                h_max = max_f16x2(h_max, h[u]);
               }
               cut3(h[0], h[1], w[0][i], w[1][i], w[2][i]);
             }
@@ -815,7 +872,13 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         }
         float sum_lo, sum_hi;
         unpair(sum2, sum_lo, sum_hi);
+        l_before = l_sum;
         l_sum += sum_lo + sum_hi;
+        // the verdict: x is not negative, so binary16 patterns order like values (NaNs do not count)
+        const uint32_t x_top = max(h_max & 0xffffu, h_max >> 16);
+        const bool past = __any_sync(0xffffffffu, valid_row && x_top > kE8Redo), near = __any_sync(0xffffffffu, valid_row && x_top > kE8Warn);
+        if (lane == 0 && near) atomicMax(&bars->verdict[grp][n_phase & 3], past && !again ? 2 : 1);
+        if (g_tid == 0) bars->verdict[grp][(n_phase + 2) & 3] = 0;   // read by everybody: the group is two phases on
         if (mask_tile) {
           // V at the end of the request, as its value MMA must see it: slots past the end are zero (they
           // hold an earlier tile's or nobody's bytes, and 0 * NaN is NaN), and a NaN at a position that some
@@ -853,13 +916,16 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         fence_async_smem();
         fence_before();
         __syncwarp();
-        if (lane == 0) { arrive(SPX_E8_BAR(p_full, grp)); arrive(SPX_E8_BAR(sc_empty, sc_slot)); }
+        if (lane == 0) arrive(SPX_E8_BAR(p_full, grp));
+        ++n_phase;
+        check = true;
+        last_slot = sc_slot;
         first = false;
         tile += 2;
       }
       if (Cfg::kOBufs == 2 && pend.valid) run_epilogue();
       if (!have) break;
-      if (tile >= e.tile_end) {
+      if (!work) {
         sL[(it & 1) * 256 + grp * 128 + part * MROWS + row] = l_sum;
         if (part == 0) sRef[(it & 1) * 2 * MROWS + grp * MROWS + row] = x_ref;
         __syncwarp();
@@ -872,7 +938,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         if (item_index(it + 1) >= 0) e_next = p.work[item_index(it + 1)];
         if (have) tile = e.tile_begin + (int)((t_first ^ (uint32_t)grp) & 1);
         x_ref = -INFINITY; l_sum = 0.f;
-        first = true;
+        first = need_max = true;
       }
     }
   }

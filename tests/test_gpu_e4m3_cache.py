@@ -119,6 +119,41 @@ def test_peaked_and_flat_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("hq,hkv,d,m", [(8, 2, 64, 3), (32, 8, 128, 6), (36, 1, 128, 1), (64, 8, 128, 9), (8, 1, 64, 16)])
+def test_scores_that_grow_from_tile_to_tile(hq, hkv, d, m, dtype):
+    """Maxima that rise by a few, by a hundred and by a million times, at any place of the sequence: the first token of a later tile,
+    the last token, one tile after another, for some rows only, beside V scales that rise with them."""
+    lens = [700, 1290, 520, 128, 385]
+    c = R.Cache(lens, hkv, d, 16, 16, seed=31, spread=0.1)
+    q = torch.randn(m * len(lens), hq, d, generator=torch.Generator().manual_seed(9)) * 0.1
+    def lift(r, t, size, lanes=slice(None)):
+        # key t of request r along the mean of some of its queries: a score near `size`
+        page, slot = int(c.table[r, t // 16]), t % 16
+        for h in range(hkv):
+            rows = q[m * r:m * r + m, h * (hq // hkv):(h + 1) * (hq // hkv)].reshape(-1, d)[lanes]
+            mean = rows.mean(0)
+            k = mean / mean.norm() ** 2 * size * math.sqrt(d)
+            s = float(k.abs().max()) / 400
+            block = torch.from_numpy(R.decode(c.k[page, h])) * float(c.k_scales[page, h, 0])
+            s = max(s, float(block.abs().max()) / 440)
+            block[slot] = k.double()
+            c.k[page, h] = torch.from_numpy(R.encode((block / s).numpy()))
+            c.k_scales[page, h, 0] = s
+    for i, t in enumerate((130, 270, 390, 513, 699)):
+        lift(0, t, 6.0 * (i + 1))
+    for t, size in ((200, 3.0), (1024, 20.0), (1289, 45.0)):
+        lift(1, t, size)
+    lift(2, 260, 15.0, slice(0, 2))
+    lift(2, 511, 30.0, slice(2, None))
+    lift(4, 384, 25.0)
+    c.v_scales[c.table[1, 70:].clamp(min=0).long()] *= 2.0 ** 9
+    q = q.to(dtype)
+    out, lse, status = _attend(c, q, lens, [m] * len(lens))
+    assert status == 0
+    _check(c, q, lens, [m] * len(lens), out, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 def test_value_scales_of_very_different_size(dtype):
     lens, m = [260, 513], [3, 2]
     c = R.Cache(lens, 2, 128, 16, 16, seed=9, spread=0.3)
