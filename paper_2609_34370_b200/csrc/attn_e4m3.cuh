@@ -18,13 +18,12 @@
 //
 // binary16 has no exponents to spare for V's scales, so a row's reference m' is the maximum of s_t + log2 v_t
 // instead of s_t: y_t = 2^(10 + s_t - m') goes into the row's sum and x_t = y_t v_t into P, both under
-// the one reference.  It is taken from an entry's first tile (a bound: max s + max log2 v where the tile's scales
-// lie within a factor of 16 of each other, element by element elsewhere) and kept: the tiles after it need no
-// maximum, and their warps no agreement, before the weights.  They look at the x they make.  One above 2^13 has the
+// the one reference.  It is taken from an entry's first tile and kept: the tiles after it need no maximum,
+// and their warps no agreement, before the weights.  They look at the x they make.  One above 2^13 has the
 // group take the next tile's maximum again; one above 2^15 is past what P can hold, and the
 // group takes the maximum and makes the same tile's weights again: scores, scales and V are held until the
 // tile's verdict is read, which the issuers do as well before they go on.  m' moves, and O is rescaled, when a tile's
-// maximum passes it by a factor of 16.  The least x with a bit left is 2^-22 of the row's largest, or better.
+// maximum passes it by a factor of 16.  The least x with a bit left is 2^-26 of the row's largest.
 //
 // Roles of the 512 threads: warp 0 TMA producer, warp 1 issuer of the score MMAs, warp 12 of the value MMAs,
 // warp 2 scales of the next tiles, warps 3 and 13-15 query pieces of the next entry, warps 4-7 and 8-11 two softmax groups
@@ -65,8 +64,8 @@ struct E8Cfg {
   static_assert(kTmemNeed <= 512, "tensor memory");
   // byte offsets into shared memory, after rounding its base up to 1024
   static constexpr int kOffK = 0, kOffV = kOffK + kStages * kTileBytes, kOffQ = kOffV + kStages * kTileBytes, kOffP = kOffQ + kQBufs * 2 * kPiece;
-  static constexpr int kOffKs = kOffP + kPBufs * 3 * kPiece, kOffVs = kOffKs + kE8ScaleSlots * 512, kOffVr = kOffVs + kE8ScaleSlots * 512;
-  static constexpr int kOffMx = kOffVr + kE8ScaleSlots * 16, kOffL = kOffMx + 2 * 1024;
+  static constexpr int kOffKs = kOffP + kPBufs * 3 * kPiece, kOffVs = kOffKs + kE8ScaleSlots * 512, kOffLv = kOffVs + kE8ScaleSlots * 512;
+  static constexpr int kOffMx = kOffLv + kE8ScaleSlots * 512, kOffL = kOffMx + 2 * 1024;
   static constexpr int kOffRef = kOffL + 2 * 1024, kOffRow = kOffRef + 2 * 2 * MROWS * 4, kOffNan = kOffRow + kE8RowSlots * MROWS * 4;
   static constexpr int kOffBar = kOffNan + kE8NanSlots * 128 * 4;
   static constexpr int kSmemBytes = kOffBar + 512 + 1024;
@@ -254,7 +253,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
   unsigned char *sK = smem + Cfg::kOffK, *sV = smem + Cfg::kOffV, *sQ = smem + Cfg::kOffQ, *sP = smem + Cfg::kOffP;
   float *sKs = reinterpret_cast<float *>(smem + Cfg::kOffKs), *sVs = reinterpret_cast<float *>(smem + Cfg::kOffVs);
-  float2 *sVr = reinterpret_cast<float2 *>(smem + Cfg::kOffVr);    // per tile: (log2 of the largest V scale, 1 if all are within a factor of 16)
+  float *sLv = reinterpret_cast<float *>(smem + Cfg::kOffLv);      // log2 of V's scales
   float *sMx = reinterpret_cast<float *>(smem + Cfg::kOffMx);   // [2 tiles][group][kSplit][MROWS]
   float *sL = reinterpret_cast<float *>(smem + Cfg::kOffL);        // [2 entries][group][kSplit][MROWS]
   float *sRef = reinterpret_cast<float *>(smem + Cfg::kOffRef);    // [2 entries][group][MROWS]
@@ -387,9 +386,16 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         if (lane == 0) arrive(SPX_E8_BAR(redo_ack, b));   // seen: the group may complete another phase
       }
     };
+    // (the score issuer looks at the last two tiles' verdicts too: a group that takes weights back waits for both)
     uint32_t n_issued = 0;
 #pragma unroll 1
-    for (uint32_t t = 0; item_index(it) >= 0 && !bars->abort; ++t, ++n_issued) {
+    for (uint32_t t = 0; !bars->abort; ++t) {
+      const bool more = item_index(it) >= 0;
+      if (!more && (!scores || t >= n_issued + 2)) break;
+      // values: the tile's weights; scores: tile t - 2's, which were made of what the buffer holds
+      if (!scores || t >= 2) wait_weights(t & 1);
+      if (!more) continue;
+      ++n_issued;
       const int slot = t % Cfg::kStages;
       const uint32_t ph = (t / Cfg::kStages) & 1;
       const bool last = i + 1 >= n_tiles;
@@ -398,8 +404,6 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         const uint32_t qb = Cfg::kQBufs == 2 ? (it & 1) : 0;
         if (i == 0) warp_wait(SPX_E8_BAR(q_full, qb), (Cfg::kQBufs == 2 ? (it >> 1) : it) & 1);
         warp_wait(SPX_E8_BAR(k_full, slot), ph);
-        // the buffer's last scores have been read once they are weights
-        if (t >= 2) wait_weights(t & 1);
         fence_after();
         const uint64_t qa = smem_desc(smem_u32(sQ + qb * 2 * Cfg::kPiece), 16, 1024), ka = kv_desc<D>(smem_u32(sK + slot * Cfg::kTileBytes));
         const uint32_t ts = tmem + Cfg::kColS + (t & 1) * Cfg::kSCols;
@@ -422,7 +426,6 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         if (i == 0 && it >= Cfg::kOBufs)
           warp_wait(SPX_E8_BAR(o_free, Cfg::kOBufs == 2 ? (it & 1) : 0), (Cfg::kOBufs == 2 ? (it >> 1) - 1 : it - 1) & 1);
         warp_wait(SPX_E8_BAR(v_full, slot), ph);
-        wait_weights(t & 1);
         fence_after();
         const uint64_t pa = smem_desc(smem_u32(sP + (Cfg::kPBufs == 2 ? (t & 1) : 0) * 3 * Cfg::kPiece), 16, 1024), va = kv_desc<D>(smem_u32(sV + slot * Cfg::kTileBytes));
         const uint32_t to = tmem + Cfg::kColO + ((Cfg::kOBufs == 2 ? (it & 1) * 2 : 0) + (t & 1)) * Cfg::kOCols;
@@ -445,92 +448,68 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       ++i;
       if (last) { ++it; i = 0; n_tiles = n_next; n_next = tiles_of(it + 1); }
     }
-    // (the score issuer looks at the last two tiles' verdicts too: a group that takes weights back waits for both)
-    if (scores)
-#pragma unroll 1
-      for (uint32_t t = n_issued < 2 ? 0 : n_issued - 2; t < n_issued && !bars->abort; ++t) wait_weights(t & 1);
   } else if (warp == 2) {
     // ------------------------------------------------------------------ scales, one float per token and tile
     // A lane owns four consecutive tokens (of one page: pages hold eight at least).  The chain table ->
-    // scale of a tile is spread over two iterations, so that no load is waited for.
-    struct TCursor { int it, tile; WorkEntry e, e_next; bool valid; };
-    auto open = [&](TCursor &c, int it) {
-      c.it = it;
-      c.valid = item_index(it) >= 0;
-      if (c.valid) {
-        c.tile = c.e.tile_begin;
-        const int idx_next = item_index(it + 1);
-        if (idx_next >= 0) c.e_next = p.work[idx_next];
+    // scale of a tile is spread over two rounds, so that no load is waited for but an entry's own (the ring is
+    // four tiles deep).
+    int it = -1, tile = 0, tile_end = 0, req = 0, g = 0, L = 0;
+    auto advance = [&]() -> bool {
+      if (++tile >= tile_end) {
+        const int idx = item_index(++it);
+        if (idx < 0) return false;
+        const WorkEntry e = p.work[idx];
+        req = e.req; g = e.g; L = e.L; tile = e.tile_begin; tile_end = e.tile_end;
       }
+      return true;
     };
-    auto advance = [&](TCursor &c) {
-      if (!c.valid) return;
-      if (++c.tile >= c.e.tile_end) { c.e = c.e_next; open(c, c.it + 1); }
-    };
-    auto load_page = [&](const TCursor &c) -> int {
-      const int t = c.tile * kTileTokens + lane * 4;
-      if (!c.valid || t >= c.e.L) return -1;
-      const int page = p.block_table[(int64_t)c.e.req * p.max_pages_per_req + (t >> p.log2P)];
-      return page < 0 || page >= p.num_pages ? 0 : page;   // (flagged by the producer)
-    };
-    auto load_scales = [&](const TCursor &c, int page, float (&ks)[4], float (&vs)[4]) {
-      const int t = c.tile * kTileTokens + lane * 4;
-      const int left = page >= 0 ? c.e.L - t : 0;   // tokens past the end have scale zero
-      const int64_t base = ((int64_t)page * p.Hkv + c.e.g) << (p.log2P - p.log2SB);
-      const int slot = t & (p.P - 1);
-      if (p.log2SB >= 2) {   // one scale for the lane's tokens
-        float k = 0.f, v = 0.f;
-        if (left > 0) {
-          k = __ldg(p.k_scales + base + (slot >> p.log2SB));
-          v = __ldg(p.v_scales + base + (slot >> p.log2SB));
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { ks[i] = i < left ? k : 0.f; vs[i] = i < left ? v : 0.f; }
-      } else {
+    int page = -1, base_t = 0, base_g = 0, base_L = 0;   // of the tile whose scales are fetched next
+    bool have_page = false, have_scales = false;
+    float ks[4], vs[4];
+#pragma unroll 1
+    for (uint32_t t = 0; !bars->abort;) {
+      float kn[4], vn[4];
+      {
+        const int left = have_page && page >= 0 ? base_L - base_t : 0;   // tokens past the end have scale zero
+        const int64_t base = ((int64_t)page * p.Hkv + base_g) << (p.log2P - p.log2SB);
+        const int slot = base_t & (p.P - 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          ks[i] = vs[i] = 0.f;
+          kn[i] = vn[i] = 0.f;
           if (i < left) {
-            ks[i] = __ldg(p.k_scales + base + ((slot + i) >> p.log2SB));
-            vs[i] = __ldg(p.v_scales + base + ((slot + i) >> p.log2SB));
+            const int64_t at = base + ((slot + i) >> p.log2SB);
+            kn[i] = __ldg(p.k_scales + at);
+            vn[i] = __ldg(p.v_scales + at);
           }
         }
       }
-    };
-    TCursor cur;
-    if (item_index(0) >= 0) cur.e = p.work[item_index(0)];
-    open(cur, 0);
-    float ks[4], vs[4], ks_next[4], vs_next[4];
-    const int page0 = load_page(cur);
-    TCursor next = cur;
-    advance(next);
-    int page_next = load_page(next);
-    load_scales(cur, page0, ks, vs);
-    bool valid = cur.valid;
-    for (uint32_t t = 0; valid && !bars->abort; ++t) {
-      const bool valid_next = next.valid;
-      load_scales(next, page_next, ks_next, vs_next);
-      advance(next);
-      page_next = load_page(next);
-      const int slot = t % kE8ScaleSlots;
-      if (t >= kE8ScaleSlots) warp_wait(SPX_E8_BAR(sc_empty, slot), ((t / kE8ScaleSlots) - 1) & 1);
-      *reinterpret_cast<float4 *>(sKs + slot * 128 + lane * 4) = make_float4(ks[0], ks[1], ks[2], ks[3]);
-      *reinterpret_cast<float4 *>(sVs + slot * 128 + lane * 4) = make_float4(vs[0], vs[1], vs[2], vs[3]);
-      // positive floats order like their patterns
-      uint32_t hi = 0, lo = 0xffffffffu;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t b = __float_as_uint(vs[i]);
-        hi = max(hi, b);
-        if (b != 0) lo = min(lo, b);
+      const bool next_scales = have_page;
+      have_page = it < 0 || item_index(it) >= 0 ? advance() : false;
+      if (have_page) {
+        base_t = tile * kTileTokens + lane * 4; base_g = g; base_L = L;
+        page = -1;
+        if (base_t < L) {
+          page = p.block_table[(int64_t)req * p.max_pages_per_req + (base_t >> p.log2P)];
+          if (page < 0 || page >= p.num_pages) page = 0;   // (flagged by the producer)
+        }
       }
-      const float v_max = __uint_as_float(__reduce_max_sync(0xffffffffu, hi)), v_min = __uint_as_float(__reduce_min_sync(0xffffffffu, lo));
-      if (lane == 0) sVr[slot] = make_float2(fmaxf(__log2f(v_max), kE8MinLog2), v_max == 0.f || v_max * 0.0625f <= v_min ? 1.f : 0.f);
-      __syncwarp();
-      if (lane == 0) arrive(SPX_E8_BAR(sc_full, slot));
-      valid = valid_next;
+      if (have_scales) {
+        const int slot = t % kE8ScaleSlots;
+        if (t >= kE8ScaleSlots) warp_wait(SPX_E8_BAR(sc_empty, slot), ((t / kE8ScaleSlots) - 1) & 1);
+        float lv[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { ks[i] = ks_next[i]; vs[i] = vs_next[i]; }
+        for (int i = 0; i < 4; ++i) lv[i] = fmaxf(__log2f(vs[i]), kE8MinLog2);
+        *reinterpret_cast<float4 *>(sKs + slot * 128 + lane * 4) = make_float4(ks[0], ks[1], ks[2], ks[3]);
+        *reinterpret_cast<float4 *>(sVs + slot * 128 + lane * 4) = make_float4(vs[0], vs[1], vs[2], vs[3]);
+        *reinterpret_cast<float4 *>(sLv + slot * 128 + lane * 4) = make_float4(lv[0], lv[1], lv[2], lv[3]);
+        __syncwarp();
+        if (lane == 0) arrive(SPX_E8_BAR(sc_full, slot));
+        ++t;
+      }
+      if (!next_scales && !have_page) break;
+      have_scales = next_scales;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { ks[i] = kn[i]; vs[i] = vn[i]; }
     }
   } else if (warp == 3 || warp > 12) {
     // ------------------------------------------------------------------ query pieces, an entry ahead
@@ -565,10 +544,11 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           waited = true;
           if (uses >= 1) warp_wait(SPX_E8_BAR(q_empty, qb), (uses - 1) & 1);
         }
-#pragma unroll
+#pragma unroll 1
         for (int u = 0; u < kAhead; ++u) {
           const int row = row0 + u * kRows + lane / kLanes;
-          const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+          const uint4 x = u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3];
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
           uint32_t a = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) a = __vmaxu2(a, w[i] & 0x7fff7fffu);
@@ -654,9 +634,12 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       const int nan_slot = it % kE8NanSlots;
       if (bars->nan_any[nan_slot]) {
         // columns of V with a NaN at a new position: into the rows that see it
+        uint64_t hit = 0;
+#pragma unroll 1
+        for (int i = 0; i < CB; ++i) hit |= (uint64_t)((sNan[nan_slot * 128 + col0 + i] & ((1u << row_j) - 1)) != 0) << i;
 #pragma unroll
         for (int i = 0; i < CB; ++i)
-          if (sNan[nan_slot * 128 + col0 + i] & ((1u << row_j) - 1)) o[i] = 0x7fc00000u;
+          if ((hit >> i) & 1) o[i] = 0x7fc00000u;
       }
       if (row < J.m * p.G) {
         if (J.part_slot < 0) {
@@ -766,30 +749,22 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         float alpha = 1.f;
         if (NCH == 1 || need_max) load_scores(0);
         if (need_max) {
-          const float2 v_range = sVr[sc_slot];
-          const bool narrow = v_range.y != 0.f;
-          float mx = -INFINITY, mx2 = -INFINITY;
+          float x_tile = -INFINITY;
+          const uint64_t f2 = pair(row_f, row_f);
 #pragma unroll 1
           for (int ch = 0;;) {
+            const ulonglong2 *lv4 = reinterpret_cast<const ulonglong2 *>(sLv + sc_slot * 128 + part * TPT + ch * CH);
 #pragma unroll
-            for (int i = 0; i < CH / 2; ++i) {
-              float a, b;
-              unpair(v[i], a, b);
-              mx = fmaxf(mx, fmaxf(a, b));
-            }
-            if (!narrow) {
-              const float *vs1 = sVs + sc_slot * 128 + part * TPT + ch * CH;
-#pragma unroll
-              for (int i = 0; i < CH / 2; ++i) {
-                float a, b;
-                unpair(v[i], a, b);
-                mx2 = fmaxf(mx2, fmaxf(fmaf(a, row_f, fmaxf(__log2f(vs1[2 * i]), kE8MinLog2)), fmaf(b, row_f, fmaxf(__log2f(vs1[2 * i + 1]), kE8MinLog2))));
-              }
+            for (int i = 0; i < CH / 4; ++i) {
+              const ulonglong2 lv = lv4[i];
+              float a, b, c, d;
+              unpair(fma2(v[2 * i], f2, lv.x), a, b);
+              unpair(fma2(v[2 * i + 1], f2, lv.y), c, d);
+              x_tile = fmaxf(x_tile, fmaxf(fmaxf(a, b), fmaxf(c, d)));
             }
             if (++ch >= NCH) break;
             load_scores(ch);
           }
-          float x_tile = narrow ? fmaf(mx, row_f, v_range.x) : mx2;
           if constexpr (kSplit > 1) {
             // agree on the row's maximum over the whole tile
             float *sm = sMx + ((ec & 1) ? 2 * 128 : 0) + grp * 128;
@@ -801,8 +776,6 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
             x_tile = -INFINITY;
 #pragma unroll
             for (int i = 0; i < kSplit; ++i) x_tile = fmaxf(x_tile, sm[i * MROWS + row]);
-          } else {
-            x_tile = fmaxf(x_tile, -INFINITY);   // (no NaN)
           }
           // the reference moves when it is passed by a factor of sixteen; a row without one adopts the tile's
           // (its O and its sum are zero)

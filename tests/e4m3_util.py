@@ -121,9 +121,8 @@ def attention(c: Cache, q: torch.Tensor, lens, m, sm_scale=0.0):
 
     For 16-bit types spread also holds what lies below the range the kernel keeps for a row.  A weight times its
     token's V scale is held in binary16 pieces with a least step of 2^-16 under a reference that puts the largest of
-    the row at 2^(10 - 4) at least (2^10 under the row's own maximum; the reference is a bound, up to a factor of 16 above
-    it): half a step, 2^-17, is 2^-23 of the largest, and a token's value is its code times that.  Divided by the
-    2^-7 that attention_bounds multiplies spread with for these types it is added here: 2^-16 max_t(p_t scale_t)
+    the row at 2^10 at least: half a step, 2^-17, is 2^-27 of the largest, and a token's value is its code times that.  Divided by the
+    2^-7 that attention_bounds multiplies spread with for these types it is added here: 2^-20 max_t(p_t scale_t)
     sum_t |code_t|.  reach likewise holds the queries' least step: an element is the sum of an e4m3 and an e5m2 value under a scale that
     puts the row's largest at 2^7 at least; below 2^-6 the first is off by 2^-10 at most and the second takes
     three bits of that, so an element is off by 2^-13, 2^-20 of the largest: 2^-20 max|q| max_t sum_d |k_td| sm_scale, divided by the
@@ -150,7 +149,7 @@ def attention(c: Cache, q: torch.Tensor, lens, m, sm_scale=0.0):
             if q.dtype == torch.bfloat16:
                 sc = c.token_scales("v", r, seen)
                 codes = np.abs(vv) / np.where(sc > 0, sc, 1.0)[..., None]
-                below = (2.0 ** -16 * (p * sc.T[:, None]).max(-1)[..., None] * codes.sum(0)[:, None]).reshape(hq, d)
+                below = (2.0 ** -20 * (p * sc.T[:, None]).max(-1)[..., None] * codes.sum(0)[:, None]).reshape(hq, d)
             lses.append((top + np.log(z)).reshape(hq))
             spreads.append(np.einsum("ght,tgd->ghd", p, np.abs(vv)).reshape(hq, d) + below)
             reach = np.einsum("ghd,tgd->ght", np.abs(x[j]), np.abs(kk)).max(-1) * scale
