@@ -97,13 +97,20 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
+// (the warp may sleep in it for some microseconds: polling warps take issue slots from the working ones)
+__device__ __forceinline__ bool try_wait_long(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
+               : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000) : "memory");
+  return ok != 0;
+}
 __device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, E8Barriers *bars) {
   const long long t0 = clock64();
 #pragma unroll 1
   for (;;) {
 #pragma unroll 1
     for (int i = 0; i < 64; ++i)
-      if (__all_sync(0xffffffffu, try_wait(bar, parity))) return;
+      if (__all_sync(0xffffffffu, try_wait_long(bar, parity))) return;
     if (__any_sync(0xffffffffu, bars->abort)) return;
     if (__any_sync(0xffffffffu, clock64() - t0 > kWaitLimitCycles)) {
       bars->abort = 1;
