@@ -21,8 +21,8 @@
 // the one reference.  It is taken from an entry's first tile and kept: the tiles after it need no maximum,
 // and their warps no agreement, before the weights.  They look at the x they make.  One above 2^13 has the
 // group take the next tile's maximum again; one above 2^15 is past what P can hold, and the
-// group takes the maximum and makes the same tile's weights again: scores, scales and V are held until the
-// tile's verdict is read, which the issuers do as well before they go on.  m' moves, and O is rescaled, when a tile's
+// group takes the maximum and makes the same tile's weights again: scores and scales are held until the tile's
+// verdict is read, and the issuer of the value MMAs reads it before it goes on.  m' moves, and O is rescaled, when a tile's
 // maximum passes it by a factor of 16.  The least x with a bit left is 2^-26 of the row's largest.
 //
 // Roles of the 512 threads: warp 0 TMA producer, warp 1 issuer of the score MMAs, warp 12 of the value MMAs,
@@ -58,7 +58,8 @@ struct E8Cfg {
   static constexpr int kStages = MROWS == 32 ? 4 : 3;
   static constexpr int kColBlock = D / kSplit / 2;                 // columns of O a thread finishes
   static constexpr int kSCols = kTileTokens / kSplit, kOCols = D / kSplit;
-  static constexpr int kColS = 0, kColO = 2 * kSCols;              // two score buffers, kOBufs pairs of O (one of each group)
+  static constexpr int kSBufs = MROWS == 128 ? 2 : 4;              // score buffers: the scores run that many tiles ahead
+  static constexpr int kColS = 0, kColO = kSBufs * kSCols;         // then kOBufs pairs of O (one of each group)
   static constexpr int kTmemNeed = kColO + 2 * kOBufs * kOCols;
   static constexpr int kTmemCols = kTmemNeed <= 128 ? 128 : kTmemNeed <= 256 ? 256 : 512;
   static_assert(kTmemNeed <= 512, "tensor memory");
@@ -74,7 +75,7 @@ struct E8Cfg {
 
 struct E8Barriers {
   uint64_t k_full[4], v_full[4], k_empty[4], v_empty[4], sc_full[kE8ScaleSlots], sc_empty[kE8ScaleSlots];
-  uint64_t s_full[2], p_full[2], q_full[2], q_empty[2], pv_done[2], o_full[2], o_free[2], item_done[2], e_bar[2], redo_ack[2];
+  uint64_t s_full[4], p_full[2], q_full[2], q_empty[2], pv_done[2], o_full[2], o_free[2], item_done[2], e_bar[2], redo_ack[2];
   uint32_t tmem_base;
   volatile int32_t abort;
   int32_t nan_any[kE8NanSlots];
@@ -276,10 +277,10 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     for (int s = 0; s < kE8ScaleSlots; ++s) { mbar_init(&bars->sc_full[s], 1); mbar_init(&bars->sc_empty[s], kE8GroupWarps); }
 #pragma unroll 1
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&bars->s_full[b], 1); mbar_init(&bars->p_full[b], kE8GroupWarps); mbar_init(&bars->q_full[b], kE8QueryWarps); mbar_init(&bars->q_empty[b], 1);
+      mbar_init(&bars->s_full[b], 1); mbar_init(&bars->s_full[b + 2], 1); mbar_init(&bars->p_full[b], kE8GroupWarps); mbar_init(&bars->q_full[b], kE8QueryWarps); mbar_init(&bars->q_empty[b], 1);
       mbar_init(&bars->pv_done[b], 1); mbar_init(&bars->o_full[b], 1); mbar_init(&bars->o_free[b], 2 * kE8GroupWarps);
       mbar_init(&bars->item_done[b], 2 * kE8GroupWarps); mbar_init(&bars->e_bar[b], kE8GroupWarps);
-      mbar_init(&bars->redo_ack[b], 2);
+      mbar_init(&bars->redo_ack[b], 1);
       for (int i = 0; i < 4; ++i) bars->verdict[b][i] = 0;
     }
     bars->abort = 0;
@@ -381,28 +382,9 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       return p.work[idx].tile_end - p.work[idx].tile_begin;
     };
     int n_tiles = tiles_of(0), n_next = tiles_of(1), i = 0;
-    // the weights of group b's next tile: those the group has not taken back
-    uint32_t phase0 = 0, phase1 = 0;
-    auto wait_weights = [&](uint32_t b) {
+    uint32_t phase0 = 0, phase1 = 0;   // of p_full: as many as a group made weights, those it took back included
 #pragma unroll 1
-      for (;;) {
-        const uint32_t n = b ? phase1++ : phase0++;
-        warp_wait(SPX_E8_BAR(p_full, b), n & 1);
-        if (*reinterpret_cast<volatile int32_t *>(&bars->verdict[b][n & 3]) != 2 || bars->abort) return;
-        __syncwarp();
-        if (lane == 0) arrive(SPX_E8_BAR(redo_ack, b));   // seen: the group may complete another phase
-      }
-    };
-    // (the score issuer looks at the last two tiles' verdicts too: a group that takes weights back waits for both)
-    uint32_t n_issued = 0;
-#pragma unroll 1
-    for (uint32_t t = 0; !bars->abort; ++t) {
-      const bool more = item_index(it) >= 0;
-      if (!more && (!scores || t >= n_issued + 2)) break;
-      // values: the tile's weights; scores: tile t - 2's, which were made of what the buffer holds
-      if (!scores || t >= 2) wait_weights(t & 1);
-      if (!more) continue;
-      ++n_issued;
+    for (uint32_t t = 0; item_index(it) >= 0 && !bars->abort; ++t) {
       const int slot = t % Cfg::kStages;
       const uint32_t ph = (t / Cfg::kStages) & 1;
       const bool last = i + 1 >= n_tiles;
@@ -411,9 +393,14 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         const uint32_t qb = Cfg::kQBufs == 2 ? (it & 1) : 0;
         if (i == 0) warp_wait(SPX_E8_BAR(q_full, qb), (Cfg::kQBufs == 2 ? (it >> 1) : it) & 1);
         warp_wait(SPX_E8_BAR(k_full, slot), ph);
+        // the tile whose scores the buffer holds is settled when its scales are handed back
+        if (t >= Cfg::kSBufs) {
+          const uint32_t u = t - Cfg::kSBufs;
+          warp_wait(SPX_E8_BAR(sc_empty, u % kE8ScaleSlots), (u / kE8ScaleSlots) & 1);
+        }
         fence_after();
         const uint64_t qa = smem_desc(smem_u32(sQ + qb * 2 * Cfg::kPiece), 16, 1024), ka = kv_desc<D>(smem_u32(sK + slot * Cfg::kTileBytes));
-        const uint32_t ts = tmem + Cfg::kColS + (t & 1) * Cfg::kSCols;
+        const uint32_t ts = tmem + Cfg::kColS + (t % Cfg::kSBufs) * Cfg::kSCols;
         if (elect_lane()) {
 #pragma unroll
           for (int k = 0; k < D / 32; k += 2) {   // descriptors count 16-byte units: 32 columns are 2
@@ -422,7 +409,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
             mma_piece<1, 0>(ts, qa + k * 2 + 2, ka + k * 2 + 2, kIdesc0, 1);
             mma_piece<1, 2>(ts, qa + k * 2 + 2 + (Cfg::kPiece >> 4), ka + k * 2 + 2, kIdesc1, 1);
           }
-          commit(SPX_E8_BAR(s_full, t & 1));
+          commit(SPX_E8_BAR(s_full, t % Cfg::kSBufs));
           commit(SPX_E8_BAR(k_empty, slot));
           if (last) commit(SPX_E8_BAR(q_empty, qb));
         }
@@ -433,6 +420,15 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         if (i == 0 && it >= Cfg::kOBufs)
           warp_wait(SPX_E8_BAR(o_free, Cfg::kOBufs == 2 ? (it & 1) : 0), (Cfg::kOBufs == 2 ? (it >> 1) - 1 : it - 1) & 1);
         warp_wait(SPX_E8_BAR(v_full, slot), ph);
+        // the tile's weights: the first its group does not take back
+#pragma unroll 1
+        for (;;) {
+          const uint32_t g = t & 1, n = g ? phase1++ : phase0++;
+          warp_wait(SPX_E8_BAR(p_full, g), n & 1);
+          if (*reinterpret_cast<volatile int32_t *>(&bars->verdict[g][n & 3]) != 2 || bars->abort) break;
+          __syncwarp();
+          if (lane == 0) arrive(SPX_E8_BAR(redo_ack, g));   // seen: the group may complete another phase
+        }
         fence_after();
         const uint64_t pa = smem_desc(smem_u32(sP + (Cfg::kPBufs == 2 ? (t & 1) : 0) * 3 * Cfg::kPiece), 16, 1024), va = kv_desc<D>(smem_u32(sV + slot * Cfg::kTileBytes));
         const uint32_t to = tmem + Cfg::kColO + ((Cfg::kOBufs == 2 ? (it & 1) * 2 : 0) + (t & 1)) * Cfg::kOCols;
@@ -724,7 +720,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         const int t0 = tile * kTileTokens + part * TPT;  // first token of this thread
         const bool mask_tile = tile * kTileTokens + kTileTokens - 1 > e.L - e.m;
         warp_wait(SPX_E8_BAR(sc_full, sc_slot), (tc_ / kE8ScaleSlots) & 1);
-        warp_wait(SPX_E8_BAR(s_full, grp), (tc_ >> 1) & 1);
+        warp_wait(SPX_E8_BAR(s_full, tc_ % Cfg::kSBufs), (tc_ / Cfg::kSBufs) & 1);
         fence_after();
         if (first) row_f = sRow[(it % kE8RowSlots) * MROWS + row];
         // 32 tokens a thread stay in registers; more are taken in chunks of 32, twice (the scores stay in tensor memory)
@@ -732,7 +728,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         uint64_t v[CH / 2];
         auto load_scores = [&](int ch) {
           uint32_t r[CH];
-          tmem_load<CH>(tmem + Cfg::kColS + grp * Cfg::kSCols + ch * CH + lane_addr, r);
+          tmem_load<CH>(tmem + Cfg::kColS + (tc_ % Cfg::kSBufs) * Cfg::kSCols + ch * CH + lane_addr, r);
           wait_ld();
 #pragma unroll
           for (int i = 0; i < CH / 2; ++i) v[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
