@@ -25,8 +25,8 @@
 // verdict is read, and the issuer of the value MMAs reads it before it goes on.  m' moves, and O is rescaled, when a tile's
 // maximum passes it by a factor of 16.  The least x with a bit left is 2^-26 of the row's largest.
 //
-// Roles of the 512 threads: warp 0 TMA producer, warp 1 issuer of the score MMAs, warp 12 of the value MMAs,
-// warp 2 scales of the next tiles, warps 3 and 13-15 query pieces of the next entry, warps 4-7 and 8-11 two softmax groups
+// Roles of the 512 threads: warps 0 and 13 TMA producers of K and of V, warp 1 issuer of the score MMAs, warp 12 of the
+// value MMAs, warp 2 scales of the next tiles, warps 3, 14 and 15 query pieces of the next entry, warps 4-7 and 8-11 two softmax groups
 // that take the tiles in turn, each with its own reference, sum and O, merged in the entry's epilogue: a tile's
 // chain (scores, weights, pieces) is some 2,000 cycles long, and two tiles in it at a time keep up with memory.
 // The plan, its work entries, partial results and bounded waits are those of the 16-bit kernels.
@@ -38,7 +38,7 @@
 namespace spx {
 
 constexpr int kE8Threads = 512;
-constexpr int kE8QueryWarps = 4;   // 3, 13, 14, 15
+constexpr int kE8QueryWarps = 3;   // 3, 14, 15
 constexpr int kE8GroupWarps = 4;   // softmax warps of a group
 constexpr int kE8ScaleSlots = 4;   // tiles whose scales are staged
 constexpr int kE8RowSlots = 8;     // entries whose row factors are kept: the query warp is at most four entries ahead of the softmax
@@ -122,6 +122,13 @@ __device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, E8Barriers
 }
 __device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t parity, E8Barriers *bars) {
   if (!__all_sync(0xffffffffu, try_wait(bar, parity))) wait_slow(bar, parity, bars);
+}
+__device__ __forceinline__ void expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c1, int c2, int page) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(c1), "r"(c2), "r"(page) : "memory");
 }
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
@@ -312,8 +319,14 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   auto warp_wait = [&](uint32_t bar, uint32_t parity) { e8::warp_wait(bar, parity, bars); };
 #define SPX_E8_BAR(member, i) (bar0 + (uint32_t)offsetof(E8Barriers, member) + 8u * (uint32_t)(i))
 
-  if (warp == 0) {
-    // ------------------------------------------------------------------ producer
+  if (warp == 0 || warp == 13) {
+    // ------------------------------------------------------------------ producers: K (warp 0), V (warp 13)
+    // One warp for both was what the tiles waited for: the copies of a tile's pages are issued one after the other,
+    // some 60 cycles each, sixteen to a tile with pages of 16 tokens.
+    const bool keys = warp == 0;
+    const CUtensorMap *map = keys ? &kmap : &vmap;
+    const uint32_t bar_full = keys ? SPX_E8_BAR(k_full, 0) : SPX_E8_BAR(v_full, 0), bar_empty = keys ? SPX_E8_BAR(k_empty, 0) : SPX_E8_BAR(v_empty, 0);
+    const uint32_t ring = smem_u32(keys ? sK : sV);
     // Tiles are walked in groups of 32/pages_per_tile so that every lane owns one page of the group:
     // one coalesced block-table read per group, a group ahead of the copies (the next entry one ahead).
     const int tiles_per_group = 32 / pages_per_tile;
@@ -363,12 +376,10 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         const int ntok = min(kTileTokens, cur.e.L - tile * kTileTokens);
         const uint32_t bytes = (uint32_t)(((ntok + p.P - 1) >> p.log2P) << p.log2P) * D;
         const bool mine = (my_tile == ti) && page >= 0;
-        warp_wait(SPX_E8_BAR(k_empty, slot), ph ^ 1);
-        if (lane == 0) mbar_expect_tx(&bars->k_full[slot], bytes);
-        if (mine) tma_load_4d(smem_u32(sK + slot * Cfg::kTileBytes + my_page * p.P * D), &kmap, &bars->k_full[slot], 0, p.head_inner ? g : 0, p.head_inner ? 0 : g, page);
-        warp_wait(SPX_E8_BAR(v_empty, slot), ph ^ 1);
-        if (lane == 0) mbar_expect_tx(&bars->v_full[slot], bytes);
-        if (mine) tma_load_4d(smem_u32(sV + slot * Cfg::kTileBytes + my_page * p.P * D), &vmap, &bars->v_full[slot], 0, p.head_inner ? g : 0, p.head_inner ? 0 : g, page);
+        warp_wait(bar_empty + 8 * slot, ph ^ 1);
+        if (lane == 0) expect_tx(bar_full + 8 * slot, bytes);
+        __syncwarp();
+        if (mine) tma_page(ring + slot * Cfg::kTileBytes + my_page * p.P * D, map, bar_full + 8 * slot, p.head_inner ? g : 0, p.head_inner ? 0 : g, page);
       }
     }
   } else if (warp == 1 || warp == 12) {
@@ -514,13 +525,13 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
 #pragma unroll
       for (int i = 0; i < 4; ++i) { ks[i] = kn[i]; vs[i] = vn[i]; }
     }
-  } else if (warp == 3 || warp > 12) {
+  } else if (warp == 3 || warp > 13) {
     // ------------------------------------------------------------------ query pieces, an entry ahead
-    // A lane owns 8 columns of a row: a pass of one warp covers 2 rows of 128 columns or 4 of 64.  Four warps,
-    // each with four passes' loads in flight, turn 32 rows in one trip to memory; a single warp took 8,500
+    // A lane owns 8 columns of a row: a pass of one warp covers 2 rows of 128 columns or 4 of 64.  Three warps,
+    // each with six passes' loads in flight, turn 36 rows in one trip to memory; a single warp took 8,500
     // cycles an entry of 32 rows, the time of six tiles.
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;
-    const int q_warp = warp == 3 ? 0 : warp - 12;
+    const int q_warp = warp == 3 ? 0 : warp - 13;
     const int c = lane % kLanes;
     const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(p.q);
     WorkEntry e, e_next;
@@ -537,7 +548,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         const int j = row / p.G, hg = row - j * p.G;
         return __ldg(reinterpret_cast<const uint4 *>(q + ((int64_t)(e.q0 + j) * p.Hq + e.g * p.G + hg) * D + c * 8));
       };
-      constexpr int kAhead = 4;   // passes whose loads are in flight together
+      constexpr int kAhead = 6;   // passes whose loads are in flight together
       bool waited = false;
       for (int row0 = q_warp * kAhead * kRows; row0 < R || !waited; row0 += kE8QueryWarps * kAhead * kRows) {
         uint4 v[kAhead];
@@ -550,7 +561,9 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
 #pragma unroll 1
         for (int u = 0; u < kAhead; ++u) {
           const int row = row0 + u * kRows + lane / kLanes;
-          const uint4 x = u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3];
+          uint4 x = v[0];
+#pragma unroll
+          for (int w = 1; w < kAhead; ++w) x = u == w ? v[w] : x;
           const uint32_t w[4] = {x.x, x.y, x.z, x.w};
           uint32_t a = 0;
 #pragma unroll

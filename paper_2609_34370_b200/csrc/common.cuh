@@ -157,6 +157,7 @@ struct AttnParams {
   // 8-bit pools: tokens per scale = 1 << log2SB, scales [page, head, P >> log2SB]
   const float *k_scales, *v_scales;
   int32_t log2SB;
+  int32_t entry_cost;      // of a work entry on the planner's cost axis, in eighths of a tile
   int32_t *dev_status;
   long long *prof;         // optional per-CTA cycle counters (profiling builds only), else NULL
 };

@@ -38,9 +38,11 @@ constexpr int kPlanMaxCta = 256;  // ranges the planner can cut the tile axis in
 // a little larger for pairs of one or two tiles, which leave nothing to overlap it with.  Fitted
 // to per-CTA run times of the attention kernel on the Llama-3-8B, Llama-3-70B and mixed-length
 // shapes, whose ranges hold 2 to 32 entries: 1.51 us per tile and 0.65 us per entry on all three
-// (0.43 tile times), pairs of one or two tiles 0.3 tile times more.
+// (0.43 tile times), pairs of one or two tiles 0.3 tile times more.  Over 8-bit pools a tile takes half the time and
+// an entry, whose queries are cut into pieces, more (see spx_api.cu).
 constexpr int kCostPerTile = 8;
-__device__ __forceinline__ int plan_entry_cost(int tiles) { return tiles <= 2 ? 5 : 3; }
+constexpr int kPlanEntryCost = 3;
+__device__ __forceinline__ int plan_entry_cost(int tiles, int entry_cost) { return tiles <= 2 ? entry_cost + 2 : entry_cost; }
 
 // One block.  Validates each request's (k+1, L, page count), cuts the tile axis of the valid
 // requests' (request, kv head) pairs into n_cta ranges of equal length, lays out partial-result
@@ -91,7 +93,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
     const int tot_t = s_total;
     const int off_v = block_exclusive_scan_1024(tiles > 0 ? 1 : 0, s_scratch, &s_total) + s_carry_v;
     const int tot_v = s_total;
-    const int cost = tiles > 0 ? kCostPerTile * tiles + plan_entry_cost(tiles) : 0;
+    const int cost = tiles > 0 ? kCostPerTile * tiles + plan_entry_cost(tiles, p.entry_cost) : 0;
     const int off_c = block_exclusive_scan_1024(cost, s_scratch, &s_total) + s_carry_c;
     const int tot_c = s_total;
     if (r < p.batch) {

@@ -384,6 +384,9 @@ static cudaError_t launch_e4m3(const CUtensorMap &kmap, const CUtensorMap &vmap,
 // ---------------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------------
+// Over 8-bit pools: 2,400 cycles an entry against 1,220 a tile, part of them beside other entries' tiles.  With 3 (the
+// 16-bit kernels') the Llama-3-8B and 70B layer shapes take 84 and 149 us, with 8 83 and 142, with 14 83 and 141.
+constexpr int kPlanEntryCostE4m3 = 8;
 enum { kPhasePlan = 1, kPhaseMain = 2, kPhaseAll = 3 };                        // attention: planner, kernels behind it
 enum { kPhaseStats = 1, kPhaseTail = 2, kPhaseFilter = 4, kPhaseSampAll = 7 };  // sampling: statistics, top-k / top-p thresholds, the rest
 
@@ -419,7 +422,9 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
   p.part_ml = reinterpret_cast<float2 *>(ws + w.part_ml);
   p.part_o = reinterpret_cast<float *>(ws + w.part_o);
   p.rows_cap = w.rows_cap;
+  p.entry_cost = kPlanEntryCost;
   if (a->cache_format == SPX_CACHE_E4M3) {
+    if (use_tensor_core_path(a)) p.entry_cost = kPlanEntryCostE4m3;
     p.k_scales = a->k_scales; p.v_scales = a->v_scales;
     p.log2SB = log2_of(a->scale_block);
   }
