@@ -41,7 +41,7 @@ constexpr int kE8Threads = 512;
 constexpr int kE8QueryWarps = 3;   // 3, 14, 15
 constexpr int kE8GroupWarps = 4;   // softmax warps of a group
 constexpr int kE8ScaleSlots = 4;   // tiles whose scales are staged
-constexpr int kE8RowSlots = 8;     // entries whose row factors are kept: the query warp is at most four entries ahead of the softmax
+constexpr int kE8RowSlots = 8;     // entries whose row factors are kept: the query pieces run at most five entries ahead of the softmax: the scores of four tiles (kSBufs) and the pieces being cut
 constexpr int kE8NanSlots = 8;
 constexpr float kE8Shift = 10.f;
 constexpr float kE8Rescale = 4.f;   // under a fresh reference x <= 2^(10 + 4)
@@ -55,7 +55,9 @@ struct E8Cfg {
   static constexpr int kTileBytes = kTileTokens * D;
   static constexpr int kPiece = MROWS * 128;                       // one piece of Q (D <= 128 columns) or of P (128 tokens), 128-byte rows
   static constexpr int kQBufs = MROWS == 128 ? 1 : 2, kPBufs = MROWS == 128 ? 1 : 2, kOBufs = MROWS == 128 && D == 128 ? 1 : 2;
-  static constexpr int kStages = MROWS == 32 ? 4 : 3;
+  // The rings of K and of V: what they hold is in flight or waits, so they take all the memory that is left.  K is done
+  // with as soon as its scores are issued, V waits for the softmax: two more of it.
+  static constexpr int kStagesK = D == 64 ? 6 : MROWS == 32 ? 4 : 3, kStagesV = D == 64 ? 8 : MROWS == 32 ? 6 : MROWS == 64 ? 5 : 4;
   static constexpr int kColBlock = D / kSplit / 2;                 // columns of O a thread finishes
   static constexpr int kSCols = kTileTokens / kSplit, kOCols = D / kSplit;
   static constexpr int kSBufs = MROWS == 128 ? 2 : 4;              // score buffers: the scores run that many tiles ahead
@@ -64,17 +66,17 @@ struct E8Cfg {
   static constexpr int kTmemCols = kTmemNeed <= 128 ? 128 : kTmemNeed <= 256 ? 256 : 512;
   static_assert(kTmemNeed <= 512, "tensor memory");
   // byte offsets into shared memory, after rounding its base up to 1024
-  static constexpr int kOffK = 0, kOffV = kOffK + kStages * kTileBytes, kOffQ = kOffV + kStages * kTileBytes, kOffP = kOffQ + kQBufs * 2 * kPiece;
+  static constexpr int kOffK = 0, kOffV = kOffK + kStagesK * kTileBytes, kOffQ = kOffV + kStagesV * kTileBytes, kOffP = kOffQ + kQBufs * 2 * kPiece;
   static constexpr int kOffKs = kOffP + kPBufs * 3 * kPiece, kOffVs = kOffKs + kE8ScaleSlots * 512, kOffLv = kOffVs + kE8ScaleSlots * 512;
   static constexpr int kOffMx = kOffLv + kE8ScaleSlots * 512, kOffL = kOffMx + 2 * 1024;
   static constexpr int kOffRef = kOffL + 2 * 1024, kOffRow = kOffRef + 2 * 2 * MROWS * 4, kOffNan = kOffRow + kE8RowSlots * MROWS * 4;
   static constexpr int kOffBar = kOffNan + kE8NanSlots * 128 * 4;
-  static constexpr int kSmemBytes = kOffBar + 512 + 1024;
+  static constexpr int kSmemBytes = kOffBar + 640 + 1024;
   static_assert(kSmemBytes <= 232448, "shared memory");
 };
 
 struct E8Barriers {
-  uint64_t k_full[4], v_full[4], k_empty[4], v_empty[4], sc_full[kE8ScaleSlots], sc_empty[kE8ScaleSlots];
+  uint64_t k_full[8], v_full[8], k_empty[8], v_empty[8], sc_full[kE8ScaleSlots], sc_empty[kE8ScaleSlots];
   uint64_t s_full[4], p_full[2], q_full[2], q_empty[2], pv_done[2], o_full[2], o_free[2], item_done[2], e_bar[2], redo_ack[2];
   uint32_t tmem_base;
   volatile int32_t abort;
@@ -82,7 +84,7 @@ struct E8Barriers {
   int32_t verdict[2][4];   // of a group's last weights, by phase of p_full: 0 fine, 1 near the end of P's range, 2 past it
   int32_t *dev_status;
 };
-static_assert(sizeof(E8Barriers) <= 512, "barrier area");
+static_assert(sizeof(E8Barriers) <= 640, "barrier area");
 
 namespace e8 {
 
@@ -279,7 +281,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
 #pragma unroll 1
-    for (int s = 0; s < 4; ++s) { mbar_init(&bars->k_full[s], 1); mbar_init(&bars->v_full[s], 1); mbar_init(&bars->k_empty[s], 1); mbar_init(&bars->v_empty[s], 1); }
+    for (int s = 0; s < 8; ++s) { mbar_init(&bars->k_full[s], 1); mbar_init(&bars->v_full[s], 1); mbar_init(&bars->k_empty[s], 1); mbar_init(&bars->v_empty[s], 1); }
 #pragma unroll 1
     for (int s = 0; s < kE8ScaleSlots; ++s) { mbar_init(&bars->sc_full[s], 1); mbar_init(&bars->sc_empty[s], kE8GroupWarps); }
 #pragma unroll 1
@@ -326,7 +328,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     const bool keys = warp == 0;
     const CUtensorMap *map = keys ? &kmap : &vmap;
     const uint32_t bar_full = keys ? SPX_E8_BAR(k_full, 0) : SPX_E8_BAR(v_full, 0), bar_empty = keys ? SPX_E8_BAR(k_empty, 0) : SPX_E8_BAR(v_empty, 0);
-    const uint32_t ring = smem_u32(keys ? sK : sV);
+    const uint32_t ring = smem_u32(keys ? sK : sV), stages = keys ? Cfg::kStagesK : Cfg::kStagesV;
     // Tiles are walked in groups of 32/pages_per_tile so that every lane owns one page of the group:
     // one coalesced block-table read per group, a group ahead of the copies (the next entry one ahead).
     const int tiles_per_group = 32 / pages_per_tile;
@@ -371,8 +373,8 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       const int g = cur.e.g;
       for (int ti = 0; ti < tiles_per_group && cur.tile0 + ti < cur.e.tile_end; ++ti, ++tc_) {
         const int tile = cur.tile0 + ti;
-        const int slot = tc_ % Cfg::kStages;
-        const uint32_t ph = (tc_ / Cfg::kStages) & 1;
+        const int slot = tc_ % stages;
+        const uint32_t ph = (tc_ / stages) & 1;
         const int ntok = min(kTileTokens, cur.e.L - tile * kTileTokens);
         const uint32_t bytes = (uint32_t)(((ntok + p.P - 1) >> p.log2P) << p.log2P) * D;
         const bool mine = (my_tile == ti) && page >= 0;
@@ -396,8 +398,9 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     uint32_t phase0 = 0, phase1 = 0;   // of p_full: as many as a group made weights, those it took back included
 #pragma unroll 1
     for (uint32_t t = 0; item_index(it) >= 0 && !bars->abort; ++t) {
-      const int slot = t % Cfg::kStages;
-      const uint32_t ph = (t / Cfg::kStages) & 1;
+      const uint32_t stages = scores ? Cfg::kStagesK : Cfg::kStagesV;
+      const int slot = t % stages;
+      const uint32_t ph = (t / stages) & 1;
       const bool last = i + 1 >= n_tiles;
       if (scores) {
         constexpr uint32_t kIdesc0 = idesc_f8(MROWS, kTileTokens, false, false), kIdesc1 = idesc_f8(MROWS, kTileTokens, true, false);
@@ -874,8 +877,8 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           // rows do not see is taken out and left to the epilogue of those that do
           const int ntok = min(kTileTokens, e.L - tile * kTileTokens);
           const int hidden = max(0, e.L - e.m + 1 - tile * kTileTokens);   // first token of the tile not seen by every row
-          const int slot = tc_ % Cfg::kStages;
-          warp_wait(SPX_E8_BAR(v_full, slot), (tc_ / Cfg::kStages) & 1);
+          const int slot = tc_ % Cfg::kStagesV;
+          warp_wait(SPX_E8_BAR(v_full, slot), (tc_ / Cfg::kStagesV) & 1);
           unsigned char *vt = sV + slot * Cfg::kTileBytes;
 #pragma unroll 1
           for (int i = g_tid; i < (kTileTokens - ntok) * (D / 16); i += 128)

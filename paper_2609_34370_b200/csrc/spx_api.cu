@@ -278,7 +278,8 @@ static bool make_pool_map(CUtensorMap *map, const void *pool, const spx_attn_arg
 }
 
 // 4-D byte view of an 8-bit pool, dims ordered as above; one box = one page x one kv-head, rows of
-// head_dim bytes swizzled over their own length.
+// head_dim bytes swizzled over their own length.  (L2 promotion to 256 bytes fetches the next head of a pool in token
+// order along: 140 us instead of 134 on the Llama-3-70B layer shape.)
 static bool make_pool_map_e4m3(CUtensorMap *map, const void *pool, const spx_attn_args_t *a, bool head_inner) {
   EncodeTiledFn encode = get_encode_fn();
   if (!encode) return false;
@@ -288,7 +289,7 @@ static bool make_pool_map_e4m3(CUtensorMap *map, const void *pool, const spx_att
   const cuuint64_t strides[3] = {head_inner ? sh : st, head_inner ? st : sh, sp};
   const cuuint32_t box[4] = {(cuuint32_t)D, head_inner ? 1 : (cuuint32_t)P, head_inner ? (cuuint32_t)P : 1, 1}, estr[4] = {1, 1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
