@@ -261,8 +261,6 @@ template <int D, int MROWS>
 __global__ void __launch_bounds__(kE8Threads, 1)
 attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, AttnParams p) {
   SPX_TL_SCOPE(kTlAttention);
-  // the combine kernel may take its places now (see attn_tc4_kernel)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   using Cfg = E8Cfg<D, MROWS>;
   using namespace e8;
   constexpr int kSplit = Cfg::kSplit, TPT = Cfg::kTokPerThread, CB = Cfg::kColBlock;
@@ -311,6 +309,8 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   // Everything above touched only this CTA's own resources; the plan, and what the caller's kernels before it
   // wrote, is read from here on.
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  // the combine kernel may take its places now, and not before: it reads the plan ahead of its own wait
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // this CTA's range of the plan: entries cta_off[c] .. cta_off[c+1] of the work list, in order
   const bool planned = !p.hdr->overflow && (int)blockIdx.x < p.hdr->n_cta;
   const int item_begin = planned ? p.cta_off[blockIdx.x] : 0;

@@ -385,9 +385,9 @@ static cudaError_t launch_e4m3(const CUtensorMap &kmap, const CUtensorMap &vmap,
 // ---------------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------------
-// Over 8-bit pools: 2,400 cycles an entry against 1,220 a tile, part of them beside other entries' tiles.  With 3 (the
-// 16-bit kernels') the Llama-3-8B and 70B layer shapes take 84 and 149 us, with 8 83 and 142, with 14 83 and 141.
-constexpr int kPlanEntryCostE4m3 = 8;
+// Over 8-bit pools, where a tile takes half the time and an entry's queries are cut into pieces.  The Llama-3-8B and 70B
+// layer shapes take 85 and 142 us with 4, 85 and 136 with 8, 85 and 128.5 with 14, 86 and 130 with 20, 87 and 132 with 28.
+constexpr int kPlanEntryCostE4m3 = 14;
 enum { kPhasePlan = 1, kPhaseMain = 2, kPhaseAll = 3 };                        // attention: planner, kernels behind it
 enum { kPhaseStats = 1, kPhaseTail = 2, kPhaseFilter = 4, kPhaseSampAll = 7 };  // sampling: statistics, top-k / top-p thresholds, the rest
 
