@@ -204,13 +204,14 @@ def _require_cuda(*tensors):
 
 
 def _on_device_of(fn):
-    """The library launches on the current device: the call is made with its first tensor's device current."""
+    """The library launches on the current device: the call is made with the device of its first argument current."""
     @functools.wraps(fn)
-    def call(first, *args, **kw):
+    def call(*args, **kw):
+        first = args[0] if args else next(iter(kw.values()), None)
         if not getattr(first, "is_cuda", False) or first.get_device() == _current_device():
-            return fn(first, *args, **kw)
+            return fn(*args, **kw)
         with torch.cuda.device(first.device):
-            return fn(first, *args, **kw)
+            return fn(*args, **kw)
     return call
 
 
