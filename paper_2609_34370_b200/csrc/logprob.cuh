@@ -50,6 +50,12 @@ __device__ __forceinline__ uint32_t logit_key32(float x) {
 }
 template <typename T>
 __device__ __forceinline__ uint32_t logit_key(float x) { return sizeof(T) == 2 ? logit_key32(x) >> 16 : logit_key32(x); }
+// the logit of a key (of -0: +0)
+template <typename T>
+__device__ __forceinline__ float key_logit(uint32_t key) {
+  const uint32_t u = sizeof(T) == 2 ? key << 16 : key;
+  return __uint_as_float((u & 0x80000000u) ? u ^ 0x80000000u : sizeof(T) == 2 ? ~u & 0xffff0000u : ~u);
+}
 
 template <typename T> struct LpVec;
 template <> struct LpVec<__nv_bfloat16> {
@@ -318,7 +324,7 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
     }
     s_key[tid] = tid < n_keys ? my_key : 0;
   }
-  if (tid == 0) { s_cand_n = 0; s_list_n = 0; }
+  if (tid == 0) { s_cand_n = 0; s_list_n = 0; s_floor = 0xffffffffu; }
   bad = __syncthreads_or(bad);
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s_f[w]);
@@ -350,28 +356,32 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
   uint4 held[kMaxVecs];
   if (n > 0) {
     if (n_keys <= kThreads) {
-      // rank by counting: every thread its key against all (they lie behind one another in shared memory)
+      // the smallest of the keys that fewer than n others exceed, every thread counting for its own (they lie behind one
+      // another in shared memory, zeros behind the last)
+      uint32_t mine = 0xffffffffu;
       if (tid < n_keys) {
-        int above = 0, level = 0;   // larger keys, equal ones
+        int above = 0;
+#pragma unroll 4
         for (int j = 0; j < n_keys; j += 4) {
           const uint4 k = *reinterpret_cast<const uint4 *>(s_key + j);
           above += (k.x > my_key) + (k.y > my_key) + (k.z > my_key) + (k.w > my_key);
-          level += (k.x == my_key) + (j + 1 < n_keys && k.y == my_key) + (j + 2 < n_keys && k.z == my_key) + (j + 3 < n_keys && k.w == my_key);
         }
-        if (above < n && above + level >= n) s_floor = my_key;   // (all that write write the same)
+        if (above < n) mine = my_key;
       }
+      mine = __reduce_min_sync(0xffffffffu, mine);
+      if (lane == 0 && mine != 0xffffffffu) atomicMin(&s_floor, mine);
       __syncthreads();
       floor_key = s_floor;
     } else {
       floor_key = kth_largest(n_keys, n, [&](int i) -> uint32_t { return i == tid ? my_key : logit_key<T>(seg[i].x); });
     }
     auto list_vec = [&](const uint4 &v, int base) {
+      uint32_t hits = 0;
 #pragma unroll
-      for (int k = 0; k < V::N; ++k)
-        if (logit_key<T>(V::at(v, k)) >= floor_key) {
-          const int at = atomicAdd(&s_cand_n, 1);
-          if (at < kLpMaxCand) s_cand[at] = base + k;
-        }
+      for (int k = 0; k < V::N; ++k) hits |= (uint32_t)(logit_key<T>(V::at(v, k)) >= floor_key) << k;
+      if (hits == 0) return;
+      for (int at = atomicAdd(&s_cand_n, __popc(hits)); hits != 0; ++at, hits &= hits - 1)
+        if (at < kLpMaxCand) s_cand[at] = base + __ffs(hits) - 1;
     };
 #pragma unroll
     for (int u = 0; u < kMaxVecs; ++u)
@@ -450,15 +460,22 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
   if (n == 0) return;
 
   // ---- the alternatives: every logit of the listed groups for which take(key) holds, behind the list's end
+  // (which of a vector's logits first, without a branch each: eight of them a vector were 3,500 cycles a row)
   auto take_vec = [&](const uint4 &v, int e0, auto take) {
+    uint32_t hits = 0, key[V::N];
 #pragma unroll
     for (int k = 0; k < V::N; ++k) {
-      const uint32_t key = logit_key<T>(V::at(v, k));
-      if (take(key) && e0 + k < p.vocab) {
-        const int at = atomicAdd(&s_list_n, 1);
-        if (at < kLpMaxList) s_list[at] = make_uint2(key, ~(uint32_t)(e0 + k));
-      }
+      key[k] = logit_key<T>(V::at(v, k));
+      hits |= (uint32_t)(take(key[k]) && e0 + k < p.vocab) << k;
     }
+    if (hits == 0) return;
+    int at = atomicAdd(&s_list_n, __popc(hits));
+#pragma unroll
+    for (int k = 0; k < V::N; ++k)
+      if (hits >> k & 1) {
+        if (at < kLpMaxList) s_list[at] = make_uint2(key[k], ~(uint32_t)(e0 + k));
+        ++at;
+      }
   };
   auto gather = [&](int i0, int cands, auto take) {
     for (int i = i0 + tid; i < cands * 8; i += kThreads) {
@@ -525,7 +542,7 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
     if (rank < n) {
       const int id = (int)~me.y;
       if (p.top_ids) p.top_ids[(int64_t)row * n + rank] = id;
-      if (p.top_logprobs) p.top_logprobs[(int64_t)row * n + rank] = bad ? nan : (float)((double)ld_as_float(x, id) - m - log_z);
+      if (p.top_logprobs) p.top_logprobs[(int64_t)row * n + rank] = bad ? nan : (float)((double)key_logit<T>(me.x) - m - log_z);
     }
   }
   if (tid >= total && tid < n) {   // fewer logits than alternatives
