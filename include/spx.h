@@ -236,11 +236,13 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
  * infinite rope_base is SPX_ERR_INVALID_ARG.
  *
  * q_out (optional, like q_rows; it may be q_rows itself) receives the rotated rows instead, and q_rows is then left as it is.
+ * (Beside 8-bit pools 16-bit query rows are rotated in binary32 from float64 angles: within two steps of binary32 before
+ * their one rounding to 16 bits.)
  *
  * Pools of 8-bit floats (cache_format = SPX_CACHE_E4M3, see spx_cache_format_t): a request may bring
  * ANY number m_r >= 1 of new rows (a prompt as well as a step), in place of at most SPX_MAX_K + 1.
- * With y the new rows' values in binary32 (K after the rotation, whose only rounding is the one from
- * float64), every scale block that receives one of them is stored anew, the older tokens of its
+ * With y the new rows' values in binary32 (K after the rotation: angles in float64, products and sum
+ * in pairs of binary32 to 2^-46, then one rounding), every scale block that receives one of them is stored anew, the older tokens of its
  * request in it included:
  *   amax  = the largest finite magnitude among the block's values: the older tokens' code * scale
  *           as they were, and the new y (slots past L_r do not count);

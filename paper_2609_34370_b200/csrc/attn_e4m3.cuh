@@ -3,18 +3,23 @@
 //
 // The 8-bit MMA multiplies e4m3 by e5m2, so K and V are its B operands as they lie in the pages (TMA
 // page gathers, as in the 16-bit kernels), and the accuracy lost nowhere is kept on the other side:
-//   * a query row, scaled by a power of two so that its largest element lies in [2^14, 2^15), is the
-//     exact sum of three e5m2 pieces: e5m2 is the upper byte of binary16, so each piece is a byte of
-//     the remainder, and 8 significant bits are 3 + 3 + 2 (elements below 2^-24 of the largest lose
-//     bits that its products round away);
-//   * S = (Q1 + Q2 + Q3) K^T accumulates in fp32; K's scale multiplies the score of its token;
-//   * a weight times V's scale, x_t = p_t v_t, is rounded to binary16 and cut the same way, the third
-//     piece rounded to nearest: 9 significant bits and a sign, half a step off by 2^-10 at most
-//     (bfloat16, which the 16-bit kernels round P to: 2^-9), O += (P1 + P2 + P3) V.
-// Three weight-stationary MMAs share one B tile, which stays in the collector: 27 cycles an MMA at
-// 32 rows, against 44 when each loads its own, and against 46 when they are issued from a branch on
-// one thread instead of by elect.sync in a converged warp.  24 of them take 650 of the 1,420 cycles a tile's
-// 32 KB need from memory: the kernel stays bound by HBM.
+//   * a query row, scaled by a power of two so that its largest element lies in [2^7, 2^8), is the sum
+//     of an e4m3 and an e5m2 piece, each rounded to nearest: 4 significant bits and 3 more of the remainder, with its sign
+//     bfloat16's 8, exact for elements down to 2^-13 of the row's largest; those below are off by 2^-21 of it at most;
+//   * S = (Q1 + Q2) K^T accumulates in fp32; K's scale multiplies the score of its token;
+//   * a weight times V's scale, x_t = p_t v_t, is rounded to binary16 and cut into three e5m2 pieces (e5m2 is the upper
+//     byte of binary16, so a piece is a byte of the remainder), the third rounded to nearest: 9 significant bits and a
+//     sign, half a step off by 2^-10 at most (bfloat16, which the 16-bit kernels round P to: 2^-9), O += (P1 + P2 + P3) V.
+// The MMAs of one B tile are weight-stationary and share it: it stays in the collector, 27 cycles an MMA at 32 rows
+// back to back, against 44 when each loads its own.  A tile's 8 score and 12 value MMAs come from two warps (by
+// elect.sync in a converged warp; a branch on one thread costs 46 cycles an MMA), 550 of the 1,420 cycles in which
+// its 32 KB can come from memory.
+//
+// What bounds it (one call, the plan and the combine kernel included, 12 us of it): the Llama-3-8B layer shape (64
+// requests of 512 to 4096 tokens, 320 MB of K and V) takes 85 to 88 us from one board to another, 81 with the softmax
+// arithmetic taken out: memory, at 5 TB/s between the first and the last tile; the 70B shape (128 requests, a pool in token
+// order, 469 MB) 129 to 134 us.  Contexts of 32,768 at 36 rows, 320 to 338 us, are bound by the softmax groups, whose
+// tiles are 64 rows wide there (211 us without their arithmetic).
 //
 // binary16 has no exponents to spare for V's scales, so a row's reference m' is the maximum of s_t + log2 v_t
 // instead of s_t: y_t = 2^(10 + s_t - m') goes into the row's sum and x_t = y_t v_t into P, both under
@@ -41,7 +46,7 @@ constexpr int kE8Threads = 512;
 constexpr int kE8QueryWarps = 3;   // 3, 14, 15
 constexpr int kE8GroupWarps = 4;   // softmax warps of a group
 constexpr int kE8ScaleSlots = 4;   // tiles whose scales are staged
-constexpr int kE8RowSlots = 8;     // entries whose row factors are kept: the query pieces run at most five entries ahead of the softmax: the scores of four tiles (kSBufs) and the pieces being cut
+constexpr int kE8RowSlots = 8;     // entries whose row factors are kept: the scores run four tiles (entries, at most) ahead of the softmax, the query pieces one more
 constexpr int kE8NanSlots = 8;
 constexpr float kE8Shift = 10.f;
 constexpr float kE8Rescale = 4.f;   // under a fresh reference x <= 2^(10 + 4)
@@ -386,7 +391,7 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     }
   } else if (warp == 1 || warp == 12) {
     // ------------------------------------------------------------------ MMA issuers: scores (warp 1), values (warp 12)
-    // One warp for both was the kernel's longest chain: a tile's MMAs take the issuing thread some 46 cycles each.
+    // One warp for both was the kernel's longest chain (waits, descriptors and commits included, some 46 cycles an MMA).
     const bool scores = warp == 1;
     int it = 0;
     auto tiles_of = [&](int i) -> int {

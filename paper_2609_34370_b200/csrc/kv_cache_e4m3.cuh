@@ -6,6 +6,11 @@
 // amax <= 448 * 2^e, code = round(value / scale).  A power of two divides exactly, so an older
 // token's change of scale rounds only where its last bits fall below the smallest subnormal, and
 // appending the same rows again changes nothing.
+//
+// A prompt has to read its rows and write half as many bytes and the rotated queries: 14.6k rows of the Llama-3-8B layer
+// shape are 329 MB, 51 us at HBM's rate.  They take 104: bound by the arithmetic between load and store, the compensated
+// rotation above all (float64 angles, products kept to 2^-46, so that a stored code is that of the exact value), and by
+// two blocks an SM, all that a tile's angles in shared memory leave room for.
 #pragma once
 #include <type_traits>
 
