@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   __shared__ int s_cut_vq[kPlanMaxCta + 1];  // index, among the valid requests' pairs, of the first pair that ends after cut c
   __shared__ int s_cut_in[kPlanMaxCta + 1];  // 1: cut c lies strictly inside that pair
   __shared__ int s_off[kPlanMaxCta + 1];     // work entries of the ranges before c
-  __shared__ int s_carry_t, s_carry_v, s_carry_c, s_carry_p, s_carry_l, s_bad;
+  __shared__ int s_bad;
   // The prefix sums of a batch of up to kPlanSmemReqs requests stay in shared memory: the searches
   // below would otherwise be chains of global loads, each a memory round trip beside the
   // bandwidth-bound kernel that runs while the plan is made (29 us instead of 6 for 64 requests).
@@ -82,48 +82,47 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   const int tid = threadIdx.x;
   const int Hkv = p.Hkv;
   if (n_cta > kPlanMaxCta) n_cta = kPlanMaxCta;
-  if (tid == 0) { s_carry_t = 0; s_carry_v = 0; s_carry_c = 0; s_carry_p = 0; s_carry_l = 0; s_bad = 0; }
-  __syncthreads();
+  if (tid == 0) s_bad = 0;
+  // (sums over the passes of 1024 requests or pairs: the same in every thread)
+  int carry_t = 0, carry_v = 0, carry_c = 0, carry_p = 0, carry_l = 0;
 
   // pass 1: validate; prefix sums of tiles and of valid requests
   for (int base = 0; base < p.batch; base += 1024) {
     const int r = base + tid;
-    int tiles = 0;
+    int tiles = 0, q0 = 0, q1 = 0, L = 0;
+    if (r < p.batch) { q0 = p.q_indptr[r]; q1 = p.q_indptr[r + 1]; L = p.seq_lens[r]; }
+    if (base == 0) __syncthreads();   // s_bad is cleared; the loads are on their way
     if (r < p.batch) {
-      const int m = p.q_indptr[r + 1] - p.q_indptr[r];
-      const int L = p.seq_lens[r];
+      const int m = q1 - q0;
       const bool ok = (m >= 1) && (m <= p.max_q_len) && (L >= m) &&
                       (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req &&
-                      (p.q_indptr[r] >= 0) && (p.q_indptr[r + 1] <= p.total_q);
+                      (q0 >= 0) && (q1 <= p.total_q);
       tiles = ok ? (L + kTileTokens - 1) / kTileTokens : 0;
       if (!ok) s_bad = 1;
       p.req_bad[r] = 0;
-      if (in_smem) { s_q0[r] = p.q_indptr[r]; s_m[r] = m; s_L[r] = L; }
+      if (in_smem) { s_q0[r] = q0; s_m[r] = m; s_L[r] = L; }
     }
     const int cost = tiles > 0 ? kCostPerTile * tiles + plan_entry_cost(tiles, p.entry_cost) : 0;
     int off[3] = {tiles, tiles > 0 ? 1 : 0, cost};
     block_exclusive_scan_1024(off, s_scratch, s_total);
-    const int off_t = off[0] + s_carry_t, off_v = off[1] + s_carry_v, off_c = off[2] + s_carry_c;
-    const int tot_t = s_total[0], tot_v = s_total[1], tot_c = s_total[2];
+    const int off_t = off[0] + carry_t, off_v = off[1] + carry_v, off_c = off[2] + carry_c;
+    carry_t += s_total[0]; carry_v += s_total[1]; carry_c += s_total[2];
     if (r < p.batch) {
       if (in_smem) { s_tp[r] = off_t; s_vp[r] = off_v; s_cp[r] = off_c; }
       else { p.tile_prefix[r] = off_t; p.valid_prefix[r] = off_v; p.cost_prefix[r] = off_c; }
     }
-    __syncthreads();
-    if (tid == 0) { s_carry_t += tot_t; s_carry_v += tot_v; s_carry_c += tot_c; }
-    __syncthreads();
   }
   if (tid == 0) {
-    if (in_smem) { s_tp[p.batch] = s_carry_t; s_vp[p.batch] = s_carry_v; s_cp[p.batch] = s_carry_c; }
-    else { p.tile_prefix[p.batch] = s_carry_t; p.valid_prefix[p.batch] = s_carry_v; p.cost_prefix[p.batch] = s_carry_c; }
+    if (in_smem) { s_tp[p.batch] = carry_t; s_vp[p.batch] = carry_v; s_cp[p.batch] = carry_c; }
+    else { p.tile_prefix[p.batch] = carry_t; p.valid_prefix[p.batch] = carry_v; p.cost_prefix[p.batch] = carry_c; }
     if (s_bad) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   }
   __syncthreads();  // the prefix arrays are read back below (same block: visible after the barrier)
-  const long long total_tiles = s_carry_t;
+  const long long total_tiles = carry_t;
   const long long T = total_tiles * Hkv;
-  const int n_valid_pairs = s_carry_v * Hkv;
-  const long long Tw = (long long)s_carry_c * Hkv;  // length of the cost axis
-  const bool too_long = T >= (1ll << 30) || s_carry_c >= (1 << 30) || s_carry_c < 0;
+  const int n_valid_pairs = carry_v * Hkv;
+  const long long Tw = (long long)carry_c * Hkv;  // length of the cost axis
+  const bool too_long = T >= (1ll << 30) || carry_c >= (1 << 30) || carry_c < 0;
   const bool may_split = T >= 2ll * kSnapTiles * n_cta;  // cuts inside pairs are then distinct
 
   // pass 2: the cuts.  Thread c places cut c at c*T/n_cta, finds the pair it falls in and moves it
@@ -178,15 +177,18 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   const bool overflow = too_long || n_work_all > p.max_work;
   if (tid <= n_cta) p.cta_off[tid] = overflow ? 0 : s_off[tid];
 
-  // range that holds axis position x: the largest c with cut[c] <= x (ranges before it that
-  // start at the same position are empty)
-  auto owner = [&](int x) -> int {
-    int lo = 0, hi = n_cta - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_cut[mid] <= x) lo = mid; else hi = mid - 1;
+  // the ranges that hold a pair's first and last tile: the largest c with cut[c] <= x (ranges before
+  // it that start at the same position are empty).  Both searches step together: they are chains of
+  // reads of shared memory.
+  auto owners = [&](int first, int last, int &c_first, int &c_last) {
+    int lo0 = 0, hi0 = n_cta - 1, lo1 = 0, hi1 = n_cta - 1;
+    while (lo0 < hi0 || lo1 < hi1) {
+      const int mid0 = (lo0 + hi0 + 1) >> 1, mid1 = (lo1 + hi1 + 1) >> 1;   // (a search that has ended stays where it is)
+      const bool up0 = s_cut[mid0] <= first, up1 = s_cut[mid1] <= last;
+      if (lo0 < hi0) { if (up0) lo0 = mid0; else hi0 = mid0 - 1; }
+      if (lo1 < hi1) { if (up1) lo1 = mid1; else hi1 = mid1 - 1; }
     }
-    return lo;
+    c_first = lo0; c_last = lo1;
   };
 
   // pass 4: one thread per pair: chunk count, partial slots, entries
@@ -200,16 +202,17 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
       tiles = tile_prefix(r + 1) - tp;
       if (tiles > 0) {
         b = tp * Hkv + g * tiles;
-        c_first = owner(b);
-        nch = owner(b + tiles - 1) - c_first + 1;
+        int c_last;
+        owners(b, b + tiles - 1, c_first, c_last);
+        nch = c_last - c_first + 1;
       }
     }
     // the pairs the combine kernel has work for: split ones, and those of invalid requests (sentinel rows)
     const bool listed = pair < n_pairs && nch != 1;
     int off[2] = {nch > 1 ? nch : 0, listed ? 1 : 0};
     block_exclusive_scan_1024(off, s_scratch, s_total);
-    const int part = off[0] + s_carry_p, lpos = off[1] + s_carry_l;
-    const int tot_p = s_total[0], tot_l = s_total[1];
+    const int part = off[0] + carry_p, lpos = off[1] + carry_l;
+    carry_p += s_total[0]; carry_l += s_total[1];
     if (listed) {
       CombineEntry ce;
       ce.pair = pair; ce.nch = nch; ce.part_base = (nch > 1 && part + nch <= p.max_part_slots) ? part : -1;
@@ -239,25 +242,23 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
         }
       }
     }
-    __syncthreads();
-    if (tid == 0) { s_carry_p += tot_p; s_carry_l += tot_l; }
-    __syncthreads();
   }
   // the combine kernel's blocks read their first entry without knowing how long the list is
-  if (tid < kCombineListPad && tid >= s_carry_l) {
+  if (tid < kCombineListPad && tid >= carry_l) {
     CombineEntry ce;
     ce.pair = -1; ce.nch = 1; ce.part_base = -1; ce.q0 = 0; ce.m = 0; ce.pad[0] = ce.pad[1] = ce.pad[2] = 0;
     p.combine_list[tid] = ce;
   }
+  __syncthreads();  // s_bad
   if (tid == 0) {
     const bool bad = overflow || s_bad == 2;
     p.hdr->n_work = bad ? 0 : n_work_all;
     p.hdr->n_cta = n_cta;
-    p.hdr->n_part_slots = s_carry_p;
+    p.hdr->n_part_slots = carry_p;
     p.hdr->total_tiles = (int)total_tiles;
     p.hdr->work_counter = 0;
     p.hdr->overflow = bad;
-    p.hdr->n_combine = s_carry_l;
+    p.hdr->n_combine = carry_l;
     if (bad) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   }
 }
