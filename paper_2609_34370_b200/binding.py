@@ -466,6 +466,8 @@ def kv_append(new_k, new_v, k_cache, v_cache, kv_strides, block_table, seq_lens,
         _require_cuda(q_rows)
         if q_rows.dtype != new_k.dtype or not q_rows.is_contiguous():
             raise SpxError(ERR_INVALID_ARG, "q_rows must be contiguous and of the cache's dtype")
+        if q_rows.dim() != 3 or q_rows.shape[0] != new_k.shape[0] or q_rows.shape[2] != new_k.shape[2]:
+            raise SpxError(ERR_INVALID_ARG, "q_rows must be [rows of new_k, query heads, head_dim]")
         a.num_q_heads, a.q_rows = q_rows.shape[1], _ptr(q_rows)
         if q_out is not None:
             _require_cuda(q_out)

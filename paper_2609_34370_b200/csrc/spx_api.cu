@@ -886,6 +886,7 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
   const bool rope = a->rope_base > 0.f;
   if (rope && ((a->head_dim & 1) || ((a->head_dim / 2) * es) % 16 != 0 || a->head_dim > kRopeMaxHeadDim)) return SPX_ERR_UNSUPPORTED;
   if (rope && a->q_rows && a->num_q_heads <= 0) return SPX_ERR_INVALID_ARG;
+  if (a->q_out && !(rope && a->q_rows)) return SPX_ERR_INVALID_ARG;   // nothing would be written to it
   if (e4m3 && (a->page_size > 128 || (a->head_dim != 64 && a->head_dim != 128))) return SPX_ERR_UNSUPPORTED;
   if (a->batch == 0) return SPX_OK;
   if (!a->new_k || !a->new_v || !a->k_cache || !a->v_cache || !a->block_table || !a->seq_lens || !a->q_indptr)

@@ -74,7 +74,8 @@ def _append(**over):
     (dict(head_dim=256, kv_stride_token=256), binding.ERR_UNSUPPORTED), (dict(page_size=256), binding.ERR_UNSUPPORTED),
     (dict(kv_stride_token=72), binding.ERR_INVALID_ARG), (dict(new_k=None), binding.ERR_INVALID_ARG), (dict(rope_base=-1.0), binding.ERR_INVALID_ARG),
     (dict(rope_base=1e4, q_rows=4096, num_q_heads=0), binding.ERR_INVALID_ARG),
-    (dict(rope_base=1e4, q_rows=4096, num_q_heads=4, q_out=4100), binding.ERR_INVALID_ARG)])
+    (dict(rope_base=1e4, q_rows=4096, num_q_heads=4, q_out=4100), binding.ERR_INVALID_ARG),
+    (dict(q_rows=4096, num_q_heads=4, q_out=4096), binding.ERR_INVALID_ARG), (dict(rope_base=1e4, q_out=4096), binding.ERR_INVALID_ARG)])
 def test_append_refusals(lib, over, code):
     a = _append(**over)
     status = C.c_int32(0)
