@@ -8,9 +8,11 @@
 // appending the same rows again changes nothing.
 //
 // A prompt has to read its rows and write half as many bytes and the rotated queries: 14.6k rows of the Llama-3-8B layer
-// shape are 329 MB, 51 us at HBM's rate.  They take 104: bound by the arithmetic between load and store, the compensated
-// rotation above all (float64 angles, products kept to 2^-46, so that a stored code is that of the exact value), and by
-// two blocks an SM, all that a tile's angles in shared memory leave room for.
+// shape are 329 MB, 51 us at HBM's rate.  They take 104, bound by latency: the 16 warps
+// of an SM (two blocks, for their registers and the angles in shared memory) alternate between a task's rows and the
+// dependent arithmetic on them, the compensated rotation above all (float64 angles, products kept to 2^-46, so that a
+// stored code is that of the exact value); 44% of the issue slots and 33% of DRAM's peak are used.  Rows fetched a task
+// ahead, whole (157 us) or item by item into the registers just read (119), were slower.
 #pragma once
 #include <type_traits>
 
