@@ -84,6 +84,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   if (n_cta > kPlanMaxCta) n_cta = kPlanMaxCta;
   if (tid == 0) s_bad = 0;
   // (sums over the passes of 1024 requests or pairs: the same in every thread)
+  bool any_long = false;
   int carry_t = 0, carry_v = 0, carry_c = 0, carry_p = 0, carry_l = 0;
 
   // pass 1: validate; prefix sums of tiles and of valid requests
@@ -105,6 +106,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
     const int cost = tiles > 0 ? kCostPerTile * tiles + plan_entry_cost(tiles, p.entry_cost) : 0;
     int off[3] = {tiles, tiles > 0 ? 1 : 0, cost};
     block_exclusive_scan_1024(off, s_scratch, s_total);
+    if (p.split_short_axis) any_long |= __syncthreads_or(tiles > 4 * kSnapTiles) != 0;
     const int off_t = off[0] + carry_t, off_v = off[1] + carry_v, off_c = off[2] + carry_c;
     carry_t += s_total[0]; carry_v += s_total[1]; carry_c += s_total[2];
     if (r < p.batch) {
@@ -123,6 +125,9 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   const int n_valid_pairs = carry_v * Hkv;
   const long long Tw = (long long)carry_c * Hkv;  // length of the cost axis
   const bool too_long = T >= (1ll << 30) || carry_c >= (1 << 30) || carry_c < 0;
+  // An axis too short to cut into n_cta ranges is cut into as many as it can be where a pair is longer than
+  // such a range's two lengths: few requests with long contexts would otherwise take one CTA a pair.
+  if (any_long && T < 2ll * kSnapTiles * n_cta) n_cta = max(1, (int)(T / (2 * kSnapTiles)));
   const bool may_split = T >= 2ll * kSnapTiles * n_cta;  // cuts inside pairs are then distinct
 
   // pass 2: the cuts.  Thread c places cut c at c*T/n_cta, finds the pair it falls in and moves it

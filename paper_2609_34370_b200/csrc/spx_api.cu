@@ -426,6 +426,7 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
   p.entry_cost = kPlanEntryCost;
   if (a->cache_format == SPX_CACHE_E4M3) {
     if (use_tensor_core_path(a)) p.entry_cost = kPlanEntryCostE4m3;
+    p.split_short_axis = 1;
     p.k_scales = a->k_scales; p.v_scales = a->v_scales;
     p.log2SB = log2_of(a->scale_block);
   }
