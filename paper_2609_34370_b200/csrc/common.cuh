@@ -158,6 +158,7 @@ struct AttnParams {
   const float *k_scales, *v_scales;
   int32_t log2SB;
   int32_t entry_cost;      // of a work entry on the planner's cost axis, in eighths of a tile
+  int32_t snap_tiles;      // planner: a cut this close to a pair boundary is moved onto the boundary
   int32_t split_short_axis;  // cut long pairs of a short axis too (8-bit pools; the others keep the sums they had)
   int32_t *dev_status;
   long long *prof;         // optional per-CTA cycle counters (profiling builds only), else NULL

@@ -81,6 +81,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   auto cost_prefix = [&](int i) -> int { return in_smem ? s_cp[i] : p.cost_prefix[i]; };  // per kv head
   const int tid = threadIdx.x;
   const int Hkv = p.Hkv;
+  const int snap = p.snap_tiles;   // a cut this close to a pair boundary is moved onto the boundary
   if (n_cta > kPlanMaxCta) n_cta = kPlanMaxCta;
   if (tid == 0) s_bad = 0;
   // (sums over the passes of 1024 requests or pairs: the same in every thread)
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
     const int cost = tiles > 0 ? kCostPerTile * tiles + plan_entry_cost(tiles, p.entry_cost) : 0;
     int off[3] = {tiles, tiles > 0 ? 1 : 0, cost};
     block_exclusive_scan_1024(off, s_scratch, s_total);
-    if (p.split_short_axis) any_long |= __syncthreads_or(tiles > 4 * kSnapTiles) != 0;
+    if (p.split_short_axis) any_long |= __syncthreads_or(tiles > 4 * snap) != 0;
     const int off_t = off[0] + carry_t, off_v = off[1] + carry_v, off_c = off[2] + carry_c;
     carry_t += s_total[0]; carry_v += s_total[1]; carry_c += s_total[2];
     if (r < p.batch) {
@@ -126,9 +127,10 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   const long long Tw = (long long)carry_c * Hkv;  // length of the cost axis
   const bool too_long = T >= (1ll << 30) || carry_c >= (1 << 30) || carry_c < 0;
   // An axis too short to cut into n_cta ranges is cut into as many as it can be where a pair is longer than
-  // such a range's two lengths: few requests with long contexts would otherwise take one CTA a pair.
-  if (any_long && T < 2ll * kSnapTiles * n_cta) n_cta = max(1, (int)(T / (2 * kSnapTiles)));
-  const bool may_split = T >= 2ll * kSnapTiles * n_cta;  // cuts inside pairs are then distinct
+  // such a range's two lengths: few requests with long contexts would otherwise take one CTA a pair
+  // (one of 4096 tokens and 8 kv heads over 8-bit pools: 39 us, so 23; in fp32 544 and 74).
+  if (any_long && T < 2ll * snap * n_cta) n_cta = max(1, (int)(T / (2 * snap)));
+  const bool may_split = T >= 2ll * snap * n_cta;  // cuts inside pairs are then distinct
 
   // pass 2: the cuts.  Thread c places cut c at c*T/n_cta, finds the pair it falls in and moves it
   // onto the pair's boundary if it is close to one (always, when the axis is too short to split).
@@ -156,8 +158,8 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
       int g = rel / pair_cost;
       const int offw = rel - g * pair_cost;
       int off = offw < entry_cost ? 0 : (offw - entry_cost) / kCostPerTile;
-      if (!may_split || off < kSnapTiles) off = 0;
-      else if (tiles - off < kSnapTiles) { off = 0; ++g; }  // onto the end of the pair = the start of the next
+      if (!may_split || off < snap) off = 0;
+      else if (tiles - off < snap) { off = 0; ++g; }  // onto the end of the pair = the start of the next
       inside = off > 0;
       cut = tp * Hkv + g * tiles + off;
       vq = valid_prefix(r) * Hkv + g;

@@ -424,8 +424,10 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
   p.part_o = reinterpret_cast<float *>(ws + w.part_o);
   p.rows_cap = w.rows_cap;
   p.entry_cost = kPlanEntryCost;
+  p.snap_tiles = kSnapTiles;
   if (a->cache_format == SPX_CACHE_E4M3) {
     if (use_tensor_core_path(a)) p.entry_cost = kPlanEntryCostE4m3;
+    else p.snap_tiles = 1;   // a tile is several microseconds of fp32 arithmetic, an entry's ends are little beside it
     p.split_short_axis = 1;
     p.k_scales = a->k_scales; p.v_scales = a->v_scales;
     p.log2SB = log2_of(a->scale_block);
