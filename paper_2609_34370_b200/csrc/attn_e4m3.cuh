@@ -28,7 +28,10 @@
 // group take the next tile's maximum again; one above 2^15 is past what P can hold, and the
 // group takes the maximum and makes the same tile's weights again: scores and scales are held until the tile's
 // verdict is read, and the issuer of the value MMAs reads it before it goes on.  m' moves, and O is rescaled, when a tile's
-// maximum passes it by a factor of 16.  The least x with a bit left is 2^-26 of the row's largest.
+// maximum passes it by a factor of 16.  The least x with a bit left is 2^-26 of the row's largest (a V scale below 2^-90
+// counted as 2^-90).  Where V's scales are zero or that small the x do not tell how large the y are (and 0 times a y
+// past fp32 is NaN): a thread's sum of a tile above 2^112 is past the range as well.  Sums add up to 2^111 a tile then,
+// 65,000 tiles of an entry before they leave fp32.
 //
 // Roles of the 512 threads: warps 0 and 13 TMA producers of K and of V, warp 1 issuer of the score MMAs, warp 12 of the
 // value MMAs, warp 2 scales of the next tiles, warps 3, 14 and 15 query pieces of the next entry, warps 4-7 and 8-11 two softmax groups
@@ -51,7 +54,8 @@ constexpr int kE8NanSlots = 8;
 constexpr float kE8Shift = 10.f;
 constexpr float kE8Rescale = 4.f;   // under a fresh reference x <= 2^(10 + 4)
 constexpr uint32_t kE8Warn = 0x7000u, kE8Redo = 0x7800u;   // 2^13, 2^15 as binary16 (its largest: 65504)
-constexpr float kE8MinLog2 = -90.f;  // smaller V scales count as this in m', so that no sum of y overflows
+constexpr float kE8MinLog2 = -90.f;  // smaller V scales (zero too) count as this in m': under a fresh reference y <= 2^(10 + 4 + 90)
+constexpr float kE8SumRedo = 5.19229686e33f;   // 2^112: 128 tokens of such y are 2^111
 
 template <int D, int MROWS>
 struct E8Cfg {
@@ -869,11 +873,12 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         }
         float sum_lo, sum_hi;
         unpair(sum2, sum_lo, sum_hi);
+        const float y_sum = sum_lo + sum_hi;
         l_before = l_sum;
-        l_sum += sum_lo + sum_hi;
+        l_sum += y_sum;
         // the verdict: x is not negative, so binary16 patterns order like values (NaNs do not count)
         const uint32_t x_top = max(h_max & 0xffffu, h_max >> 16);
-        const bool past = __any_sync(0xffffffffu, valid_row && x_top > kE8Redo), near = __any_sync(0xffffffffu, valid_row && x_top > kE8Warn);
+        const bool past = __any_sync(0xffffffffu, valid_row && (x_top > kE8Redo || y_sum > kE8SumRedo)), near = past || __any_sync(0xffffffffu, valid_row && x_top > kE8Warn);
         if (lane == 0 && near) atomicMax(&bars->verdict[grp][n_phase & 3], past && !again ? 2 : 1);
         if (g_tid == 0) bars->verdict[grp][(n_phase + 2) & 3] = 0;   // read by everybody: the group is two phases on
         if (mask_tile) {
