@@ -412,6 +412,7 @@ __global__ void __launch_bounds__(kLpTailThreads) logprob_merge_kernel(LogprobPa
       if (f.x == -INFINITY) continue;
       const float d = f.x - m;   // (a rounded difference is a factor off by 2^-24 |d|)
       const float w = expf(d);
+      if (w == 0.f) continue;    // its tokens have p = 0 (and d may be past the largest float: no product is 0 * inf)
       prod += (double)w * fma((double)f.z, 0.6931471805599453, (double)f.y * (double)d);
       if (d == 0.f && top == 0x7fffffff) { top = i; top_sum = f.y; }   // (a thread's first)
       else rest += (double)w * (double)f.y;
