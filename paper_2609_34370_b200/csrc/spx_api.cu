@@ -474,8 +474,10 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
     const int threads = e4m3 ? kSfThreads : kSimtThreads;
     const int smem = e4m3 ? SfSmem(p.rows_cap, p.D).total : SimtSmem(p.rows_cap, p.D).total;
     if (smem > dev.max_smem_optin) return SPX_ERR_UNSUPPORTED;
-    auto launch_simt = [&](auto kernel) -> cudaError_t {
-      cudaError_t er = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    // The limit belongs to the kernel, not to the call: it is raised once, to what the kernel's largest call needs.  Set to each
+    // call's own size it could be lowered by another host thread between a call's limit and its launch.
+    auto launch_simt = [&](auto kernel, SmemOnce &limit, int largest) -> cudaError_t {
+      cudaError_t er = limit.raise(kernel, largest, dev.device);
       if (er != cudaSuccess) return er;
       int per_sm = 0;
       er = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem);
@@ -487,26 +489,29 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
       ++t_launches;
       return cudaGetLastError();
     };
+    auto launch_simt_kv = [&](auto type, auto dim) -> cudaError_t {
+      using T = decltype(type);
+      constexpr int D = decltype(dim)::value;
+      static SmemOnce limit;
+      return launch_simt(attn_simt_kernel<T, D>, limit, SimtSmem(SPX_MAX_PACKED_ROWS, D).total);
+    };
     // 8-bit pools: packed rows per warp of the smallest kernel that holds them
     auto launch_simt_e4m3 = [&](auto type, auto dim) -> cudaError_t {
       using T = decltype(type);
       constexpr int D = decltype(dim)::value;
-      if (p.rows_cap <= 16) return launch_simt(attn_simt_e4m3_kernel<T, D, 2>);
-      if (p.rows_cap <= 32) return launch_simt(attn_simt_e4m3_kernel<T, D, 4>);
-      if (p.rows_cap <= 64) return launch_simt(attn_simt_e4m3_kernel<T, D, 8>);
-      return launch_simt(attn_simt_e4m3_kernel<T, D, 16>);
+      static SmemOnce limit[4];
+      if (p.rows_cap <= 16) return launch_simt(attn_simt_e4m3_kernel<T, D, 2>, limit[0], SfSmem(16, D).total);
+      if (p.rows_cap <= 32) return launch_simt(attn_simt_e4m3_kernel<T, D, 4>, limit[1], SfSmem(32, D).total);
+      if (p.rows_cap <= 64) return launch_simt(attn_simt_e4m3_kernel<T, D, 8>, limit[2], SfSmem(64, D).total);
+      return launch_simt(attn_simt_e4m3_kernel<T, D, 16>, limit[3], SfSmem(128, D).total);
     };
-    if (e4m3) {
-      using D64 = std::integral_constant<int, 64>;
-      using D128 = std::integral_constant<int, 128>;
-      if (a->kv_dtype == SPX_F32)
-        e = p.D == 64 ? launch_simt_e4m3(float(), D64()) : launch_simt_e4m3(float(), D128());
-      else
-        e = p.D == 64 ? launch_simt_e4m3(__nv_bfloat16(), D64()) : launch_simt_e4m3(__nv_bfloat16(), D128());
-    } else if (a->kv_dtype == SPX_F32)
-      e = p.D == 64 ? launch_simt(attn_simt_kernel<float, 64>) : launch_simt(attn_simt_kernel<float, 128>);
+    auto launch_dim = [&](auto type, auto launch) -> cudaError_t {
+      return p.D == 64 ? launch(type, std::integral_constant<int, 64>()) : launch(type, std::integral_constant<int, 128>());
+    };
+    if (e4m3)
+      e = a->kv_dtype == SPX_F32 ? launch_dim(float(), launch_simt_e4m3) : launch_dim(__nv_bfloat16(), launch_simt_e4m3);
     else
-      e = p.D == 64 ? launch_simt(attn_simt_kernel<__nv_bfloat16, 64>) : launch_simt(attn_simt_kernel<__nv_bfloat16, 128>);
+      e = a->kv_dtype == SPX_F32 ? launch_dim(float(), launch_simt_kv) : launch_dim(__nv_bfloat16(), launch_simt_kv);
   }
   if (e != cudaSuccess) return SPX_ERR_CUDA;
   // one row of blocks per listed pair on the named workloads (a cut of the tile axis lists at most one
@@ -860,15 +865,20 @@ static spx_status_t launch_append_e4m3(const spx_kv_append_args_t *a, int32_t *d
   if (splits < 3) splits = 3;
   if (splits > (tasks + slots - 1) / slots) splits = (tasks + slots - 1) / slots;
   const int smem = p.rope ? tile * (a->head_dim / 2) * 16 : 0;
-  auto launch = [&](auto kernel) -> spx_status_t {
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return SPX_ERR_CUDA;
+  auto launch = [&](auto type, auto dim) -> spx_status_t {
+    constexpr int D = decltype(dim)::value;
+    auto kernel = kv_append_e4m3_kernel<decltype(type), D>;
+    // (raised once to the angles of the largest tile, a scale block of 128 tokens: the limit is the kernel's, not the call's)
+    static SmemOnce limit;
+    if (limit.raise(kernel, 128 * (D / 2) * 16, dev.device) != cudaSuccess) return SPX_ERR_CUDA;
     kernel<<<dim3((unsigned)tiles, (unsigned)splits), kQuantThreads, smem, stream>>>(p);
     ++t_launches;
     return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
   };
-  if (a->kv_dtype == SPX_F32)
-    return a->head_dim == 64 ? launch(kv_append_e4m3_kernel<float, 64>) : launch(kv_append_e4m3_kernel<float, 128>);
-  return a->head_dim == 64 ? launch(kv_append_e4m3_kernel<__nv_bfloat16, 64>) : launch(kv_append_e4m3_kernel<__nv_bfloat16, 128>);
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (a->kv_dtype == SPX_F32) return a->head_dim == 64 ? launch(float(), D64()) : launch(float(), D128());
+  return a->head_dim == 64 ? launch(__nv_bfloat16(), D64()) : launch(__nv_bfloat16(), D128());
 }
 
 spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, void *cuda_stream) {
