@@ -444,7 +444,8 @@ def kv_append(new_k, new_v, k_cache, v_cache, kv_strides, block_table, seq_lens,
               status: Optional[torch.Tensor] = None, rope_base: float = 0.0, q_rows: Optional[torch.Tensor] = None,
               k_scales=None, v_scales=None, q_out: Optional[torch.Tensor] = None):
     """spx_kv_append on the current stream: the new positions' K/V go into their pages, in place.
-    rope_base > 0: the K rows (and q_rows [TQ, Hq, D], in place or into ``q_out``) are rotated to their positions.
+    rope_base > 0: the K rows (and q_rows [TQ or more, Hq, D], in place or into ``q_out``) are rotated to their positions;
+    rows of q_rows and q_out behind the new ones are left as they are.
     With ``k_scales`` / ``v_scales`` ([num_pages, Hkv, page_size / scale_block] float32) the pools hold
     float8_e4m3fn: rows are quantised on the way, the touched blocks' scales are written, and a request may
     bring any number of rows."""
@@ -462,20 +463,21 @@ def kv_append(new_k, new_v, k_cache, v_cache, kv_strides, block_table, seq_lens,
     a.kv_stride_page, a.kv_stride_head, a.kv_stride_token = (int(x) for x in kv_strides)
     a.block_table, a.seq_lens, a.q_indptr = _ptr(block_table), _ptr(seq_lens), q_indptr.data_ptr()
     a.rope_base = float(rope_base)
-    if q_rows is not None:
+    if q_rows is not None and a.rope_base != 0:   # (without a rotation the rows are ignored, whatever they are)
         _require_cuda(q_rows)
         if q_rows.dtype != new_k.dtype or not q_rows.is_contiguous():
             raise SpxError(ERR_INVALID_ARG, "q_rows must be contiguous and of the cache's dtype")
-        if q_rows.dim() != 3 or q_rows.shape[0] != new_k.shape[0] or q_rows.shape[2] != new_k.shape[2]:
-            raise SpxError(ERR_INVALID_ARG, "q_rows must be [rows of new_k, query heads, head_dim]")
+        if q_rows.dim() != 3 or q_rows.shape[0] < new_k.shape[0] or q_rows.shape[2] != new_k.shape[2]:
+            raise SpxError(ERR_INVALID_ARG, "q_rows must be [rows of new_k at least, query heads, head_dim]")
         a.num_q_heads, a.q_rows = q_rows.shape[1], _ptr(q_rows)
         if q_out is not None:
             _require_cuda(q_out)
-            if q_out.dtype != q_rows.dtype or q_out.shape != q_rows.shape or not q_out.is_contiguous():
-                raise SpxError(ERR_INVALID_ARG, "q_out must be contiguous and like q_rows")
+            if (q_out.dtype != q_rows.dtype or q_out.dim() != 3 or q_out.shape[0] < new_k.shape[0] or q_out.shape[1:] != q_rows.shape[1:] or
+                    not q_out.is_contiguous()):
+                raise SpxError(ERR_INVALID_ARG, "q_out must be contiguous and like q_rows (rows of new_k at least)")
             a.q_out = _ptr(q_out)
     elif q_out is not None:
-        raise SpxError(ERR_INVALID_ARG, "q_out needs q_rows")
+        raise SpxError(ERR_INVALID_ARG, "q_out needs q_rows and a rotation")
     _set_cache_scales(a, k_cache, v_cache, new_k.shape[1], page_size, num_pages, k_scales, v_scales)
     if a.cache_format == CACHE_E4M3 and (new_v.dtype != new_k.dtype or new_v.shape != new_k.shape or
                                          not new_k.is_contiguous() or not new_v.is_contiguous()):
