@@ -236,7 +236,7 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
  * infinite rope_base is SPX_ERR_INVALID_ARG.
  *
  * q_out (optional, like q_rows; it may be q_rows itself) receives the rotated rows instead, and q_rows is then left as it is.
- * Without q_rows or without a rotation it is SPX_ERR_INVALID_ARG.
+ * Without q_rows or without a rotation, or where its TQ rows overlap those of q_rows in part, it is SPX_ERR_INVALID_ARG.
  * (Beside 8-bit pools 16-bit query rows are rotated in binary32 from float64 angles: within two steps of binary32 before
  * their one rounding to 16 bits.)
  *

@@ -906,6 +906,12 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
     return SPX_ERR_INVALID_ARG;
   if (((uintptr_t)a->new_k | (uintptr_t)a->new_v | (uintptr_t)a->k_cache | (uintptr_t)a->v_cache) & 15) return SPX_ERR_INVALID_ARG;
   if (rope && (((uintptr_t)a->q_rows | (uintptr_t)a->q_out) & 15)) return SPX_ERR_INVALID_ARG;
+  if (a->q_out && a->q_out != a->q_rows) {
+    // rows written where others are still to be read: in place or apart
+    const uintptr_t in = (uintptr_t)a->q_rows, out = (uintptr_t)a->q_out;
+    const uintptr_t apart = in < out ? out - in : in - out;
+    if (apart < (uintptr_t)a->total_q * a->num_q_heads * a->head_dim * es) return SPX_ERR_INVALID_ARG;
+  }
   if (((a->kv_stride_page * cache_es) | (a->kv_stride_head * cache_es) | (a->kv_stride_token * cache_es)) & 15) return SPX_ERR_INVALID_ARG;
   if (e4m3) return launch_append_e4m3(a, dev_status, static_cast<cudaStream_t>(cuda_stream));
   KvAppendParams p{};

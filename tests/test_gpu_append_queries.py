@@ -88,7 +88,7 @@ def test_shapes_that_do_not_fit_are_refused(e4m3):
     call = _Call(e4m3, BF)
     q, n = call.q, call.total
     for rows, out in ((q[:n - 1], None), (q.view(-1, 64), None), (q[:, :, :32].contiguous(), None), (q, q[:n - 1].clone()), (q, q[:, :4].contiguous()),
-                      (q, q.float()), (None, q), (q[:, ::2], None)):
+                      (q, q.float()), (None, q), (q[:, ::2], None), (q[:n + 2], q[1:n + 3])):
         with pytest.raises(spx.SpxError):
             spx.kv_append(*call.args, **call.kw, rope_base=10000.0, q_rows=rows, q_out=out)
     with pytest.raises(spx.SpxError):
