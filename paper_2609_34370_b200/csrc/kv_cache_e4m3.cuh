@@ -49,13 +49,14 @@ struct KvQuantParams {
   double inv_freq[64];     // base^(-2i/D)
 };
 
-// Eight elements of a row as they are stored, and as floats.
+// Eight elements of a row as they are stored, and as floats.  (Plain loads: query rows may be rotated in place, so they are
+// not read-only for the kernel's life, which the non-coherent load promises.)
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
   uint4 a;
   __device__ void set_codes(uint2 lo, uint2 hi) { a = make_uint4(lo.x, lo.y, hi.x, hi.y); }
   __device__ void codes(uint2 &lo, uint2 &hi) const { lo = make_uint2(a.x, a.y); hi = make_uint2(a.z, a.w); }
-  __device__ void load(const __nv_bfloat16 *p) { a = __ldg(reinterpret_cast<const uint4 *>(p)); }
+  __device__ void load(const __nv_bfloat16 *p) { a = *reinterpret_cast<const uint4 *>(p); }
   __device__ void values(float (&x)[8]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -69,7 +70,7 @@ template <> struct Raw8<float> {
     lo = make_uint2(__float_as_uint(a.x), __float_as_uint(a.y));
     hi = make_uint2(__float_as_uint(a.z), __float_as_uint(a.w));
   }
-  __device__ void load(const float *p) { a = __ldg(reinterpret_cast<const float4 *>(p)); b = __ldg(reinterpret_cast<const float4 *>(p) + 1); }
+  __device__ void load(const float *p) { a = *reinterpret_cast<const float4 *>(p); b = *(reinterpret_cast<const float4 *>(p) + 1); }
   __device__ void values(float (&x)[8]) const {
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
   }
