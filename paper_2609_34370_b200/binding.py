@@ -193,7 +193,8 @@ def _stream(device) -> int:
     return _raw_stream(_current_device() if index is None else index)
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# (a torch built without CUDA has no such call; the host-only functions need none)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = torch.cuda.current_device
 
 
