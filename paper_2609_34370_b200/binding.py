@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import inspect
 import os
 from dataclasses import dataclass
 from typing import Optional, Tuple
@@ -206,9 +207,11 @@ def _require_cuda(*tensors):
 
 def _on_device_of(fn):
     """The library launches on the current device: the call is made with the device of its first argument current."""
+    name = next(iter(inspect.signature(fn).parameters))
+
     @functools.wraps(fn)
     def call(*args, **kw):
-        first = args[0] if args else next(iter(kw.values()), None)
+        first = args[0] if args else kw.get(name)
         if not getattr(first, "is_cuda", False) or first.get_device() == _current_device():
             return fn(*args, **kw)
         with torch.cuda.device(first.device):
