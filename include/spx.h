@@ -522,6 +522,14 @@ spx_status_t spx_debug_timeline(uint64_t *host_out, int64_t capacity, int32_t *k
  */
 spx_status_t spx_debug_wait_expiry(int32_t *report, int32_t *dev_status, void *cuda_stream);
 
+/*
+ * The same for the wait of the attention over 8-bit pools, which a whole warp makes, which sleeps in the barrier and which
+ * tells its outcome by the abort flag alone.  One block of two warps: each waits on a barrier of its own, then on another.
+ * report (device, int32 [6]): [0..1] cycles of each warp's first wait, [2..3] of its second, which leaves by the abort flag;
+ * [4] that flag; [5] waits that were satisfied (0).
+ */
+spx_status_t spx_debug_warp_wait_expiry(int32_t *report, int32_t *dev_status, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1261,6 +1261,17 @@ spx_status_t spx_debug_wait_expiry(int32_t *report, int32_t *dev_status, void *c
 #endif
 }
 
+spx_status_t spx_debug_warp_wait_expiry(int32_t *report, int32_t *dev_status, void *cuda_stream) {
+#if SPX_WAIT_TEST
+  if (!report || !dev_status) return SPX_ERR_INVALID_ARG;
+  warp_wait_expiry_kernel<<<1, 64, 0, static_cast<cudaStream_t>(cuda_stream)>>>(report, dev_status);
+  return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
+#else
+  (void)report; (void)dev_status; (void)cuda_stream;
+  return SPX_ERR_UNSUPPORTED;
+#endif
+}
+
 spx_status_t spx_plan_layout(const spx_attn_args_t *attn, int64_t *out) {
   if (!out) return SPX_ERR_INVALID_ARG;
   const spx_status_t st = check_attn(attn, false);

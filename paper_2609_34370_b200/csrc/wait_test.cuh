@@ -3,6 +3,7 @@
 // Nothing faults and nothing spins without a limit: every wait ends by its cycle limit or by the
 // abort flag another role raised, the kernel returns, and the host reads what happened.
 #pragma once
+#include "attn_e4m3.cuh"
 #include "attn_tc.cuh"
 #include "lm_head.cuh"
 #include "sampler.cuh"
@@ -46,6 +47,34 @@ __global__ void __launch_bounds__(128) wait_expiry_kernel(int32_t *report, int32
     report[9] = lbars.abort;
     report[10] = ring_abort;
   }
+}
+
+// The warp-wide wait of the kernel over 8-bit pools, which hands no outcome back: two warps wait on a barrier each, then
+// each on another one.  report[w], report[2 + w]: clock cycles warp w spent in its first and second wait; report[4]: the CTA's
+// abort flag; report[5]: how many of the four waits were satisfied (must be none).
+__global__ void __launch_bounds__(64) warp_wait_expiry_kernel(int32_t *report, int32_t *dev_status) {
+  __shared__ E8Barriers bars;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 4; ++i) tc::mbar_init(&bars.s_full[i], 1);
+    bars.abort = 0;
+    bars.dev_status = dev_status;
+    report[5] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t bar = tc::smem_u32(&bars.s_full[2 * i + warp]);
+    const long long t0 = clock64();
+    e8::warp_wait(bar, 0, &bars);
+    if (lane == 0) {
+      report[2 * i + warp] = (int32_t)min(clock64() - t0, (long long)0x7fffffff);
+      if (e8::try_wait(bar, 0)) atomicAdd(report + 5, 1);
+    }
+    __syncwarp();
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) report[4] = bars.abort;
 }
 
 }  // namespace spx
