@@ -39,6 +39,15 @@
 extern "C" {
 #endif
 
+/*
+ * The argument structs grow at their ends as calls learn to do more; a field of zero bytes means what its absence meant.
+ * The library reads them at the size that this header gives them, so a program zeroes the whole struct, and one that may meet
+ * a library built from another header compares spx_abi_version() with SPX_ABI_VERSION before its first call.  (1: without the
+ * 8-bit pools; no spx_abi_version.)
+ */
+#define SPX_ABI_VERSION 2
+int32_t spx_abi_version(void);
+
 #define SPX_MAX_K 15            /* at most 15 draft tokens (16 query positions) per request   */
 #define SPX_MAX_PACKED_ROWS 128 /* (num_q_heads / num_kv_heads) * (k+1) must not exceed this  */
 

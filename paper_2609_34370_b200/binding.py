@@ -17,8 +17,9 @@ DEV_BAD_PAGE, DEV_BAD_TOKEN, DEV_BAD_LEN, DEV_TIMEOUT, DEV_DEGENERATE, DEV_BAD_P
 BF16, F32 = 0, 1
 CACHE_KV_DTYPE, CACHE_E4M3 = 0, 1
 MAX_TOP_N = 32
+ABI_VERSION = 2   # of the structs below
 
-EXPORTS = ("spx_workspace_size", "spx_verify_attention", "spx_rejection_sample", "spx_verify_step",
+EXPORTS = ("spx_abi_version", "spx_workspace_size", "spx_verify_attention", "spx_rejection_sample", "spx_verify_step",
            "spx_host_step_arena_size", "spx_verify_step_host", "spx_status_string", "spx_last_launch_count",
            "spx_set_timing_events", "spx_plan_layout", "spx_debug_timeline", "spx_debug_wait_expiry", "spx_debug_warp_wait_expiry", "spx_rejection_sample_static", "spx_kv_append", "spx_kv_rollback",
            "spx_draft_confidence_workspace", "spx_draft_confidence", "spx_select_speculation",
@@ -110,6 +111,9 @@ def load_library():
             raise SpxError(-1, f"{LIB_PATH} is missing: run paper_2609_34370_b200.build.build() "
                                "(or __graft_entry__.build()) first")
         lib = C.CDLL(LIB_PATH)
+        version = lib.spx_abi_version() if hasattr(lib, "spx_abi_version") else 1
+        if version != ABI_VERSION:
+            raise SpxError(-1, f"{LIB_PATH} has argument structs of version {version}, the binding of {ABI_VERSION}: build it anew")
         lib.spx_workspace_size.restype = C.c_size_t
         lib.spx_workspace_size.argtypes = [C.POINTER(AttnArgs), C.POINTER(SampleArgs)]
         for name in ("spx_verify_attention", "spx_rejection_sample"):

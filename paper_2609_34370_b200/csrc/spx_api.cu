@@ -1219,6 +1219,8 @@ spx_status_t spx_rejection_sample_static(const spx_sample_args_t *args, int32_t 
                         dev.num_sms);
 }
 
+int32_t spx_abi_version(void) { return SPX_ABI_VERSION; }
+
 const char *spx_status_string(spx_status_t status) {
   switch (status) {
     case SPX_OK: return "ok";
