@@ -651,7 +651,8 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       const bool use0 = !one_tile || (pend.t_first & 1) == 0, use1 = !one_tile || (pend.t_first & 1) == 1;
       float ref = fmaxf(ref0, ref1);
       const float w0 = ref0 == -INFINITY ? 0.f : fast_exp2(ref0 - ref), w1 = ref1 == -INFINITY ? 0.f : fast_exp2(ref1 - ref);
-      const float l_row = w0 * l0 + w1 * l1;
+      // (a group without a reference has a sum of zero, or NaN)
+      const float l_row = rescaled_sum(l0, ref0 == -INFINITY ? -INFINITY : ref0 - ref) + rescaled_sum(l1, ref1 == -INFINITY ? -INFINITY : ref1 - ref);
       if (l_row != l_row) ref = 0.f;   // a NaN row stays one where its chunks are merged
 #pragma unroll
       for (int i = 0; i < CB; ++i) {
@@ -811,8 +812,8 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
             x_ref = x_tile;
           } else if (x_tile > x_ref + kE8Rescale) {
             alpha = fast_exp2(x_ref - x_tile);
+            l_sum = rescaled_sum(l_sum, x_ref - x_tile);
             x_ref = x_tile;
-            l_sum *= alpha;
           }
           need_max = false;
         }

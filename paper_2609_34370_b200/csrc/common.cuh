@@ -67,6 +67,14 @@ __device__ __forceinline__ float fast_exp2(float x) {
   return y;
 }
 
+// 2^d l of a sum l that is brought under another reference, d <= 0.  2^d may lie below the normal numbers where l makes up for
+// it: over 8-bit pools the sum of tokens whose V scales are zero or tiny is up to 2^100 times that of others.
+__device__ __forceinline__ float rescaled_sum(float l, float d) {
+  if (d > -100.f) return fast_exp2(d) * l;
+  const float h = fast_exp2(0.5f * d);
+  return l * h * h;
+}
+
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));

@@ -344,8 +344,8 @@ __global__ void __launch_bounds__(kCombineThreads) combine_kernel(AttnParams p) 
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           if (u >= nch || ml[u].x == -INFINITY) continue;
-          const float w = fast_exp2(ml[u].x - mstar);
-          lstar += w * ml[u].y;
+          const float d = ml[u].x - mstar, w = fast_exp2(d);
+          lstar = d > -100.f ? fmaf(w, ml[u].y, lstar) : lstar + rescaled_sum(ml[u].y, d);
           acc.x += w * o[u].x; acc.y += w * o[u].y; acc.z += w * o[u].z; acc.w += w * o[u].w;
         }
       } else {
@@ -362,8 +362,8 @@ __global__ void __launch_bounds__(kCombineThreads) combine_kernel(AttnParams p) 
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             if (c0 + u >= nch || ml[u].x == -INFINITY) continue;
-            const float w = fast_exp2(ml[u].x - mstar);
-            lstar += w * ml[u].y;
+            const float d = ml[u].x - mstar, w = fast_exp2(d);
+            lstar = d > -100.f ? fmaf(w, ml[u].y, lstar) : lstar + rescaled_sum(ml[u].y, d);
             acc.x += w * o[u].x; acc.y += w * o[u].y; acc.z += w * o[u].z; acc.w += w * o[u].w;
           }
         }

@@ -132,3 +132,21 @@ def test_a_chunk_of_zero_scales_among_others(hq, hkv, d, m):
             c.v_scales[int(c.table[0, t0 // 16])] = 0.0
     q = _queries(signs, m, hq, hkv, d, 8).to(BF)
     _check(c, q, [n], [m])
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("large", [30, 60, 90])
+@pytest.mark.parametrize("hq,hkv,d,m", SHAPES)
+def test_zero_and_large_value_scales_in_one_row(hq, hkv, d, m, large, dtype):
+    """Scales of zero beside scales of 2^30 to 2^90: what has weight and what has size lie in different tiles (every other one, the first or the
+    last ones), or in different chunks of a long request; the row's sum is that of the weights."""
+    lens = [770, 515, 900, 700, 7000]
+    c, signs = _rising_cache(lens, hkv, d, [[0] * 64, [6, 0, 6, 0, 6], [0] * 64, [4, 3, 2, 1, 0, 0], [0] * 64], seed=9)
+    for r, n in enumerate(lens):
+        tiles = -(-n // TILE)
+        for t0 in range(0, n, 16):
+            page, i = int(c.table[r, t0 // 16]), t0 // TILE
+            zero = (i % 2 == 0, i % 2 == 1, i < tiles // 2, i >= tiles // 2, i % 9 < 5)[r]
+            c.v_scales[page] = 0.0 if zero else c.v_scales[page] * 2.0 ** large
+    q = _queries(signs, m * len(lens), hq, hkv, d, 10).to(dtype)
+    _check(c, q, lens, [m] * len(lens))
