@@ -878,8 +878,8 @@ attn_e4m3_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         l_before = l_sum;
         l_sum += y_sum;
         // the verdict: x is not negative, so binary16 patterns order like values (NaNs do not count)
-        const uint32_t x_top = max(h_max & 0xffffu, h_max >> 16);
-        const bool past = __any_sync(0xffffffffu, valid_row && (x_top > kE8Redo || y_sum > kE8SumRedo)), near = past || __any_sync(0xffffffffu, valid_row && x_top > kE8Warn);
+        const uint32_t x_top = y_sum > kE8SumRedo ? 0xffffu : max(h_max & 0xffffu, h_max >> 16);
+        const bool past = __any_sync(0xffffffffu, valid_row && x_top > kE8Redo), near = __any_sync(0xffffffffu, valid_row && x_top > kE8Warn);
         if (lane == 0 && near) atomicMax(&bars->verdict[grp][n_phase & 3], past && !again ? 2 : 1);
         if (g_tid == 0) bars->verdict[grp][(n_phase + 2) & 3] = 0;   // read by everybody: the group is two phases on
         if (mask_tile) {
