@@ -473,17 +473,18 @@ def kv_append(new_k, new_v, k_cache, v_cache, kv_strides, block_table, seq_lens,
     a.kv_stride_page, a.kv_stride_head, a.kv_stride_token = (int(x) for x in kv_strides)
     a.block_table, a.seq_lens, a.q_indptr = _ptr(block_table), _ptr(seq_lens), q_indptr.data_ptr()
     a.rope_base = float(rope_base)
-    if q_rows is not None and a.rope_base != 0:   # (without a rotation the rows are ignored, whatever they are)
+    if q_rows is not None and rope_base != 0:   # (without a rotation the rows are ignored, whatever they are)
         _require_cuda(q_rows)
         if q_rows.dtype != new_k.dtype or not q_rows.is_contiguous():
             raise SpxError(ERR_INVALID_ARG, "q_rows must be contiguous and of the cache's dtype")
-        if q_rows.dim() != 3 or q_rows.shape[0] < new_k.shape[0] or q_rows.shape[2] != new_k.shape[2]:
+        shape = q_rows.shape
+        if len(shape) != 3 or shape[0] < a.total_q or shape[2] != a.head_dim:
             raise SpxError(ERR_INVALID_ARG, "q_rows must be [rows of new_k at least, query heads, head_dim]")
-        a.num_q_heads, a.q_rows = q_rows.shape[1], _ptr(q_rows)
+        a.num_q_heads, a.q_rows = shape[1], _ptr(q_rows)
         if q_out is not None:
             _require_cuda(q_out)
-            if (q_out.dtype != q_rows.dtype or q_out.dim() != 3 or q_out.shape[0] < new_k.shape[0] or q_out.shape[1:] != q_rows.shape[1:] or
-                    not q_out.is_contiguous()):
+            like = q_out.shape == shape or (q_out.dim() == 3 and q_out.shape[0] >= a.total_q and q_out.shape[1:] == shape[1:])
+            if not like or q_out.dtype != q_rows.dtype or not q_out.is_contiguous():
                 raise SpxError(ERR_INVALID_ARG, "q_out must be contiguous and like q_rows (rows of new_k at least)")
             a.q_out = _ptr(q_out)
     elif q_out is not None:
