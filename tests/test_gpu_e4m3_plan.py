@@ -65,8 +65,16 @@ def _loads(P, entry_cost):
 
 
 def _lens(spec):
-    b = W.generate(W.scaled(spec, vocab=64)) if spec.batch < 200 else W.generate(W.scaled(spec, batch=160, vocab=64))
-    return b.seq_lens.tolist(), np.diff(b.q_indptr.numpy()).tolist()
+    """Lengths and new positions as the named workload draws them (its tensors are not needed)."""
+    rng = np.random.default_rng(spec.index)
+    batch = min(spec.batch, 160)
+    m = [k + 1 for k in (rng.choice(spec.k[1], batch).tolist() if spec.k[0] == "choice" else [spec.k[1]] * batch)]
+    if spec.ctx[0] == "uniform":
+        lens = rng.integers(spec.ctx[1], spec.ctx[2] + 1, batch)
+    else:
+        _, median, sigma, lo, hi = spec.ctx
+        lens = np.clip(median * np.exp(sigma * rng.standard_normal(batch)), lo, hi).astype(int)
+    return [max(int(n), k) for n, k in zip(lens, m)], m
 
 
 @pytest.mark.parametrize("index", [1, 2, 4])
