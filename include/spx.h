@@ -107,7 +107,10 @@ typedef enum { SPX_CACHE_KV_DTYPE = 0, SPX_CACHE_E4M3 = 1 } spx_cache_format_t;
  * (cache_format = SPX_CACHE_E4M3, see spx_cache_format_t; every combination of the above is
  * supported).  K and V are then the scaled values, and a NaN in the V of a position reaches only the
  * queries that see that position.  Scales are finite and not negative; those of blocks past L_r are
- * never read.
+ * never read.  With BF16 queries (pages of 8 tokens at least) a weight times its token's V scale keeps 9 significant bits
+ * (off by 2^-9 + 2^-11 of itself at most) and is off by 2^-27 of the row's largest at most where that is more (V scales
+ * below 2^-90 counted as 2^-90 there); a query element below 2^-13 of its row's largest is off by 2^-21 of that.  Where a V
+ * scale is 2^a with a > 100, tokens of a weight below 2^(a - 136) of that token's are not in the row's sum.
  */
 typedef struct {
   int32_t batch;             /* B >= 0                                                        */
@@ -247,13 +250,13 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
  * q_out (optional, like q_rows; it may be q_rows itself) receives the rotated rows instead, and q_rows is then left as it is.
  * Without q_rows or without a rotation, or where its TQ rows overlap those of q_rows in part, it is SPX_ERR_INVALID_ARG.
  * (Beside 8-bit pools 16-bit query rows are rotated in binary32 from float64 angles: within two steps of binary32 before
- * their one rounding to 16 bits.)
+ * their one rounding to 16 bits.  There an infinite element, or a result past binary32, gives an infinity or a NaN.)
  *
  * Pools of 8-bit floats (cache_format = SPX_CACHE_E4M3, see spx_cache_format_t): a request may bring
  * ANY number m_r >= 1 of new rows (a prompt as well as a step), in place of at most SPX_MAX_K + 1.
  * With y the new rows' values in binary32 (K after the rotation: angles in float64, products and sum
- * in pairs of binary32 to 2^-46, then one rounding), every scale block that receives one of them is stored anew, the older tokens of its
- * request in it included:
+ * in pairs of binary32 to 2^-46, then one rounding; the sign of a zero that comes out is not told), every scale block that receives
+ * one of them is stored anew, the older tokens of its request in it included:
  *   amax  = the largest finite magnitude among the block's values: the older tokens' code * scale
  *           as they were, and the new y (slots past L_r do not count);
  *   scale = 2^e with the smallest e for which amax <= 448 * 2^e (-126 <= e), 1 when amax is 0;

@@ -8,18 +8,20 @@
 //     bfloat16's 8, exact for elements down to 2^-13 of the row's largest; those below are off by 2^-21 of it at most;
 //   * S = (Q1 + Q2) K^T accumulates in fp32; K's scale multiplies the score of its token;
 //   * a weight times V's scale, x_t = p_t v_t, is rounded to binary16 and cut into three e5m2 pieces (e5m2 is the upper
-//     byte of binary16, so a piece is a byte of the remainder), the third rounded to nearest: 9 significant bits and a
-//     sign, half a step off by 2^-10 at most (bfloat16, which the 16-bit kernels round P to: 2^-9), O += (P1 + P2 + P3) V.
+//     byte of binary16, so a piece is a byte of the remainder), the third rounded to nearest: 9 significant bits, off by
+//     2^-9 at most, 2^-10.9 in the mean square with the rounding to binary16 (bfloat16, which the 16-bit kernels round P to:
+//     2^-8 and 2^-9.3), O += (P1 + P2 + P3) V.
 // The MMAs of one B tile are weight-stationary and share it: it stays in the collector, 27 cycles an MMA at 32 rows
 // back to back, against 44 when each loads its own.  A tile's 8 score and 12 value MMAs come from two warps (by
 // elect.sync in a converged warp; a branch on one thread costs 46 cycles an MMA), 550 of the 1,420 cycles in which
 // its 32 KB can come from memory.
 //
 // What bounds it (one call, the plan and the combine kernel included, 12 us of it): the Llama-3-8B layer shape (64
-// requests of 512 to 4096 tokens, 320 MB of K and V) takes 85 to 88 us from one board to another, 81 with the softmax
-// arithmetic taken out: memory, at 5 TB/s between the first and the last tile; the 70B shape (128 requests, a pool in token
-// order, 469 MB) 129 to 134 us.  Contexts of 32,768 at 36 rows, 320 to 338 us, are bound by the softmax groups, whose
-// tiles are 64 rows wide there (211 us without their arithmetic).
+// requests of 512 to 4096 tokens, 320 MB of K and V) takes 85 to 89 us from one board to another, 81 with the softmax
+// arithmetic taken out: the stream of tiles, 5 TB/s between the first and the last (the 16-bit kernel, whose copies are
+// twice as large, reaches 5.5 on this shape; what holds this one is not shown); the 70B shape (128 requests, a pool in token
+// order, 469 MB) 128 to 135 us.  Contexts of 32,768 at 36 rows, 300 to 344 us by the clock the power limit leaves, are bound
+// by the softmax groups, whose tiles are 64 rows wide there (211 us without their arithmetic).
 //
 // binary16 has no exponents to spare for V's scales, so a row's reference m' is the maximum of s_t + log2 v_t
 // instead of s_t: y_t = 2^(10 + s_t - m') goes into the row's sum and x_t = y_t v_t into P, both under

@@ -10,9 +10,11 @@
 // A prompt has to read its rows and write half as many bytes and the rotated queries: 14.6k rows of the Llama-3-8B layer
 // shape are 329 MB, 51 us at HBM's rate.  They take 104, bound by latency: the 16 warps
 // of an SM (two blocks, for their registers and the angles in shared memory) alternate between a task's rows and the
-// dependent arithmetic on them, the compensated rotation above all (float64 angles, products kept to 2^-46, so that a
-// stored code is that of the exact value); 44% of the issue slots and 33% of DRAM's peak are used.  Rows fetched a task
-// ahead, whole (157 us) or item by item into the registers just read (119), were slower.
+// dependent arithmetic on them, the compensated rotation above all (float64 angles t f, off by 2^-53 of themselves, that is
+// 2^-40 at position 8191; products kept to 2^-46: a stored code is that of float64 arithmetic); 44% of the issue slots and
+// 33% of DRAM's peak are used.  Rows fetched a task ahead, whole (157 us) or item by item into the registers just read
+// (119), were slower.  Every block of a tile looks at all page ids of its request's new positions; that does not show up to
+// 131,072 rows (6.2 to 6.5 ns a row with pages of 16 and 32 tokens, like a prompt of 2048).
 #pragma once
 #include <type_traits>
 
@@ -119,11 +121,12 @@ __device__ __forceinline__ float amax8(const float (&x)[8], float m) {   // NaNs
 struct CosSin { uint64_t ch, cl, sh, sl; };   // of two pairs
 __device__ __forceinline__ uint64_t neg2(uint64_t a) { return e8::mul2(a, e8::pair(-1.f, -1.f)); }
 __device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) { return e8::fma2(b, e8::pair(-1.f, -1.f), a); }
-// y0 = x0 cos - x1 sin, y1 = x1 cos + x0 sin.  kExact: products and sum with their rounding errors, one rounding
-// to fp32 at the end of a value good to 2^-46 of |x| (what float64 arithmetic gives but for one in some millions
-// of last bits, at a third of its time: conversions from and to float64 alone are 8 cycles each); what goes into the
-// 8-bit codes and into fp32 rows.  Otherwise the leading errors only: within 2 steps of fp32 of the value, for
-// rows that are rounded to 16 bits.
+// y0 = x0 cos - x1 sin, y1 = x1 cos + x0 sin.  kExact: products and sum with their rounding errors (a product's by a fused
+// multiply-add, a sum's by Knuth's two-sum), one rounding to fp32 at the end of a value good to 2^-46 of |x| (what float64
+// arithmetic gives but for one in some millions of last bits and the sign of a zero, at a third of its time: conversions
+// from and to float64 alone are 8 cycles each); what goes into the 8-bit codes and into fp32 rows.  Otherwise the leading
+// errors only: within 2 steps of fp32 of the value, for rows that are rounded to 16 bits.  An infinite x, or a result past
+// fp32, gives an infinity or a NaN.
 template <bool kExact>
 __device__ __forceinline__ void rotate2(uint64_t x0, uint64_t x1, const CosSin &k, uint64_t &y0, uint64_t &y1) {
   using namespace e8;
