@@ -245,6 +245,34 @@ def time_extras(spx, binding, spec, b, attn_args, dev, iters: int = 200):
         out[f"sample_{name}_us"] = timed(sample_call(sv))
         out[f"step_{name}_us"] = timed(lambda: spx.verify_step(attn_args, sv, ws, dev))
     ws.status.bitwise_and_(~spx.DEV_DEGENERATE)
+    # the same step over pools of 8-bit floats (one scale per page and kv head), their append, and the log-probabilities
+    if spec.dtype == "bf16":
+        pools8, scales8 = [], []
+        for pool in (b.k_cache, b.v_cache):
+            heads_first = pool if b.layout == "HND" else pool.transpose(1, 2)
+            amax = heads_first.float().clamp(-16, 16).abs().amax((2, 3), keepdim=True).clamp(min=2.0 ** -100)
+            scale = torch.exp2(torch.ceil(torch.log2(amax / 448)))
+            codes = (heads_first.float().clamp(-16, 16) / scale).to(torch.float8_e4m3fn)
+            pools8.append(codes if b.layout == "HND" else codes.view(torch.uint8).transpose(1, 2).contiguous().view(torch.float8_e4m3fn))
+            scales8.append(scale[..., 0].contiguous())
+        kw8 = dict(k_scales=scales8[0], v_scales=scales8[1])
+        out8, lse8 = torch.empty_like(b.q), torch.empty(b.q.shape[:2], dtype=torch.float32, device=dev)
+        most = max(b.k_host) + 1
+        a8 = binding.make_attn_args(b.q, *pools8, b.kv_strides, b.block_table, b.seq_lens, b.q_indptr, spec.num_kv_heads, spec.page_size,
+                                    b.num_pages, out8, lse8, max_q_len=most, **kw8)
+        ws8 = spx.Workspace.allocate(spx.workspace_size(a8, base), dev)
+        out["attention_e4m3_us"] = timed(lambda: spx.verify_attention(b.q, *pools8, b.kv_strides, b.block_table, b.seq_lens, b.q_indptr,
+                                                                      spec.num_kv_heads, spec.page_size, b.num_pages, out=out8, lse=lse8,
+                                                                      max_q_len=most, ws=ws8, **kw8))
+        out["step_e4m3_us"] = timed(lambda: spx.verify_step(a8, base, ws8, dev))
+        out["kv_append_e4m3_rope_us"] = timed(lambda: spx.kv_append(new_k, new_v, *pools8, b.kv_strides, b.block_table, b.seq_lens, b.q_indptr,
+                                                                    spec.page_size, b.num_pages, status=status, rope_base=500000.0,
+                                                                    q_rows=b.q, q_out=q_rot, **kw8))
+        lws = spx.Workspace.allocate(1 << 20, dev)
+        out["token_logprobs_top20_us"] = timed(lambda: spx.token_logprobs(b.target_logits, tok, top_n=20, vocab=spec.vocab, ws=lws))
+        if int(ws8.status.item()) != 0 or int(lws.status.item()) != 0:
+            out["status_e4m3"] = [int(ws8.status.item()), int(lws.status.item())]
+        del pools8, scales8, out8, lse8
     # selective-speculation support and Algorithm 1
     cws = spx.Workspace.allocate(1 << 20, dev)
     out["draft_confidence_us"] = timed(lambda: spx.draft_confidence(b.draft_logits, b.draft_ids, b.q_indptr, ws=cws))
@@ -491,7 +519,7 @@ def main():
     ap.add_argument("--no-others", action="store_true", help="skip the table of the other four workloads (profiling runs)")
     ap.add_argument("--other-steps", type=int, default=300, help="timed steps per workload of the `workloads` table")
     ap.add_argument("--extras", action="store_true",
-                    help="also time the pieces around the step: KV append / rollback, verification variants")
+                    help="also time the pieces around the step: KV append / rollback, verification variants, 8-bit pools, log-probabilities")
     ap.add_argument("--extras-iters", type=int, default=200, help="timed calls per extras entry (profiling runs: a few)")
     ap.add_argument("--batch", type=int, default=0, help="override the workload's batch size (profiling captures of a smaller case)")
     ap.add_argument("--timeline", action="store_true",
