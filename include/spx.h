@@ -43,9 +43,9 @@ extern "C" {
  * The argument structs grow at their ends as calls learn to do more; a field of zero bytes means what its absence meant.
  * The library reads them at the size that this header gives them, so a program zeroes the whole struct, and one that may meet
  * a library built from another header compares spx_abi_version() with SPX_ABI_VERSION before its first call.  (1: without the
- * 8-bit pools; no spx_abi_version.)
+ * 8-bit pools; no spx_abi_version.  2: without shared prefixes and positions of several axes.)
  */
-#define SPX_ABI_VERSION 2
+#define SPX_ABI_VERSION 3
 int32_t spx_abi_version(void);
 
 #define SPX_MAX_K 15            /* at most 15 draft tokens (16 query positions) per request   */
@@ -111,7 +111,17 @@ typedef enum { SPX_CACHE_KV_DTYPE = 0, SPX_CACHE_E4M3 = 1 } spx_cache_format_t;
  * (off by 2^-9 + 2^-11 of itself at most) and is off by 2^-27 of the row's largest at most where that is more (V scales
  * below 2^-90 counted as 2^-90 there); a query element below 2^-13 of its row's largest is off by 2^-21 of that.  Where a V
  * scale is 2^a with a > 100, tokens of a weight below 2^(a - 136) of that token's are not in the row's sum.
+ *
+ * Shared prefixes (num_groups > 0).  The requests group_indptr[i] .. group_indptr[i+1]-1 share their first prefix_lens[i]
+ * tokens: their block-table rows name the same pages there (whole pages; what a prefix leaves in a page it does not fill may
+ * lie in a page of each request's own).  The results are those of the formula above; but the whole tiles of SPX_PREFIX_TILE
+ * tokens of a prefix are read once for all query rows of its group, in one product, and joined with each request's own
+ * tokens in fp32.  Requests that no group holds, groups of one and prefixes shorter than a tile share nothing.  A request
+ * whose block-table row differs from its group's first within those tiles sets SPX_DEV_BAD_PAGE, one with L_r - m_r below
+ * them (the new positions belong to no prefix) SPX_DEV_BAD_LEN; both get the sentinel outputs, and so do all requests of a
+ * group with a page id out of range in its prefix.  prefix_lens below zero count as zero.  The workspace is larger with groups: size it with num_groups set.
  */
+#define SPX_PREFIX_TILE 128
 typedef struct {
   int32_t batch;             /* B >= 0                                                        */
   int32_t total_q;           /* TQ = q_indptr[B] = rows of q/out (host copy of that number)   */
@@ -134,6 +144,10 @@ typedef struct {
   spx_cache_format_t cache_format;
   int32_t scale_block;        /* E4M3: tokens per scale                                         */
   const float *k_scales, *v_scales; /* E4M3: [num_pages, num_kv_heads, page_size/scale_block]   */
+  /* shared prefixes; all zero: none                                                            */
+  int32_t num_groups;          /* groups of consecutive requests                                */
+  const int32_t *group_indptr; /* [num_groups+1] requests, non-decreasing                       */
+  const int32_t *prefix_lens;  /* [num_groups] tokens that the requests of a group share        */
 } spx_attn_args_t;
 
 /*
@@ -224,6 +238,21 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
                              size_t ws_bytes, int32_t *dev_status, void *cuda_stream);
 
 /*
+ * Attention for prompts: the formula of spx_attn_args_t, with ANY number m_r >= 0 of new rows a request (a whole prompt, a chunk of one behind
+ * what is cached of it, single positions), packed one request behind the other in q and out.  Every type, cache format, page
+ * size, layout and stride of spx_verify_attention; (num_q_heads/num_kv_heads) <= SPX_MAX_PACKED_ROWS.  max_q_len is not looked
+ * at; total_q may be below batch.  Row j of request r sees the tokens 0 .. L_r - m_r + j, and nothing behind them reaches it: not a NaN or
+ * an infinity either, in K or in V.  Rows of q and out behind q_indptr[B] are left as they are.  Workspace from
+ * spx_prompt_workspace_size (0 = invalid arguments).  Errors in device data as for spx_verify_attention (L_r < m_r:
+ * SPX_DEV_BAD_LEN).  Shared prefixes (num_groups > 0) are SPX_ERR_UNSUPPORTED here: a prompt's own rows
+ * fill the tensor cores' tiles.
+ * BF16 rows: fp32 accumulation, weights rounded to bfloat16 before they meet V (as in spx_verify_attention over 16-bit pools; also over 8-bit pools), their
+ * sum before that rounding.  F32 rows, and pages of fewer than 8 tokens: fp32 products.
+ */
+size_t spx_prompt_workspace_size(const spx_attn_args_t *args);
+spx_status_t spx_prompt_attention(const spx_attn_args_t *args, void *ws, size_t ws_bytes, int32_t *dev_status, void *cuda_stream);
+
+/*
  * Cache maintenance around the step (the paper's Section 4: speculative execution shares the
  * paged cache with normal execution; its Figure 3: accepted speculation continues, rejected
  * speculation is re-executed).
@@ -231,7 +260,8 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
  * spx_kv_append writes the K/V of every request's k_r+1 new positions into their pages BEFORE
  * attention: row q_indptr[r]+j of new_k/new_v ([TQ, num_kv_heads, head_dim], contiguous, same
  * dtype as the pools) goes to logical token L_r-(k_r+1)+j of request r, i.e. page
- * block_table[r][t/page_size], slot t%page_size (seq_lens already counts the new positions).
+ * block_table[r][t/page_size], slot t%page_size (seq_lens already counts the new positions).  A request may bring any number
+ * >= 1 of rows (a prompt as well as a step).
  * Values are copied bit for bit; no other slot is touched.  Requests with an invalid length or
  * page id set SPX_DEV_BAD_LEN / SPX_DEV_BAD_PAGE and are skipped.  Pools and strides as in
  * spx_attn_args_t; head_dim * element size must be a multiple of 16 bytes.
@@ -252,8 +282,17 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
  * (Beside 8-bit pools 16-bit query rows are rotated in binary32 from float64 angles: within two steps of binary32 before
  * their one rounding to 16 bits.  There an infinite element, or a result past binary32, gives an infinity or a NaN.)
  *
- * Pools of 8-bit floats (cache_format = SPX_CACHE_E4M3, see spx_cache_format_t): a request may bring
- * ANY number m_r >= 1 of new rows (a prompt as well as a step), in place of at most SPX_MAX_K + 1.
+ * Positions of several axes (rope_axes = A > 0; images and video count time, height and width apart, and text behind
+ * an image goes on from the largest of them): pair i of a row (K and query rows alike) turns by
+ * positions[axis(i) * position_stride + row] * rope_base^(-2i/D), any int32 position, in place of its place t in the request, which still says
+ * where the row is stored.  axis(i): the sections lie one behind the other (the first rope_sections[0] pairs belong to axis 0,
+ * the next rope_sections[1] to axis 1, ...), or, rope_interleaved, the axes take the pairs in turn: pair i belongs to
+ * axis a = i mod A while i < A * rope_sections[a], and to axis 0 otherwise.  rope_sections: none negative, their sum D/2; interleaved,
+ * each axis but the first must find its pairs (a + A * (rope_sections[a] - 1) < D/2).  Anything else, a null
+ * positions, a position_stride below total_q, or A > 0 without a rotation is SPX_ERR_INVALID_ARG, A above SPX_MAX_ROPE_AXES
+ * SPX_ERR_UNSUPPORTED.
+ *
+ * Pools of 8-bit floats (cache_format = SPX_CACHE_E4M3, see spx_cache_format_t).
  * With y the new rows' values in binary32 (K after the rotation: angles in float64, products and sum
  * in pairs of binary32 to 2^-46, then one rounding; the sign of a zero that comes out is not told), every scale block that receives
  * one of them is stored anew, the older tokens of its request in it included:
@@ -273,6 +312,7 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
  * stay; the emitted token is the next step's position 0 and is not cached yet).  An accepted
  * length outside [0, k_r] sets SPX_DEV_BAD_LEN and writes -1.  new_seq_lens may alias seq_lens.
  */
+#define SPX_MAX_ROPE_AXES 4
 typedef struct {
   int32_t batch, total_q;
   int32_t num_kv_heads, head_dim, page_size, num_pages, max_pages_per_req;
@@ -291,6 +331,12 @@ typedef struct {
   spx_cache_format_t cache_format;
   int32_t scale_block;                /* E4M3: tokens per scale                               */
   float *k_scales, *v_scales;         /* E4M3: [num_pages, num_kv_heads, page_size/scale_block], written */
+  /* positions of several axes; all zero: a row's position is its place in the request               */
+  int32_t rope_axes;                  /* 1..SPX_MAX_ROPE_AXES                                 */
+  int32_t rope_interleaved;           /* 0 or 1                                               */
+  int32_t rope_sections[4];           /* pairs of elements of each axis; their sum is D/2     */
+  int64_t position_stride;            /* elements from an axis to the next, >= total_q        */
+  const int32_t *positions;           /* [rope_axes] x [TQ]                                   */
 } spx_kv_append_args_t;
 
 spx_status_t spx_kv_append(const spx_kv_append_args_t *args, int32_t *dev_status, void *cuda_stream);

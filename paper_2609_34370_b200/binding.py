@@ -17,14 +17,16 @@ DEV_BAD_PAGE, DEV_BAD_TOKEN, DEV_BAD_LEN, DEV_TIMEOUT, DEV_DEGENERATE, DEV_BAD_P
 BF16, F32 = 0, 1
 CACHE_KV_DTYPE, CACHE_E4M3 = 0, 1
 MAX_TOP_N = 32
-ABI_VERSION = 2   # of the structs below
+PREFIX_TILE = 128        # tokens: whole tiles of a shared prefix are read once for its group
+MAX_ROPE_AXES = 4
+ABI_VERSION = 3   # of the structs below
 
 EXPORTS = ("spx_abi_version", "spx_workspace_size", "spx_verify_attention", "spx_rejection_sample", "spx_verify_step",
            "spx_host_step_arena_size", "spx_verify_step_host", "spx_status_string", "spx_last_launch_count",
            "spx_set_timing_events", "spx_plan_layout", "spx_debug_timeline", "spx_debug_wait_expiry", "spx_debug_warp_wait_expiry", "spx_rejection_sample_static", "spx_kv_append", "spx_kv_rollback",
            "spx_draft_confidence_workspace", "spx_draft_confidence", "spx_select_speculation",
            "spx_lookahead_memory", "spx_sp_effective_batch", "spx_selective_batch", "spx_selective_effective_batch",
-           "spx_delay_gain", "spx_lm_head", "spx_token_logprobs_workspace", "spx_token_logprobs")
+           "spx_delay_gain", "spx_lm_head", "spx_prompt_workspace_size", "spx_prompt_attention", "spx_token_logprobs_workspace", "spx_token_logprobs")
 
 
 class AttnArgs(C.Structure):
@@ -38,6 +40,7 @@ class AttnArgs(C.Structure):
         ("block_table", C.c_void_p), ("seq_lens", C.c_void_p), ("q_indptr", C.c_void_p),
         ("out", C.c_void_p), ("lse", C.c_void_p),
         ("cache_format", C.c_int), ("scale_block", C.c_int32), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+        ("num_groups", C.c_int32), ("group_indptr", C.c_void_p), ("prefix_lens", C.c_void_p),
     ]
 
 
@@ -62,6 +65,8 @@ class KvAppendArgs(C.Structure):
         ("block_table", C.c_void_p), ("seq_lens", C.c_void_p), ("q_indptr", C.c_void_p),
         ("rope_base", C.c_float), ("num_q_heads", C.c_int32), ("q_rows", C.c_void_p), ("q_out", C.c_void_p),
         ("cache_format", C.c_int), ("scale_block", C.c_int32), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+        ("rope_axes", C.c_int32), ("rope_interleaved", C.c_int32), ("rope_sections", C.c_int32 * 4),
+        ("position_stride", C.c_int64), ("positions", C.c_void_p),
     ]
 
 
@@ -163,6 +168,10 @@ def load_library():
         lib.spx_delay_gain.argtypes = [C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double)]
         lib.spx_lm_head.restype = C.c_int
         lib.spx_lm_head.argtypes = [C.POINTER(LmHeadArgs), C.c_void_p, C.c_void_p]
+        lib.spx_prompt_workspace_size.restype = C.c_size_t
+        lib.spx_prompt_workspace_size.argtypes = [C.POINTER(AttnArgs)]
+        lib.spx_prompt_attention.restype = C.c_int
+        lib.spx_prompt_attention.argtypes = [C.POINTER(AttnArgs), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         lib.spx_token_logprobs_workspace.restype = C.c_size_t
         lib.spx_token_logprobs_workspace.argtypes = [C.POINTER(LogprobArgs)]
         lib.spx_token_logprobs.restype = C.c_int
@@ -248,9 +257,12 @@ def _set_cache_scales(a, k_cache, v_cache, num_kv_heads, page_size, num_pages, k
 
 
 def make_attn_args(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, num_kv_heads, page_size,
-                   num_pages, out, lse=None, sm_scale=0.0, max_q_len=0, k_scales=None, v_scales=None) -> AttnArgs:
+                   num_pages, out, lse=None, sm_scale=0.0, max_q_len=0, k_scales=None, v_scales=None, group_indptr=None,
+                   prefix_lens=None) -> AttnArgs:
     """``k_scales`` / ``v_scales`` ([num_pages, num_kv_heads, page_size / scale_block] float32): the pools hold
-    float8_e4m3fn, one scale per block of tokens and kv head; everything else keeps the type of ``q``."""
+    float8_e4m3fn, one scale per block of tokens and kv head; everything else keeps the type of ``q``.
+    ``group_indptr`` ([groups + 1] int32) and ``prefix_lens`` ([groups] int32): the requests group_indptr[i] ..
+    group_indptr[i + 1] - 1 share the pages of their first prefix_lens[i] tokens, which are read once for the group."""
     TQ, Hq, D = q.shape
     a = AttnArgs()
     a.batch = seq_lens.numel()
@@ -266,6 +278,15 @@ def make_attn_args(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_ind
     a.block_table, a.seq_lens, a.q_indptr = _ptr(block_table), _ptr(seq_lens), q_indptr.data_ptr()
     a.out, a.lse = _ptr(out), _ptr(lse)
     _set_cache_scales(a, k_cache, v_cache, num_kv_heads, page_size, num_pages, k_scales, v_scales)
+    if group_indptr is not None or prefix_lens is not None:
+        if group_indptr is None or prefix_lens is None:
+            raise SpxError(ERR_INVALID_ARG, "group_indptr and prefix_lens come together")
+        if group_indptr.numel() != prefix_lens.numel() + 1:
+            raise SpxError(ERR_INVALID_ARG, "group_indptr has one element more than prefix_lens")
+        for t in (group_indptr, prefix_lens):
+            if t.dtype != torch.int32 or not t.is_contiguous():
+                raise SpxError(ERR_INVALID_ARG, "group_indptr and prefix_lens must be contiguous int32")
+        a.num_groups, a.group_indptr, a.prefix_lens = prefix_lens.numel(), _ptr(group_indptr), _ptr(prefix_lens)
     return a
 
 
@@ -315,22 +336,51 @@ class Workspace:
 @_on_device_of
 def verify_attention(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, num_kv_heads, page_size,
                      num_pages, out=None, lse=None, sm_scale=0.0, max_q_len=0, ws: Optional[Workspace] = None,
-                     want_lse=True, k_scales=None, v_scales=None):
-    """spx_verify_attention on the current stream.  Returns (out, lse, ws).  8-bit pools: see make_attn_args."""
-    _require_cuda(q, k_cache, v_cache, block_table, seq_lens, q_indptr, k_scales, v_scales)
+                     want_lse=True, k_scales=None, v_scales=None, group_indptr=None, prefix_lens=None):
+    """spx_verify_attention on the current stream.  Returns (out, lse, ws).  8-bit pools and shared prefixes: see make_attn_args."""
+    _require_cuda(q, k_cache, v_cache, block_table, seq_lens, q_indptr, k_scales, v_scales, group_indptr, prefix_lens)
     lib = load_library()
     if out is None:
         out = torch.empty_like(q)
     if lse is None and want_lse:
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
     a = make_attn_args(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, num_kv_heads, page_size,
-                       num_pages, out, lse, sm_scale, max_q_len, k_scales, v_scales)
+                       num_pages, out, lse, sm_scale, max_q_len, k_scales, v_scales, group_indptr, prefix_lens)
     need = workspace_size(a, None)
     if ws is None:
         ws = Workspace.allocate(need, q.device)
     ws.ensure(need)
     _check(lib.spx_verify_attention(C.byref(a), ws.buf.data_ptr(), ws.buf.numel(), ws.status.data_ptr(),
                                     _stream(q.device)))
+    return out, lse, ws
+
+
+@_on_device_of
+def prompt_attention(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, num_kv_heads, page_size, num_pages,
+                     out=None, lse=None, sm_scale=0.0, ws: Optional[Workspace] = None, want_lse=True, k_scales=None, v_scales=None):
+    """spx_prompt_attention on the current stream: causal attention of any number of new rows a request (whole prompts, chunks
+    behind what is cached) over the paged pools they have entered.  Returns (out, lse, ws); rows of ``out`` and ``lse``
+    behind the last request's are left as they are.  8-bit pools: see make_attn_args."""
+    _require_cuda(q, k_cache, v_cache, block_table, seq_lens, q_indptr, k_scales, v_scales)
+    lib = load_library()
+    if q.dim() != 3 or not q.is_contiguous():
+        raise SpxError(ERR_INVALID_ARG, "q must be contiguous [rows, query heads, head_dim]")
+    if out is None:
+        out = torch.empty_like(q)
+    _check_output(out, q.shape, q.dtype, "out")
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _check_output(lse, q.shape[:2], torch.float32, "lse")
+    a = make_attn_args(q, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, num_kv_heads, page_size,
+                       num_pages, out, lse, sm_scale, 0, k_scales, v_scales)
+    need = int(lib.spx_prompt_workspace_size(C.byref(a)))
+    if need == 0:
+        raise SpxError(ERR_INVALID_ARG, "invalid arguments for workspace sizing")
+    if ws is None:
+        ws = Workspace.allocate(need, q.device)
+    ws.ensure(need)
+    _check(lib.spx_prompt_attention(C.byref(a), ws.buf.data_ptr(), ws.buf.numel(), ws.status.data_ptr(), _stream(q.device)))
     return out, lse, ws
 
 
@@ -452,14 +502,17 @@ def rejection_sample_static(target_logits, draft_logits, draft_ids, q_indptr, u_
 @_on_device_of
 def kv_append(new_k, new_v, k_cache, v_cache, kv_strides, block_table, seq_lens, q_indptr, page_size, num_pages,
               status: Optional[torch.Tensor] = None, rope_base: float = 0.0, q_rows: Optional[torch.Tensor] = None,
-              k_scales=None, v_scales=None, q_out: Optional[torch.Tensor] = None):
+              k_scales=None, v_scales=None, q_out: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+              rope_sections=None, rope_interleaved: bool = False):
     """spx_kv_append on the current stream: the new positions' K/V go into their pages, in place.
     rope_base > 0: the K rows (and q_rows [TQ or more, Hq, D], in place or into ``q_out``) are rotated to their positions;
     rows of q_rows and q_out behind the new ones are left as they are.
     With ``k_scales`` / ``v_scales`` ([num_pages, Hkv, page_size / scale_block] float32) the pools hold
-    float8_e4m3fn: rows are quantised on the way, the touched blocks' scales are written, and a request may
-    bring any number of rows."""
-    _require_cuda(new_k, new_v, k_cache, v_cache, block_table, seq_lens, q_indptr, k_scales, v_scales)
+    float8_e4m3fn: rows are quantised on the way and the touched blocks' scales are written.
+    ``positions`` ([axes, rows of new_k at least] int32): the rows turn by these instead of by their places in the requests, pair
+    i by the axis that ``rope_sections`` (pairs of each axis) gives it, sections one behind the other or dealt out in turn
+    (``rope_interleaved``)."""
+    _require_cuda(new_k, new_v, k_cache, v_cache, block_table, seq_lens, q_indptr, k_scales, v_scales, positions)
     lib = load_library()
     dev = new_k.device
     if status is None:
@@ -489,6 +542,19 @@ def kv_append(new_k, new_v, k_cache, v_cache, kv_strides, block_table, seq_lens,
             a.q_out = _ptr(q_out)
     elif q_out is not None:
         raise SpxError(ERR_INVALID_ARG, "q_out needs q_rows and a rotation")
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.dim() != 2 or (positions.shape[1] > 1 and positions.stride(1) != 1):
+            raise SpxError(ERR_INVALID_ARG, "positions must be int32 [axes, rows] with contiguous rows")
+        if positions.shape[1] < a.total_q or rope_sections is None or len(rope_sections) != positions.shape[0]:
+            raise SpxError(ERR_INVALID_ARG, "positions need a column for every row of new_k and a section for every axis")
+        if not 1 <= len(rope_sections) <= MAX_ROPE_AXES:
+            raise SpxError(ERR_UNSUPPORTED, f"positions have 1 to {MAX_ROPE_AXES} axes")
+        a.rope_axes, a.rope_interleaved, a.positions = len(rope_sections), int(bool(rope_interleaved)), _ptr(positions)
+        a.position_stride = positions.stride(0) if len(rope_sections) > 1 else max(positions.shape[1], a.total_q)
+        for i, n in enumerate(rope_sections):
+            a.rope_sections[i] = int(n)
+    elif rope_sections is not None:
+        raise SpxError(ERR_INVALID_ARG, "rope_sections needs positions")
     _set_cache_scales(a, k_cache, v_cache, new_k.shape[1], page_size, num_pages, k_scales, v_scales)
     if a.cache_format == CACHE_E4M3 and (new_v.dtype != new_k.dtype or new_v.shape != new_k.shape or
                                          not new_k.is_contiguous() or not new_v.is_contiguous()):

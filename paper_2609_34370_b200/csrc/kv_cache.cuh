@@ -5,10 +5,14 @@
 
 namespace spx {
 
-constexpr int kRopeMaxHeadDim = 512;  // the rotary path keeps base^(-2i/D) of one head in shared memory
+constexpr int kRopeMaxHeadDim = 512;
+constexpr int kAppendThreads = 256;
+constexpr int kAppendRows = 16;         // new rows of a block, at most
+constexpr int kAppendAngles = 1024;     // (row, pair) angles a block keeps: 16 rows of 128 elements, 4 of 512
 
 struct KvAppendParams {
   int32_t batch, total_q, Hkv, D, P, log2P, num_pages, max_pages_per_req, elem_size;
+  int32_t log2_rows;       // new rows of a block
   const unsigned char *new_k, *new_v;
   unsigned char *k_cache, *v_cache;
   int64_t stride_page, stride_head, stride_token;  // elements
@@ -18,118 +22,123 @@ struct KvAppendParams {
   unsigned char *q_rows;   // optional [TQ, Hq, D], rotated into q_out (in place when the two are one)
   unsigned char *q_out;
   int32_t Hq;
+  // positions of several axes (axes = 0: a row's position is its place in the request)
+  int32_t axes;
+  const int32_t *positions;
+  int64_t position_stride;
+  unsigned char axis_of[kRopeMaxHeadDim / 2];
 };
 
-// Rotary embedding of the pairs (x[i], x[i + D/2]), i = i0 .. i0+N-1, of one head vector at
-// absolute position t: angle t * inv_freq[i], inv_freq[i] = base^(-2i/D), in double; results rounded
-// double -> binary32 -> element type (round-to-nearest-even each).  lo / hi are the 16-byte vectors
-// that hold the pairs' first and second elements.
+// Rotary embedding of the pairs (x[i], x[i + D/2]) of one head vector: x in double, cosine and sine of the pair's
+// angle in double; results rounded double -> binary32 -> element type (round-to-nearest-even each).  lo / hi are the
+// 16-byte vectors that hold the pairs' first and second elements, cs the (cos, sin) of the first.
 template <typename T>
-__device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, int i0, int t, const double *inv_freq) {
+__device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2 *cs) {
   constexpr int N = 16 / sizeof(T);
   union U { uint4 q; T e[N]; } a, b;
   a.q = lo; b.q = hi;
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const double ang = (double)t * inv_freq[i0 + u];
-    double sn, cs;
-    sincos(ang, &sn, &cs);
+    const double2 k = cs[u];
     const double x0 = (double)ld_as_float(a.e, u), x1 = (double)ld_as_float(b.e, u);
-    st_from_float(a.e, u, __double2float_rn(x0 * cs - x1 * sn));
-    st_from_float(b.e, u, __double2float_rn(x1 * cs + x0 * sn));
+    st_from_float(a.e, u, __double2float_rn(x0 * k.x - x1 * k.y));
+    st_from_float(b.e, u, __double2float_rn(x1 * k.x + x0 * k.y));
   }
   lo = a.q; hi = b.q;
 }
 
-// grid = B, block = 256.  One block copies one request's (k+1) x Hkv rows of D elements, 16 bytes
-// per thread and step, K and V.  Pure copy: bound by launch latency at verify-step sizes (a few
-// MB), by HBM beyond that.  With a rotary base the K rows (and the caller's query rows, in place)
-// are rotated to their absolute positions on the way.
-__global__ void __launch_bounds__(256) kv_append_kernel(KvAppendParams p) {
-  const int r = blockIdx.x;
+// A block takes up to kAppendRows new rows of a request, all heads of K, V and the query rows, 16 bytes a thread and step.
+// Block b belongs to the request r with base(r) <= b < base(r + 1), base(r) = q_indptr[r] / rows + r: m rows are at most
+// m / rows + 1 blocks, so no prefix sums are needed; blocks past a request's last one leave at once.  The angles are
+// worked out once a block and shared by its heads.
+// Pure copy and rotation: bound by launch latency at verify-step sizes (a few MB), by HBM beyond that.
+__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ KvAppendParams p) {
+  __shared__ int s_req, s_page[kAppendRows];
+  __shared__ double s_inv_freq[kRopeMaxHeadDim / 2];
+  __shared__ __align__(16) double2 s_cs[kAppendAngles];
+  const int tid = threadIdx.x, lane = tid & 31;
+  const bool rope = p.rope_base > 0.0;
+  if (tid < 32) {
+    // 32 probes at a time
+    int lo = 0, hi = p.batch;   // base(lo) <= block, hi past the last candidate
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, c = lo + lane * step;
+      const bool below = c < hi && (int64_t)(p.q_indptr[c] >> p.log2_rows) + c <= (int64_t)blockIdx.x;
+      const int n = __popc(__ballot_sync(0xffffffffu, below || lane == 0));   // the probes ascend
+      const int at = lo + (n - 1) * step;
+      hi = min(hi, at + step);
+      lo = at;
+    }
+    if (lane == 0) s_req = lo;
+  } else if (rope) {
+    for (int i = tid - 32; i < (p.D >> 1); i += kAppendThreads - 32) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
+  }
+  __syncthreads();
+  const int r = s_req;
   const int q0 = p.q_indptr[r];
   const int m = p.q_indptr[r + 1] - q0;
   const int L = p.seq_lens[r];
-  __shared__ int s_page[SPX_MAX_K + 1];
-  __shared__ int s_bad;
-  if (threadIdx.x == 0) s_bad = 0;
-  __syncthreads();
-  const bool ok_len = m >= 1 && m <= SPX_MAX_K + 1 && L >= m && q0 >= 0 && q0 + m <= p.total_q &&
+  const bool ok_len = m >= 1 && L >= m && q0 >= 0 && m <= p.total_q - q0 &&
                       (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req;
   if (!ok_len) {
-    if (threadIdx.x == 0) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
+    if (tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
     return;
   }
-  if (threadIdx.x < m) {
-    const int t = L - m + threadIdx.x;
-    const int page = p.block_table[(int64_t)r * p.max_pages_per_req + (t >> p.log2P)];
-    s_page[threadIdx.x] = page;
-    if (page < 0 || page >= p.num_pages) s_bad = 1;
+  const int64_t j0_64 = ((int64_t)blockIdx.x - ((q0 >> p.log2_rows) + (int64_t)r)) << p.log2_rows;
+  if (j0_64 < 0 || j0_64 >= m) return;
+  const int j0 = (int)j0_64, n = min(1 << p.log2_rows, m - j0), t0 = L - m + j0;
+  const int32_t *table = p.block_table + (int64_t)r * p.max_pages_per_req;
+  if (tid < n) s_page[tid] = table[(t0 + tid) >> p.log2P];
+  // a request with a bad page among its new positions is skipped as a whole: every one of its blocks looks at all of them
+  int bad = 0;
+  for (int i = ((L - m) >> p.log2P) + tid; i <= (L - 1) >> p.log2P; i += kAppendThreads) {
+    const int pg = table[i];
+    bad |= pg < 0 || pg >= p.num_pages;
   }
-  __syncthreads();
-  if (s_bad) {
-    if (threadIdx.x == 0) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
+  if (rope) {
+    const int half = p.D >> 1;
+    for (int i = tid; i < n * half; i += kAppendThreads) {
+      const int row = i / half, pair = i % half;
+      const int t = p.axes ? p.positions[(int64_t)p.axis_of[pair] * p.position_stride + q0 + j0 + row] : t0 + row;
+      double2 cs;
+      sincos((double)t * s_inv_freq[pair], &cs.y, &cs.x);
+      s_cs[i] = cs;
+    }
+  }
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
     return;
   }
-  const int row_bytes = p.D * p.elem_size;
-  const int vec_per_row = row_bytes >> 4;
-  const int n_vec = m * p.Hkv * vec_per_row;
-  if (p.rope_base > 0.0) {
-    __shared__ double s_inv_freq[kRopeMaxHeadDim / 2];
-    for (int i = threadIdx.x; i < (p.D >> 1); i += blockDim.x) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
-    __syncthreads();
-    // K: a thread takes one vector of the first half of a head row and its partner in the second
-    // half, rotates the pairs and stores both; V is copied; the query rows are rotated in place.
-    const int half_vecs = vec_per_row >> 1, elems_per_vec = 16 / p.elem_size;
-    const int n_k = m * p.Hkv * half_vecs;
-    for (int i = threadIdx.x; i < n_k; i += blockDim.x) {
-      const int v = i % half_vecs, jg = i / half_vecs, g = jg % p.Hkv, j = jg / p.Hkv;
-      const int t = L - m + j;
-      const int64_t src = (((int64_t)(q0 + j) * p.Hkv + g) * p.D) * p.elem_size + (int64_t)v * 16;
-      const int64_t dst = ((int64_t)s_page[j] * p.stride_page + (int64_t)g * p.stride_head +
-                           (int64_t)(t & (p.P - 1)) * p.stride_token) * p.elem_size + (int64_t)v * 16;
-      const int64_t half_bytes = (int64_t)(p.D >> 1) * p.elem_size;
-      uint4 lo = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src));
-      uint4 hi = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src + half_bytes));
-      if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(lo, hi, v * elems_per_vec, t, s_inv_freq);
-      else rope_vectors<float>(lo, hi, v * elems_per_vec, t, s_inv_freq);
-      *reinterpret_cast<uint4 *>(p.k_cache + dst) = lo;
-      *reinterpret_cast<uint4 *>(p.k_cache + dst + half_bytes) = hi;
+  const int row_bytes = p.D * p.elem_size, vecs = row_bytes >> 4;
+  auto cache_at = [&](int row, int g) -> int64_t {
+    return ((int64_t)s_page[row] * p.stride_page + (int64_t)g * p.stride_head + (int64_t)((t0 + row) & (p.P - 1)) * p.stride_token) * p.elem_size;
+  };
+  if (rope) {
+    // a thread takes one vector of the first half of a head row and its partner in the second half
+    const int half_vecs = vecs >> 1, per_vec = 16 / p.elem_size, half_bytes = row_bytes >> 1;
+    auto turn = [&](const unsigned char *src, unsigned char *dst, int row, int v) {
+      uint4 lo = *reinterpret_cast<const uint4 *>(src), hi = *reinterpret_cast<const uint4 *>(src + half_bytes);
+      const double2 *cs = s_cs + row * (p.D >> 1) + v * per_vec;
+      if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(lo, hi, cs);
+      else rope_vectors<float>(lo, hi, cs);
+      *reinterpret_cast<uint4 *>(dst) = lo;
+      *reinterpret_cast<uint4 *>(dst + half_bytes) = hi;
+    };
+    for (int i = tid; i < n * p.Hkv * half_vecs; i += kAppendThreads) {
+      const int v = i % half_vecs, jg = i / half_vecs, g = jg % p.Hkv, row = jg / p.Hkv;
+      turn(p.new_k + ((int64_t)(q0 + j0 + row) * p.Hkv + g) * row_bytes + v * 16, p.k_cache + cache_at(row, g) + v * 16, row, v);
     }
-    for (int i = threadIdx.x; i < n_vec; i += blockDim.x) {
-      const int v = i % vec_per_row, jg = i / vec_per_row, g = jg % p.Hkv, j = jg / p.Hkv;
-      const int t = L - m + j;
-      const int64_t src = (((int64_t)(q0 + j) * p.Hkv + g) * p.D) * p.elem_size + (int64_t)v * 16;
-      const int64_t dst = ((int64_t)s_page[j] * p.stride_page + (int64_t)g * p.stride_head +
-                           (int64_t)(t & (p.P - 1)) * p.stride_token) * p.elem_size + (int64_t)v * 16;
-      *reinterpret_cast<uint4 *>(p.v_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_v + src));
-    }
-    if (p.q_rows) {
-      const int n_q = m * p.Hq * half_vecs;
-      for (int i = threadIdx.x; i < n_q; i += blockDim.x) {
-        const int v = i % half_vecs, jh = i / half_vecs, h = jh % p.Hq, j = jh / p.Hq;
-        const int t = L - m + j;
-        const int64_t at = (((int64_t)(q0 + j) * p.Hq + h) * p.D) * p.elem_size + (int64_t)v * 16;
-        const unsigned char *row = p.q_rows + at;
-        unsigned char *dst = p.q_out + at;
-        const int64_t half_bytes = (int64_t)(p.D >> 1) * p.elem_size;
-        uint4 lo = *reinterpret_cast<const uint4 *>(row);
-        uint4 hi = *reinterpret_cast<const uint4 *>(row + half_bytes);
-        if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(lo, hi, v * elems_per_vec, t, s_inv_freq);
-        else rope_vectors<float>(lo, hi, v * elems_per_vec, t, s_inv_freq);
-        *reinterpret_cast<uint4 *>(dst) = lo;
-        *reinterpret_cast<uint4 *>(dst + half_bytes) = hi;
+    if (p.q_rows)
+      for (int i = tid; i < n * p.Hq * half_vecs; i += kAppendThreads) {
+        const int v = i % half_vecs, jh = i / half_vecs, h = jh % p.Hq, row = jh / p.Hq;
+        const int64_t at = ((int64_t)(q0 + j0 + row) * p.Hq + h) * row_bytes + v * 16;
+        turn(p.q_rows + at, p.q_out + at, row, v);
       }
-    }
-    return;
   }
-  for (int i = threadIdx.x; i < n_vec; i += blockDim.x) {
-    const int v = i % vec_per_row, jg = i / vec_per_row, g = jg % p.Hkv, j = jg / p.Hkv;
-    const int t = L - m + j;
-    const int64_t src = (((int64_t)(q0 + j) * p.Hkv + g) * p.D) * p.elem_size + (int64_t)v * 16;
-    const int64_t dst = ((int64_t)s_page[j] * p.stride_page + (int64_t)g * p.stride_head +
-                         (int64_t)(t & (p.P - 1)) * p.stride_token) * p.elem_size + (int64_t)v * 16;
-    *reinterpret_cast<uint4 *>(p.k_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src));
+  for (int i = tid; i < n * p.Hkv * vecs; i += kAppendThreads) {
+    const int v = i % vecs, jg = i / vecs, g = jg % p.Hkv, row = jg / p.Hkv;
+    const int64_t src = ((int64_t)(q0 + j0 + row) * p.Hkv + g) * row_bytes + v * 16, dst = cache_at(row, g) + v * 16;
+    if (!rope) *reinterpret_cast<uint4 *>(p.k_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src));
     *reinterpret_cast<uint4 *>(p.v_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_v + src));
   }
 }

@@ -49,6 +49,11 @@ struct KvQuantParams {
   int32_t *dev_status;
   int32_t rope;
   double inv_freq[64];     // base^(-2i/D)
+  // positions of several axes (axes = 0: a row's position is its place in the request)
+  int32_t axes;
+  const int32_t *positions;
+  int64_t position_stride;
+  unsigned char axis_of[64];
 };
 
 // Eight elements of a row as they are stored, and as floats.  (Plain loads: query rows may be rotated in place, so they are
@@ -244,7 +249,25 @@ __global__ void __launch_bounds__(kQuantThreads, 2) kv_append_e4m3_kernel(const 
     const int pg = table[i];
     bad |= pg < 0 || pg >= p.num_pages;
   }
-  if (p.rope) {
+  // (ch, cl) and (sh, sl) of a token's pair
+  auto angle_at = [&](int tok, int pair) -> float * {
+    return s_cs + ((((tok * 4 + ((pair & 7) >> 1)) * 2) * kVecs + (pair >> 3)) << 2) + (pair & 1);
+  };
+  auto keep = [&](float *at, double c, double sn) {
+    const float ch = (float)c, sh = (float)sn;
+    at[0] = ch; at[2] = (float)(c - (double)ch);
+    at[4 * kVecs] = sh; at[4 * kVecs + 2] = (float)(sn - (double)sh);
+  };
+  if (p.rope && p.axes) {
+    const int t_lo = max(t0, t_new), n = min(t0 + tile_tokens, L) - t_lo;   // the tile's new tokens
+    for (int i = tid; i < n * (D / 2); i += kQuantThreads) {
+      const int pair = i % (D / 2), tok = t_lo - t0 + i / (D / 2);
+      const int at = p.positions[(int64_t)p.axis_of[pair] * p.position_stride + q0 + (t0 + tok - t_new)];
+      double c, sn;
+      sincos((double)at * p.inv_freq[pair], &sn, &c);
+      keep(angle_at(tok, pair), c, sn);
+    }
+  } else if (p.rope) {
     // angles in float64; a thread takes four tokens of a pair: one sine and cosine, and three turns by the pair's
     // frequency (each adds 2^-52)
     const int t_lo = max(t0, t_new), n = min(t0 + tile_tokens, L) - t_lo;   // the tile's new tokens
@@ -254,14 +277,10 @@ __global__ void __launch_bounds__(kQuantThreads, 2) kv_append_e4m3_kernel(const 
       double c, sn, cf, sf;
       sincos((double)(t0 + tok) * f, &sn, &c);
       sincos(f, &sf, &cf);
-      float *at = s_cs + ((((tok * 4 + ((pair & 7) >> 1)) * 2) * kVecs + (pair >> 3)) << 2) + (pair & 1);
+      float *at = angle_at(tok, pair);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        if (tok + u < t_lo - t0 + n) {
-          const float ch = (float)c, sh = (float)sn;
-          at[0] = ch; at[2] = (float)(c - (double)ch);
-          at[4 * kVecs] = sh; at[4 * kVecs + 2] = (float)(sn - (double)sh);
-        }
+        if (tok + u < t_lo - t0 + n) keep(at, c, sn);
         at += 4 * 2 * kVecs * 4;
         const double c2 = c * cf - sn * sf;
         sn = sn * cf + c * sf;

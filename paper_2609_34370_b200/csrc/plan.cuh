@@ -78,6 +78,11 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   const bool in_smem = p.batch <= kPlanSmemReqs;
   auto tile_prefix = [&](int i) -> int { return in_smem ? s_tp[i] : p.tile_prefix[i]; };
   auto valid_prefix = [&](int i) -> int { return in_smem ? s_vp[i] : p.valid_prefix[i]; };
+  auto first_tile = [&](int r) -> int {   // behind a shared prefix
+    if (!p.req_group) return 0;
+    const int u = p.req_group[r];
+    return u < 0 ? 0 : p.group_tiles[u];
+  };
   auto cost_prefix = [&](int i) -> int { return in_smem ? s_cp[i] : p.cost_prefix[i]; };  // per kv head
   const int tid = threadIdx.x;
   const int Hkv = p.Hkv;
@@ -98,8 +103,8 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
       const int m = q1 - q0;
       const bool ok = (m >= 1) && (m <= p.max_q_len) && (L >= m) &&
                       (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req &&
-                      (q0 >= 0) && (q1 <= p.total_q);
-      tiles = ok ? (L + kTileTokens - 1) / kTileTokens : 0;
+                      (q0 >= 0) && (q1 <= p.total_q) && (int64_t)first_tile(r) * kTileTokens <= (int64_t)L - m;
+      tiles = ok ? (L + kTileTokens - 1) / kTileTokens - first_tile(r) : 0;
       if (!ok) s_bad = 1;
       p.req_bad[r] = 0;
       if (in_smem) { s_q0[r] = q0; s_m[r] = m; s_L[r] = L; }
@@ -216,7 +221,8 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
     }
     // the pairs the combine kernel has work for: split ones, and those of invalid requests (sentinel rows)
     const bool listed = pair < n_pairs && nch != 1;
-    int off[2] = {nch > 1 ? nch : 0, listed ? 1 : 0};
+    const bool partial = nch > 1 || (p.req_group && nch == 1);   // behind a shared prefix every pair is joined with it
+    int off[2] = {partial ? nch : 0, listed ? 1 : 0};
     block_exclusive_scan_1024(off, s_scratch, s_total);
     const int part = off[0] + carry_p, lpos = off[1] + carry_l;
     carry_p += s_total[0]; carry_l += s_total[1];
@@ -229,8 +235,8 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
       p.combine_list[lpos] = ce;
     }
     if (pair < n_pairs) {
-      const bool split = nch > 1 && part + nch <= p.max_part_slots;
-      if (nch > 1 && !split) s_bad = 2;  // cannot happen: at most n_cta - 1 cuts, two slots each
+      const bool split = partial && part + nch <= p.max_part_slots;
+      if (partial && !split) s_bad = 2;  // cannot happen: at most n_cta - 1 cuts, two slots each
       p.pair_nchunks[pair] = nch;
       p.pair_part_base[pair] = split ? part : -1;
       if (nch > 0) {
@@ -238,11 +244,11 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
         e.req = r; e.g = g;
         if (in_smem) { e.q0 = s_q0[r]; e.m = s_m[r]; e.L = s_L[r]; }
         else { e.q0 = p.q_indptr[r]; e.m = p.q_indptr[r + 1] - e.q0; e.L = p.seq_lens[r]; }
-        const int vq = valid_prefix(r) * Hkv + g;
+        const int vq = valid_prefix(r) * Hkv + g, t0 = first_tile(r);
         for (int j = 0; j < nch; ++j) {
           const int c = c_first + j;
-          e.tile_begin = max(s_cut[c], b) - b;
-          e.tile_end = min(s_cut[c + 1], b + tiles) - b;
+          e.tile_begin = max(s_cut[c], b) - b + t0;
+          e.tile_end = min(s_cut[c + 1], b + tiles) - b + t0;
           e.part_slot = split ? part + j : -1;
           const int pos = s_off[c] + (vq - s_cut_vq[c]);
           if (pos >= 0 && pos < p.max_work) p.work[pos] = e;

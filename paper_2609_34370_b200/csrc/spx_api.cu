@@ -20,6 +20,8 @@
 #include "lookahead.cuh"
 #include "lm_head.cuh"
 #include "plan.cuh"
+#include "prompt_plan.cuh"
+#include "prompt_simt.cuh"
 #include "sampler.cuh"
 #include "logprob.cuh"
 #include "spx.h"
@@ -109,9 +111,16 @@ constexpr int kPlanSmCount = 148;  // workspace sizing must not depend on a devi
 // ---------------------------------------------------------------------------------------------
 // workspace layout
 // ---------------------------------------------------------------------------------------------
+// The plan and the partial results of the attention of many rows (prompts; the prefixes of groups).
+struct PromptWs {
+  size_t hdr, unit_item0, unit_bad, item_tiles, item_cost, entries, range_off, join, entry_part, req_group, group_tiles, req_flag, part_ml, part_o, total;
+  int32_t units, unit_rows, workers, max_items, max_entries, whole_slot0;
+  bool fits;
+};
 struct AttnWs {
-  size_t hdr, nchunks, part_base, combine_list, tile_prefix, valid_prefix, cost_prefix, cta_off, req_bad, work, part_ml, part_o, total;
+  size_t hdr, nchunks, part_base, combine_list, tile_prefix, valid_prefix, cost_prefix, cta_off, req_bad, work, part_ml, part_o, prefix, total;
   int32_t max_work, max_part_slots, rows_cap;
+  bool fits;
 };
 
 static int cache_elem_size(const spx_attn_args_t *a) {
@@ -134,9 +143,10 @@ static int log2_of(int x) {
   return n;
 }
 
-static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs) {
+// prompts: any number of rows a request
+static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs, bool prompts = false) {
   if (!a) return SPX_ERR_INVALID_ARG;
-  if (a->batch < 0 || a->total_q < a->batch || a->num_q_heads <= 0 || a->num_kv_heads <= 0 || a->head_dim <= 0 ||
+  if (a->batch < 0 || a->total_q < (prompts ? 0 : a->batch) || a->num_q_heads <= 0 || a->num_kv_heads <= 0 || a->head_dim <= 0 ||
       a->page_size <= 0 || a->num_pages < 0 || a->max_pages_per_req < 0 || a->max_q_len < 0)
     return SPX_ERR_INVALID_ARG;
   if (a->kv_dtype != SPX_BF16 && a->kv_dtype != SPX_F32) return SPX_ERR_INVALID_ARG;
@@ -144,12 +154,16 @@ static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs) {
   if (a->head_dim != 64 && a->head_dim != 128) return SPX_ERR_UNSUPPORTED;
   if (a->num_q_heads % a->num_kv_heads != 0) return SPX_ERR_UNSUPPORTED;
   if (a->page_size > 128 || (a->page_size & (a->page_size - 1)) != 0) return SPX_ERR_UNSUPPORTED;
-  const int max_q = a->max_q_len == 0 ? SPX_MAX_K + 1 : a->max_q_len;
+  const int max_q = prompts ? 1 : a->max_q_len == 0 ? SPX_MAX_K + 1 : a->max_q_len;
   if (max_q > SPX_MAX_K + 1) return SPX_ERR_UNSUPPORTED;
   if ((a->num_q_heads / a->num_kv_heads) * max_q > SPX_MAX_PACKED_ROWS) return SPX_ERR_UNSUPPORTED;
   if (a->kv_stride_page < 0 || a->kv_stride_head < 0 || a->kv_stride_token < a->head_dim) return SPX_ERR_INVALID_ARG;
   const spx_status_t cf = check_cache_format(a->cache_format, a->scale_block, a->page_size);
   if (cf != SPX_OK) return cf;
+  if (a->num_groups < 0) return SPX_ERR_INVALID_ARG;
+  if (prompts && a->num_groups > 0) return SPX_ERR_UNSUPPORTED;
+  if (need_ptrs && a->batch > 0 && a->num_groups > 0 && (!a->group_indptr || !a->prefix_lens)) return SPX_ERR_INVALID_ARG;
+  if (need_ptrs && prompts && a->total_q == 0) return SPX_OK;
   if (need_ptrs && a->batch > 0) {
     if (!a->q || !a->k_cache || !a->v_cache || !a->block_table || !a->seq_lens || !a->q_indptr || !a->out)
       return SPX_ERR_INVALID_ARG;
@@ -161,8 +175,45 @@ static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs) {
   return SPX_OK;
 }
 
+static bool use_tensor_core_path(const spx_attn_args_t *a);
+static bool prompt_tensor_cores(const spx_attn_args_t *a) { (void)a; return false; }
+
+static PromptWs prompt_ws_layout(const spx_attn_args_t *a) {
+  PromptWs w{};
+  const int G = a->num_q_heads / a->num_kv_heads;
+  const bool tc = prompt_tensor_cores(a), prefixes = a->num_groups > 0;
+  w.units = prefixes ? a->num_groups : a->batch;
+  w.unit_rows = tc ? 2 * (128 / G) * G : kPsRows;
+  w.workers = kPlanSmCount * (tc ? 1 : 2);
+  const int64_t items = (int64_t)a->total_q * G / w.unit_rows + w.units;
+  const int64_t slots = 2 * (int64_t)w.workers + (prefixes ? items * a->num_kv_heads : 0);
+  w.fits = items <= (1 << 22) && items * a->num_kv_heads <= 0x7fffffff && slots <= (1 << 24);
+  if (!w.fits) return w;
+  w.max_items = (int)items;
+  const int64_t ranged = items * a->num_kv_heads;
+  const int64_t entries = (ranged < kPromptMaxRanged ? ranged : kPromptMaxRanged) + w.workers;
+  w.max_entries = (int)(entries > items ? entries : items);
+  w.whole_slot0 = 2 * w.workers;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
+  w.hdr = take(sizeof(PromptHeader));
+  w.unit_item0 = take(4 * ((size_t)w.units + 1)); w.unit_bad = take(4 * (size_t)w.units);
+  w.item_tiles = take(4 * (size_t)items); w.item_cost = take(8 * ((size_t)items + 1));
+  w.entries = take(sizeof(PromptEntry) * (size_t)w.max_entries);
+  w.range_off = take(4 * ((size_t)w.workers + 1)); w.join = take(sizeof(PromptJoin) * (size_t)w.workers);
+  if (prefixes) {
+    w.entry_part = take(sizeof(int4) * (size_t)ranged);
+    w.req_group = take(4 * (size_t)a->batch); w.group_tiles = take(4 * (size_t)w.units); w.req_flag = take(4 * (size_t)a->batch);
+  }
+  w.part_ml = take(sizeof(float2) * (size_t)slots * w.unit_rows);
+  w.part_o = take(sizeof(float) * (size_t)slots * w.unit_rows * a->head_dim);
+  w.total = off;
+  return w;
+}
+
 static AttnWs attn_ws_layout(const spx_attn_args_t *a) {
   AttnWs w{};
+  w.fits = true;
   const int max_q = a->max_q_len == 0 ? SPX_MAX_K + 1 : a->max_q_len;
   const int G = a->num_q_heads / a->num_kv_heads;
   w.rows_cap = G * max_q;
@@ -170,7 +221,7 @@ static AttnWs attn_ws_layout(const spx_attn_args_t *a) {
   // one chunk to a pair, so the split pairs have at most two chunks per cut between them
   const size_t pairs = (size_t)a->batch * a->num_kv_heads;
   w.max_work = (int)(pairs + kPlanSmCount + 1);
-  w.max_part_slots = 2 * kPlanSmCount;
+  w.max_part_slots = 2 * kPlanSmCount + (a->num_groups > 0 ? (int)pairs : 0);   // (behind a shared prefix every pair has one)
   size_t off = 0;
   w.hdr = off; off = align_up(off + sizeof(PlanHeader), 256);
   w.nchunks = off; off = align_up(off + sizeof(int32_t) * pairs, 256);
@@ -185,6 +236,11 @@ static AttnWs attn_ws_layout(const spx_attn_args_t *a) {
   const size_t slots = (size_t)w.max_part_slots;
   w.part_ml = off; off = align_up(off + sizeof(float2) * slots * w.rows_cap, 256);
   w.part_o = off; off = align_up(off + sizeof(float) * slots * w.rows_cap * a->head_dim, 256);
+  if (a->num_groups > 0) {
+    const PromptWs pw = prompt_ws_layout(a);
+    w.fits = pw.fits;
+    w.prefix = off; off = align_up(off + pw.total, 256);
+  }
   w.total = off;
   return w;
 }
@@ -391,10 +447,91 @@ constexpr int kPlanEntryCostE4m3 = 14;
 enum { kPhasePlan = 1, kPhaseMain = 2, kPhaseAll = 3 };                        // attention: planner, kernels behind it
 enum { kPhaseStats = 1, kPhaseTail = 2, kPhaseFilter = 4, kPhaseSampAll = 7 };  // sampling: statistics, top-k / top-p thresholds, the rest
 
+static PromptParams prompt_params(const spx_attn_args_t *a, const PromptWs &w, unsigned char *ws, int32_t *dev_status, const DeviceInfo &dev) {
+  PromptParams p{};
+  p.batch = a->batch; p.total_q = a->total_q;
+  p.Hq = a->num_q_heads; p.Hkv = a->num_kv_heads; p.G = p.Hq / p.Hkv; p.D = a->head_dim; p.P = a->page_size; p.log2P = log2_of(p.P);
+  p.num_pages = a->num_pages; p.max_pages_per_req = a->max_pages_per_req;
+  p.scale_log2 = (a->sm_scale == 0.f ? 1.f / sqrtf((float)a->head_dim) : a->sm_scale) * kLog2e;
+  p.q = a->q; p.k_cache = a->k_cache; p.v_cache = a->v_cache;
+  p.stride_page = a->kv_stride_page; p.stride_head = a->kv_stride_head; p.stride_token = a->kv_stride_token;
+  p.block_table = a->block_table; p.seq_lens = a->seq_lens; p.q_indptr = a->q_indptr;
+  p.out = a->out; p.lse = a->lse;
+  if (a->cache_format == SPX_CACHE_E4M3) { p.k_scales = a->k_scales; p.v_scales = a->v_scales; p.log2SB = log2_of(a->scale_block); }
+  p.head_inner = a->kv_stride_head < a->kv_stride_token ? 1 : 0;
+  p.dev_status = dev_status;
+  p.groups = a->num_groups; p.group_indptr = a->group_indptr; p.prefix_lens = a->prefix_lens;
+  p.req_group = reinterpret_cast<int32_t *>(ws + w.req_group);
+  p.group_tiles = reinterpret_cast<int32_t *>(ws + w.group_tiles);
+  p.req_flag = reinterpret_cast<int32_t *>(ws + w.req_flag);
+  p.units = w.units; p.unit_rows = w.unit_rows;
+  const bool tc = prompt_tensor_cores(a);
+  const int sms = dev.num_sms < kPlanSmCount ? dev.num_sms : kPlanSmCount;
+  p.workers = sms * (tc ? 1 : 2);
+  // tiles: of 128 tokens by 64 rows in fp32 arithmetic (10 us), by 256 rows on the tensor cores (1.5 us)
+  p.min_range = tc ? 4 : 1;
+  p.overhead = tc ? 8 : 2;
+  p.hdr = reinterpret_cast<PromptHeader *>(ws + w.hdr);
+  p.unit_item0 = reinterpret_cast<int32_t *>(ws + w.unit_item0);
+  p.unit_bad = reinterpret_cast<int32_t *>(ws + w.unit_bad);
+  p.item_tiles = reinterpret_cast<int32_t *>(ws + w.item_tiles);
+  p.item_cost = reinterpret_cast<int64_t *>(ws + w.item_cost);
+  p.entries = reinterpret_cast<PromptEntry *>(ws + w.entries);
+  p.range_off = reinterpret_cast<int32_t *>(ws + w.range_off);
+  p.join = reinterpret_cast<PromptJoin *>(ws + w.join);
+  p.entry_part = reinterpret_cast<int4 *>(ws + w.entry_part);
+  p.max_items = w.max_items; p.max_entries = w.max_entries; p.whole_slot0 = w.whole_slot0;
+  p.part_ml = reinterpret_cast<float2 *>(ws + w.part_ml);
+  p.part_o = reinterpret_cast<float *>(ws + w.part_o);
+  return p;
+}
+
+// The attention kernel of a plan by prompt_plan_kernel, directly behind it or another kernel that ran to its end behind it.
+static cudaError_t launch_prompt_main(const spx_attn_args_t *a, const PromptParams &p, cudaStream_t stream, const DeviceInfo &dev) {
+  auto launch = [&](auto rows, auto pool, auto dim) -> cudaError_t {
+    using T = decltype(rows);
+    using KV = decltype(pool);
+    constexpr int D = decltype(dim)::value;
+    auto kernel = prompt_simt_kernel<T, KV, D>;
+    static SmemOnce limit;
+    const cudaError_t e = limit.raise(kernel, kPsSmem<D>, dev.device);
+    if (e != cudaSuccess) return e;
+    ++t_launches;
+    return launch_pdl(kernel, dim3(p.workers), dim3(kPsThreads), kPsSmem<D>, stream, p);
+  };
+  auto launch_dim = [&](auto rows, auto pool) -> cudaError_t {
+    return p.D == 64 ? launch(rows, pool, std::integral_constant<int, 64>()) : launch(rows, pool, std::integral_constant<int, 128>());
+  };
+  const bool e4m3 = a->cache_format == SPX_CACHE_E4M3;
+  if (a->kv_dtype == SPX_F32) return e4m3 ? launch_dim(float(), (unsigned char)0) : launch_dim(float(), float());
+  return e4m3 ? launch_dim(__nv_bfloat16(), (unsigned char)0) : launch_dim(__nv_bfloat16(), __nv_bfloat16());
+}
+
+static spx_status_t launch_prompts(const spx_attn_args_t *a, const PromptWs &w, unsigned char *ws, int32_t *dev_status, cudaStream_t stream,
+                                   const DeviceInfo &dev) {
+  if (a->batch == 0 || a->total_q == 0) return SPX_OK;
+  const PromptParams p = prompt_params(a, w, ws, dev_status, dev);
+  prompt_plan_kernel<<<1, 1024, 0, stream>>>(p);
+  ++t_launches;
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return SPX_ERR_CUDA;
+  e = launch_prompt_main(a, p, stream, dev);
+  if (e != cudaSuccess) return SPX_ERR_CUDA;
+  const dim3 grid(64, (p.unit_rows * (p.D / 4) + 255) / 256);
+  e = a->kv_dtype == SPX_F32 ? launch_pdl(prompt_join_kernel<float>, grid, dim3(256), 0, stream, p)
+                             : launch_pdl(prompt_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, stream, p);
+  ++t_launches;
+  return e == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
+}
+
 static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws, int32_t *dev_status,
                                      cudaStream_t stream, const DeviceInfo &dev, int phases = kPhaseAll) {
   if (a->batch == 0) return SPX_OK;
   const AttnWs w = attn_ws_layout(a);
+  if (!w.fits) return SPX_ERR_UNSUPPORTED;
+  const bool grouped = a->num_groups > 0;
+  PromptParams pre{};
+  if (grouped) pre = prompt_params(a, prompt_ws_layout(a), ws + w.prefix, dev_status, dev);
   AttnParams p{};
   p.batch = a->batch; p.total_q = a->total_q;
   p.max_q_len = a->max_q_len == 0 ? SPX_MAX_K + 1 : a->max_q_len;
@@ -437,7 +574,12 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
 
   // one range of the plan per CTA of the persistent kernels, never more than the workspace was sized for
   const int sms = dev.num_sms < kPlanSmCount ? dev.num_sms : kPlanSmCount;
+  if (grouped) { p.req_group = pre.req_group; p.group_tiles = pre.group_tiles; }
   if (phases & kPhasePlan) {
+    if (grouped) {
+      prompt_plan_kernel<<<1 + (a->batch < 1024 ? a->batch : 1024), 1024, 0, stream>>>(pre);
+      ++t_launches;
+    }
     plan_kernel<<<1, 1024, 0, stream>>>(p, sms);
     ++t_launches;
     if (cudaGetLastError() != cudaSuccess) return SPX_ERR_CUDA;
@@ -445,6 +587,8 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
   if (!(phases & kPhaseMain)) return SPX_OK;
 
   cudaError_t e;
+  // the prefixes first (a kernel behind this one that comes up early waits for it, and so for the plans)
+  if (grouped && launch_prompt_main(a, pre, stream, dev) != cudaSuccess) return SPX_ERR_CUDA;
   if (use_tensor_core_path(a)) {
     p.head_inner = a->kv_stride_head < a->kv_stride_token ? 1 : 0;
     CUtensorMap kmap, vmap;
@@ -514,6 +658,14 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
       e = a->kv_dtype == SPX_F32 ? launch_dim(float(), launch_simt_kv) : launch_dim(__nv_bfloat16(), launch_simt_kv);
   }
   if (e != cudaSuccess) return SPX_ERR_CUDA;
+  if (grouped) {
+    const int64_t items = (int64_t)p.max_q_len * p.Hq * (p.D / 4);
+    const dim3 grid(p.batch, (unsigned)((items + 255) / 256));
+    e = a->kv_dtype == SPX_F32 ? launch_pdl(prefix_join_kernel<float>, grid, dim3(256), 0, stream, p, pre)
+                               : launch_pdl(prefix_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, stream, p, pre);
+    ++t_launches;
+    return e == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
+  }
   // one row of blocks per listed pair on the named workloads (a cut of the tile axis lists at most one
   // pair); longer lists - many invalid requests - are walked
   const int pairs_all = p.batch * p.Hkv;
@@ -649,7 +801,9 @@ size_t spx_workspace_size(const spx_attn_args_t *attn, const spx_sample_args_t *
   size_t total = 0;
   if (attn) {
     if (check_attn(attn, false) != SPX_OK) return 0;
-    total += attn_ws_layout(attn).total;
+    const AttnWs w = attn_ws_layout(attn);
+    if (!w.fits) return 0;
+    total += w.total;
   }
   if (sample) {
     if (check_sample(sample, false) != SPX_OK) return 0;
@@ -668,6 +822,25 @@ spx_status_t spx_verify_attention(const spx_attn_args_t *args, void *ws, size_t 
   DeviceInfo dev;
   if (!get_device_info(&dev) || dev.cc_major < 10) return SPX_ERR_CUDA;
   return launch_attention(args, static_cast<unsigned char *>(ws), dev_status, static_cast<cudaStream_t>(cuda_stream), dev);
+}
+
+size_t spx_prompt_workspace_size(const spx_attn_args_t *args) {
+  if (check_attn(args, false, true) != SPX_OK) return 0;
+  const PromptWs w = prompt_ws_layout(args);
+  return w.fits ? w.total : 0;
+}
+
+spx_status_t spx_prompt_attention(const spx_attn_args_t *args, void *ws, size_t ws_bytes, int32_t *dev_status, void *cuda_stream) {
+  t_launches = 0;
+  spx_status_t st = check_attn(args, true, true);
+  if (st != SPX_OK) return st;
+  const PromptWs w = prompt_ws_layout(args);
+  if (!w.fits) return SPX_ERR_UNSUPPORTED;
+  st = check_ws(ws, ws_bytes, w.total, dev_status);
+  if (st != SPX_OK) return st;
+  DeviceInfo dev;
+  if (!get_device_info(&dev) || dev.cc_major < 10) return SPX_ERR_CUDA;
+  return launch_prompts(args, w, static_cast<unsigned char *>(ws), dev_status, static_cast<cudaStream_t>(cuda_stream), dev);
 }
 
 spx_status_t spx_rejection_sample(const spx_sample_args_t *args, void *ws, size_t ws_bytes, int32_t *dev_status,
@@ -742,7 +915,7 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
 // ---- host-buffer convenience ---------------------------------------------------------------
 namespace {
 struct HostStepLayout {
-  size_t q, k, v, ks, vs, bt, sl, qi, out, lse, tl, dl, ids, ua, us, tau, topk, topp, acc, tok, status, ws, total;
+  size_t q, k, v, ks, vs, bt, sl, qi, gi, pl, out, lse, tl, dl, ids, ua, us, tau, topk, topp, acc, tok, status, ws, total;
   size_t q_bytes, kv_bytes, scale_bytes, bt_bytes, out_bytes, lse_bytes, tl_bytes, dl_bytes, ws_bytes;
 };
 HostStepLayout host_layout(const spx_attn_args_t *a, const spx_sample_args_t *s, int64_t kv_pool_elems) {
@@ -762,7 +935,9 @@ HostStepLayout host_layout(const spx_attn_args_t *a, const spx_sample_args_t *s,
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
   L.q = take(L.q_bytes); L.k = take(L.kv_bytes); L.v = take(L.kv_bytes);
   L.ks = take(L.scale_bytes); L.vs = take(L.scale_bytes); L.bt = take(L.bt_bytes);
-  L.sl = take(B * 4); L.qi = take((B + 1) * 4); L.out = take(L.out_bytes); L.lse = take(L.lse_bytes);
+  L.sl = take(B * 4); L.qi = take((B + 1) * 4);
+  L.gi = take(a->num_groups > 0 ? ((size_t)a->num_groups + 1) * 4 : 0); L.pl = take((size_t)a->num_groups * 4);
+  L.out = take(L.out_bytes); L.lse = take(L.lse_bytes);
   L.tl = take(L.tl_bytes); L.dl = take(L.dl_bytes); L.ids = take(TD * 4); L.ua = take(TD * 4); L.us = take(B * 4);
   L.tau = take(s->temperature ? B * 4 : 0); L.topk = take(s->top_k ? B * 4 : 0); L.topp = take(s->top_p ? B * 4 : 0);
   L.acc = take(B * 4); L.tok = take(TQ * 4); L.status = take(4); L.ws = take(L.ws_bytes);
@@ -798,6 +973,7 @@ spx_status_t spx_verify_step_host(const spx_attn_args_t *attn, const spx_sample_
   h2d(L.q, attn->q, L.q_bytes); h2d(L.k, attn->k_cache, L.kv_bytes); h2d(L.v, attn->v_cache, L.kv_bytes);
   h2d(L.ks, attn->k_scales, L.scale_bytes); h2d(L.vs, attn->v_scales, L.scale_bytes);
   h2d(L.bt, attn->block_table, L.bt_bytes); h2d(L.sl, attn->seq_lens, B * 4); h2d(L.qi, attn->q_indptr, (B + 1) * 4);
+  if (attn->num_groups > 0) { h2d(L.gi, attn->group_indptr, ((size_t)attn->num_groups + 1) * 4); h2d(L.pl, attn->prefix_lens, (size_t)attn->num_groups * 4); }
   h2d(L.tl, sample->target_logits, L.tl_bytes); h2d(L.dl, sample->draft_logits, L.dl_bytes);
   h2d(L.ids, sample->draft_token_ids, TD * 4); h2d(L.ua, sample->u_accept, TD * 4); h2d(L.us, sample->u_sample, B * 4);
   h2d(L.tau, sample->temperature, B * 4); h2d(L.topk, sample->top_k, B * 4); h2d(L.topp, sample->top_p, B * 4);
@@ -809,6 +985,8 @@ spx_status_t spx_verify_step_host(const spx_attn_args_t *attn, const spx_sample_
   a.k_scales = attn->k_scales ? reinterpret_cast<float *>(d + L.ks) : nullptr;
   a.v_scales = attn->v_scales ? reinterpret_cast<float *>(d + L.vs) : nullptr;
   a.block_table = reinterpret_cast<int32_t *>(d + L.bt); a.seq_lens = reinterpret_cast<int32_t *>(d + L.sl);
+  a.group_indptr = attn->group_indptr ? reinterpret_cast<int32_t *>(d + L.gi) : nullptr;
+  a.prefix_lens = attn->prefix_lens ? reinterpret_cast<int32_t *>(d + L.pl) : nullptr;
   a.q_indptr = reinterpret_cast<int32_t *>(d + L.qi); a.out = d + L.out;
   a.lse = attn->lse ? reinterpret_cast<float *>(d + L.lse) : nullptr;
   s.target_logits = d + L.tl; s.draft_logits = d + L.dl; s.draft_token_ids = reinterpret_cast<int32_t *>(d + L.ids);
@@ -827,6 +1005,37 @@ spx_status_t spx_verify_step_host(const spx_attn_args_t *attn, const spx_sample_
 }
 
 // ---- cache maintenance ------------------------------------------------------------------------
+// Positions of several axes: the fields' check, and the axis of each pair.
+static spx_status_t check_axes(const spx_kv_append_args_t *a, bool need_ptrs) {
+  if (a->rope_axes == 0) return SPX_OK;
+  if (a->rope_axes < 0 || !(a->rope_base > 0.f)) return SPX_ERR_INVALID_ARG;
+  if (a->rope_axes > SPX_MAX_ROPE_AXES) return SPX_ERR_UNSUPPORTED;
+  if (a->rope_interleaved != 0 && a->rope_interleaved != 1) return SPX_ERR_INVALID_ARG;
+  int64_t sum = 0;
+  for (int i = 0; i < a->rope_axes; ++i) {
+    if (a->rope_sections[i] < 0) return SPX_ERR_INVALID_ARG;
+    sum += a->rope_sections[i];
+    if (a->rope_interleaved && i > 0 && a->rope_sections[i] > 0 &&
+        i + (int64_t)a->rope_axes * (a->rope_sections[i] - 1) >= a->head_dim / 2)
+      return SPX_ERR_INVALID_ARG;
+  }
+  if (sum != a->head_dim / 2) return SPX_ERR_INVALID_ARG;
+  if (need_ptrs && (!a->positions || ((uintptr_t)a->positions & 3) || a->position_stride < a->total_q)) return SPX_ERR_INVALID_ARG;
+  return SPX_OK;
+}
+static void fill_axes(const spx_kv_append_args_t *a, unsigned char *axis_of) {
+  int axis = 0, end = a->rope_sections[0];
+  for (int i = 0; i < a->head_dim / 2; ++i) {
+    if (a->rope_interleaved) {
+      axis = i % a->rope_axes;
+      if (i >= (int64_t)a->rope_axes * a->rope_sections[axis]) axis = 0;
+    } else {
+      while (i >= end) end += a->rope_sections[++axis];
+    }
+    axis_of[i] = (unsigned char)axis;
+  }
+}
+
 static spx_status_t launch_append_e4m3(const spx_kv_append_args_t *a, int32_t *dev_status, cudaStream_t stream) {
   if (!scales_ok(a->k_scales, a->v_scales)) return SPX_ERR_INVALID_ARG;
   DeviceInfo dev;
@@ -842,6 +1051,10 @@ static spx_status_t launch_append_e4m3(const spx_kv_append_args_t *a, int32_t *d
   p.rope = a->rope_base > 0.f;
   p.q_in = p.rope ? a->q_rows : nullptr;
   p.q_out = a->q_out ? a->q_out : a->q_rows;
+  if (a->rope_axes > 0) {
+    p.axes = a->rope_axes; p.positions = a->positions; p.position_stride = a->position_stride;
+    fill_axes(a, p.axis_of);
+  }
   if (p.rope) {
     // base^(-2i/D) as a product of two of twelve to sixteen powers: a call of pow for each was 2 us of the host's time
     double fine[8];
@@ -901,6 +1114,8 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
   if (rope && a->q_rows && a->num_q_heads <= 0) return SPX_ERR_INVALID_ARG;
   if (a->q_out && !(rope && a->q_rows)) return SPX_ERR_INVALID_ARG;   // nothing would be written to it
   if (e4m3 && (a->page_size > 128 || (a->head_dim != 64 && a->head_dim != 128))) return SPX_ERR_UNSUPPORTED;
+  const spx_status_t ax = check_axes(a, a->batch > 0);
+  if (ax != SPX_OK) return ax;
   if (a->batch == 0) return SPX_OK;
   if (!a->new_k || !a->new_v || !a->k_cache || !a->v_cache || !a->block_table || !a->seq_lens || !a->q_indptr)
     return SPX_ERR_INVALID_ARG;
@@ -926,7 +1141,15 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
   p.q_rows = rope ? static_cast<unsigned char *>(a->q_rows) : nullptr;
   p.q_out = a->q_out ? static_cast<unsigned char *>(a->q_out) : p.q_rows;
   p.Hq = a->num_q_heads;
-  kv_append_kernel<<<a->batch, 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+  if (a->rope_axes > 0) {
+    p.axes = a->rope_axes; p.positions = a->positions; p.position_stride = a->position_stride;
+    fill_axes(a, p.axis_of);
+  }
+  p.log2_rows = log2_of(kAppendRows);
+  while (rope && (a->head_dim / 2) << p.log2_rows > kAppendAngles) --p.log2_rows;
+  const int64_t blocks = ((int64_t)a->total_q >> p.log2_rows) + a->batch;
+  if (blocks > 0x7fffffff) return SPX_ERR_UNSUPPORTED;
+  kv_append_kernel<<<(unsigned)blocks, kAppendThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
   ++t_launches;
   return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
 }
