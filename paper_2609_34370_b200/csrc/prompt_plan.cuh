@@ -48,6 +48,10 @@ struct __align__(16) PromptJoin {
   int32_t g, first, next, nch;
 };
 
+// Elements of a V row that are not finite, by column: infinities of either sign, NaN in both (prompt_tc.cuh).
+struct __align__(16) PromptNote { uint32_t plus[4], minus[4]; int32_t token, pad[3]; };
+constexpr int kPtNotes = 256;      // noted tokens of an item: those its rows do not all see, one per position at most
+
 struct PromptParams {
   int32_t batch, total_q, Hq, Hkv, G, D, P, log2P, num_pages, max_pages_per_req;
   float scale_log2;
@@ -84,6 +88,7 @@ struct PromptParams {
   int32_t max_items, max_entries, whole_slot0;
   float *part_o;                      // [slot][unit_rows][D]
   float2 *part_ml;                    // [slot][unit_rows]  (m in log2 units, l)
+  PromptNote *notes;                  // [workers][2][kPtNotes]  (tensor-core kernel)
 };
 
 // Exclusive scan over the 1024 threads of a block; total in every thread.  scratch: 33 values of shared memory.

@@ -1,0 +1,541 @@
+// Attention of many query rows on the 5th-generation tensor cores (tcgen05 + TMEM), fed by TMA page gathers.
+//
+// An item is up to 256 packed rows of one kv head: two groups of 128 rows, the M of a score and a value MMA, that share every K and
+// V tile.  One persistent CTA per SM, warp-specialised:
+//   warps 0-3, 4-7  softmax of group 0 and 1: a thread holds one row's 128 scores of a tile in registers (one read
+//                   of tensor memory, no exchange between threads), keeps the row's maximum and sum, and writes
+//                   its weights over the scores as bf16, the A operand of the value MMA;
+//   warp 8          producer: takes entries of the plan, copies query rows, and K and V tiles, page by page, into a ring;
+//   warp 9          issuer.  While one group is at its softmax the other's MMAs run: S0 S1 | V0 S0' | V1 S1' | ...
+//   warps 10, 11    look after the V tiles at the edge of what rows see (below).
+// Tensor memory is full: two score buffers of 128 columns and two outputs of D.
+//
+// The running maximum of a row is a reference that moves only when a tile's maximum passes it by 2^8 (the output
+// is then rescaled by the row's own thread; the score MMA of a tile completes behind the value MMA of the one before, so the
+// output is at rest).  Weights are rounded to bf16 (half a step of 2^-8 each, the type V has to be multiplied in); their sum is
+// taken in fp32 before that.
+//
+// What rows do not see must not reach them.  Scores are masked before the maximum.  A weight of zero does not
+// mask an infinity or a NaN in V, so in the tiles at the edge (some row of the item does not see all of them) V is
+// looked through: rows past the last one seen become zero, and elements that are not finite become zero and are noted; the rows that
+// do see one get it (an infinity of its sign, NaN otherwise) at the end.
+#pragma once
+#include "attn_e4m3.cuh"
+#include "attn_tc.cuh"
+#include "attn_tc4.cuh"
+#include "prompt_plan.cuh"
+
+namespace spx {
+
+constexpr int kPtThreads = 384;
+constexpr int kPtRegsSoftmax = 216, kPtRegsOther = 72;   // 2 * 128 * 216 + 128 * 72 = 384 * 168
+
+template <int D>
+struct PtCfg {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kHalfBytes = 128 * 128;             // 128 rows of 64 elements: a half of a tile, or of a group's query rows
+  static constexpr int kTileBytes = kHalves * kHalfBytes;
+  static constexpr int kSlots = D == 128 ? 5 : 8;
+  static constexpr int kOffKv = 2 * kTileBytes;            // behind the query rows of the two groups
+  static constexpr int kOffBar = kOffKv + kSlots * kTileBytes;
+  static constexpr int kSmemBytes = kOffBar + 1024 + 1024;
+  static_assert(kSmemBytes <= 232448, "shared memory");
+  static constexpr int kColS = 0, kColO = 256;             // group x: S at 128 x, O at 256 + D x
+};
+
+struct PtBars {
+  uint64_t kv_full[8], kv_empty[8], q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_free[2], item_full[2], item_empty[2], v_ask, v_clean, item_clean[2];
+  PromptEntry item[2];
+  int32_t notes[2];
+  uint32_t tmem_base;
+  volatile int32_t abort;
+  int32_t *dev_status;
+};
+static_assert(sizeof(PtBars) <= 1024, "barrier area");
+
+namespace pt {
+
+using namespace tc;
+using e8::add2;
+using e8::arrive;
+using e8::commit;
+using e8::elect_lane;
+using e8::expect_tx;
+using e8::fma2;
+using e8::pair;
+using e8::try_wait;
+using e8::try_wait_long;
+using e8::unpair;
+
+// Bounded wait of a converged warp; the outcome is told by the abort flag alone, which every role's loop looks at once a tile.
+// (In line: a call's convention and a split of the registers among the warps do not go together.)
+__device__ __forceinline__ void wait(uint64_t *b, uint32_t parity, PtBars *bars) {
+  const uint32_t bar = smem_u32(b);
+  if (__all_sync(0xffffffffu, try_wait(bar, parity & 1))) return;
+  const long long t0 = clock64();
+#pragma unroll 1
+  while (!__all_sync(0xffffffffu, try_wait_long(bar, parity & 1))) {
+    const bool late = clock64() - t0 > kWaitLimitCycles;
+    if (late) {
+      bars->abort = 1;
+      atomicOr(bars->dev_status, SPX_DEV_TIMEOUT);
+    }
+    if (__any_sync(0xffffffffu, late || bars->abort)) return;
+  }
+}
+// one arrival for the warp, behind what its lanes did
+__device__ __forceinline__ void warp_arrive(uint64_t *b, int lane) {
+  __syncwarp();
+  if (lane == 0) arrive(smem_u32(b));
+}
+
+}  // namespace pt
+
+template <int D>
+__global__ void __launch_bounds__(kPtThreads, 1)
+prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap,
+                 PromptParams p) {
+  using Cfg = PtCfg<D>;
+  using namespace pt;
+  extern __shared__ __align__(1024) unsigned char smem_dyn[];
+  unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
+  unsigned char *sQ = smem, *sKv = smem + Cfg::kOffKv;
+  PtBars *bars = reinterpret_cast<PtBars *>(smem + Cfg::kOffBar);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+#pragma unroll 1
+    for (int s = 0; s < 8; ++s) { mbar_init(&bars->kv_full[s], 1); mbar_init(&bars->kv_empty[s], 1); }
+#pragma unroll 1
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&bars->q_full[b], 1); mbar_init(&bars->q_empty[b], 1); mbar_init(&bars->s_full[b], 1); mbar_init(&bars->p_full[b], 4);
+      mbar_init(&bars->o_full[b], 1); mbar_init(&bars->o_free[b], 4);
+      mbar_init(&bars->item_full[b], 1); mbar_init(&bars->item_empty[b], 11);   // eight softmax warps, issuer, two edge warps
+      mbar_init(&bars->item_clean[b], 2);
+      bars->notes[b] = 0;
+    }
+    mbar_init(&bars->v_ask, 1); mbar_init(&bars->v_clean, 2);
+    bars->abort = 0;
+    bars->dev_status = p.dev_status;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = bars->tmem_base;
+  // everything above touched only this CTA's own resources; the plan, and what the caller's kernels before it wrote, is read from here on
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  const bool causal = p.groups == 0;
+  const int half_rows = p.unit_rows >> 1;    // packed rows of a group: whole positions, at most 128
+  // first tile of an entry in which some of its rows do not see every token
+  auto edge_tile = [&](const PromptEntry &e) -> int {
+    return causal ? max(e.tile_begin, min(e.tile_end, (e.vis0 + e.row0 / p.G + 1) / kTileTokens)) : e.tile_end;
+  };
+  // The entry of item n for the roles that follow the producer: false when there is none, or another role gave up.
+  auto next_item = [&](uint32_t n, PromptEntry &e) -> bool {
+    wait(&bars->item_full[n & 1], n >> 1, bars);
+    e = bars->item[n & 1];
+    return e.unit >= 0 && !bars->abort;
+  };
+
+  if (warp >= 8) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPtRegsOther));
+  if (warp == 8) {
+    // ------------------------------------------------------------------ producer
+    const int n_units = p.hdr->n_units, ranged = p.hdr->ranged;
+    const int pages_per_tile = kTileTokens >> p.log2P, tiles_per_group = 32 / pages_per_tile;
+    uint32_t n_item = 0, n_kv = 0, n_q[2] = {0, 0};
+    auto take = [&]() -> int {
+      int u = 0;
+      if (lane == 0) u = atomicAdd(&p.hdr->counter, 1);
+      return u;
+    };
+    int unit_next = take();
+    for (;;) {
+      const int unit = __shfl_sync(0xffffffffu, unit_next, 0);
+      if (unit >= n_units || bars->abort) break;
+      unit_next = take();    // in flight until this one is done
+      const int e0 = ranged ? p.range_off[unit] : unit / p.Hkv, e1 = ranged ? p.range_off[unit + 1] : e0 + 1;
+#pragma unroll 1
+      for (int ei = e0; ei < e1; ++ei, ++n_item) {
+        PromptEntry e = p.entries[ei];
+        if (!ranged) {
+          e.g = unit % p.Hkv;
+          if (e.slot >= 0) e.slot += e.g;
+        }
+        wait(&bars->item_empty[n_item & 1], (n_item >> 1) ^ 1, bars);
+        if (lane == 0) { bars->item[n_item & 1] = e; bars->notes[n_item & 1] = 0; }
+        warp_arrive(&bars->item_full[n_item & 1], lane);
+        const int32_t *table = p.block_table + (int64_t)e.table_row * p.max_pages_per_req;
+        const int t_end = min(e.t_end, e.tile_end * kTileTokens);
+        // page ids of a group of tiles, a lane's (tile, page) each, one group ahead of the copies
+        auto pages_of = [&](int tile0) -> int {
+          const int tile = tile0 + lane / pages_per_tile, t = tile * kTileTokens + (lane % pages_per_tile) * p.P;
+          return tile < e.tile_end && t < t_end ? table[t >> p.log2P] : 0;
+        };
+        int page_next = pages_of(e.tile_begin);
+        for (int x = 0; x < 2; ++x) {
+          if (x * half_rows >= e.rows) break;
+          wait(&bars->q_empty[x], n_q[x] ^ 1, bars);
+          if (elect_lane()) {
+            const uint32_t bar = smem_u32(&bars->q_full[x]);
+            expect_tx(bar, (uint32_t)p.box_rows * p.G * D * 2);
+#pragma unroll
+            for (int h = 0; h < Cfg::kHalves; ++h)
+              tma_load_3d(smem_u32(sQ + x * Cfg::kTileBytes + h * Cfg::kHalfBytes), &qmap, &bars->q_full[x], h * 64, e.g * p.G,
+                          e.q0 + (e.row0 + x * half_rows) / p.G);
+          }
+          __syncwarp();
+          ++n_q[x];
+        }
+        int page = 0, tile0 = e.tile_begin;
+#pragma unroll 1
+        for (int tile = e.tile_begin; tile < e.tile_end; ++tile) {
+          if (tile == tile0) {
+            page = page_next;
+            tile0 += tiles_per_group;
+            page_next = pages_of(tile0);
+            if (page < 0 || page >= p.num_pages) {
+              page = 0;    // keep the copy in bounds; the request is flagged and its rows are voided
+              atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
+              p.unit_bad[e.unit] = 1;
+              p.hdr->any_bad = 1;
+            }
+          }
+          const int my_page = __shfl_sync(0xffffffffu, page, ((tile - tile0 + tiles_per_group) * pages_per_tile + lane) & 31);
+          const int npages = (min(kTileTokens, t_end - tile * kTileTokens) + p.P - 1) >> p.log2P;
+#pragma unroll
+          for (int v = 0; v < 2; ++v, ++n_kv) {
+            const uint32_t slot = n_kv % Cfg::kSlots;
+            wait(&bars->kv_empty[slot], n_kv / Cfg::kSlots ^ 1, bars);
+            if (lane == 0) expect_tx(smem_u32(&bars->kv_full[slot]), (uint32_t)npages * p.P * D * 2);
+            __syncwarp();
+            if (lane < npages) {
+#pragma unroll
+              for (int h = 0; h < Cfg::kHalves; ++h)
+                tma_load_4d(smem_u32(sKv + slot * Cfg::kTileBytes + h * Cfg::kHalfBytes + lane * p.P * 128), v ? &vmap : &kmap, &bars->kv_full[slot], h * 64,
+                            p.head_inner ? e.g : 0, p.head_inner ? 0 : e.g, my_page);
+            }
+            __syncwarp();
+          }
+          if (bars->abort) break;
+        }
+      }
+    }
+    // no more: an entry of no unit
+    wait(&bars->item_empty[n_item & 1], (n_item >> 1) ^ 1, bars);
+    if (lane == 0) bars->item[n_item & 1].unit = -1;
+    warp_arrive(&bars->item_full[n_item & 1], lane);
+  } else if (warp == 9) {
+    // ------------------------------------------------------------------ issuer
+    constexpr uint32_t kIdescQK = idesc(kTileTokens, false), kIdescPV = idesc(D, true);
+    uint32_t n_kv = 0, n_p[2] = {0, 0}, n_own[2] = {0, 0}, n_clean = 0;   // tiles and items of a group so far; edge tiles
+    PromptEntry e;
+    for (uint32_t n = 0; next_item(n, e); ++n) {
+      const int groups = e.rows > half_rows ? 2 : 1, n_tiles = e.tile_end - e.tile_begin, edge = edge_tile(e) - e.tile_begin;
+      auto scores = [&](int x, uint32_t slot, bool last) {
+        if (elect_lane()) {
+          const uint32_t qa = smem_u32(sQ + x * Cfg::kTileBytes), ka = smem_u32(sKv + slot * Cfg::kTileBytes), ts = tmem + Cfg::kColS + x * 128;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = (k / 4) * Cfg::kHalfBytes + (k % 4) * 32;
+            mma_ss(ts, smem_desc(qa + off, 16, 1024), smem_desc(ka + off, 16, 1024), kIdescQK, k > 0);
+          }
+          commit(smem_u32(&bars->s_full[x]));
+          if (last) commit(smem_u32(&bars->q_empty[x]));
+        }
+        __syncwarp();
+      };
+      auto release = [&](uint32_t slot) {
+        if (elect_lane()) commit(smem_u32(&bars->kv_empty[slot]));
+        __syncwarp();
+      };
+      uint32_t slot_k = n_kv % Cfg::kSlots;
+      wait(&bars->kv_full[slot_k], n_kv / Cfg::kSlots, bars);
+      for (int x = 0; x < groups; ++x) {
+        wait(&bars->q_full[x], n_own[x], bars);
+        fence_after();
+        scores(x, slot_k, n_tiles == 1);
+      }
+      release(slot_k);
+      if (edge <= 0) warp_arrive(&bars->v_ask, lane);
+#pragma unroll 1
+      for (int i = 0; i < n_tiles && !bars->abort; ++i) {
+        const uint32_t at_v = n_kv + 1, at_k = n_kv + 2, slot_v = at_v % Cfg::kSlots;
+        const bool more = i + 1 < n_tiles;
+        slot_k = at_k % Cfg::kSlots;
+        n_kv += 2;
+        wait(&bars->kv_full[slot_v], at_v / Cfg::kSlots, bars);
+        if (i >= edge) wait(&bars->v_clean, n_clean++, bars);
+        if (more && i + 1 >= edge) warp_arrive(&bars->v_ask, lane);
+#pragma unroll 1
+        for (int x = 0; x < groups; ++x) {
+          wait(&bars->p_full[x], n_p[x], bars);
+          ++n_p[x];
+          if (i == 0 && n_own[x] > 0) wait(&bars->o_free[x], n_own[x] - 1, bars);
+          fence_after();
+          if (elect_lane()) {
+            const uint32_t va = smem_u32(sKv + slot_v * Cfg::kTileBytes), to = tmem + Cfg::kColO + x * D, tp = tmem + Cfg::kColS + x * 128;
+#pragma unroll
+            for (int k = 0; k < kTileTokens / 16; ++k)
+              mma_ts(to, tp + k * 8, smem_desc(va + k * 2 * 1024, Cfg::kHalfBytes, 1024), kIdescPV, i > 0 || k > 0);
+            if (!more) commit(smem_u32(&bars->o_full[x]));
+            if (x == groups - 1) commit(smem_u32(&bars->kv_empty[slot_v]));
+          }
+          __syncwarp();
+          if (more) {
+            if (x == 0) wait(&bars->kv_full[slot_k], at_k / Cfg::kSlots, bars);
+            fence_after();
+            scores(x, slot_k, i + 2 == n_tiles);
+            if (x == groups - 1) release(slot_k);
+          }
+        }
+      }
+      for (int x = 0; x < groups; ++x) ++n_own[x];
+      warp_arrive(&bars->item_empty[n & 1], lane);
+    }
+  } else {
+    // ------------------------------------------------------------------ V tiles at the edge
+    const int id = tid - 320;    // 0..63
+    // The issuer asks for a tile while it works on the one before (so that the slot's barrier is in the phase waited for, and
+    // not one that the ring is yet to come to) and does not go past it without an answer.
+    uint32_t n_kv = 0, n_ask = 0;
+    PromptNote *notes = p.notes + (int64_t)blockIdx.x * 2 * kPtNotes;
+    PromptEntry e;
+    for (uint32_t n = 0; next_item(n, e); ++n) {
+      const int edge = edge_tile(e);
+      const int whole = e.vis0 + e.row0 / p.G;             // every row sees the tokens up to here
+#pragma unroll 1
+      for (int tile = edge; tile < e.tile_end; ++tile) {
+        const uint32_t at = n_kv + 2 * (uint32_t)(tile - e.tile_begin) + 1, slot = at % Cfg::kSlots;
+        wait(&bars->v_ask, n_ask++, bars);
+        wait(&bars->kv_full[slot], at / Cfg::kSlots, bars);
+        unsigned char *vt = sKv + slot * Cfg::kTileBytes;
+        const int t0 = tile * kTileTokens, n_tok = min(kTileTokens, e.t_end - t0);
+#pragma unroll 1
+        for (int tok = id; tok < kTileTokens; tok += 64) {
+          if (t0 + tok <= whole) continue;
+          uint4 *row = reinterpret_cast<uint4 *>(vt + (tok >> 3) * 1024 + (tok & 7) * 128);
+          if (tok >= n_tok) {
+#pragma unroll
+            for (int i = 0; i < 8 * Cfg::kHalves; ++i) row[(i >> 3) * (Cfg::kHalfBytes / 16) + (i & 7)] = make_uint4(0, 0, 0, 0);
+            continue;
+          }
+          // 0 * x is zero for a finite x, NaN otherwise
+          const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+          __nv_bfloat162 acc = zero;
+#pragma unroll
+          for (int i = 0; i < 8 * Cfg::kHalves; ++i) {
+            const uint4 w = row[(i >> 3) * (Cfg::kHalfBytes / 16) + (i & 7)];
+            acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.x), zero, acc);
+            acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.y), zero, acc);
+            acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.z), zero, acc);
+            acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.w), zero, acc);
+          }
+          if (*reinterpret_cast<const uint32_t *>(&acc) & 0x7fff7fffu) {
+            const int note = atomicAdd(&bars->notes[n & 1], 1);
+            if (note >= kPtNotes) continue;                 // (cannot be: a token for each position but the first)
+            PromptNote &out = notes[(n & 1) * kPtNotes + note];
+            out.token = t0 + tok;
+#pragma unroll 1
+            for (int b = 0; b < 4; ++b) {                   // 32 columns
+              uint32_t plus = 0, minus = 0;
+              if (b < D / 32) {
+#pragma unroll 1
+                for (int c = 0; c < 32; ++c) {
+                  const int col = b * 32 + c, chunk = (col & 63) >> 3;
+                  uint16_t *at_x = reinterpret_cast<uint16_t *>(reinterpret_cast<unsigned char *>(row) + (col >> 6) * Cfg::kHalfBytes + ((chunk ^ (tok & 7)) << 4)) + (col & 7);
+                  const uint16_t x = *at_x;
+                  if ((x & 0x7f80u) != 0x7f80u) continue;
+                  const bool nan = (x & 0x7fu) != 0;
+                  if (nan || !(x & 0x8000u)) plus |= 1u << c;
+                  if (nan || (x & 0x8000u)) minus |= 1u << c;
+                  *at_x = 0;
+                }
+              }
+              out.plus[b] = plus; out.minus[b] = minus;
+            }
+          }
+        }
+        fence_async_smem();
+        warp_arrive(&bars->v_clean, lane);
+        if (bars->abort) break;
+      }
+      n_kv += 2 * (uint32_t)(e.tile_end - e.tile_begin);
+      warp_arrive(&bars->item_clean[n & 1], lane);
+      warp_arrive(&bars->item_empty[n & 1], lane);
+    }
+  }
+  } else {
+    // ------------------------------------------------------------------ softmax and output
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPtRegsSoftmax));
+    const int x = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
+    const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+    const uint32_t ts = tmem + Cfg::kColS + x * 128 + lane_addr, to = tmem + Cfg::kColO + x * D + lane_addr;
+    const PromptNote *notes = p.notes + (int64_t)blockIdx.x * 2 * kPtNotes;
+    __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(p.out);
+    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2);
+    uint32_t n_s = 0, n_own = 0;
+    PromptEntry e;
+    for (uint32_t n = 0; next_item(n, e); ++n) {
+      const int rows = min(e.rows - x * half_rows, half_rows);
+      if (rows <= 0) {
+        warp_arrive(&bars->item_empty[n & 1], lane);
+        continue;
+      }
+      const int pr = e.row0 + x * half_rows + row;                       // packed row of the unit
+      const bool active = quad * 32 < rows, valid = row < rows;
+      const int limit = valid ? (causal ? e.vis0 + pr / p.G : e.vis0) : e.vis0 + (causal ? e.row0 / p.G : 0);   // last token the row sees
+      const int whole = causal ? e.vis0 + (e.row0 + x * half_rows) / p.G : e.vis0;                               // ... and every row of the group
+      float m_ref = -INFINITY;
+      uint64_t sum_a = pair(0.f, 0.f), sum_b = sum_a;
+#pragma unroll 1
+      for (int tile = e.tile_begin; tile < e.tile_end; ++tile, ++n_s) {
+        wait(&bars->s_full[x], n_s, bars);
+        fence_after();
+        if (active) {
+          float s[128];
+          uint32_t(&su)[4][32] = reinterpret_cast<uint32_t(&)[4][32]>(s);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, su[c]);
+          wait_ld();
+          const int t0 = tile * kTileTokens;
+          if (t0 + kTileTokens - 1 > whole) {
+            const int last = limit - t0;
+#pragma unroll
+            for (int i = 0; i < 128; ++i) s[i] = i <= last ? s[i] : -INFINITY;
+          }
+          float mx[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            mx[c] = fmaxf(s[c * 32], s[c * 32 + 1]);
+#pragma unroll
+            for (int i = 2; i < 32; i += 2) mx[c] = fmaxf(mx[c], fmaxf(s[c * 32 + i], s[c * 32 + i + 1]));
+          }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+          float alpha = 1.f;
+          bool rescale = false;
+          if (m_ref == -INFINITY) {
+            m_ref = top;                        // (what is there so far is zero, or about to be overwritten)
+          } else if (top > m_ref + kRescaleThreshold) {
+            alpha = fast_exp2(m_ref - top);
+            m_ref = top;
+            rescale = true;
+          }
+          if (__any_sync(0xffffffffu, rescale)) {
+            sum_a = e8::mul2(sum_a, pair(alpha, alpha));
+            sum_b = e8::mul2(sum_b, pair(alpha, alpha));
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t r[16];
+              tmem_ld16(to + c * 16, r);
+              wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+              tmem_st16(to + c * 16, r);
+            }
+          }
+          const float ref = m_ref == -INFINITY ? 0.f : -m_ref;
+          const uint64_t ref2 = pair(ref, ref);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float a, b;
+              unpair(fma2(pair(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale2, ref2), a, b);
+              a = fast_exp2(a);
+              b = fast_exp2(b);
+              if (i & 1) sum_b = add2(sum_b, pair(a, b));
+              else sum_a = add2(sum_a, pair(a, b));
+              pk[i] = pack_bf16(a, b);
+            }
+            tmem_st16(ts + c * 16, pk);
+          }
+          wait_st();
+        }
+        fence_before();
+        warp_arrive(&bars->p_full[x], lane);
+        if (bars->abort) break;
+      }
+      // ---- output
+      wait(&bars->item_clean[n & 1], n >> 1, bars);
+      const int n_notes = min(bars->notes[n & 1], kPtNotes);
+      wait(&bars->o_full[x], n_own, bars);
+      ++n_own;
+      fence_after();
+      if (active) {
+        float l0, l1, l2, l3;
+        unpair(sum_a, l0, l1);
+        unpair(sum_b, l2, l3);
+        const float l = (l0 + l1) + (l2 + l3);
+        const int64_t qh = (int64_t)(e.q0 + pr / p.G) * p.Hq + e.g * p.G + pr % p.G;
+        const int64_t part = (int64_t)e.slot * p.unit_rows + x * half_rows + row;
+        const float inv = e.slot < 0 ? 1.f / l : 1.f;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t r[32];
+          tmem_ld32(to + c * 32, r);
+          wait_ld();
+          if (n_notes > 0) {
+            uint32_t plus = 0, minus = 0;
+#pragma unroll 1
+            for (int i = 0; i < n_notes; ++i)
+              if (notes[(n & 1) * kPtNotes + i].token <= limit) { plus |= notes[(n & 1) * kPtNotes + i].plus[c]; minus |= notes[(n & 1) * kPtNotes + i].minus[c]; }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              float v = __uint_as_float(r[i]);
+              if (plus >> i & 1) v += INFINITY;
+              if (minus >> i & 1) v -= INFINITY;
+              r[i] = __float_as_uint(v);
+            }
+          }
+          if (valid && e.slot < 0) {
+            __nv_bfloat16 *dst = out + qh * D + c * 32;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              uint4 o;
+              o.x = pack_bf16(__uint_as_float(r[8 * v + 0]) * inv, __uint_as_float(r[8 * v + 1]) * inv);
+              o.y = pack_bf16(__uint_as_float(r[8 * v + 2]) * inv, __uint_as_float(r[8 * v + 3]) * inv);
+              o.z = pack_bf16(__uint_as_float(r[8 * v + 4]) * inv, __uint_as_float(r[8 * v + 5]) * inv);
+              o.w = pack_bf16(__uint_as_float(r[8 * v + 6]) * inv, __uint_as_float(r[8 * v + 7]) * inv);
+              *reinterpret_cast<uint4 *>(dst + v * 8) = o;
+            }
+          } else if (valid) {
+            float *dst = p.part_o + part * D + c * 32;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4 *>(dst + v * 4) = make_uint4(r[4 * v], r[4 * v + 1], r[4 * v + 2], r[4 * v + 3]);
+          }
+          __syncwarp();
+        }
+        if (valid) {
+          if (e.slot >= 0) p.part_ml[part] = make_float2(m_ref, l);
+          else if (p.lse) p.lse[qh] = (m_ref + log2f(l)) * kLn2;
+        }
+      }
+      fence_before();
+      warp_arrive(&bars->o_free[x], lane);
+      warp_arrive(&bars->item_empty[n & 1], lane);
+    }
+  }
+
+  // ---------------------------------------------------------------------- teardown
+  __syncwarp();
+  if (bars->abort) {
+    // give copies that are still in flight time to land before shared memory is released
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+  }
+}
+
+}  // namespace spx

@@ -22,6 +22,7 @@
 #include "plan.cuh"
 #include "prompt_plan.cuh"
 #include "prompt_simt.cuh"
+#include "prompt_tc.cuh"
 #include "sampler.cuh"
 #include "logprob.cuh"
 #include "spx.h"
@@ -113,7 +114,7 @@ constexpr int kPlanSmCount = 148;  // workspace sizing must not depend on a devi
 // ---------------------------------------------------------------------------------------------
 // The plan and the partial results of the attention of many rows (prompts; the prefixes of groups).
 struct PromptWs {
-  size_t hdr, unit_item0, unit_bad, item_tiles, item_cost, entries, range_off, join, entry_part, req_group, group_tiles, req_flag, part_ml, part_o, total;
+  size_t hdr, unit_item0, unit_bad, item_tiles, item_cost, entries, range_off, join, entry_part, req_group, group_tiles, req_flag, part_ml, part_o, notes, total;
   int32_t units, unit_rows, workers, max_items, max_entries, whole_slot0;
   bool fits;
 };
@@ -176,7 +177,7 @@ static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs, bool pr
 }
 
 static bool use_tensor_core_path(const spx_attn_args_t *a);
-static bool prompt_tensor_cores(const spx_attn_args_t *a) { (void)a; return false; }
+static bool prompt_tensor_cores(const spx_attn_args_t *a) { return use_tensor_core_path(a) && a->cache_format == SPX_CACHE_KV_DTYPE; }
 
 static PromptWs prompt_ws_layout(const spx_attn_args_t *a) {
   PromptWs w{};
@@ -207,6 +208,7 @@ static PromptWs prompt_ws_layout(const spx_attn_args_t *a) {
   }
   w.part_ml = take(sizeof(float2) * (size_t)slots * w.unit_rows);
   w.part_o = take(sizeof(float) * (size_t)slots * w.unit_rows * a->head_dim);
+  w.notes = take(tc ? sizeof(PromptNote) * 2 * kPtNotes * (size_t)w.workers : 0);
   w.total = off;
   return w;
 }
@@ -483,11 +485,31 @@ static PromptParams prompt_params(const spx_attn_args_t *a, const PromptWs &w, u
   p.max_items = w.max_items; p.max_entries = w.max_entries; p.whole_slot0 = w.whole_slot0;
   p.part_ml = reinterpret_cast<float2 *>(ws + w.part_ml);
   p.part_o = reinterpret_cast<float *>(ws + w.part_o);
+  p.notes = reinterpret_cast<PromptNote *>(ws + w.notes);
+  p.box_rows = 128 / p.G < p.total_q ? 128 / p.G : p.total_q;
   return p;
 }
 
 // The attention kernel of a plan by prompt_plan_kernel, directly behind it or another kernel that ran to its end behind it.
 static cudaError_t launch_prompt_main(const spx_attn_args_t *a, const PromptParams &p, cudaStream_t stream, const DeviceInfo &dev) {
+  if (prompt_tensor_cores(a)) {
+    CUtensorMap kmap, vmap, qmap;
+    if (!make_pool_map(&kmap, a->k_cache, a, p.head_inner) || !make_pool_map(&vmap, a->v_cache, a, p.head_inner) || !make_q_map(&qmap, a, p.box_rows))
+      return cudaErrorInvalidValue;
+    auto launch_tc = [&](auto dim) -> cudaError_t {
+      constexpr int D = decltype(dim)::value;
+      auto kernel = prompt_tc_kernel<D>;
+      static SmemOnce limit;
+      cudaError_t e = limit.raise(kernel, PtCfg<D>::kSmemBytes, dev.device);
+      if (e != cudaSuccess) return e;
+      // the split of the registers among its warps adds up to what it is launched with, or it would wait for ever
+      static const int regs = [kernel] { cudaFuncAttributes at{}; return cudaFuncGetAttributes(&at, kernel) == cudaSuccess ? at.numRegs : 0; }();
+      if (regs * kPtThreads < 256 * kPtRegsSoftmax + (kPtThreads - 256) * kPtRegsOther) return cudaErrorLaunchOutOfResources;
+      ++t_launches;
+      return launch_pdl(kernel, dim3(p.workers), dim3(kPtThreads), PtCfg<D>::kSmemBytes, stream, kmap, vmap, qmap, p);
+    };
+    return p.D == 64 ? launch_tc(std::integral_constant<int, 64>()) : launch_tc(std::integral_constant<int, 128>());
+  }
   auto launch = [&](auto rows, auto pool, auto dim) -> cudaError_t {
     using T = decltype(rows);
     using KV = decltype(pool);
