@@ -20,6 +20,8 @@
 // looked through: rows past the last one seen become zero, and elements that are not finite become zero and are noted; the rows that
 // do see one get it (an infinity of its sign, NaN otherwise) at the end.
 #pragma once
+#include <type_traits>
+
 #include "attn_e4m3.cuh"
 #include "attn_tc.cuh"
 #include "attn_tc4.cuh"
@@ -27,17 +29,27 @@
 
 namespace spx {
 
-constexpr int kPtThreads = 384;
-constexpr int kPtRegsSoftmax = 216, kPtRegsOther = 72;   // 2 * 128 * 216 + 128 * 72 = 384 * 168
+// Threads, and registers of a softmax warp, of warps 8-11, of the converting warps 12-15: together what 65536 registers give each thread at launch.
+template <bool kCodes>
+struct PtSplit {
+  static constexpr int kThreads = kCodes ? 512 : 384;
+  static constexpr int kSoftmax = kCodes ? 200 : 216, kOther = kCodes ? 48 : 72, kConvert = 64;
+  static constexpr int kLaunch = 65536 / kThreads / 8 * 8;
+  static_assert(2 * kSoftmax + kOther + (kCodes ? kConvert : 0) == kLaunch * (kThreads / 128), "what is given is what is there");
+};
+constexpr int kPtScaleSlots = 4;   // tiles whose scales are staged
 
-template <int D>
+template <int D, bool kCodes>
 struct PtCfg {
   static constexpr int kHalves = D / 64;
   static constexpr int kHalfBytes = 128 * 128;             // 128 rows of 64 elements: a half of a tile, or of a group's query rows
   static constexpr int kTileBytes = kHalves * kHalfBytes;
-  static constexpr int kSlots = D == 128 ? 5 : 8;
+  static constexpr int kSlots = kCodes ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);
+  static constexpr int kRawBytes = kTileTokens * D, kRawSlots = D == 128 ? 3 : 6;   // 8-bit pools: tiles as they lie there
   static constexpr int kOffKv = 2 * kTileBytes;            // behind the query rows of the two groups
-  static constexpr int kOffBar = kOffKv + kSlots * kTileBytes;
+  static constexpr int kOffRaw = kOffKv + kSlots * kTileBytes;
+  static constexpr int kOffScale = kOffRaw + (kCodes ? kRawSlots * kRawBytes : 0);      // [slot][K, V][128]
+  static constexpr int kOffBar = kOffScale + (kCodes ? kPtScaleSlots * 1024 : 0);
   static constexpr int kSmemBytes = kOffBar + 1024 + 1024;
   static_assert(kSmemBytes <= 232448, "shared memory");
   static constexpr int kColS = 0, kColO = 256;             // group x: S at 128 x, O at 256 + D x
@@ -45,8 +57,10 @@ struct PtCfg {
 
 struct PtBars {
   uint64_t kv_full[8], kv_empty[8], q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_free[2], item_full[2], item_empty[2], v_ask, v_clean, item_clean[2];
+  uint64_t raw_full[6], raw_empty[6], sc_full[kPtScaleSlots], sc_empty[kPtScaleSlots];
   PromptEntry item[2];
   int32_t notes[2];
+  int32_t general[kPtScaleSlots];   // some scale of the tile is no power of two
   uint32_t tmem_base;
   volatile int32_t abort;
   int32_t *dev_status;
@@ -89,13 +103,54 @@ __device__ __forceinline__ void warp_arrive(uint64_t *b, int lane) {
   if (lane == 0) arrive(smem_u32(b));
 }
 
+// Looks through a V row that some rows do not see: what is not finite becomes zero and is noted.
+template <int D>
+__device__ __forceinline__ void look_through(unsigned char *row_at, int tok, int token, PromptNote *notes, int32_t *count) {
+  constexpr int kHalfBytes = 128 * 128;
+  const uint4 *row = reinterpret_cast<const uint4 *>(row_at);
+  // 0 * x is zero for a finite x, NaN otherwise
+  const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+  __nv_bfloat162 acc = zero;
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) {
+    const uint4 w = row[(i >> 3) * (kHalfBytes / 16) + (i & 7)];
+    acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.x), zero, acc);
+    acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.y), zero, acc);
+    acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.z), zero, acc);
+    acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.w), zero, acc);
+  }
+  if ((*reinterpret_cast<const uint32_t *>(&acc) & 0x7fff7fffu) == 0) return;
+  const int note = atomicAdd(count, 1);
+  if (note >= kPtNotes) return;                   // (cannot be: a token for each position but the first)
+  notes[note].token = token;
+#pragma unroll 1
+  for (int b = 0; b < 4; ++b) {                   // 32 columns
+    uint32_t plus = 0, minus = 0;
+    if (b < D / 32) {
+#pragma unroll 1
+      for (int c = 0; c < 32; ++c) {
+        const int col = b * 32 + c, chunk = (col & 63) >> 3;
+        uint16_t *at = reinterpret_cast<uint16_t *>(row_at + (col >> 6) * kHalfBytes + ((chunk ^ (tok & 7)) << 4)) + (col & 7);
+        const uint16_t x = *at;
+        if ((x & 0x7f80u) != 0x7f80u) continue;
+        const bool nan = (x & 0x7fu) != 0;
+        if (nan || !(x & 0x8000u)) plus |= 1u << c;
+        if (nan || (x & 0x8000u)) minus |= 1u << c;
+        *at = 0;
+      }
+    }
+    notes[note].plus[b] = plus; notes[note].minus[b] = minus;
+  }
+}
+
 }  // namespace pt
 
-template <int D>
-__global__ void __launch_bounds__(kPtThreads, 1)
+template <int D, bool kCodes>
+__global__ void __launch_bounds__(PtSplit<kCodes>::kThreads, 1)
 prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap,
                  PromptParams p) {
-  using Cfg = PtCfg<D>;
+  using Cfg = PtCfg<D, kCodes>;
+  using Split = PtSplit<kCodes>;
   using namespace pt;
   extern __shared__ __align__(1024) unsigned char smem_dyn[];
   unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
@@ -104,13 +159,19 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
 #pragma unroll 1
-    for (int s = 0; s < 8; ++s) { mbar_init(&bars->kv_full[s], 1); mbar_init(&bars->kv_empty[s], 1); }
+    for (int s = 0; s < 8; ++s) { mbar_init(&bars->kv_full[s], kCodes ? 4 : 1); mbar_init(&bars->kv_empty[s], 1); }
+    if (kCodes) {
+#pragma unroll 1
+      for (int s = 0; s < 6; ++s) { mbar_init(&bars->raw_full[s], 1); mbar_init(&bars->raw_empty[s], 4); }
+#pragma unroll 1
+      for (int s = 0; s < kPtScaleSlots; ++s) { mbar_init(&bars->sc_full[s], 1); mbar_init(&bars->sc_empty[s], 12); }   // eight softmax, four converting warps
+    }
 #pragma unroll 1
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->q_full[b], 1); mbar_init(&bars->q_empty[b], 1); mbar_init(&bars->s_full[b], 1); mbar_init(&bars->p_full[b], 4);
       mbar_init(&bars->o_full[b], 1); mbar_init(&bars->o_free[b], 4);
-      mbar_init(&bars->item_full[b], 1); mbar_init(&bars->item_empty[b], 11);   // eight softmax warps, issuer, two edge warps
-      mbar_init(&bars->item_clean[b], 2);
+      mbar_init(&bars->item_full[b], 1); mbar_init(&bars->item_empty[b], kCodes ? 14 : 11);   // eight softmax warps, issuer, two edge warps (or four converting ones and the scales')
+      mbar_init(&bars->item_clean[b], kCodes ? 4 : 2);
       bars->notes[b] = 0;
     }
     mbar_init(&bars->v_ask, 1); mbar_init(&bars->v_clean, 2);
@@ -143,8 +204,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     return e.unit >= 0 && !bars->abort;
   };
 
-  if (warp >= 8) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPtRegsOther));
+  if (warp >= 8 && warp < 12) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Split::kOther));
   if (warp == 8) {
     // ------------------------------------------------------------------ producer
     const int n_units = p.hdr->n_units, ranged = p.hdr->ranged;
@@ -211,6 +272,17 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           const int npages = (min(kTileTokens, t_end - tile * kTileTokens) + p.P - 1) >> p.log2P;
 #pragma unroll
           for (int v = 0; v < 2; ++v, ++n_kv) {
+            if constexpr (kCodes) {
+              const uint32_t slot = n_kv % Cfg::kRawSlots;
+              wait(&bars->raw_empty[slot], n_kv / Cfg::kRawSlots ^ 1, bars);
+              if (lane == 0) expect_tx(smem_u32(&bars->raw_full[slot]), (uint32_t)npages * p.P * D);
+              __syncwarp();
+              if (lane < npages)
+                e8::tma_page(smem_u32(smem + Cfg::kOffRaw + slot * Cfg::kRawBytes + lane * p.P * D), v ? &vmap : &kmap, smem_u32(&bars->raw_full[slot]),
+                             p.head_inner ? e.g : 0, p.head_inner ? 0 : e.g, my_page);
+              __syncwarp();
+              continue;
+            }
             const uint32_t slot = n_kv % Cfg::kSlots;
             wait(&bars->kv_empty[slot], n_kv / Cfg::kSlots ^ 1, bars);
             if (lane == 0) expect_tx(smem_u32(&bars->kv_full[slot]), (uint32_t)npages * p.P * D * 2);
@@ -263,7 +335,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         scores(x, slot_k, n_tiles == 1);
       }
       release(slot_k);
-      if (edge <= 0) warp_arrive(&bars->v_ask, lane);
+      if (!kCodes && edge <= 0) warp_arrive(&bars->v_ask, lane);
 #pragma unroll 1
       for (int i = 0; i < n_tiles && !bars->abort; ++i) {
         const uint32_t at_v = n_kv + 1, at_k = n_kv + 2, slot_v = at_v % Cfg::kSlots;
@@ -271,8 +343,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         slot_k = at_k % Cfg::kSlots;
         n_kv += 2;
         wait(&bars->kv_full[slot_v], at_v / Cfg::kSlots, bars);
-        if (i >= edge) wait(&bars->v_clean, n_clean++, bars);
-        if (more && i + 1 >= edge) warp_arrive(&bars->v_ask, lane);
+        if (!kCodes && i >= edge) wait(&bars->v_clean, n_clean++, bars);
+        if (!kCodes && more && i + 1 >= edge) warp_arrive(&bars->v_ask, lane);
 #pragma unroll 1
         for (int x = 0; x < groups; ++x) {
           wait(&bars->p_full[x], n_p[x], bars);
@@ -299,11 +371,11 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       for (int x = 0; x < groups; ++x) ++n_own[x];
       warp_arrive(&bars->item_empty[n & 1], lane);
     }
-  } else {
+  } else if (!kCodes) {
     // ------------------------------------------------------------------ V tiles at the edge
-    const int id = tid - 320;    // 0..63
     // The issuer asks for a tile while it works on the one before (so that the slot's barrier is in the phase waited for, and
     // not one that the ring is yet to come to) and does not go past it without an answer.
+    const int id = tid - 320;    // 0..63
     uint32_t n_kv = 0, n_ask = 0;
     PromptNote *notes = p.notes + (int64_t)blockIdx.x * 2 * kPtNotes;
     PromptEntry e;
@@ -320,46 +392,12 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
 #pragma unroll 1
         for (int tok = id; tok < kTileTokens; tok += 64) {
           if (t0 + tok <= whole) continue;
-          uint4 *row = reinterpret_cast<uint4 *>(vt + (tok >> 3) * 1024 + (tok & 7) * 128);
-          if (tok >= n_tok) {
+          unsigned char *row = vt + (tok >> 3) * 1024 + (tok & 7) * 128;
+          if (tok < n_tok) {
+            look_through<D>(row, tok, t0 + tok, notes + (n & 1) * kPtNotes, &bars->notes[n & 1]);
+          } else {
 #pragma unroll
-            for (int i = 0; i < 8 * Cfg::kHalves; ++i) row[(i >> 3) * (Cfg::kHalfBytes / 16) + (i & 7)] = make_uint4(0, 0, 0, 0);
-            continue;
-          }
-          // 0 * x is zero for a finite x, NaN otherwise
-          const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
-          __nv_bfloat162 acc = zero;
-#pragma unroll
-          for (int i = 0; i < 8 * Cfg::kHalves; ++i) {
-            const uint4 w = row[(i >> 3) * (Cfg::kHalfBytes / 16) + (i & 7)];
-            acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.x), zero, acc);
-            acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.y), zero, acc);
-            acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.z), zero, acc);
-            acc = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w.w), zero, acc);
-          }
-          if (*reinterpret_cast<const uint32_t *>(&acc) & 0x7fff7fffu) {
-            const int note = atomicAdd(&bars->notes[n & 1], 1);
-            if (note >= kPtNotes) continue;                 // (cannot be: a token for each position but the first)
-            PromptNote &out = notes[(n & 1) * kPtNotes + note];
-            out.token = t0 + tok;
-#pragma unroll 1
-            for (int b = 0; b < 4; ++b) {                   // 32 columns
-              uint32_t plus = 0, minus = 0;
-              if (b < D / 32) {
-#pragma unroll 1
-                for (int c = 0; c < 32; ++c) {
-                  const int col = b * 32 + c, chunk = (col & 63) >> 3;
-                  uint16_t *at_x = reinterpret_cast<uint16_t *>(reinterpret_cast<unsigned char *>(row) + (col >> 6) * Cfg::kHalfBytes + ((chunk ^ (tok & 7)) << 4)) + (col & 7);
-                  const uint16_t x = *at_x;
-                  if ((x & 0x7f80u) != 0x7f80u) continue;
-                  const bool nan = (x & 0x7fu) != 0;
-                  if (nan || !(x & 0x8000u)) plus |= 1u << c;
-                  if (nan || (x & 0x8000u)) minus |= 1u << c;
-                  *at_x = 0;
-                }
-              }
-              out.plus[b] = plus; out.minus[b] = minus;
-            }
+            for (int i = 0; i < D / 8; ++i) *reinterpret_cast<uint4 *>(row + (i >> 3) * Cfg::kHalfBytes + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
           }
         }
         fence_async_smem();
@@ -370,21 +408,144 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       warp_arrive(&bars->item_clean[n & 1], lane);
       warp_arrive(&bars->item_empty[n & 1], lane);
     }
+  } else if (warp == 10) {
+    // ------------------------------------------------------------------ scales of 8-bit pools: four tokens of a tile a lane
+    float *sScale = reinterpret_cast<float *>(smem + Cfg::kOffScale);
+    uint32_t n_tile = 0;
+    PromptEntry e;
+    for (uint32_t n = 0; next_item(n, e); ++n) {
+      const int32_t *table = p.block_table + (int64_t)e.table_row * p.max_pages_per_req;
+      const int t_end = min(e.t_end, e.tile_end * kTileTokens);
+      int page[4];
+      auto pages_of = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = tile * kTileTokens + lane + 32 * i;
+          page[i] = t < t_end ? table[t >> p.log2P] : -1;
+        }
+      };
+      pages_of(e.tile_begin);
+#pragma unroll 1
+      for (int tile = e.tile_begin; tile < e.tile_end; ++tile, ++n_tile) {
+        float ks[4], vs[4];
+        bool general = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = tile * kTileTokens + lane + 32 * i;
+          ks[i] = vs[i] = 1.f;
+          if (page[i] >= 0 && page[i] < p.num_pages) {
+            const int64_t at = (((int64_t)page[i] * p.Hkv + e.g) << (p.log2P - p.log2SB)) + ((t & (p.P - 1)) >> p.log2SB);
+            ks[i] = p.k_scales[at];
+            vs[i] = p.v_scales[at];
+          }
+        }
+        pages_of(tile + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a = __float_as_uint(ks[i]), b = __float_as_uint(vs[i]);
+          general |= ((a & 0x7fffffu) && (a & 0x7f800000u)) || ((b & 0x7fffffu) && (b & 0x7f800000u));
+        }
+        const uint32_t slot = n_tile % kPtScaleSlots;
+        wait(&bars->sc_empty[slot], n_tile / kPtScaleSlots ^ 1, bars);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sScale[slot * 256 + lane + 32 * i] = ks[i];
+          sScale[slot * 256 + 128 + lane + 32 * i] = vs[i];
+        }
+        general = __any_sync(0xffffffffu, general);
+        if (lane == 0) bars->general[slot] = general;
+        warp_arrive(&bars->sc_full[slot], lane);
+        if (bars->abort) break;
+      }
+      warp_arrive(&bars->item_empty[n & 1], lane);
+    }
   }
+  } else if (kCodes && warp >= 12) {
+    // ------------------------------------------------------------------ 8-bit tiles to bf16 ones: a thread a token
+    // A code times the power of two in its scale is exact in bf16; what is left of a scale, 1 <= f < 2, multiplies the score,
+    // or the weight, of its token.
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Split::kConvert));
+    const int tok = tid - 384;
+    const float *sScale = reinterpret_cast<const float *>(smem + Cfg::kOffScale);
+    PromptNote *notes = p.notes + (int64_t)blockIdx.x * 2 * kPtNotes;
+    uint32_t n_tile = 0;
+    PromptEntry e;
+    for (uint32_t n = 0; next_item(n, e); ++n) {
+      const int edge = edge_tile(e), whole = e.vis0 + e.row0 / p.G;
+#pragma unroll 1
+      for (int tile = e.tile_begin; tile < e.tile_end; ++tile, ++n_tile) {
+        const uint32_t sc = n_tile % kPtScaleSlots;
+        wait(&bars->sc_full[sc], n_tile / kPtScaleSlots, bars);
+        const float ks = sScale[sc * 256 + tok], vs = sScale[sc * 256 + 128 + tok];
+        warp_arrive(&bars->sc_empty[sc], lane);
+#pragma unroll 1
+        for (int v = 0; v < 2; ++v) {
+          const uint32_t at = 2 * n_tile + v, rs = at % Cfg::kRawSlots, slot = at % Cfg::kSlots;
+          const uint32_t bits = __float_as_uint(v ? vs : ks);
+          const float mul = __uint_as_float((bits & 0x7f800000u) ? bits & 0xff800000u : bits);
+          const uint64_t mul2_ = pair(mul, mul);
+          wait(&bars->raw_full[rs], at / Cfg::kRawSlots, bars);
+          wait(&bars->kv_empty[slot], at / Cfg::kSlots ^ 1, bars);
+          const unsigned char *src = smem + Cfg::kOffRaw + rs * Cfg::kRawBytes + tok * D;
+          unsigned char *row = sKv + slot * Cfg::kTileBytes + (tok >> 3) * 1024 + (tok & 7) * 128;
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(src + ((D == 128 ? c ^ (tok & 7) : c ^ ((tok >> 1) & 3)) << 4));
+            const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+            uint32_t o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(in[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
+              const float2 f = __half22float2(__half2(h));
+              float a, b;
+              unpair(e8::mul2(pair(f.x, f.y), mul2_), a, b);
+              o[i] = pack_bf16(a, b);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int oc = 2 * c + i;
+              *reinterpret_cast<uint4 *>(row + (oc >> 3) * Cfg::kHalfBytes + (((oc & 7) ^ (tok & 7)) << 4)) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+          }
+          if (v && tile >= edge && tile * kTileTokens + tok > whole) {
+            if (tile * kTileTokens + tok < e.t_end) {
+              look_through<D>(row, tok, tile * kTileTokens + tok, notes + (n & 1) * kPtNotes, &bars->notes[n & 1]);
+            } else {
+#pragma unroll 1
+              for (int i = 0; i < D / 8; ++i) *reinterpret_cast<uint4 *>(row + (i >> 3) * Cfg::kHalfBytes + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+            }
+          }
+          fence_async_smem();
+          warp_arrive(&bars->kv_full[slot], lane);
+          warp_arrive(&bars->raw_empty[rs], lane);
+        }
+        if (bars->abort) break;
+      }
+      warp_arrive(&bars->item_clean[n & 1], lane);
+      warp_arrive(&bars->item_empty[n & 1], lane);
+    }
   } else {
     // ------------------------------------------------------------------ softmax and output
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPtRegsSoftmax));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Split::kSoftmax));
     const int x = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     const uint32_t ts = tmem + Cfg::kColS + x * 128 + lane_addr, to = tmem + Cfg::kColO + x * D + lane_addr;
     const PromptNote *notes = p.notes + (int64_t)blockIdx.x * 2 * kPtNotes;
     __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(p.out);
     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2);
-    uint32_t n_s = 0, n_own = 0;
+    const float *sScale = reinterpret_cast<const float *>(smem + Cfg::kOffScale);
+    uint32_t n_s = 0, n_own = 0, n_tile = 0;
     PromptEntry e;
     for (uint32_t n = 0; next_item(n, e); ++n) {
       const int rows = min(e.rows - x * half_rows, half_rows);
       if (rows <= 0) {
+        if constexpr (kCodes) {
+#pragma unroll 1
+          for (int tile = e.tile_begin; tile < e.tile_end && !bars->abort; ++tile, ++n_tile) {
+            wait(&bars->sc_full[n_tile % kPtScaleSlots], n_tile / kPtScaleSlots, bars);
+            warp_arrive(&bars->sc_empty[n_tile % kPtScaleSlots], lane);
+          }
+        }
         warp_arrive(&bars->item_empty[n & 1], lane);
         continue;
       }
@@ -395,7 +556,18 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       float m_ref = -INFINITY;
       uint64_t sum_a = pair(0.f, 0.f), sum_b = sum_a;
 #pragma unroll 1
-      for (int tile = e.tile_begin; tile < e.tile_end; ++tile, ++n_s) {
+      for (int tile = e.tile_begin; tile < e.tile_end; ++tile, ++n_s, ++n_tile) {
+        const float4 *factors = reinterpret_cast<const float4 *>(sScale + (n_tile % kPtScaleSlots) * 256);
+        bool general = false;
+        if constexpr (kCodes) {
+          wait(&bars->sc_full[n_tile % kPtScaleSlots], n_tile / kPtScaleSlots, bars);
+          general = bars->general[n_tile % kPtScaleSlots];
+        }
+        // what the power of two leaves of a scale
+        auto factor = [](float scale) -> float {
+          const uint32_t b = __float_as_uint(scale);
+          return (b & 0x7f800000u) ? __uint_as_float((b & 0x7fffffu) | 0x3f800000u) : 1.f;
+        };
         wait(&bars->s_full[x], n_s, bars);
         fence_after();
         if (active) {
@@ -405,6 +577,13 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, su[c]);
           wait_ld();
           const int t0 = tile * kTileTokens;
+          if (kCodes && general) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float4 f = factors[i];
+              s[4 * i] *= factor(f.x); s[4 * i + 1] *= factor(f.y); s[4 * i + 2] *= factor(f.z); s[4 * i + 3] *= factor(f.w);
+            }
+          }
           if (t0 + kTileTokens - 1 > whole) {
             const int last = limit - t0;
 #pragma unroll
@@ -442,25 +621,35 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           }
           const float ref = m_ref == -INFINITY ? 0.f : -m_ref;
           const uint64_t ref2 = pair(ref, ref);
+          auto weights = [&](auto scaled) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t pk[16];
+            for (int c = 0; c < 4; ++c) {
+              uint32_t pk[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float a, b;
-              unpair(fma2(pair(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale2, ref2), a, b);
-              a = fast_exp2(a);
-              b = fast_exp2(b);
-              if (i & 1) sum_b = add2(sum_b, pair(a, b));
-              else sum_a = add2(sum_a, pair(a, b));
-              pk[i] = pack_bf16(a, b);
+              for (int i = 0; i < 16; ++i) {
+                float a, b;
+                unpair(fma2(pair(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale2, ref2), a, b);
+                a = fast_exp2(a);
+                b = fast_exp2(b);
+                if (i & 1) sum_b = add2(sum_b, pair(a, b));
+                else sum_a = add2(sum_a, pair(a, b));
+                if constexpr (decltype(scaled)::value) {
+                  const float2 f = reinterpret_cast<const float2 *>(factors + 32)[c * 16 + i];
+                  a *= factor(f.x);
+                  b *= factor(f.y);
+                }
+                pk[i] = pack_bf16(a, b);
+              }
+              tmem_st16(ts + c * 16, pk);
             }
-            tmem_st16(ts + c * 16, pk);
-          }
+          };
+          if (kCodes && general) weights(std::true_type());
+          else weights(std::false_type());
           wait_st();
         }
         fence_before();
         warp_arrive(&bars->p_full[x], lane);
+        if constexpr (kCodes) warp_arrive(&bars->sc_empty[n_tile % kPtScaleSlots], lane);
         if (bars->abort) break;
       }
       // ---- output

@@ -177,7 +177,7 @@ static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs, bool pr
 }
 
 static bool use_tensor_core_path(const spx_attn_args_t *a);
-static bool prompt_tensor_cores(const spx_attn_args_t *a) { return use_tensor_core_path(a) && a->cache_format == SPX_CACHE_KV_DTYPE; }
+static bool prompt_tensor_cores(const spx_attn_args_t *a) { return use_tensor_core_path(a); }
 
 static PromptWs prompt_ws_layout(const spx_attn_args_t *a) {
   PromptWs w{};
@@ -494,21 +494,29 @@ static PromptParams prompt_params(const spx_attn_args_t *a, const PromptWs &w, u
 static cudaError_t launch_prompt_main(const spx_attn_args_t *a, const PromptParams &p, cudaStream_t stream, const DeviceInfo &dev) {
   if (prompt_tensor_cores(a)) {
     CUtensorMap kmap, vmap, qmap;
-    if (!make_pool_map(&kmap, a->k_cache, a, p.head_inner) || !make_pool_map(&vmap, a->v_cache, a, p.head_inner) || !make_q_map(&qmap, a, p.box_rows))
+    const bool codes = a->cache_format == SPX_CACHE_E4M3;
+    auto pool_map = codes ? make_pool_map_e4m3 : make_pool_map;
+    if (!pool_map(&kmap, a->k_cache, a, p.head_inner) || !pool_map(&vmap, a->v_cache, a, p.head_inner) || !make_q_map(&qmap, a, p.box_rows))
       return cudaErrorInvalidValue;
-    auto launch_tc = [&](auto dim) -> cudaError_t {
+    auto launch_tc = [&](auto dim, auto coded) -> cudaError_t {
       constexpr int D = decltype(dim)::value;
-      auto kernel = prompt_tc_kernel<D>;
+      constexpr bool kCodes = decltype(coded)::value;
+      using Cfg = PtCfg<D, kCodes>;
+      using Split = PtSplit<kCodes>;
+      auto kernel = prompt_tc_kernel<D, kCodes>;
       static SmemOnce limit;
-      cudaError_t e = limit.raise(kernel, PtCfg<D>::kSmemBytes, dev.device);
+      cudaError_t e = limit.raise(kernel, Cfg::kSmemBytes, dev.device);
       if (e != cudaSuccess) return e;
       // the split of the registers among its warps adds up to what it is launched with, or it would wait for ever
       static const int regs = [kernel] { cudaFuncAttributes at{}; return cudaFuncGetAttributes(&at, kernel) == cudaSuccess ? at.numRegs : 0; }();
-      if (regs * kPtThreads < 256 * kPtRegsSoftmax + (kPtThreads - 256) * kPtRegsOther) return cudaErrorLaunchOutOfResources;
+      if (regs < Split::kLaunch) return cudaErrorLaunchOutOfResources;
       ++t_launches;
-      return launch_pdl(kernel, dim3(p.workers), dim3(kPtThreads), PtCfg<D>::kSmemBytes, stream, kmap, vmap, qmap, p);
+      return launch_pdl(kernel, dim3(p.workers), dim3(Split::kThreads), Cfg::kSmemBytes, stream, kmap, vmap, qmap, p);
     };
-    return p.D == 64 ? launch_tc(std::integral_constant<int, 64>()) : launch_tc(std::integral_constant<int, 128>());
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    if (codes) return p.D == 64 ? launch_tc(D64(), std::true_type()) : launch_tc(D128(), std::true_type());
+    return p.D == 64 ? launch_tc(D64(), std::false_type()) : launch_tc(D128(), std::false_type());
   }
   auto launch = [&](auto rows, auto pool, auto dim) -> cudaError_t {
     using T = decltype(rows);

@@ -23,7 +23,7 @@ class Batch:
     dealt out at random from a pool that is larger than needed; every slot that no request owns is `poison`."""
 
     def __init__(self, lens, m, hq, hkv, d, page, dtype=torch.bfloat16, kind="rows", layout="HND", sb=None, seed=0, poison=math.nan,
-                 shared=None, spread=1.0, tail_rows=0):
+                 shared=None, spread=1.0, tail_rows=0, scale_kind="any"):
         g = torch.Generator().manual_seed(seed)
         self.lens, self.m, self.hq, self.hkv, self.d, self.page, self.dtype, self.kind = lens, m, hq, hkv, d, page, dtype, kind
         self.sb = sb or page
@@ -46,6 +46,11 @@ class Batch:
                 x = getattr(self, w).double().clamp(-5.5, 5.5).numpy() * 80
                 codes = torch.from_numpy(R.encode(x))
                 scales = (torch.exp(0.7 * torch.randn(total, hkv, page // self.sb, generator=g)) / 80).float()
+                if scale_kind == "powers":           # as the append writes them
+                    scales = torch.exp2(torch.round(torch.log2(scales)))
+                elif scale_kind == "mixed":          # powers of two, others, zeros
+                    pick = torch.randint(0, 3, scales.shape, generator=g)
+                    scales = torch.where(pick == 0, scales, torch.where(pick == 1, torch.exp2(torch.round(torch.log2(scales))), torch.zeros(())))
                 setattr(self, w, codes)
                 setattr(self, w + "_scales", scales)
         else:

@@ -52,6 +52,17 @@ def test_ragged_8_bit(hq, hkv, d, page, sb, layout, dtype):
     b.check(out, lse)
 
 
+@pytest.mark.parametrize("scale_kind", ["powers", "mixed"])
+@pytest.mark.parametrize("hq,hkv,d,page,sb", [(8, 2, 128, 16, 16), (7, 1, 64, 32, 1), (4, 2, 128, 128, 128)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_scales_of_8_bit_pools(hq, hkv, d, page, sb, dtype, scale_kind):
+    lens, m = _ragged(RAGGED)
+    b = Batch(lens, m, hq, hkv, d, page, dtype=dtype, kind="e4m3", sb=sb, seed=hq + page, scale_kind=scale_kind)
+    out, lse, status = prompt(b)
+    assert status == 0
+    b.check(out, lse)
+
+
 @pytest.mark.parametrize("dtype,kind", [(BF16, "rows"), (F32, "rows"), (BF16, "e4m3")])
 @pytest.mark.parametrize("m,hist", [(3, 9000), (40, 6000), (500, 5000), (1, 12345)])
 def test_few_rows_behind_a_long_history(m, hist, dtype, kind):
