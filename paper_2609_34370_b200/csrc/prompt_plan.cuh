@@ -76,6 +76,7 @@ struct PromptParams {
   int32_t unit_rows;                  // packed rows of an item (whole positions in the tensor-core kernel)
   int32_t workers;                    // CTAs of the persistent kernel
   int32_t min_range, overhead;        // tiles: the shortest range worth a CTA, what cuts cost
+  int32_t entry_cost;                 // of an entry's ends, in eighths of a tile
   PromptHeader *hdr;
   int32_t *unit_item0;                // [units + 1]
   int32_t *unit_bad;                  // [units]
@@ -133,6 +134,7 @@ __device__ __forceinline__ int last_at_most(const T *a, int n, X x) {
 // Block 0 plans.  Of a plan over groups the blocks behind it compare the block-table rows of the requests with
 // their groups' first, so that a request that does not share what its group reads once is found, not answered wrongly.
 __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
+  SPX_TL_SCOPE(kTlPlan);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x;
   __shared__ int64_t s_scratch[33];
@@ -216,7 +218,7 @@ __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
   const int NI = (int)n_items;
 
   // tiles of the items, their sum and how many there are of each length
-  const int entry_cost = 8;   // an entry's ends, in eighths of a tile
+  const int entry_cost = p.entry_cost;   // an entry's ends, in eighths of a tile
   int64_t cost_sum = 0, tile_sum = 0;
   for (int base = 0; base < NI; base += 1024) {
     const int i = base + tid;
@@ -366,6 +368,7 @@ __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
 // Blocks (b, y): entry b of the list, items (row, four columns) y * 256 + t of it.
 template <typename T>
 __global__ void __launch_bounds__(256) prompt_join_kernel(PromptParams p) {
+  SPX_TL_SCOPE(kTlCombine);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   T *out = reinterpret_cast<T *>(p.out);
   const int vecs = p.D / 4;
@@ -434,6 +437,7 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(PromptParams p) {
 // head, four columns) y * 256 + t.  a: the plan of the requests' own tokens; p: that of the prefixes.
 template <typename T>
 __global__ void __launch_bounds__(256) prefix_join_kernel(AttnParams a, PromptParams p) {
+  SPX_TL_SCOPE(kTlCombine);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int r = blockIdx.x;
   T *out = reinterpret_cast<T *>(a.out);

@@ -39,6 +39,7 @@ template <> struct PsLoad<unsigned char> {   // e4m3 codes
 // T: rows and output; KV: pool elements (T, or unsigned char for 8-bit floats).
 template <typename T, typename KV, int D>
 __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p) {
+  SPX_TL_SCOPE(kTlAttention);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // (the kernel behind this one reads the plan ahead of its own wait)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

@@ -6,13 +6,14 @@
 //                   of tensor memory, no exchange between threads), keeps the row's maximum and sum, and writes
 //                   its weights over the scores as bf16, the A operand of the value MMA;
 //   warp 8          producer: takes entries of the plan, copies query rows, and K and V tiles, page by page, into a ring;
-//   warp 9          issuer.  While one group is at its softmax the other's MMAs run: S0 S1 | V0 S0' | V1 S1' | ...
-//   warps 10, 11    look after the V tiles at the edge of what rows see (below).
+//   warps 9, 10     issuers of the MMAs of group 0 and 1 (one warp for both was the bound: 12 waits, elections and commits
+//                   a tile, 200 cycles each).  While one group is at its softmax the other's MMAs run;
+//   warp 11         looks after the V tiles at the edge of what rows see (below); over 8-bit pools it fetches scales,
+//                   and warps 12-15 turn the codes into bf16 tiles.
 // Tensor memory is full: two score buffers of 128 columns and two outputs of D.
 //
-// The running maximum of a row is a reference that moves only when a tile's maximum passes it by 2^8 (the output
-// is then rescaled by the row's own thread; the score MMA of a tile completes behind the value MMA of the one before, so the
-// output is at rest).  Weights are rounded to bf16 (half a step of 2^-8 each, the type V has to be multiplied in); their sum is
+// The running maximum of a row is a reference that moves only when a weight under it would pass 2^8 (the output
+// is then rescaled by the row's own thread).  Weights are rounded to bf16 (half a step of 2^-8 each, the type V has to be multiplied in); their sum is
 // taken in fp32 before that.
 //
 // What rows do not see must not reach them.  Scores are masked before the maximum.  A weight of zero does not
@@ -33,7 +34,7 @@ namespace spx {
 template <bool kCodes>
 struct PtSplit {
   static constexpr int kThreads = kCodes ? 512 : 384;
-  static constexpr int kSoftmax = kCodes ? 200 : 216, kOther = kCodes ? 48 : 72, kConvert = 64;
+  static constexpr int kSoftmax = kCodes ? 176 : 192, kOther = kCodes ? 96 : 120, kConvert = 64;
   static constexpr int kLaunch = 65536 / kThreads / 8 * 8;
   static_assert(2 * kSoftmax + kOther + (kCodes ? kConvert : 0) == kLaunch * (kThreads / 128), "what is given is what is there");
 };
@@ -56,7 +57,7 @@ struct PtCfg {
 };
 
 struct PtBars {
-  uint64_t kv_full[8], kv_empty[8], q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_free[2], item_full[2], item_empty[2], v_ask, v_clean, item_clean[2];
+  uint64_t kv_full[8], kv_empty[8], q_full[2], q_empty[2], s_full[2][2], p_full[2][2], h_done[2], o_full[2], o_free[2], item_full[2], item_empty[2], v_ask, v_clean, item_clean[2];
   uint64_t raw_full[6], raw_empty[6], sc_full[kPtScaleSlots], sc_empty[kPtScaleSlots];
   PromptEntry item[2];
   int32_t notes[2];
@@ -149,6 +150,7 @@ template <int D, bool kCodes>
 __global__ void __launch_bounds__(PtSplit<kCodes>::kThreads, 1)
 prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap,
                  PromptParams p) {
+  SPX_TL_SCOPE(kTlAttention);
   using Cfg = PtCfg<D, kCodes>;
   using Split = PtSplit<kCodes>;
   using namespace pt;
@@ -159,7 +161,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
 #pragma unroll 1
-    for (int s = 0; s < 8; ++s) { mbar_init(&bars->kv_full[s], kCodes ? 4 : 1); mbar_init(&bars->kv_empty[s], 1); }
+    for (int s = 0; s < 8; ++s) { mbar_init(&bars->kv_full[s], kCodes ? 4 : 1); mbar_init(&bars->kv_empty[s], 2); }
     if (kCodes) {
 #pragma unroll 1
       for (int s = 0; s < 6; ++s) { mbar_init(&bars->raw_full[s], 1); mbar_init(&bars->raw_empty[s], 4); }
@@ -168,13 +170,14 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     }
 #pragma unroll 1
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&bars->q_full[b], 1); mbar_init(&bars->q_empty[b], 1); mbar_init(&bars->s_full[b], 1); mbar_init(&bars->p_full[b], 4);
+      mbar_init(&bars->q_full[b], 1); mbar_init(&bars->q_empty[b], 1); mbar_init(&bars->s_full[b][0], 1); mbar_init(&bars->s_full[b][1], 1);
+      mbar_init(&bars->p_full[b][0], 4); mbar_init(&bars->p_full[b][1], 4); mbar_init(&bars->h_done[b], 1);
       mbar_init(&bars->o_full[b], 1); mbar_init(&bars->o_free[b], 4);
-      mbar_init(&bars->item_full[b], 1); mbar_init(&bars->item_empty[b], kCodes ? 14 : 11);   // eight softmax warps, issuer, two edge warps (or four converting ones and the scales')
-      mbar_init(&bars->item_clean[b], kCodes ? 4 : 2);
+      mbar_init(&bars->item_full[b], 1); mbar_init(&bars->item_empty[b], kCodes ? 15 : 11);   // eight softmax warps, two issuers, the edge warp (or four converting ones and the scales')
+      mbar_init(&bars->item_clean[b], kCodes ? 4 : 1);
       bars->notes[b] = 0;
     }
-    mbar_init(&bars->v_ask, 1); mbar_init(&bars->v_clean, 2);
+    mbar_init(&bars->v_ask, 2); mbar_init(&bars->v_clean, 1);
     bars->abort = 0;
     bars->dev_status = p.dev_status;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -303,79 +306,79 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     wait(&bars->item_empty[n_item & 1], (n_item >> 1) ^ 1, bars);
     if (lane == 0) bars->item[n_item & 1].unit = -1;
     warp_arrive(&bars->item_full[n_item & 1], lane);
-  } else if (warp == 9) {
-    // ------------------------------------------------------------------ issuer
-    constexpr uint32_t kIdescQK = idesc(kTileTokens, false), kIdescPV = idesc(D, true);
-    uint32_t n_kv = 0, n_p[2] = {0, 0}, n_own[2] = {0, 0}, n_clean = 0;   // tiles and items of a group so far; edge tiles
+  } else if (warp <= 10) {
+    // ------------------------------------------------------------------ issuer of a group
+    constexpr uint32_t kIdescQK = idesc(64, false), kIdescPV = idesc(D, true);
+    const int x = warp - 9;
+    const uint32_t ts = tmem + Cfg::kColS + x * 128, to = tmem + Cfg::kColO + x * D;
+    const uint64_t qd = smem_desc(smem_u32(sQ + x * Cfg::kTileBytes), 16, 1024);
+    uint32_t n_kv = 0, n_p = 0, n_own = 0, n_clean = 0;   // tiles of the ring, the group's tiles and items, edge tiles
     PromptEntry e;
     for (uint32_t n = 0; next_item(n, e); ++n) {
-      const int groups = e.rows > half_rows ? 2 : 1, n_tiles = e.tile_end - e.tile_begin, edge = edge_tile(e) - e.tile_begin;
-      auto scores = [&](int x, uint32_t slot, bool last) {
+      const bool active = x * half_rows < e.rows;           // (an idle group's issuer hands the tiles back)
+      const int n_tiles = e.tile_end - e.tile_begin, edge = edge_tile(e) - e.tile_begin;
+      // scores of half a tile, 64 tokens, over what the half's weights of the tile before leave
+      auto scores = [&](uint32_t at, int h, bool last) {
+        const uint32_t slot = at % Cfg::kSlots;
+        if (h == 0) wait(&bars->kv_full[slot], at / Cfg::kSlots, bars);
+        if (!active) {
+          if (h == 1) warp_arrive(&bars->kv_empty[slot], lane);
+          return;
+        }
+        fence_after();
         if (elect_lane()) {
-          const uint32_t qa = smem_u32(sQ + x * Cfg::kTileBytes), ka = smem_u32(sKv + slot * Cfg::kTileBytes), ts = tmem + Cfg::kColS + x * 128;
+          const uint64_t kd = smem_desc(smem_u32(sKv + slot * Cfg::kTileBytes), 16, 1024) + h * 512;
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
-            const uint32_t off = (k / 4) * Cfg::kHalfBytes + (k % 4) * 32;
-            mma_ss(ts, smem_desc(qa + off, 16, 1024), smem_desc(ka + off, 16, 1024), kIdescQK, k > 0);
+            const uint64_t off = ((k / 4) * Cfg::kHalfBytes + (k % 4) * 32) >> 4;   // (descriptors count 16 bytes)
+            mma_ss(ts + h * 64, qd + off, kd + off, kIdescQK, k > 0);
           }
-          commit(smem_u32(&bars->s_full[x]));
-          if (last) commit(smem_u32(&bars->q_empty[x]));
+          commit(smem_u32(&bars->s_full[x][h]));
+          if (h == 1) commit(smem_u32(&bars->kv_empty[slot]));
+          if (h == 1 && last) commit(smem_u32(&bars->q_empty[x]));
         }
         __syncwarp();
       };
-      auto release = [&](uint32_t slot) {
-        if (elect_lane()) commit(smem_u32(&bars->kv_empty[slot]));
-        __syncwarp();
-      };
-      uint32_t slot_k = n_kv % Cfg::kSlots;
-      wait(&bars->kv_full[slot_k], n_kv / Cfg::kSlots, bars);
-      for (int x = 0; x < groups; ++x) {
-        wait(&bars->q_full[x], n_own[x], bars);
-        fence_after();
-        scores(x, slot_k, n_tiles == 1);
-      }
-      release(slot_k);
+      if (active) wait(&bars->q_full[x], n_own, bars);
+      scores(n_kv, 0, n_tiles == 1);
+      scores(n_kv, 1, n_tiles == 1);
       if (!kCodes && edge <= 0) warp_arrive(&bars->v_ask, lane);
 #pragma unroll 1
-      for (int i = 0; i < n_tiles && !bars->abort; ++i) {
-        const uint32_t at_v = n_kv + 1, at_k = n_kv + 2, slot_v = at_v % Cfg::kSlots;
+      for (int i = 0; i < n_tiles && !bars->abort; ++i, n_kv += 2) {
+        const uint32_t at = n_kv + 1, slot = at % Cfg::kSlots;
         const bool more = i + 1 < n_tiles;
-        slot_k = at_k % Cfg::kSlots;
-        n_kv += 2;
-        wait(&bars->kv_full[slot_v], at_v / Cfg::kSlots, bars);
+        wait(&bars->kv_full[slot], at / Cfg::kSlots, bars);
         if (!kCodes && i >= edge) wait(&bars->v_clean, n_clean++, bars);
         if (!kCodes && more && i + 1 >= edge) warp_arrive(&bars->v_ask, lane);
-#pragma unroll 1
-        for (int x = 0; x < groups; ++x) {
-          wait(&bars->p_full[x], n_p[x], bars);
-          ++n_p[x];
-          if (i == 0 && n_own[x] > 0) wait(&bars->o_free[x], n_own[x] - 1, bars);
-          fence_after();
-          if (elect_lane()) {
-            const uint32_t va = smem_u32(sKv + slot_v * Cfg::kTileBytes), to = tmem + Cfg::kColO + x * D, tp = tmem + Cfg::kColS + x * 128;
 #pragma unroll
-            for (int k = 0; k < kTileTokens / 16; ++k)
-              mma_ts(to, tp + k * 8, smem_desc(va + k * 2 * 1024, Cfg::kHalfBytes, 1024), kIdescPV, i > 0 || k > 0);
-            if (!more) commit(smem_u32(&bars->o_full[x]));
-            if (x == groups - 1) commit(smem_u32(&bars->kv_empty[slot_v]));
-          }
-          __syncwarp();
-          if (more) {
-            if (x == 0) wait(&bars->kv_full[slot_k], at_k / Cfg::kSlots, bars);
+        for (int h = 0; h < 2; ++h) {
+          if (active) {
+            wait(&bars->p_full[x][h], n_p, bars);
+            if (h == 0 && i == 0 && n_own > 0) wait(&bars->o_free[x], n_own - 1, bars);
             fence_after();
-            scores(x, slot_k, i + 2 == n_tiles);
-            if (x == groups - 1) release(slot_k);
+            if (elect_lane()) {
+              const uint64_t vd = smem_desc(smem_u32(sKv + slot * Cfg::kTileBytes), Cfg::kHalfBytes, 1024);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mma_ts(to, ts + h * 64 + k * 8, vd + (4 * h + k) * 128, kIdescPV, i > 0 || h > 0 || k > 0);
+              if (h == 0 && !more) commit(smem_u32(&bars->h_done[x]));
+              if (h == 1) commit(smem_u32(&bars->kv_empty[slot]));
+              if (h == 1 && !more) commit(smem_u32(&bars->o_full[x]));
+            }
+            __syncwarp();
+          } else if (h == 1) {
+            warp_arrive(&bars->kv_empty[slot], lane);
           }
+          if (more) scores(at + 1, h, i + 2 == n_tiles);
         }
+        if (active) ++n_p;
       }
-      for (int x = 0; x < groups; ++x) ++n_own[x];
+      if (active) ++n_own;
       warp_arrive(&bars->item_empty[n & 1], lane);
     }
   } else if (!kCodes) {
     // ------------------------------------------------------------------ V tiles at the edge
-    // The issuer asks for a tile while it works on the one before (so that the slot's barrier is in the phase waited for, and
-    // not one that the ring is yet to come to) and does not go past it without an answer.
-    const int id = tid - 320;    // 0..63
+    // The issuers ask for a tile while they work on the one before (so that the slot's barrier is in the phase waited for, and
+    // not one that the ring is yet to come to) and do not go past it without an answer.
     uint32_t n_kv = 0, n_ask = 0;
     PromptNote *notes = p.notes + (int64_t)blockIdx.x * 2 * kPtNotes;
     PromptEntry e;
@@ -390,7 +393,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         unsigned char *vt = sKv + slot * Cfg::kTileBytes;
         const int t0 = tile * kTileTokens, n_tok = min(kTileTokens, e.t_end - t0);
 #pragma unroll 1
-        for (int tok = id; tok < kTileTokens; tok += 64) {
+        for (int tok = lane; tok < kTileTokens; tok += 32) {
           if (t0 + tok <= whole) continue;
           unsigned char *row = vt + (tok >> 3) * 1024 + (tok & 7) * 128;
           if (tok < n_tok) {
@@ -408,7 +411,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       warp_arrive(&bars->item_clean[n & 1], lane);
       warp_arrive(&bars->item_empty[n & 1], lane);
     }
-  } else if (warp == 10) {
+  } else {
     // ------------------------------------------------------------------ scales of 8-bit pools: four tokens of a tile a lane
     float *sScale = reinterpret_cast<float *>(smem + Cfg::kOffScale);
     uint32_t n_tile = 0;
@@ -568,87 +571,107 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           const uint32_t b = __float_as_uint(scale);
           return (b & 0x7f800000u) ? __uint_as_float((b & 0x7fffffu) | 0x3f800000u) : 1.f;
         };
-        wait(&bars->s_full[x], n_s, bars);
-        fence_after();
-        if (active) {
-          float s[128];
-          uint32_t(&su)[4][32] = reinterpret_cast<uint32_t(&)[4][32]>(s);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, su[c]);
-          wait_ld();
-          const int t0 = tile * kTileTokens;
-          if (kCodes && general) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float4 f = factors[i];
-              s[4 * i] *= factor(f.x); s[4 * i + 1] *= factor(f.y); s[4 * i + 2] *= factor(f.z); s[4 * i + 3] *= factor(f.w);
-            }
-          }
-          if (t0 + kTileTokens - 1 > whole) {
-            const int last = limit - t0;
-#pragma unroll
-            for (int i = 0; i < 128; ++i) s[i] = i <= last ? s[i] : -INFINITY;
-          }
-          float mx[4];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            mx[c] = fmaxf(s[c * 32], s[c * 32 + 1]);
-#pragma unroll
-            for (int i = 2; i < 32; i += 2) mx[c] = fmaxf(mx[c], fmaxf(s[c * 32 + i], s[c * 32 + i + 1]));
-          }
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-          float alpha = 1.f;
-          bool rescale = false;
-          if (m_ref == -INFINITY) {
-            m_ref = top;                        // (what is there so far is zero, or about to be overwritten)
-          } else if (top > m_ref + kRescaleThreshold) {
-            alpha = fast_exp2(m_ref - top);
-            m_ref = top;
-            rescale = true;
-          }
-          if (__any_sync(0xffffffffu, rescale)) {
-            sum_a = e8::mul2(sum_a, pair(alpha, alpha));
-            sum_b = e8::mul2(sum_b, pair(alpha, alpha));
+        const int t0 = tile * kTileTokens;
+        const bool edge = t0 + kTileTokens - 1 > whole;
 #pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-              uint32_t r[16];
-              tmem_ld16(to + c * 16, r);
+        for (int h = 0; h < 2; ++h) {
+          wait(&bars->s_full[x][h], n_s, bars);
+          fence_after();
+          if (active) {
+            const float4 *fk = factors + h * 16;
+            const float2 *fv = reinterpret_cast<const float2 *>(factors + 32 + h * 16);
+            const uint64_t was_a = sum_a, was_b = sum_b;
+            uint32_t pk[32];
+            // The weights are made under the reference as it is; only if one is past 2^8 (or a row has none yet) is the maximum
+            // taken, the reference moved and the weights made once more from the scores, which are still there.
+            bool look = __any_sync(0xffffffffu, m_ref == -INFINITY);
+#pragma unroll 1
+            for (;;) {
+              float s[64];
+              uint32_t(&su)[2][32] = reinterpret_cast<uint32_t(&)[2][32]>(s);
+              tmem_ld32(ts + h * 64, su[0]);
+              tmem_ld32(ts + h * 64 + 32, su[1]);
               wait_ld();
+              if (kCodes && general) {
 #pragma unroll
-              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-              tmem_st16(to + c * 16, r);
-            }
-          }
-          const float ref = m_ref == -INFINITY ? 0.f : -m_ref;
-          const uint64_t ref2 = pair(ref, ref);
-          auto weights = [&](auto scaled) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              uint32_t pk[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                float a, b;
-                unpair(fma2(pair(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale2, ref2), a, b);
-                a = fast_exp2(a);
-                b = fast_exp2(b);
-                if (i & 1) sum_b = add2(sum_b, pair(a, b));
-                else sum_a = add2(sum_a, pair(a, b));
-                if constexpr (decltype(scaled)::value) {
-                  const float2 f = reinterpret_cast<const float2 *>(factors + 32)[c * 16 + i];
-                  a *= factor(f.x);
-                  b *= factor(f.y);
+                for (int i = 0; i < 16; ++i) {
+                  const float4 f = fk[i];
+                  s[4 * i] *= factor(f.x); s[4 * i + 1] *= factor(f.y); s[4 * i + 2] *= factor(f.z); s[4 * i + 3] *= factor(f.w);
                 }
-                pk[i] = pack_bf16(a, b);
               }
-              tmem_st16(ts + c * 16, pk);
+              if (edge) {
+                const int last = limit - t0 - h * 64;
+#pragma unroll
+                for (int i = 0; i < 64; ++i) s[i] = i <= last ? s[i] : -INFINITY;
+              }
+              if (look) {
+                float mx[2] = {s[0], s[1]};
+#pragma unroll
+                for (int i = 2; i < 64; i += 2) { mx[0] = fmaxf(mx[0], s[i]); mx[1] = fmaxf(mx[1], s[i + 1]); }
+                const float top = fmaxf(mx[0], mx[1]) * p.scale_log2;
+                float alpha = 1.f;
+                bool rescale = false;
+                if (m_ref == -INFINITY) {
+                  m_ref = top;                        // (what is there so far is zero, or about to be overwritten)
+                } else if (top > m_ref + kRescaleThreshold) {
+                  alpha = fast_exp2(m_ref - top);
+                  m_ref = top;
+                  rescale = true;
+                }
+                if (__any_sync(0xffffffffu, rescale)) {
+                  sum_a = e8::mul2(sum_a, pair(alpha, alpha));
+                  sum_b = e8::mul2(sum_b, pair(alpha, alpha));
+                  // The output has to be at rest: the half before this one is in it.  The scores that take its weights' place are
+                  // made behind it; behind an entry's last tile there are none.
+                  if (h == 0) wait(&bars->s_full[x][1], n_s, bars);
+                  else if (tile + 1 < e.tile_end) wait(&bars->s_full[x][0], n_s + 1, bars);
+                  else wait(&bars->h_done[x], n_own, bars);
+                  fence_after();
+#pragma unroll 1
+                  for (int c = 0; c < D / 16; ++c) {
+                    uint32_t r[16];
+                    tmem_ld16(to + c * 16, r);
+                    wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+                    tmem_st16(to + c * 16, r);
+                  }
+                }
+              }
+              const float ref = m_ref == -INFINITY ? 0.f : -m_ref;
+              const uint64_t ref2 = pair(ref, ref);
+              float most = 0.f;
+              auto weights = [&](auto scaled) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                  float a, b;
+                  unpair(fma2(pair(s[2 * i], s[2 * i + 1]), scale2, ref2), a, b);
+                  a = fast_exp2(a);
+                  b = fast_exp2(b);
+                  most = fmaxf(most, fmaxf(a, b));
+                  if (i & 1) sum_b = add2(sum_b, pair(a, b));
+                  else sum_a = add2(sum_a, pair(a, b));
+                  if constexpr (decltype(scaled)::value) {
+                    const float2 f = fv[i];
+                    a *= factor(f.x);
+                    b *= factor(f.y);
+                  }
+                  pk[i] = pack_bf16(a, b);
+                }
+              };
+              if (kCodes && general) weights(std::true_type());
+              else weights(std::false_type());
+              if (look || !__any_sync(0xffffffffu, most > 256.f)) break;
+              look = true;
+              sum_a = was_a;
+              sum_b = was_b;
             }
-          };
-          if (kCodes && general) weights(std::true_type());
-          else weights(std::false_type());
-          wait_st();
+            tmem_st32(ts + h * 64, pk);
+            wait_st();
+          }
+          fence_before();
+          warp_arrive(&bars->p_full[x][h], lane);
         }
-        fence_before();
-        warp_arrive(&bars->p_full[x], lane);
         if constexpr (kCodes) warp_arrive(&bars->sc_empty[n_tile % kPtScaleSlots], lane);
         if (bars->abort) break;
       }

@@ -472,7 +472,8 @@ static PromptParams prompt_params(const spx_attn_args_t *a, const PromptWs &w, u
   p.workers = sms * (tc ? 1 : 2);
   // tiles: of 128 tokens by 64 rows in fp32 arithmetic (10 us), by 256 rows on the tensor cores (1.5 us)
   p.min_range = tc ? 4 : 1;
-  p.overhead = tc ? 8 : 2;
+  p.overhead = tc ? 12 : 2;
+  p.entry_cost = tc ? 16 : 8;
   p.hdr = reinterpret_cast<PromptHeader *>(ws + w.hdr);
   p.unit_item0 = reinterpret_cast<int32_t *>(ws + w.unit_item0);
   p.unit_bad = reinterpret_cast<int32_t *>(ws + w.unit_bad);
