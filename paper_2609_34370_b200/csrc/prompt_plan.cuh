@@ -7,27 +7,25 @@
 //
 // Entries are independent, so the persistent kernel's CTAs take them through a counter, the longest first:
 // the shorter ones then fill what the longer ones leave uneven.  Where there are too few of them for that (a chunk of a
-// prompt behind a long history: 64 entries of 238 tiles), the axis of all entries' tiles is cut into ranges of equal cost
-// instead, one for each CTA; the parts of an entry that a cut crosses are joined by a second kernel.
+// prompt behind a long history: 64 entries of 238 tiles for 148 CTAs), long entries are cut into equal pieces along the tokens,
+// whose partial results a second kernel joins.  All items of a request are cut at the same tokens and are neighbours in the list,
+// so that the CTAs that read the same tokens do so together (a range of the tiles for each CTA, cut where it fell, balanced
+// better on paper and read the cache from HBM several times over: 250 to 420 us for that chunk, from board to board).
 #pragma once
 #include "common.cuh"
 
 namespace spx {
 
-constexpr int kPromptMaxWorkers = 512;     // ranges
-constexpr int kPromptMaxRanged = 8192;     // entries of a plan that is cut into ranges
 constexpr int kPromptBuckets = 1024;       // lengths the entries are sorted by (longer ones share the last)
 
 struct PromptHeader {
-  int32_t n_units;       // units of work: entries (ranged = 0) or ranges (ranged = 1)
-  int32_t ranged;
+  int32_t n_units;       // units of work: entries times kv heads
   int32_t counter;       // next unit of work
-  int32_t n_items;       // items of all units
-  int32_t n_join;        // entries to be joined (ranged plans of whole outputs)
+  int32_t n_join;        // items in pieces (of plans whose whole items go to the output)
   int32_t any_bad;       // some request's rows are to be voided
-  int32_t pad[2];
 };
 
+// A piece of an item, or a whole one, for every kv head.
 struct __align__(16) PromptEntry {
   int32_t unit;                  // request, or group
   int32_t table_row;             // block-table row
@@ -36,16 +34,16 @@ struct __align__(16) PromptEntry {
   int32_t vis0;                  // position j of the unit sees tokens 0 .. vis0 + j (causal), 0 .. vis0 (prefix)
   int32_t tile_begin, tile_end;
   int32_t t_end;                 // tokens the item's last row sees
-  int32_t slot;                  // partial result, -1: the entry is whole and goes to the output
-  int32_t g;                     // kv head (ranged plans)
+  int32_t slot;                  // partial result of kv head 0 (the others' follow), -1: the entry is whole and goes to the output
+  int32_t g;                     // kv head (filled in by the kernel that takes it)
   int32_t pad;
 };
 static_assert(sizeof(PromptEntry) == 48, "read as three 16-byte vectors");
 
-// An entry's partial results: chunk 0 in slot first, chunk j in slot next + 2 (j - 1).
+// An item in pieces: piece c of kv head g is in slot first + c * Hkv + g.
 struct __align__(16) PromptJoin {
   int32_t unit, q0, row0, rows;
-  int32_t g, first, next, nch;
+  int32_t first, pieces, pad[2];
 };
 
 // Elements of a V row that are not finite, by column: infinities of either sign, NaN in both (prompt_tc.cuh).
@@ -75,18 +73,17 @@ struct PromptParams {
   int32_t units;                      // batch or groups
   int32_t unit_rows;                  // packed rows of an item (whole positions in the tensor-core kernel)
   int32_t workers;                    // CTAs of the persistent kernel
-  int32_t min_range, overhead;        // tiles: the shortest range worth a CTA, what cuts cost
-  int32_t entry_cost;                 // of an entry's ends, in eighths of a tile
+  int32_t entry_cost, join_cost;      // of an entry's ends, of the join, in eighths of a tile
+  int32_t min_piece;                  // tiles
   PromptHeader *hdr;
   int32_t *unit_item0;                // [units + 1]
   int32_t *unit_bad;                  // [units]
   int32_t *item_tiles;                // [max_items]
-  int64_t *item_cost;                 // [max_items + 1]
-  PromptEntry *entries;               // [max_entries]
-  int32_t *range_off;                 // [workers + 1]
-  PromptJoin *join;                   // [workers]
-  int4 *entry_part;                   // prefixes: [max_items * Hkv] (first, next, chunks, 0)
-  int32_t max_items, max_entries, whole_slot0;
+  PromptEntry *entries;               // [max_items + max_pieces]
+  PromptJoin *join;                   // [max_pieces]
+  int2 *item_part;                    // prefixes: [max_items] (first slot, pieces)
+  int32_t max_items;
+  int32_t max_pieces;                 // pieces that items are cut into; times Hkv slots, in front of those of a prefix plan's whole items
   float *part_o;                      // [slot][unit_rows][D]
   float2 *part_ml;                    // [slot][unit_rows]  (m in log2 units, l)
   PromptNote *notes;                  // [workers][2][kPtNotes]  (tensor-core kernel)
@@ -138,9 +135,9 @@ __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x;
   __shared__ int64_t s_scratch[33];
-  __shared__ int s_off[kPromptMaxWorkers + 1], s_cut_e[kPromptMaxWorkers + 1], s_cut_t[kPromptMaxWorkers + 1];
   __shared__ int s_hist[kPromptBuckets];
-  __shared__ int s_level, s_longest, s_bad;
+  __shared__ int s_longest, s_bad, s_group;
+  __shared__ long long s_best;
 
   // what a unit is: first query row, positions, tokens, block-table row, whether it is to be voided
   struct Unit { int q0, m, L, row; bool bad; };
@@ -168,12 +165,12 @@ __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
     for (int r = blockIdx.x - 1; r < p.batch; r += gridDim.x - 1) {
       // its group (requests that no group holds share nothing)
       __syncthreads();
-      if (tid == 0) s_level = -1;
+      if (tid == 0) s_group = -1;
       __syncthreads();
       for (int i = tid; i < p.groups; i += blockDim.x)
-        if (p.group_indptr[i] <= r && r < p.group_indptr[i + 1]) atomicMax(&s_level, i);
+        if (p.group_indptr[i] <= r && r < p.group_indptr[i + 1]) atomicMax(&s_group, i);
       __syncthreads();
-      const int u = s_level;
+      const int u = s_group;
       if (tid == 0) p.req_group[r] = u;
       int differs = 0;
       if (u >= 0) {
@@ -193,7 +190,7 @@ __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
   }
 
   for (int i = tid; i < kPromptBuckets; i += 1024) s_hist[i] = 0;
-  if (tid == 0) { s_level = kPromptBuckets; s_longest = 0; s_bad = 0; }
+  if (tid == 0) { s_longest = 0; s_bad = 0; s_best = 0x7fffffffffffffffll; }
   __syncthreads();
 
   // items of the units
@@ -217,48 +214,83 @@ __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
   __syncthreads();
   const int NI = (int)n_items;
 
-  // tiles of the items, their sum and how many there are of each length
-  const int entry_cost = p.entry_cost;   // an entry's ends, in eighths of a tile
-  int64_t cost_sum = 0, tile_sum = 0;
-  for (int base = 0; base < NI; base += 1024) {
-    const int i = base + tid;
-    int tiles = 0;
-    if (i < NI) {
-      const int u = last_at_most(p.unit_item0, p.units, i);   // (units without items start where the next one does)
-      const Unit x = unit_of(u);
-      const int64_t row0 = (int64_t)(i - p.unit_item0[u]) * p.unit_rows;
-      const int64_t last = (min(row0 + p.unit_rows, (int64_t)x.m * p.G) - 1) / p.G;
-      const int64_t seen = p.groups ? (int64_t)x.L : (int64_t)x.L - x.m + last + 1;
-      tiles = (int)((seen + kTileTokens - 1) / kTileTokens);
-      p.item_tiles[i] = tiles;
-      atomicAdd(&s_hist[min(tiles, kPromptBuckets) - 1], 1);
-      atomicMax(&s_longest, tiles);
-    }
-    const int64_t off = scan_1024(i < NI ? 8 * (int64_t)tiles + entry_cost : 0, s_scratch, total) + cost_sum;
-    cost_sum += total;
-    if (i < NI) p.item_cost[i] = off;
-    scan_1024(tiles, s_scratch, total);
-    tile_sum += total;
+  // tiles of the items, and how many there are of each length
+  for (int i = tid; i < NI; i += 1024) {
+    const int u = last_at_most(p.unit_item0, p.units, i);   // (units without items start where the next one does)
+    const Unit x = unit_of(u);
+    const int64_t row0 = (int64_t)(i - p.unit_item0[u]) * p.unit_rows;
+    const int64_t last = (min(row0 + p.unit_rows, (int64_t)x.m * p.G) - 1) / p.G;
+    const int64_t seen = p.groups ? (int64_t)x.L : (int64_t)x.L - x.m + last + 1;
+    const int tiles = (int)((seen + kTileTokens - 1) / kTileTokens);
+    p.item_tiles[i] = tiles;
+    atomicAdd(&s_hist[min(tiles, kPromptBuckets) - 1], 1);
+    atomicMax(&s_longest, tiles);
   }
-  if (tid == 0) p.item_cost[NI] = cost_sum;
   __syncthreads();
 
-  // How long does taking whole entries, the longest first, take?  Entries up to the level x fill what those above it leave
-  // uneven if there are x tiles of them for each worker; past that the last entries are x long.
-  const int64_t N = (int64_t)NI * p.Hkv, T = tile_sum * p.Hkv;
+  // Pieces of at most `piece` tiles: each warp works out what cutting the longest item into n would take (in eighths of a tile): the
+  // work for each CTA, the longest piece, and the rounds that the pieces of the longer half need.  (Items past the last
+  // bucket count as long as the longest.)
+  const int longest = s_longest;
+  auto pieces_of = [](int tiles, int piece) -> int { return (tiles + piece - 1) / piece; };
   {
-    int64_t work = tid < kPromptBuckets ? (int64_t)s_hist[tid] * (tid + 1) * p.Hkv : 0;
-    const int64_t below = scan_1024(work, s_scratch, total) + work;
-    if (below >= (int64_t)p.workers * (tid + 1)) atomicMin(&s_level, tid + 1);
+    const int warp = tid >> 5, lane = tid & 31;
+    const int n = warp < 16 ? warp + 1 : warp < 24 ? 16 + 4 * (warp - 15) : 48 + 16 * (warp - 23);   // 1 .. 16, 20 .. 48, 64 .. 176
+    const int piece = max(max(1, p.min_piece), pieces_of(longest, n));
+    int64_t work = 0, cut = 0, most = 0, big = 0, big_len = 0;
+    if (n == 1 || pieces_of(longest, n) >= p.min_piece) {
+      for (int b = lane; b < min(longest, kPromptBuckets); b += 32) {
+        const int64_t count = (int64_t)s_hist[b] * p.Hkv;
+        if (count == 0) continue;
+        const int tiles = b == kPromptBuckets - 1 ? longest : b + 1, k = pieces_of(tiles, piece), len = pieces_of(tiles, k);
+        work += count * (8 * (int64_t)tiles + (int64_t)k * p.entry_cost);
+        if (k > 1) cut += count * k;
+        most = max(most, (int64_t)len);
+        if (2 * len > piece) { big += count * k; big_len += count * k * len; }
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      work += __shfl_xor_sync(0xffffffffu, work, o); cut += __shfl_xor_sync(0xffffffffu, cut, o);
+      big += __shfl_xor_sync(0xffffffffu, big, o); big_len += __shfl_xor_sync(0xffffffffu, big_len, o);
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    }
+    if (lane == 0 && work > 0 && cut <= (int64_t)p.max_pieces * p.Hkv) {
+      int64_t time = max(work / p.workers, 8 * most + p.entry_cost);
+      if (big > 0) time = max(time, (big + p.workers - 1) / p.workers * (8 * big_len / big + p.entry_cost));
+      if (cut > 0) time += p.join_cost;
+      atomicMin(&s_best, (long long)(time << 8 | n));
+    }
+  }
+  __syncthreads();
+  const int best = NI > 0 ? (int)(s_best & 255) : 1, piece = max(max(1, p.min_piece), pieces_of(max(longest, 1), best));
+  const int piece_of_all = best == 1 ? 1 << 30 : piece;   // (tiles are below 2^24)
+
+  // places of the pieces: sorted by length, the longest first; their slots
+  __syncthreads();
+  if (best > 1) {   // lengths of pieces now, not of items
+    for (int i = tid; i < kPromptBuckets; i += 1024) s_hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < NI; i += 1024) {
+      const int tiles = p.item_tiles[i], k = pieces_of(tiles, piece_of_all);
+      atomicAdd(&s_hist[min(pieces_of(tiles, k), kPromptBuckets) - 1], k);
+    }
     __syncthreads();
   }
-  const int64_t even = (T + p.workers - 1) / p.workers;
-  const int64_t whole = N <= p.workers ? s_longest : min(even + s_level, (N + p.workers - 1) / p.workers * (int64_t)s_longest);
-  const int n_ranges = (int)max((int64_t)1, min((int64_t)p.workers, T / p.min_range));
-  const int64_t cut = (T + n_ranges - 1) / n_ranges + p.overhead;
-  const bool ranged = N <= kPromptMaxRanged && N > 0 && cut < whole;
-
-  auto entry_of = [&](int i) -> PromptEntry {
+  const int place = (int)scan_1024(s_hist[kPromptBuckets - 1 - tid], s_scratch, total);
+  const int n_entries = (int)total;
+  __syncthreads();
+  s_hist[kPromptBuckets - 1 - tid] = place;
+  __syncthreads();
+  int64_t slots = 0, joins = 0;
+  for (int base = 0; base < NI; base += 1024) {
+    const int i = base + tid;
+    const int tiles = i < NI ? p.item_tiles[i] : 0, k = i < NI ? pieces_of(tiles, piece_of_all) : 0;
+    const int64_t slot = scan_1024(k > 1 ? k : 0, s_scratch, total) + slots;
+    slots += total;
+    const int64_t at_join = scan_1024(k > 1 ? 1 : 0, s_scratch, total) + joins;
+    joins += total;
+    if (i >= NI) continue;
     PromptEntry e;
     const int u = last_at_most(p.unit_item0, p.units, i);
     const Unit x = unit_of(u);
@@ -266,106 +298,34 @@ __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
     e.unit = u; e.table_row = x.row; e.q0 = x.q0;
     e.row0 = (int)row0; e.rows = (int)min((int64_t)p.unit_rows, all - row0);
     e.vis0 = p.groups ? x.L - 1 : x.L - x.m;
-    e.tile_begin = 0; e.tile_end = p.item_tiles[i];
     e.t_end = p.groups ? x.L : x.L - x.m + (e.row0 + e.rows - 1) / p.G + 1;
-    e.slot = -1; e.g = 0; e.pad = 0;
-    return e;
-  };
-
-  if (!ranged) {
-    // sorted by length, the longest first: a bucket's first place, then a place for each of its entries
-    const int mine = tid < kPromptBuckets ? s_hist[kPromptBuckets - 1 - tid] : 0;
-    const int place = (int)scan_1024(mine, s_scratch, total);
-    __syncthreads();
-    if (tid < kPromptBuckets) s_hist[kPromptBuckets - 1 - tid] = place;
-    __syncthreads();
-    for (int i = tid; i < NI; i += 1024) {
-      PromptEntry e = entry_of(i);
-      const int at = atomicAdd(&s_hist[min(e.tile_end, kPromptBuckets) - 1], 1);
-      if (p.groups) {
-        e.slot = p.whole_slot0 + i * p.Hkv;   // plus the kv head, which the kernel knows
-        for (int g = 0; g < p.Hkv; ++g) p.entry_part[(int64_t)i * p.Hkv + g] = make_int4(e.slot + g, 0, 1, 0);
-      }
+    e.g = 0; e.pad = 0;
+    const int first = k > 1 ? (int)slot * p.Hkv : (p.max_pieces + i) * p.Hkv;   // (behind the pieces' slots: whole items of a prefix plan)
+    const int len = pieces_of(tiles, k);
+    int at = atomicAdd(&s_hist[min(len, kPromptBuckets) - 1], k);
+    for (int c = 0; c < k; ++c, ++at) {
+      e.tile_begin = min(c * len, tiles); e.tile_end = min(e.tile_begin + len, tiles);
+      e.slot = k > 1 || p.groups ? first + c * p.Hkv : -1;
       p.entries[at] = e;
     }
-  } else {
-    // cuts at equal steps of the cost axis of all entries (item, kv head), moved onto an entry's end if close to one
-    const int snap = max(1, min(p.min_range / 2, 3));
-    if (tid <= n_ranges) {
-      int e = 0, t = 0;
-      if (tid == n_ranges) {
-        e = (int)N;
-      } else if (tid > 0) {
-        const int64_t x = (int64_t)((double)cost_sum * p.Hkv * tid / n_ranges);
-        const int i = last_at_most(p.item_cost, NI, x / p.Hkv);
-        const int tiles = p.item_tiles[i], c = 8 * tiles + entry_cost;
-        const int64_t rel = x - p.item_cost[i] * p.Hkv;
-        int g = (int)min(rel / c, (int64_t)p.Hkv - 1);
-        t = (int)max((int64_t)0, (rel - (int64_t)g * c - entry_cost) / 8);
-        if (t < snap) t = 0;
-        else if (tiles - t < snap) { t = 0; ++g; }
-        e = i * p.Hkv + g;
-      }
-      s_cut_e[tid] = e; s_cut_t[tid] = t;
+    if (p.groups) p.item_part[i] = make_int2(first, k);
+    if (k > 1) {
+      PromptJoin j;
+      j.unit = u; j.q0 = e.q0; j.row0 = e.row0; j.rows = e.rows; j.first = first; j.pieces = k; j.pad[0] = j.pad[1] = 0;
+      p.join[at_join] = j;
     }
-    __syncthreads();
-    int n = 0;
-    if (tid < n_ranges) n = max(0, s_cut_e[tid + 1] - s_cut_e[tid] + (s_cut_t[tid + 1] > 0 ? 1 : 0));
-    if (tid < n_ranges && s_cut_e[tid + 1] == s_cut_e[tid] && s_cut_t[tid + 1] <= s_cut_t[tid]) n = 0;   // two cuts in one place
-    const int off = (int)scan_1024(n, s_scratch, total);
-    if (tid <= n_ranges) { s_off[tid] = tid < n_ranges ? off : (int)total; p.range_off[tid] = s_off[tid]; }
-    __syncthreads();
-    // (an entry that a cut opens: its first part belongs to the range before the cut, whose last entry it is)
-    for (int k = tid; k < s_off[n_ranges]; k += 1024) {
-      const int c = last_at_most(s_off, n_ranges, k);   // (empty ranges start where the next one does)
-      const int e = s_cut_e[c] + k - s_off[c];
-      PromptEntry x = entry_of(e / p.Hkv);
-      x.g = e % p.Hkv;
-      const int tiles = x.tile_end;
-      if (e == s_cut_e[c]) x.tile_begin = s_cut_t[c];
-      if (e == s_cut_e[c + 1]) x.tile_end = s_cut_t[c + 1];
-      if (x.tile_begin > 0) x.slot = 2 * c;
-      else if (x.tile_end < tiles) x.slot = 2 * c + 1;
-      else if (p.groups) {
-        x.slot = p.whole_slot0 + e;
-        p.entry_part[e] = make_int4(x.slot, 0, 1, 0);
-      }
-      p.entries[k] = x;
-    }
-  }
-  // the entries that cuts open: the first cut inside one tells how many there are
-  int joins = 0;
-  if (ranged && tid >= 1 && tid < n_ranges && s_cut_t[tid] > 0) {
-    // the first cut in the entry, and the one whose range is not empty among equal ones
-    const bool first = s_cut_e[tid - 1] != s_cut_e[tid] || s_cut_t[tid - 1] == 0;
-    if (first) joins = 1;
-  }
-  const int at = (int)scan_1024(joins, s_scratch, total);
-  const int n_join = ranged ? (int)total : 0;
-  if (joins) {
-    const int e = s_cut_e[tid];
-    int nch = 1;
-    for (int c = tid; c < n_ranges && s_cut_e[c] == e && s_cut_t[c] > 0; ++c) ++nch;
-    const PromptEntry x = entry_of(e / p.Hkv);
-    PromptJoin j;
-    j.unit = x.unit; j.q0 = x.q0; j.row0 = x.row0; j.rows = x.rows; j.g = e % p.Hkv;
-    j.first = 2 * (tid - 1) + 1; j.next = 2 * tid; j.nch = nch;
-    if (p.groups) p.entry_part[e] = make_int4(j.first, j.next, nch, 0);
-    p.join[at] = j;
   }
   if (tid == 0) {
-    p.hdr->n_units = ranged ? n_ranges : (int)N;
-    p.hdr->ranged = ranged;
+    p.hdr->n_units = n_entries * p.Hkv;
     p.hdr->counter = 0;
-    p.hdr->n_items = NI;
-    p.hdr->n_join = n_join;
+    p.hdr->n_join = (int)joins;
     p.hdr->any_bad = s_bad;
     if (s_bad) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   }
 }
 
-// Joins the parts of the entries that cuts opened (see combine_kernel) and voids the rows of requests with a bad length or page id.
-// Blocks (b, y): entry b of the list, items (row, four columns) y * 256 + t of it.
+// Joins the pieces of items (see combine_kernel) and voids the rows of requests with a bad length or page id.
+// Blocks (b, y): kv head b mod Hkv of item b / Hkv of the list, (row, four columns) y * 256 + t of it.
 template <typename T>
 __global__ void __launch_bounds__(256) prompt_join_kernel(PromptParams p) {
   SPX_TL_SCOPE(kTlCombine);
@@ -373,28 +333,29 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(PromptParams p) {
   T *out = reinterpret_cast<T *>(p.out);
   const int vecs = p.D / 4;
   const int n_join = p.hdr->n_join, any_bad = p.hdr->any_bad;
-  for (int li = blockIdx.x; li < n_join; li += gridDim.x) {
-    const PromptJoin e = p.join[li];
+  for (int li = blockIdx.x; li < n_join * p.Hkv; li += gridDim.x) {
+    const PromptJoin e = p.join[li / p.Hkv];
+    const int g = li % p.Hkv;
     if (p.unit_bad[e.unit]) continue;
     for (int item = blockIdx.y * blockDim.x + threadIdx.x; item < e.rows * vecs; item += gridDim.y * blockDim.x) {
       const int row = item / vecs, dv = item % vecs;
       float mstar = -INFINITY, lstar = 0.f;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto slot_row = [&](int c) -> int64_t { return (int64_t)(c == 0 ? e.first : e.next + 2 * (c - 1)) * p.unit_rows + row; };
-      for (int c0 = 0; c0 < e.nch; c0 += 4) {
+      auto slot_row = [&](int c) -> int64_t { return (int64_t)(e.first + c * p.Hkv + g) * p.unit_rows + row; };
+      for (int c0 = 0; c0 < e.pieces; c0 += 4) {
         // four chunks' loads in flight at a time, their maximum taken first
         float2 ml[4];
         float4 o[4];
         float top = mstar;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const int64_t at = slot_row(min(c0 + u, e.nch - 1));
+          const int64_t at = slot_row(min(c0 + u, e.pieces - 1));
           ml[u] = p.part_ml[at];
           o[u] = *reinterpret_cast<const float4 *>(p.part_o + at * p.D + dv * 4);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          if (c0 + u < e.nch) top = fmaxf(top, ml[u].x);
+          if (c0 + u < e.pieces) top = fmaxf(top, ml[u].x);
         if (mstar != -INFINITY && top > mstar) {
           const float w = fast_exp2(mstar - top);
           lstar = rescaled_sum(lstar, mstar - top);
@@ -403,13 +364,13 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(PromptParams p) {
         mstar = top;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          if (c0 + u >= e.nch || (ml[u].x == -INFINITY && ml[u].y == 0.f)) continue;   // (saw nothing)
+          if (c0 + u >= e.pieces || (ml[u].x == -INFINITY && ml[u].y == 0.f)) continue;   // (saw nothing)
           const float d = ml[u].x == -INFINITY ? 0.f : ml[u].x - mstar, w = fast_exp2(d);
           lstar += rescaled_sum(ml[u].y, d);
           acc.x += w * o[u].x; acc.y += w * o[u].y; acc.z += w * o[u].z; acc.w += w * o[u].w;
         }
       }
-      const int pr = e.row0 + row, h = e.g * p.G + pr % p.G;
+      const int pr = e.row0 + row, h = g * p.G + pr % p.G;
       const int64_t qrow = e.q0 + pr / p.G, at = (qrow * p.Hq + h) * p.D + dv * 4;
       const float inv = 1.f / lstar;
       st_from_float(out, at + 0, acc.x * inv);
@@ -465,16 +426,16 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnParams a, PromptPa
       if (dv == 0 && a.lse) a.lse[qh] = __int_as_float(0x7fc00000);
       continue;
     }
-    int4 part = make_int4(0, 0, 0, 0);
+    int2 part = make_int2(0, 0);     // first slot, pieces
     int64_t prow = 0;
     if (tiles > 0) {
       const int64_t row = row0 + (int64_t)j * G + hg;
-      part = p.entry_part[(p.unit_item0[u] + row / p.unit_rows) * p.Hkv + g];
+      part = p.item_part[p.unit_item0[u] + row / p.unit_rows];
       prow = row % p.unit_rows;
     }
     float mstar = -INFINITY, lstar = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int n = nch + part.z;
+    const int n = nch + part.y;
     for (int c0 = 0; c0 < n; c0 += 4) {
       float2 ml[4];
       float4 o[4];
@@ -488,7 +449,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnParams a, PromptPa
           const int64_t s = (int64_t)(base + c + nch) * a.rows_cap + j * G + hg;
           ml_at = a.part_ml + s; o_at = a.part_o + s * a.D;
         } else {
-          const int64_t s = (int64_t)(c == 0 ? part.x : part.y + 2 * (c - 1)) * p.unit_rows + prow;
+          const int64_t s = (int64_t)(part.x + c * p.Hkv + g) * p.unit_rows + prow;
           ml_at = p.part_ml + s; o_at = p.part_o + s * a.D;
         }
         ml[i] = *ml_at;

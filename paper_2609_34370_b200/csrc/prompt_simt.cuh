@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
   const KV *Kc = reinterpret_cast<const KV *>(p.k_cache), *Vc = reinterpret_cast<const KV *>(p.v_cache);
   T *out = reinterpret_cast<T *>(p.out);
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  const int n_units = p.hdr->n_units, ranged = p.hdr->ranged;
+  const int n_units = p.hdr->n_units;
 
   for (;;) {
     __syncthreads();
@@ -63,11 +63,10 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
     __syncthreads();
     const int unit = s_unit;
     if (unit >= n_units) break;
-    const int e0 = ranged ? p.range_off[unit] : unit / p.Hkv, e1 = ranged ? p.range_off[unit + 1] : e0 + 1;
-    for (int ei = e0; ei < e1; ++ei) {
-      const PromptEntry e = p.entries[ei];
-      const int g = ranged ? e.g : unit % p.Hkv;
-      const int slot = ranged || e.slot < 0 ? e.slot : e.slot + g;
+    {
+      const PromptEntry e = p.entries[unit / p.Hkv];
+      const int g = unit % p.Hkv;
+      const int slot = e.slot < 0 ? -1 : e.slot + g;
       const int32_t *table = p.block_table + (int64_t)e.table_row * p.max_pages_per_req;
       const int t_begin = e.tile_begin * kTileTokens, t_end = min(e.t_end, e.tile_end * kTileTokens);
       const bool causal = p.groups == 0;

@@ -58,6 +58,7 @@ struct PtCfg {
 
 struct PtBars {
   uint64_t kv_full[8], kv_empty[8], q_full[2], q_empty[2], s_full[2][2], p_full[2][2], h_done[2], o_full[2], o_free[2], item_full[2], item_empty[2], v_ask, v_clean, item_clean[2];
+  uint64_t turn[2][4];
   uint64_t raw_full[6], raw_empty[6], sc_full[kPtScaleSlots], sc_empty[kPtScaleSlots];
   PromptEntry item[2];
   int32_t notes[2];
@@ -97,6 +98,21 @@ __device__ __forceinline__ void wait(uint64_t *b, uint32_t parity, PtBars *bars)
     }
     if (__any_sync(0xffffffffu, late || bars->abort)) return;
   }
+}
+// (volatile: a batch of them is issued in a row, while the one before is made use of)
+__device__ __forceinline__ float exp2_in_turn(float x) {
+  float y;
+  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 32 bytes: a whole sector, where the address allows it
+__device__ __forceinline__ void store_sector(void *at, const uint32_t (&r)[8], bool aligned) {
+  if (!aligned) {
+    *reinterpret_cast<uint4 *>(at) = make_uint4(r[0], r[1], r[2], r[3]);
+    *(reinterpret_cast<uint4 *>(at) + 1) = make_uint4(r[4], r[5], r[6], r[7]);
+    return;
+  }
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 // one arrival for the warp, behind what its lanes did
 __device__ __forceinline__ void warp_arrive(uint64_t *b, int lane) {
@@ -177,6 +193,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       mbar_init(&bars->item_clean[b], kCodes ? 4 : 1);
       bars->notes[b] = 0;
     }
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) mbar_init(&bars->turn[i >> 2][i & 3], 1);
     mbar_init(&bars->v_ask, 2); mbar_init(&bars->v_clean, 1);
     bars->abort = 0;
     bars->dev_status = p.dev_status;
@@ -211,7 +229,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Split::kOther));
   if (warp == 8) {
     // ------------------------------------------------------------------ producer
-    const int n_units = p.hdr->n_units, ranged = p.hdr->ranged;
+    const int n_units = p.hdr->n_units;
     const int pages_per_tile = kTileTokens >> p.log2P, tiles_per_group = 32 / pages_per_tile;
     uint32_t n_item = 0, n_kv = 0, n_q[2] = {0, 0};
     auto take = [&]() -> int {
@@ -224,14 +242,10 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       const int unit = __shfl_sync(0xffffffffu, unit_next, 0);
       if (unit >= n_units || bars->abort) break;
       unit_next = take();    // in flight until this one is done
-      const int e0 = ranged ? p.range_off[unit] : unit / p.Hkv, e1 = ranged ? p.range_off[unit + 1] : e0 + 1;
-#pragma unroll 1
-      for (int ei = e0; ei < e1; ++ei, ++n_item) {
-        PromptEntry e = p.entries[ei];
-        if (!ranged) {
-          e.g = unit % p.Hkv;
-          if (e.slot >= 0) e.slot += e.g;
-        }
+      {
+        PromptEntry e = p.entries[unit / p.Hkv];
+        e.g = unit % p.Hkv;
+        if (e.slot >= 0) e.slot += e.g;
         wait(&bars->item_empty[n_item & 1], (n_item >> 1) ^ 1, bars);
         if (lane == 0) { bars->item[n_item & 1] = e; bars->notes[n_item & 1] = 0; }
         warp_arrive(&bars->item_full[n_item & 1], lane);
@@ -300,6 +314,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           }
           if (bars->abort) break;
         }
+        ++n_item;
       }
     }
     // no more: an entry of no unit
@@ -535,9 +550,10 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
     const uint32_t ts = tmem + Cfg::kColS + x * 128 + lane_addr, to = tmem + Cfg::kColO + x * D + lane_addr;
     const PromptNote *notes = p.notes + (int64_t)blockIdx.x * 2 * kPtNotes;
     __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(p.out);
+    const bool sectors = (reinterpret_cast<uintptr_t>(out) & 31) == 0;
     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2);
     const float *sScale = reinterpret_cast<const float *>(smem + Cfg::kOffScale);
-    uint32_t n_s = 0, n_own = 0, n_tile = 0;
+    uint32_t n_s = 0, n_own = 0, n_tile = 0, n_turn = 0;
     PromptEntry e;
     for (uint32_t n = 0; next_item(n, e); ++n) {
       const int rows = min(e.rows - x * half_rows, half_rows);
@@ -556,7 +572,11 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       const bool active = quad * 32 < rows, valid = row < rows;
       const int limit = valid ? (causal ? e.vis0 + pr / p.G : e.vis0) : e.vis0 + (causal ? e.row0 / p.G : 0);   // last token the row sees
       const int whole = causal ? e.vis0 + (e.row0 + x * half_rows) / p.G : e.vis0;                               // ... and every row of the group
+      // The warp of the other group on the same scheduler takes turns with this one at the exponentials: left alone the two fall into step, at the
+      // exponential unit together and away from it together.
+      const bool turns = e.rows > half_rows + quad * 32;
       float m_ref = -INFINITY;
+      bool fresh = true;          // some row of the warp has no reference yet
       uint64_t sum_a = pair(0.f, 0.f), sum_b = sum_a;
 #pragma unroll 1
       for (int tile = e.tile_begin; tile < e.tile_end; ++tile, ++n_s, ++n_tile) {
@@ -584,7 +604,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
             uint32_t pk[32];
             // The weights are made under the reference as it is; only if one is past 2^8 (or a row has none yet) is the maximum
             // taken, the reference moved and the weights made once more from the scores, which are still there.
-            bool look = __any_sync(0xffffffffu, m_ref == -INFINITY);
+            bool look = fresh, held = false;
 #pragma unroll 1
             for (;;) {
               float s[64];
@@ -640,24 +660,37 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
               }
               const float ref = m_ref == -INFINITY ? 0.f : -m_ref;
               const uint64_t ref2 = pair(ref, ref);
+              if (look) fresh = __any_sync(0xffffffffu, m_ref == -INFINITY);
               float most = 0.f;
+              if (turns && !held) wait(&bars->turn[x][quad], x == 0 ? n_turn ^ 1 : n_turn, bars);
               auto weights = [&](auto scaled) {
+                constexpr int kBatch = 16, kHandOn = 48;
+                auto consume = [&](int at) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                  float a, b;
-                  unpair(fma2(pair(s[2 * i], s[2 * i + 1]), scale2, ref2), a, b);
-                  a = fast_exp2(a);
-                  b = fast_exp2(b);
-                  most = fmaxf(most, fmaxf(a, b));
-                  if (i & 1) sum_b = add2(sum_b, pair(a, b));
-                  else sum_a = add2(sum_a, pair(a, b));
-                  if constexpr (decltype(scaled)::value) {
-                    const float2 f = fv[i];
-                    a *= factor(f.x);
-                    b *= factor(f.y);
+                  for (int i = 0; i < kBatch / 2; ++i) {
+                    float a = s[at + 2 * i], b = s[at + 2 * i + 1];
+                    most = fmaxf(most, fmaxf(a, b));
+                    if (i & 1) sum_b = add2(sum_b, pair(a, b));
+                    else sum_a = add2(sum_a, pair(a, b));
+                    if constexpr (decltype(scaled)::value) {
+                      const float2 f = fv[at / 2 + i];
+                      a *= factor(f.x);
+                      b *= factor(f.y);
+                    }
+                    pk[at / 2 + i] = pack_bf16(a, b);
                   }
-                  pk[i] = pack_bf16(a, b);
+                };
+#pragma unroll
+                for (int at = 0; at < 64; at += kBatch) {
+                  // (handed on a batch early: the other warp is a hundred cycles in coming)
+                  if (at == kHandOn && turns && !held) { warp_arrive(&bars->turn[x ^ 1][quad], lane); ++n_turn; held = true; }
+#pragma unroll
+                  for (int i = 0; i < kBatch; i += 2) unpair(fma2(pair(s[at + i], s[at + i + 1]), scale2, ref2), s[at + i], s[at + i + 1]);
+#pragma unroll
+                  for (int i = 0; i < kBatch; ++i) s[at + i] = exp2_in_turn(s[at + i]);
+                  if (at > 0) consume(at - kBatch);
                 }
+                consume(64 - kBatch);
               };
               if (kCodes && general) weights(std::true_type());
               else weights(std::false_type());
@@ -708,20 +741,16 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
             }
           }
           if (valid && e.slot < 0) {
-            __nv_bfloat16 *dst = out + qh * D + c * 32;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              uint4 o;
-              o.x = pack_bf16(__uint_as_float(r[8 * v + 0]) * inv, __uint_as_float(r[8 * v + 1]) * inv);
-              o.y = pack_bf16(__uint_as_float(r[8 * v + 2]) * inv, __uint_as_float(r[8 * v + 3]) * inv);
-              o.z = pack_bf16(__uint_as_float(r[8 * v + 4]) * inv, __uint_as_float(r[8 * v + 5]) * inv);
-              o.w = pack_bf16(__uint_as_float(r[8 * v + 6]) * inv, __uint_as_float(r[8 * v + 7]) * inv);
-              *reinterpret_cast<uint4 *>(dst + v * 8) = o;
+            for (int v = 0; v < 2; ++v) {
+              uint32_t o[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[i] = pack_bf16(__uint_as_float(r[16 * v + 2 * i]) * inv, __uint_as_float(r[16 * v + 2 * i + 1]) * inv);
+              store_sector(out + qh * D + c * 32 + v * 16, o, sectors);
             }
           } else if (valid) {
-            float *dst = p.part_o + part * D + c * 32;
 #pragma unroll
-            for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4 *>(dst + v * 4) = make_uint4(r[4 * v], r[4 * v + 1], r[4 * v + 2], r[4 * v + 3]);
+            for (int v = 0; v < 4; ++v) store_sector(p.part_o + part * D + c * 32 + v * 8, reinterpret_cast<const uint32_t(&)[8]>(r[8 * v]), true);
           }
           __syncwarp();
         }

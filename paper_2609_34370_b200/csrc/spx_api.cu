@@ -114,8 +114,8 @@ constexpr int kPlanSmCount = 148;  // workspace sizing must not depend on a devi
 // ---------------------------------------------------------------------------------------------
 // The plan and the partial results of the attention of many rows (prompts; the prefixes of groups).
 struct PromptWs {
-  size_t hdr, unit_item0, unit_bad, item_tiles, item_cost, entries, range_off, join, entry_part, req_group, group_tiles, req_flag, part_ml, part_o, notes, total;
-  int32_t units, unit_rows, workers, max_items, max_entries, whole_slot0;
+  size_t hdr, unit_item0, unit_bad, item_tiles, entries, join, item_part, req_group, group_tiles, req_flag, part_ml, part_o, notes, total;
+  int32_t units, unit_rows, workers, max_items, max_pieces;
   bool fits;
 };
 struct AttnWs {
@@ -187,23 +187,21 @@ static PromptWs prompt_ws_layout(const spx_attn_args_t *a) {
   w.unit_rows = tc ? 2 * (128 / G) * G : kPsRows;
   w.workers = kPlanSmCount * (tc ? 1 : 2);
   const int64_t items = (int64_t)a->total_q * G / w.unit_rows + w.units;
-  const int64_t slots = 2 * (int64_t)w.workers + (prefixes ? items * a->num_kv_heads : 0);
-  w.fits = items <= (1 << 22) && items * a->num_kv_heads <= 0x7fffffff && slots <= (1 << 24);
+  // pieces of all kv heads: two for each worker, so that a cut always leaves every worker something to do
+  w.max_pieces = (2 * w.workers + a->num_kv_heads - 1) / a->num_kv_heads;
+  const int64_t slots = ((int64_t)w.max_pieces + (prefixes ? items : 0)) * a->num_kv_heads;
+  w.fits = items <= (1 << 22) && slots <= (1 << 24) && (items + w.max_pieces) * a->num_kv_heads <= 0x7fffffff;
   if (!w.fits) return w;
   w.max_items = (int)items;
-  const int64_t ranged = items * a->num_kv_heads;
-  const int64_t entries = (ranged < kPromptMaxRanged ? ranged : kPromptMaxRanged) + w.workers;
-  w.max_entries = (int)(entries > items ? entries : items);
-  w.whole_slot0 = 2 * w.workers;
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
   w.hdr = take(sizeof(PromptHeader));
   w.unit_item0 = take(4 * ((size_t)w.units + 1)); w.unit_bad = take(4 * (size_t)w.units);
-  w.item_tiles = take(4 * (size_t)items); w.item_cost = take(8 * ((size_t)items + 1));
-  w.entries = take(sizeof(PromptEntry) * (size_t)w.max_entries);
-  w.range_off = take(4 * ((size_t)w.workers + 1)); w.join = take(sizeof(PromptJoin) * (size_t)w.workers);
+  w.item_tiles = take(4 * (size_t)items);
+  w.entries = take(sizeof(PromptEntry) * (size_t)(items + w.max_pieces));
+  w.join = take(sizeof(PromptJoin) * (size_t)w.max_pieces);
   if (prefixes) {
-    w.entry_part = take(sizeof(int4) * (size_t)ranged);
+    w.item_part = take(sizeof(int2) * (size_t)items);
     w.req_group = take(4 * (size_t)a->batch); w.group_tiles = take(4 * (size_t)w.units); w.req_flag = take(4 * (size_t)a->batch);
   }
   w.part_ml = take(sizeof(float2) * (size_t)slots * w.unit_rows);
@@ -470,20 +468,19 @@ static PromptParams prompt_params(const spx_attn_args_t *a, const PromptWs &w, u
   const bool tc = prompt_tensor_cores(a);
   const int sms = dev.num_sms < kPlanSmCount ? dev.num_sms : kPlanSmCount;
   p.workers = sms * (tc ? 1 : 2);
-  // tiles: of 128 tokens by 64 rows in fp32 arithmetic (10 us), by 256 rows on the tensor cores (1.5 us)
-  p.min_range = tc ? 4 : 1;
-  p.overhead = tc ? 12 : 2;
+  // in eighths of a tile: of 128 tokens by 256 rows on the tensor cores (2 us; an entry's ends 4, the join 12), by 64 rows in fp32
+  // arithmetic (10 us)
   p.entry_cost = tc ? 16 : 8;
+  p.join_cost = tc ? 48 : 8;
+  p.min_piece = tc ? 4 : 1;
   p.hdr = reinterpret_cast<PromptHeader *>(ws + w.hdr);
   p.unit_item0 = reinterpret_cast<int32_t *>(ws + w.unit_item0);
   p.unit_bad = reinterpret_cast<int32_t *>(ws + w.unit_bad);
   p.item_tiles = reinterpret_cast<int32_t *>(ws + w.item_tiles);
-  p.item_cost = reinterpret_cast<int64_t *>(ws + w.item_cost);
   p.entries = reinterpret_cast<PromptEntry *>(ws + w.entries);
-  p.range_off = reinterpret_cast<int32_t *>(ws + w.range_off);
   p.join = reinterpret_cast<PromptJoin *>(ws + w.join);
-  p.entry_part = reinterpret_cast<int4 *>(ws + w.entry_part);
-  p.max_items = w.max_items; p.max_entries = w.max_entries; p.whole_slot0 = w.whole_slot0;
+  p.item_part = reinterpret_cast<int2 *>(ws + w.item_part);
+  p.max_items = w.max_items; p.max_pieces = w.max_pieces;
   p.part_ml = reinterpret_cast<float2 *>(ws + w.part_ml);
   p.part_o = reinterpret_cast<float *>(ws + w.part_o);
   p.notes = reinterpret_cast<PromptNote *>(ws + w.notes);
