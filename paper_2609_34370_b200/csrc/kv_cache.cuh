@@ -1,14 +1,17 @@
 // Cache maintenance around the verify step: append the new positions' K/V into their pages,
 // shrink the lengths by the rejected drafts afterwards.
 #pragma once
+#include <type_traits>
+
 #include "common.cuh"
+#include "rotate.cuh"
 
 namespace spx {
 
 constexpr int kRopeMaxHeadDim = 512;
 constexpr int kAppendThreads = 256;
-constexpr int kAppendRows = 16;         // new rows of a block, at most
-constexpr int kAppendAngles = 1024;     // (row, pair) angles a block keeps: 16 rows of 128 elements, 4 of 512
+constexpr int kAppendRows = 8;          // new rows of a block, at most
+constexpr int kAppendAngles = 1024;     // (row, pair) angles a block keeps: 8 rows of 256 elements, 4 of 512
 
 struct KvAppendParams {
   int32_t batch, total_q, Hkv, D, P, log2P, num_pages, max_pages_per_req, elem_size;
@@ -29,22 +32,65 @@ struct KvAppendParams {
   unsigned char axis_of[kRopeMaxHeadDim / 2];
 };
 
-// Rotary embedding of the pairs (x[i], x[i + D/2]) of one head vector: x in double, cosine and sine of the pair's
-// angle in double; results rounded double -> binary32 -> element type (round-to-nearest-even each).  lo / hi are the
-// 16-byte vectors that hold the pairs' first and second elements, cs the (cos, sin) of the first.
+// Rotary embedding of the pairs (x[i], x[i + D/2]) of one head vector by angles whose cosine and sine are float64's; results
+// rounded to binary32 and then to the element type (nearest even each).  lo / hi are the 16-byte vectors that hold the
+// pairs' first and second elements.  cs: the angles of a row, 16 bytes a pair, laid out so that neighbouring vectors' lie side by
+// side, vecs vectors to half a row.
+//   float32 rows: products and sum in float64, (cos, sin) of vector v's pair u at [u * vecs + v].
+//   16-bit rows: products and sum in pairs of binary32 to 2^-46 of |x| (float64's arithmetic but for one in some millions of last
+//   bits of binary32, at a third of its time: conversions from and to float64 take 8 cycles each), (cos, cos', low parts) of pairs
+//   2u, 2u + 1 at [2u * vecs + v], the sines at [(2u + 1) * vecs + v].
 template <typename T>
-__device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2 *cs) {
-  constexpr int N = 16 / sizeof(T);
-  union U { uint4 q; T e[N]; } a, b;
-  a.q = lo; b.q = hi;
+__device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2 *cs, int vecs, int v) {
+  if constexpr (sizeof(T) == 4) {
+    union U { uint4 q; T e[4]; } a, b;
+    a.q = lo; b.q = hi;
 #pragma unroll
-  for (int u = 0; u < N; ++u) {
-    const double2 k = cs[u];
-    const double x0 = (double)ld_as_float(a.e, u), x1 = (double)ld_as_float(b.e, u);
-    st_from_float(a.e, u, __double2float_rn(x0 * k.x - x1 * k.y));
-    st_from_float(b.e, u, __double2float_rn(x1 * k.x + x0 * k.y));
+    for (int u = 0; u < 4; ++u) {
+      const double2 k = cs[u * vecs + v];
+      const double x0 = (double)a.e[u], x1 = (double)b.e[u];
+      a.e[u] = __double2float_rn(x0 * k.x - x1 * k.y);
+      b.e[u] = __double2float_rn(x1 * k.x + x0 * k.y);
+    }
+    lo = a.q; hi = b.q;
+  } else {
+    const ulonglong2 *at = reinterpret_cast<const ulonglong2 *>(cs);
+    uint32_t a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
+    uint64_t finite = e8::pair(0.f, 0.f);      // stays zero as long as results are finite
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const ulonglong2 c = at[2 * u * vecs + v], s = at[(2 * u + 1) * vecs + v];
+      const CosSin k{c.x, c.y, s.x, s.y};
+      uint64_t y0, y1;
+      rotate2<true>(e8::pair(__uint_as_float(a[u] << 16), __uint_as_float(a[u] & 0xffff0000u)),
+                    e8::pair(__uint_as_float(b[u] << 16), __uint_as_float(b[u] & 0xffff0000u)), k, y0, y1);
+      finite = e8::fma2(y0, e8::pair(0.f, 0.f), e8::fma2(y1, e8::pair(0.f, 0.f), finite));
+      float p, q;
+      e8::unpair(y0, p, q);
+      const __nv_bfloat162 r0 = __floats2bfloat162_rn(p, q);
+      e8::unpair(y1, p, q);
+      const __nv_bfloat162 r1 = __floats2bfloat162_rn(p, q);
+      a[u] = *reinterpret_cast<const uint32_t *>(&r0); b[u] = *reinterpret_cast<const uint32_t *>(&r1);
+    }
+    float p, q;
+    e8::unpair(finite, p, q);
+    if (p != 0.f || q != 0.f) {
+      // an infinity, a NaN or a result past binary32: the remainders above are none then, float64's arithmetic stands
+      const float *cs32 = reinterpret_cast<const float *>(cs);
+      const __nv_bfloat16 *x = reinterpret_cast<const __nv_bfloat16 *>(&lo), *y = reinterpret_cast<const __nv_bfloat16 *>(&hi);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float *k = cs32 + ((i & 6) * vecs + v) * 4 + (i & 1);
+        const double c = (double)k[0] + (double)k[2], sn = (double)k[4 * vecs] + (double)k[4 * vecs + 2];
+        const double x0 = (double)__bfloat162float(x[i]), x1 = (double)__bfloat162float(y[i]);
+        const __nv_bfloat16 r0 = __float2bfloat16_rn(__double2float_rn(x0 * c - x1 * sn)), r1 = __float2bfloat16_rn(__double2float_rn(x1 * c + x0 * sn));
+        const uint32_t w0 = *reinterpret_cast<const uint16_t *>(&r0), w1 = *reinterpret_cast<const uint16_t *>(&r1);
+        a[i >> 1] = (i & 1) ? (a[i >> 1] & 0xffffu) | w0 << 16 : (a[i >> 1] & 0xffff0000u) | w0;
+        b[i >> 1] = (i & 1) ? (b[i >> 1] & 0xffffu) | w1 << 16 : (b[i >> 1] & 0xffff0000u) | w1;
+      }
+    }
+    lo = make_uint4(a[0], a[1], a[2], a[3]); hi = make_uint4(b[0], b[1], b[2], b[3]);
   }
-  lo = a.q; hi = b.q;
 }
 
 // A block takes up to kAppendRows new rows of a request, all heads of K, V and the query rows, 16 bytes a thread and step.
@@ -100,9 +146,17 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
     for (int i = tid; i < n * half; i += kAppendThreads) {
       const int row = i / half, pair = i % half;
       const int t = p.axes ? p.positions[(int64_t)p.axis_of[pair] * p.position_stride + q0 + j0 + row] : t0 + row;
-      double2 cs;
-      sincos((double)t * s_inv_freq[pair], &cs.y, &cs.x);
-      s_cs[i] = cs;
+      double c, sn;
+      sincos((double)t * s_inv_freq[pair], &sn, &c);
+      if (p.elem_size == 4) {
+        s_cs[row * half + (pair & 3) * (half >> 2) + (pair >> 2)] = make_double2(c, sn);
+      } else {
+        float *at = reinterpret_cast<float *>(s_cs + row * half + (pair & 6) * (half >> 3) + (pair >> 3)) + (pair & 1);
+        const float ch = (float)c, sh = (float)sn;
+        at[0] = ch; at[2] = (float)(c - (double)ch);
+        at += (half >> 3) * 4;
+        at[0] = sh; at[2] = (float)(sn - (double)sh);
+      }
     }
   }
   if (__syncthreads_or(bad)) {
@@ -114,26 +168,49 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
     return ((int64_t)s_page[row] * p.stride_page + (int64_t)g * p.stride_head + (int64_t)((t0 + row) & (p.P - 1)) * p.stride_token) * p.elem_size;
   };
   if (rope) {
-    // a thread takes one vector of the first half of a head row and its partner in the second half
-    const int half_vecs = vecs >> 1, per_vec = 16 / p.elem_size, half_bytes = row_bytes >> 1;
-    auto turn = [&](const unsigned char *src, unsigned char *dst, int row, int v) {
-      uint4 lo = *reinterpret_cast<const uint4 *>(src), hi = *reinterpret_cast<const uint4 *>(src + half_bytes);
-      const double2 *cs = s_cs + row * (p.D >> 1) + v * per_vec;
-      if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(lo, hi, cs);
-      else rope_vectors<float>(lo, hi, cs);
-      *reinterpret_cast<uint4 *>(dst) = lo;
-      *reinterpret_cast<uint4 *>(dst + half_bytes) = hi;
-    };
-    for (int i = tid; i < n * p.Hkv * half_vecs; i += kAppendThreads) {
-      const int v = i % half_vecs, jg = i / half_vecs, g = jg % p.Hkv, row = jg / p.Hkv;
-      turn(p.new_k + ((int64_t)(q0 + j0 + row) * p.Hkv + g) * row_bytes + v * 16, p.k_cache + cache_at(row, g) + v * 16, row, v);
-    }
-    if (p.q_rows)
-      for (int i = tid; i < n * p.Hq * half_vecs; i += kAppendThreads) {
-        const int v = i % half_vecs, jh = i / half_vecs, h = jh % p.Hq, row = jh / p.Hq;
-        const int64_t at = ((int64_t)(q0 + j0 + row) * p.Hq + h) * row_bytes + v * 16;
-        turn(p.q_rows + at, p.q_out + at, row, v);
+    // a thread takes one vector of the first half of a head row and its partner in the second half: K's rows, then the
+    // query rows, two at a time
+    const int half_vecs = vecs >> 1, half_bytes = row_bytes >> 1;
+    const int n_k = n * p.Hkv * half_vecs, n_all = n_k + (p.q_rows ? n * p.Hq * half_vecs : 0);
+    struct Task { const unsigned char *src; unsigned char *dst; int row, v; uint4 lo, hi; };
+    auto open = [&](int i) -> Task {
+      Task t;
+      if (i < n_k) {
+        t.v = i % half_vecs;
+        const int jg = i / half_vecs, g = jg % p.Hkv;
+        t.row = jg / p.Hkv;
+        t.src = p.new_k + ((int64_t)(q0 + j0 + t.row) * p.Hkv + g) * row_bytes + t.v * 16;
+        t.dst = p.k_cache + cache_at(t.row, g) + t.v * 16;
+      } else {
+        i -= n_k;
+        t.v = i % half_vecs;
+        const int jh = i / half_vecs, h = jh % p.Hq;
+        t.row = jh / p.Hq;
+        const int64_t at = ((int64_t)(q0 + j0 + t.row) * p.Hq + h) * row_bytes + t.v * 16;
+        t.src = p.q_rows + at;
+        t.dst = p.q_out + at;
       }
+      t.lo = *reinterpret_cast<const uint4 *>(t.src);
+      t.hi = *reinterpret_cast<const uint4 *>(t.src + half_bytes);
+      return t;
+    };
+    auto close = [&](Task &t) {
+      const double2 *cs = s_cs + t.row * (p.D >> 1);
+      if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(t.lo, t.hi, cs, half_vecs, t.v);
+      else rope_vectors<float>(t.lo, t.hi, cs, half_vecs, t.v);
+      *reinterpret_cast<uint4 *>(t.dst) = t.lo;
+      *reinterpret_cast<uint4 *>(t.dst + half_bytes) = t.hi;
+    };
+    for (int i = tid; i < n_all; i += 2 * kAppendThreads) {
+      Task t = open(i);
+      if (i + kAppendThreads < n_all) {
+        Task u = open(i + kAppendThreads);
+        close(t);
+        close(u);
+      } else {
+        close(t);
+      }
+    }
   }
   for (int i = tid; i < n * p.Hkv * vecs; i += kAppendThreads) {
     const int v = i % vecs, jg = i / vecs, g = jg % p.Hkv, row = jg / p.Hkv;

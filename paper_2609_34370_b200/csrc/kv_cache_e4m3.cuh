@@ -20,6 +20,7 @@
 
 #include "attn_e4m3.cuh"   // e8::pair and the packed fp32 arithmetic
 #include "common.cuh"
+#include "rotate.cuh"
 
 namespace spx {
 
@@ -120,40 +121,6 @@ __device__ __forceinline__ float amax8(const float (&x)[8], float m) {   // NaNs
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
   return m;
-}
-
-// The rotation.  cos = ch + cl and sin = sh + sl, each as two floats of the float64 value (2^-48 of it left out).
-struct CosSin { uint64_t ch, cl, sh, sl; };   // of two pairs
-__device__ __forceinline__ uint64_t neg2(uint64_t a) { return e8::mul2(a, e8::pair(-1.f, -1.f)); }
-__device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) { return e8::fma2(b, e8::pair(-1.f, -1.f), a); }
-// y0 = x0 cos - x1 sin, y1 = x1 cos + x0 sin.  kExact: products and sum with their rounding errors (a product's by a fused
-// multiply-add, a sum's by Knuth's two-sum), one rounding to fp32 at the end of a value good to 2^-46 of |x| (what float64
-// arithmetic gives but for one in some millions of last bits and the sign of a zero, at a third of its time: conversions
-// from and to float64 alone are 8 cycles each); what goes into the 8-bit codes and into fp32 rows.  Otherwise the leading
-// errors only: within 2 steps of fp32 of the value, for rows that are rounded to 16 bits.  An infinite x, or a result past
-// fp32, gives an infinity or a NaN.
-template <bool kExact>
-__device__ __forceinline__ void rotate2(uint64_t x0, uint64_t x1, const CosSin &k, uint64_t &y0, uint64_t &y1) {
-  using namespace e8;
-  const uint64_t n0 = neg2(x0), n1 = neg2(x1);
-  if constexpr (kExact) {
-    {
-      const uint64_t p = mul2(x0, k.ch), np = fma2(n0, k.ch, p), q = mul2(x1, k.sh), nq = fma2(n1, k.sh, q);
-      const uint64_t s = sub2(p, q), bb = sub2(s, p);
-      const uint64_t err = sub2(sub2(p, sub2(s, bb)), add2(q, bb));
-      y0 = add2(s, add2(fma2(n1, k.sl, fma2(x0, k.cl, err)), sub2(nq, np)));
-    }
-    {
-      const uint64_t p = mul2(x1, k.ch), np = fma2(n1, k.ch, p), q = mul2(x0, k.sh), nq = fma2(n0, k.sh, q);
-      const uint64_t s = add2(p, q), bb = sub2(s, p);
-      const uint64_t err = add2(sub2(p, sub2(s, bb)), sub2(q, bb));
-      y1 = add2(s, sub2(fma2(x0, k.sl, fma2(x1, k.cl, err)), add2(np, nq)));
-    }
-  } else {
-    const uint64_t w = mul2(x1, k.sh), nw = mul2(n1, k.sh), u = mul2(x0, k.sh), nu = mul2(n0, k.sh);
-    y0 = add2(fma2(x0, k.ch, nw), fma2(n1, k.sl, fma2(x0, k.cl, fma2(n1, k.sh, w))));
-    y1 = add2(fma2(x1, k.ch, u), fma2(x0, k.sl, fma2(x1, k.cl, fma2(x0, k.sh, nu))));
-  }
 }
 
 // The exponent field of 2^e with the smallest e for which amax <= 448 * 2^e = 1.75 * 2^(e+8); amax as
@@ -259,13 +226,36 @@ __global__ void __launch_bounds__(kQuantThreads, 2) kv_append_e4m3_kernel(const 
     at[4 * kVecs] = sh; at[4 * kVecs + 2] = (float)(sn - (double)sh);
   };
   if (p.rope && p.axes) {
+    // positions of several axes: as below, where a token's position is that of the one before or the next (an axis of a grid
+    // stands still or counts up for most tokens), by a sine and cosine of its own elsewhere
     const int t_lo = max(t0, t_new), n = min(t0 + tile_tokens, L) - t_lo;   // the tile's new tokens
-    for (int i = tid; i < n * (D / 2); i += kQuantThreads) {
-      const int pair = i % (D / 2), tok = t_lo - t0 + i / (D / 2);
-      const int at = p.positions[(int64_t)p.axis_of[pair] * p.position_stride + q0 + (t0 + tok - t_new)];
-      double c, sn;
-      sincos((double)at * p.inv_freq[pair], &sn, &c);
+    for (int i = tid; i < (n + 3) / 4 * (D / 2); i += kQuantThreads) {
+      const int pair = i % (D / 2), tok = t_lo - t0 + i / (D / 2) * 4;
+      const int32_t *at_pos = p.positions + (int64_t)p.axis_of[pair] * p.position_stride + q0 + (t0 + tok - t_new);
+      const int left = t_lo - t0 + n - tok;
+      int pos[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) pos[u] = u < left ? at_pos[u] : 0;
+      const double f = p.inv_freq[pair];
+      double c, sn, cf = 1.0, sf = 0.0;
+      sincos((double)pos[0] * f, &sn, &c);
+      bool turning = false;
+#pragma unroll
+      for (int u = 1; u < 4; ++u) turning |= u < left && pos[u] == pos[u - 1] + 1ll;
+      if (turning) sincos(f, &sf, &cf);
       keep(angle_at(tok, pair), c, sn);
+#pragma unroll
+      for (int u = 1; u < 4; ++u) {
+        if (u >= left) break;
+        if (pos[u] == pos[u - 1] + 1ll) {
+          const double c2 = c * cf - sn * sf;
+          sn = sn * cf + c * sf;
+          c = c2;
+        } else if (pos[u] != pos[u - 1]) {
+          sincos((double)pos[u] * f, &sn, &c);
+        }
+        keep(angle_at(tok + u, pair), c, sn);
+      }
     }
   } else if (p.rope) {
     // angles in float64; a thread takes four tokens of a pair: one sine and cosine, and three turns by the pair's
