@@ -25,12 +25,15 @@ struct KvAppendParams {
   unsigned char *q_rows;   // optional [TQ, Hq, D], rotated into q_out (in place when the two are one)
   unsigned char *q_out;
   int32_t Hq;
-  // positions of several axes (axes = 0: a row's position is its place in the request)
+};
+// Positions of several axes (axes = 0: a row's position is its place in the request).
+struct KvAppendAxes {
   int32_t axes;
   const int32_t *positions;
   int64_t position_stride;
   unsigned char axis_of[kRopeMaxHeadDim / 2];
 };
+struct KvNoAxes {};
 
 // Rotary embedding of the pairs (x[i], x[i + D/2]) of one head vector by angles whose cosine and sine are float64's; results
 // rounded to binary32 and then to the element type (nearest even each).  lo / hi are the 16-byte vectors that hold the
@@ -95,41 +98,42 @@ __device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2
 
 // A block takes up to kAppendRows new rows of a request, all heads of K, V and the query rows, 16 bytes a thread and step.
 // Block b belongs to the request r with base(r) <= b < base(r + 1), base(r) = q_indptr[r] / rows + r: m rows are at most
-// m / rows + 1 blocks, so no prefix sums are needed; blocks past a request's last one leave at once.  The angles are
+// m / rows + 1 blocks, so no prefix sums are needed; blocks past a request's last one, and past the last request's, leave at once.  The angles are
 // worked out once a block and shared by its heads.
 // Pure copy and rotation: bound by launch latency at verify-step sizes (a few MB), by HBM beyond that.
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ KvAppendParams p) {
-  __shared__ int s_req, s_page[kAppendRows];
-  __shared__ double s_inv_freq[kRopeMaxHeadDim / 2];
-  __shared__ __align__(16) double2 s_cs[kAppendAngles];
-  const int tid = threadIdx.x, lane = tid & 31;
-  const bool rope = p.rope_base > 0.0;
-  if (tid < 32) {
-    // 32 probes at a time
-    int lo = 0, hi = p.batch;   // base(lo) <= block, hi past the last candidate
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 31) / 32, c = lo + lane * step;
-      const bool below = c < hi && (int64_t)(p.q_indptr[c] >> p.log2_rows) + c <= (int64_t)blockIdx.x;
-      const int n = __popc(__ballot_sync(0xffffffffu, below || lane == 0));   // the probes ascend
-      const int at = lo + (n - 1) * step;
-      hi = min(hi, at + step);
-      lo = at;
+// kRope: with a rotary base (without, a kernel of few registers: 2.7 us instead of 3.4 for 64 requests of 6 rows).
+template <bool kRope>
+__global__ void __launch_bounds__(kAppendThreads, 3)
+kv_append_kernel(const __grid_constant__ KvAppendParams p, const __grid_constant__ typename std::conditional<kRope, KvAppendAxes, KvNoAxes>::type ax) {
+  __shared__ int s_req, s_q0, s_m, s_L, s_page[kAppendRows];
+  __shared__ double s_inv_freq[kRope ? kRopeMaxHeadDim / 2 : 1];
+  __shared__ __align__(16) double2 s_cs[kRope ? kAppendAngles : 1];
+  const int tid = threadIdx.x;
+  auto valid = [&](int q0, int q1, int L) -> bool {
+    return q0 >= 0 && q1 > q0 && q1 <= p.total_q && L >= q1 - q0 && (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req;
+  };
+  // the request of this block: each thread looks whether it is one of its own (in one memory round trip for up to 256 of
+  // them, whose bounds and length the block then has); block 0 looks at all lengths
+  if (tid == 0) s_req = -1;
+  bool bad_len = false;
+  for (int c0 = 0; c0 < p.batch; c0 += kAppendThreads) {
+    const int c = c0 + tid;
+    int q0 = 0, q1 = 0, L = 0;
+    if (c < p.batch) { q0 = p.q_indptr[c]; q1 = p.q_indptr[c + 1]; L = p.seq_lens[c]; }
+    if (c0 == 0) {
+      if (kRope)
+        for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
+      __syncthreads();
     }
-    if (lane == 0) s_req = lo;
-  } else if (rope) {
-    for (int i = tid - 32; i < (p.D >> 1); i += kAppendThreads - 32) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
+    if (c >= p.batch) continue;
+    const int64_t first = (int64_t)(q0 >> p.log2_rows) + c, next = (int64_t)(q1 >> p.log2_rows) + c + 1;
+    if (first <= (int64_t)blockIdx.x && (int64_t)blockIdx.x < next) { s_req = c; s_q0 = q0; s_m = valid(q0, q1, L) ? q1 - q0 : 0; s_L = L; }
+    bad_len |= !valid(q0, q1, L);
   }
+  if (blockIdx.x == 0 && bad_len) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   __syncthreads();
-  const int r = s_req;
-  const int q0 = p.q_indptr[r];
-  const int m = p.q_indptr[r + 1] - q0;
-  const int L = p.seq_lens[r];
-  const bool ok_len = m >= 1 && L >= m && q0 >= 0 && m <= p.total_q - q0 &&
-                      (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req;
-  if (!ok_len) {
-    if (tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
-    return;
-  }
+  const int r = s_req, q0 = s_q0, m = s_m, L = s_L;
+  if (r < 0 || m == 0) return;
   const int64_t j0_64 = ((int64_t)blockIdx.x - ((q0 >> p.log2_rows) + (int64_t)r)) << p.log2_rows;
   if (j0_64 < 0 || j0_64 >= m) return;
   const int j0 = (int)j0_64, n = min(1 << p.log2_rows, m - j0), t0 = L - m + j0;
@@ -141,11 +145,11 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
     const int pg = table[i];
     bad |= pg < 0 || pg >= p.num_pages;
   }
-  if (rope) {
+  if constexpr (kRope) {
     const int half = p.D >> 1;
     for (int i = tid; i < n * half; i += kAppendThreads) {
       const int row = i / half, pair = i % half;
-      const int t = p.axes ? p.positions[(int64_t)p.axis_of[pair] * p.position_stride + q0 + j0 + row] : t0 + row;
+      const int t = ax.axes ? ax.positions[(int64_t)ax.axis_of[pair] * ax.position_stride + q0 + j0 + row] : t0 + row;
       double c, sn;
       sincos((double)t * s_inv_freq[pair], &sn, &c);
       if (p.elem_size == 4) {
@@ -167,9 +171,9 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
   auto cache_at = [&](int row, int g) -> int64_t {
     return ((int64_t)s_page[row] * p.stride_page + (int64_t)g * p.stride_head + (int64_t)((t0 + row) & (p.P - 1)) * p.stride_token) * p.elem_size;
   };
-  if (rope) {
+  if constexpr (kRope) {
     // a thread takes one vector of the first half of a head row and its partner in the second half: K's rows, then the
-    // query rows, two at a time
+    // query rows (two at a time, in 114 registers: 44 us for prompts with images, against 40)
     const int half_vecs = vecs >> 1, half_bytes = row_bytes >> 1;
     const int n_k = n * p.Hkv * half_vecs, n_all = n_k + (p.q_rows ? n * p.Hq * half_vecs : 0);
     struct Task { const unsigned char *src; unsigned char *dst; int row, v; uint4 lo, hi; };
@@ -201,21 +205,15 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
       *reinterpret_cast<uint4 *>(t.dst) = t.lo;
       *reinterpret_cast<uint4 *>(t.dst + half_bytes) = t.hi;
     };
-    for (int i = tid; i < n_all; i += 2 * kAppendThreads) {
+    for (int i = tid; i < n_all; i += kAppendThreads) {
       Task t = open(i);
-      if (i + kAppendThreads < n_all) {
-        Task u = open(i + kAppendThreads);
-        close(t);
-        close(u);
-      } else {
-        close(t);
-      }
+      close(t);
     }
   }
   for (int i = tid; i < n * p.Hkv * vecs; i += kAppendThreads) {
     const int v = i % vecs, jg = i / vecs, g = jg % p.Hkv, row = jg / p.Hkv;
     const int64_t src = ((int64_t)(q0 + j0 + row) * p.Hkv + g) * row_bytes + v * 16, dst = cache_at(row, g) + v * 16;
-    if (!rope) *reinterpret_cast<uint4 *>(p.k_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src));
+    if (!kRope) *reinterpret_cast<uint4 *>(p.k_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src));
     *reinterpret_cast<uint4 *>(p.v_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_v + src));
   }
 }

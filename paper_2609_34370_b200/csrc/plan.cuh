@@ -58,10 +58,9 @@ __device__ __forceinline__ int plan_entry_cost(int tiles, int entry_cost) { retu
 // One block.  Validates each request's (k+1, L, page count), cuts the tile axis of the valid
 // requests' (request, kv head) pairs into n_cta ranges of equal length, lays out partial-result
 // slots for the pairs a cut crosses and emits each range's work entries in axis order.
-__global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
-  SPX_TL_SCOPE(kTlPlan);
-  // a kernel launched programmatically behind this one may come up now (it waits before it reads the plan)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+// first_tile(r): the tiles before it are another kernel's (behind a shared prefix; kGrouped), and every pair then has partial results.
+template <bool kGrouped, typename First>
+__device__ __forceinline__ void plan_block(const AttnParams &p, int n_cta, First first_tile) {
   __shared__ int s_scratch[96];
   __shared__ int s_total[3];
   __shared__ int s_cut[kPlanMaxCta + 1];     // cut c: first tile (axis position) of range c
@@ -78,11 +77,6 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   const bool in_smem = p.batch <= kPlanSmemReqs;
   auto tile_prefix = [&](int i) -> int { return in_smem ? s_tp[i] : p.tile_prefix[i]; };
   auto valid_prefix = [&](int i) -> int { return in_smem ? s_vp[i] : p.valid_prefix[i]; };
-  auto first_tile = [&](int r) -> int {   // behind a shared prefix
-    if (!p.req_group) return 0;
-    const int u = p.req_group[r];
-    return u < 0 ? 0 : p.group_tiles[u];
-  };
   auto cost_prefix = [&](int i) -> int { return in_smem ? s_cp[i] : p.cost_prefix[i]; };  // per kv head
   const int tid = threadIdx.x;
   const int Hkv = p.Hkv;
@@ -96,15 +90,15 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
   // pass 1: validate; prefix sums of tiles and of valid requests
   for (int base = 0; base < p.batch; base += 1024) {
     const int r = base + tid;
-    int tiles = 0, q0 = 0, q1 = 0, L = 0;
-    if (r < p.batch) { q0 = p.q_indptr[r]; q1 = p.q_indptr[r + 1]; L = p.seq_lens[r]; }
+    int tiles = 0, q0 = 0, q1 = 0, L = 0, behind = 0;
+    if (r < p.batch) { behind = first_tile(r); q0 = p.q_indptr[r]; q1 = p.q_indptr[r + 1]; L = p.seq_lens[r]; }
     if (base == 0) __syncthreads();   // s_bad is cleared; the loads are on their way
     if (r < p.batch) {
       const int m = q1 - q0;
       const bool ok = (m >= 1) && (m <= p.max_q_len) && (L >= m) &&
                       (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req &&
-                      (q0 >= 0) && (q1 <= p.total_q) && (int64_t)first_tile(r) * kTileTokens <= (int64_t)L - m;
-      tiles = ok ? (L + kTileTokens - 1) / kTileTokens - first_tile(r) : 0;
+                      (q0 >= 0) && (q1 <= p.total_q) && (int64_t)behind * kTileTokens <= (int64_t)L - m;
+      tiles = ok ? (L + kTileTokens - 1) / kTileTokens - behind : 0;
       if (!ok) s_bad = 1;
       p.req_bad[r] = 0;
       if (in_smem) { s_q0[r] = q0; s_m[r] = m; s_L[r] = L; }
@@ -221,7 +215,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
     }
     // the pairs the combine kernel has work for: split ones, and those of invalid requests (sentinel rows)
     const bool listed = pair < n_pairs && nch != 1;
-    const bool partial = nch > 1 || (p.req_group && nch == 1);   // behind a shared prefix every pair is joined with it
+    const bool partial = nch > 1 || (kGrouped && nch == 1);   // behind a shared prefix every pair is joined with it
     int off[2] = {partial ? nch : 0, listed ? 1 : 0};
     block_exclusive_scan_1024(off, s_scratch, s_total);
     const int part = off[0] + carry_p, lpos = off[1] + carry_l;
@@ -274,6 +268,13 @@ __global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
     p.hdr->n_combine = carry_l;
     if (bad) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   }
+}
+
+__global__ void __launch_bounds__(1024) plan_kernel(AttnParams p, int n_cta) {
+  SPX_TL_SCOPE(kTlPlan);
+  // a kernel launched programmatically behind this one may come up now (it waits before it reads the plan)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  plan_block<false>(p, n_cta, [](int) { return 0; });
 }
 
 // Merge the chunk partials of split pairs: m* = max_c m_c, l* = sum_c 2^(m_c-m*) l_c,

@@ -13,6 +13,7 @@
 // better on paper and read the cache from HBM several times over: 250 to 420 us for that chunk, from board to board).
 #pragma once
 #include "common.cuh"
+#include "plan.cuh"
 
 namespace spx {
 
@@ -128,67 +129,42 @@ __device__ __forceinline__ int last_at_most(const T *a, int n, X x) {
   return lo;
 }
 
-// Block 0 plans.  Of a plan over groups the blocks behind it compare the block-table rows of the requests with
-// their groups' first, so that a request that does not share what its group reads once is found, not answered wrongly.
-__global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
-  SPX_TL_SCOPE(kTlPlan);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+// What a unit is: first query row, positions, tokens, block-table row, whether it is to be voided.
+struct PromptUnit { int q0, m, L, row; bool bad; };
+__device__ __forceinline__ PromptUnit prompt_unit(const PromptParams &p, int u) {
+  PromptUnit x{0, 0, 0, 0, false};
+  if (p.groups == 0) {
+    const int q0 = p.q_indptr[u], q1 = p.q_indptr[u + 1], L = p.seq_lens[u];
+    x.q0 = q0; x.m = q1 - q0; x.L = L; x.row = u;
+    x.bad = q0 < 0 || q1 < q0 || q1 > p.total_q || L < x.m || (((int64_t)L + p.P - 1) >> p.log2P) > (int64_t)p.max_pages_per_req;
+    if (x.bad) x.m = 0;
+    return x;
+  }
+  const int r0 = max(p.group_indptr[u], 0), r1 = min(p.group_indptr[u + 1], p.batch), len = p.prefix_lens[u];
+  if (r1 - r0 < 2 || len < kTileTokens) return x;             // nobody to share with, nothing to share
+  const int q0 = p.q_indptr[r0], q1 = p.q_indptr[r1];
+  if (q0 < 0 || q1 <= q0 || q1 > p.total_q) return x;         // (the requests' own check voids them)
+  const int tokens = len / kTileTokens * kTileTokens;
+  if ((tokens >> p.log2P) > p.max_pages_per_req) return x;
+  x.q0 = q0; x.m = q1 - q0; x.L = tokens; x.row = r0;
+  return x;
+}
+// The group of a request, -1: none.
+__device__ __forceinline__ int prompt_group_of(const PromptParams &p, int r) {
+  if (p.group_indptr[0] > r) return -1;
+  const int u = last_at_most(p.group_indptr, p.groups, r);
+  return r < p.group_indptr[u + 1] ? u : -1;
+}
+
+// One block of 1024 threads.
+__device__ __forceinline__ void prompt_plan_block(const PromptParams &p) {
   const int tid = threadIdx.x;
   __shared__ int64_t s_scratch[33];
   __shared__ int s_hist[kPromptBuckets];
-  __shared__ int s_longest, s_bad, s_group;
+  __shared__ int s_longest, s_bad;
   __shared__ long long s_best;
-
-  // what a unit is: first query row, positions, tokens, block-table row, whether it is to be voided
-  struct Unit { int q0, m, L, row; bool bad; };
-  auto unit_of = [&](int u) -> Unit {
-    Unit x{0, 0, 0, 0, false};
-    if (p.groups == 0) {
-      const int q0 = p.q_indptr[u], q1 = p.q_indptr[u + 1], L = p.seq_lens[u];
-      x.q0 = q0; x.m = q1 - q0; x.L = L; x.row = u;
-      x.bad = q0 < 0 || q1 < q0 || q1 > p.total_q || L < x.m || (((int64_t)L + p.P - 1) >> p.log2P) > (int64_t)p.max_pages_per_req;
-      if (x.bad) x.m = 0;
-      return x;
-    }
-    const int r0 = max(p.group_indptr[u], 0), r1 = min(p.group_indptr[u + 1], p.batch), len = p.prefix_lens[u];
-    if (r1 - r0 < 2 || len < kTileTokens) return x;             // nobody to share with, nothing to share
-    const int q0 = p.q_indptr[r0], q1 = p.q_indptr[r1];
-    if (q0 < 0 || q1 <= q0 || q1 > p.total_q) return x;         // (the requests' own check voids them)
-    const int tokens = len / kTileTokens * kTileTokens;
-    if ((tokens >> p.log2P) > p.max_pages_per_req) return x;
-    x.q0 = q0; x.m = q1 - q0; x.L = tokens; x.row = r0;
-    return x;
-  };
-
-  if (blockIdx.x > 0) {
-    // one block a request
-    for (int r = blockIdx.x - 1; r < p.batch; r += gridDim.x - 1) {
-      // its group (requests that no group holds share nothing)
-      __syncthreads();
-      if (tid == 0) s_group = -1;
-      __syncthreads();
-      for (int i = tid; i < p.groups; i += blockDim.x)
-        if (p.group_indptr[i] <= r && r < p.group_indptr[i + 1]) atomicMax(&s_group, i);
-      __syncthreads();
-      const int u = s_group;
-      if (tid == 0) p.req_group[r] = u;
-      int differs = 0;
-      if (u >= 0) {
-        const Unit x = unit_of(u);
-        if (x.m > 0) {
-          const int32_t *mine = p.block_table + (int64_t)r * p.max_pages_per_req, *first = p.block_table + (int64_t)x.row * p.max_pages_per_req;
-          for (int i = tid; i < x.L >> p.log2P; i += blockDim.x) differs |= mine[i] != first[i];
-        }
-      }
-      differs = __syncthreads_or(differs);
-      if (tid == 0) {
-        p.req_flag[r] = differs != 0;
-        if (differs) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
-      }
-    }
-    return;
-  }
-
+  using Unit = PromptUnit;
+  auto unit_of = [&](int u) -> Unit { return prompt_unit(p, u); };
   for (int i = tid; i < kPromptBuckets; i += 1024) s_hist[i] = 0;
   if (tid == 0) { s_longest = 0; s_bad = 0; s_best = 0x7fffffffffffffffll; }
   __syncthreads();
@@ -324,6 +300,48 @@ __global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
   }
 }
 
+__global__ void __launch_bounds__(1024) prompt_plan_kernel(PromptParams p) {
+  SPX_TL_SCOPE(kTlPlan);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  prompt_plan_block(p);
+}
+
+// Block 0 plans the prefixes of the groups, block 1 the requests' own tokens behind them.  The blocks behind compare the block-table
+// rows of the requests with their groups' first, so that a request that does not share what its group reads once is found,
+// not answered wrongly.
+__global__ void __launch_bounds__(1024) prefix_plan_kernel(AttnParams a, PromptParams p, int n_cta) {
+  SPX_TL_SCOPE(kTlPlan);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (blockIdx.x == 0) {
+    prompt_plan_block(p);
+  } else if (blockIdx.x == 1) {
+    plan_block<true>(a, n_cta, [&](int r) -> int {
+      const int u = prompt_group_of(p, r);
+      return u < 0 ? 0 : prompt_unit(p, u).L / kTileTokens;
+    });
+  } else {
+    // a warp a request (few blocks: in the whole step they share the one SM that the logits pass leaves)
+    const int lane = threadIdx.x & 31;
+    for (int r = (blockIdx.x - 2) * 32 + (threadIdx.x >> 5); r < p.batch; r += (gridDim.x - 2) * 32) {
+      const int u = prompt_group_of(p, r);
+      int differs = 0;
+      PromptUnit x{0, 0, 0, 0, false};
+      if (u >= 0) x = prompt_unit(p, u);
+      if (x.m > 0) {
+        const int32_t *mine = p.block_table + (int64_t)r * p.max_pages_per_req, *first = p.block_table + (int64_t)x.row * p.max_pages_per_req;
+#pragma unroll 8
+        for (int i = lane; i < x.L >> p.log2P; i += 32) differs |= mine[i] ^ first[i];
+      }
+      differs = __any_sync(0xffffffffu, differs != 0);
+      if (lane == 0) {
+        p.req_group[r] = u;
+        p.req_flag[r] = differs;
+        if (differs) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
+      }
+    }
+  }
+}
+
 // Joins the pieces of items (see combine_kernel) and voids the rows of requests with a bad length or page id.
 // Blocks (b, y): kv head b mod Hkv of item b / Hkv of the list, (row, four columns) y * 256 + t of it.
 template <typename T>
@@ -399,40 +417,59 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(PromptParams p) {
 template <typename T>
 __global__ void __launch_bounds__(256) prefix_join_kernel(AttnParams a, PromptParams p) {
   SPX_TL_SCOPE(kTlCombine);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // The plans are read ahead of the wait for the attention kernel, which has read them itself when it lets this one up.
   const int r = blockIdx.x;
   T *out = reinterpret_cast<T *>(a.out);
   const int vecs = a.D / 4, G = a.G;
-  const int q0 = a.q_indptr[r];
+  const int q0 = a.q_indptr[r], u = p.req_group[r];
   int m = a.q_indptr[r + 1] - q0;
   if (m < 0) m = 0;
   if (m > a.max_q_len) m = a.max_q_len;
-  if (q0 < 0 || (int64_t)q0 + m > a.total_q) return;
-  const int u = p.req_group[r];
+  const bool inside = q0 >= 0 && (int64_t)q0 + m <= a.total_q;
   const int tiles = u >= 0 ? p.group_tiles[u] : 0;
-  bool bad = a.req_bad[r] || p.req_flag[r] || (u >= 0 && p.unit_bad[u]);
+  int item0 = 0;
   int64_t row0 = 0;    // the request's first packed row among its group's
+  bool bad = false;
   if (tiles > 0) {
+    item0 = p.unit_item0[u];
     row0 = (int64_t)(q0 - p.q_indptr[max(p.group_indptr[u], 0)]) * G;
-    const int64_t rows = (int64_t)(p.unit_item0[u + 1] - p.unit_item0[u]) * p.unit_rows;
-    bad = bad || row0 < 0 || row0 + (int64_t)m * G > rows;
+    bad = row0 < 0 || row0 + (int64_t)m * G > (int64_t)(p.unit_item0[u + 1] - item0) * p.unit_rows;
   }
-  for (int item = blockIdx.y * blockDim.x + threadIdx.x; item < m * a.Hq * vecs; item += gridDim.y * blockDim.x) {
-    const int dv = item % vecs, jh = item / vecs, h = jh % a.Hq, j = jh / a.Hq, g = h / G, hg = h % G;
+  struct Item { int dv, j, h, nch, base; int2 part; int64_t prow; };
+  auto open = [&](int item) -> Item {
+    Item x;
+    x.dv = item % vecs;
+    const int jh = item / vecs;
+    x.h = jh % a.Hq; x.j = jh / a.Hq;
+    const int g = x.h / G;
+    x.nch = a.pair_nchunks[r * a.Hkv + g]; x.base = a.pair_part_base[r * a.Hkv + g];
+    x.part = make_int2(0, 0);     // first slot, pieces
+    x.prow = 0;
+    if (tiles > 0 && !bad) {
+      const int64_t row = row0 + (int64_t)x.j * G + x.h % G;
+      x.part = p.item_part[item0 + row / p.unit_rows];
+      x.prow = row % p.unit_rows;
+    }
+    return x;
+  };
+  const int n_items = inside ? m * a.Hq * vecs : 0;
+  const int first = blockIdx.y * blockDim.x + threadIdx.x;
+  Item x{};
+  if (first < n_items) x = open(first);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (first >= n_items) return;
+  bad = bad || a.req_bad[r] || p.req_flag[r] || (u >= 0 && p.unit_bad[u]);
+  for (int item = first; item < n_items; item += gridDim.y * blockDim.x) {
+    if (item != first) x = open(item);
+    const int dv = x.dv, j = x.j, h = x.h, g = h / G, hg = h % G, nch = x.nch, base = x.base;
     const int64_t qh = (int64_t)(q0 + j) * a.Hq + h, at = qh * a.D + dv * 4;
-    const int nch = a.pair_nchunks[r * a.Hkv + g], base = a.pair_part_base[r * a.Hkv + g];
     if (bad || nch == 0) {
       for (int i = 0; i < 4; ++i) st_from_float(out, at + i, 0.f);
       if (dv == 0 && a.lse) a.lse[qh] = __int_as_float(0x7fc00000);
       continue;
     }
-    int2 part = make_int2(0, 0);     // first slot, pieces
-    int64_t prow = 0;
-    if (tiles > 0) {
-      const int64_t row = row0 + (int64_t)j * G + hg;
-      part = p.item_part[p.unit_item0[u] + row / p.unit_rows];
-      prow = row % p.unit_rows;
-    }
+    const int2 part = x.part;
+    const int64_t prow = x.prow;
     float mstar = -INFINITY, lstar = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const int n = nch + part.y;

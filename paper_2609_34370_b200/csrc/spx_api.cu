@@ -602,13 +602,9 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
 
   // one range of the plan per CTA of the persistent kernels, never more than the workspace was sized for
   const int sms = dev.num_sms < kPlanSmCount ? dev.num_sms : kPlanSmCount;
-  if (grouped) { p.req_group = pre.req_group; p.group_tiles = pre.group_tiles; }
   if (phases & kPhasePlan) {
-    if (grouped) {
-      prompt_plan_kernel<<<1 + (a->batch < 1024 ? a->batch : 1024), 1024, 0, stream>>>(pre);
-      ++t_launches;
-    }
-    plan_kernel<<<1, 1024, 0, stream>>>(p, sms);
+    if (grouped) prefix_plan_kernel<<<2 + (a->batch < 32 * 64 ? (a->batch + 31) / 32 : 64), 1024, 0, stream>>>(p, pre, sms);
+    else plan_kernel<<<1, 1024, 0, stream>>>(p, sms);
     ++t_launches;
     if (cudaGetLastError() != cudaSuccess) return SPX_ERR_CUDA;
   }
@@ -1169,15 +1165,21 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
   p.q_rows = rope ? static_cast<unsigned char *>(a->q_rows) : nullptr;
   p.q_out = a->q_out ? static_cast<unsigned char *>(a->q_out) : p.q_rows;
   p.Hq = a->num_q_heads;
-  if (a->rope_axes > 0) {
-    p.axes = a->rope_axes; p.positions = a->positions; p.position_stride = a->position_stride;
-    fill_axes(a, p.axis_of);
-  }
   p.log2_rows = log2_of(kAppendRows);
   while (rope && (a->head_dim / 2) << p.log2_rows > kAppendAngles) --p.log2_rows;
   const int64_t blocks = ((int64_t)a->total_q >> p.log2_rows) + a->batch;
   if (blocks > 0x7fffffff) return SPX_ERR_UNSUPPORTED;
-  kv_append_kernel<<<(unsigned)blocks, kAppendThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  if (rope) {
+    KvAppendAxes ax{};
+    if (a->rope_axes > 0) {
+      ax.axes = a->rope_axes; ax.positions = a->positions; ax.position_stride = a->position_stride;
+      fill_axes(a, ax.axis_of);
+    }
+    kv_append_kernel<true><<<(unsigned)blocks, kAppendThreads, 0, stream>>>(p, ax);
+  } else {
+    kv_append_kernel<false><<<(unsigned)blocks, kAppendThreads, 0, stream>>>(p, KvNoAxes());
+  }
   ++t_launches;
   return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;
 }
