@@ -342,6 +342,12 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(AttnParams a, PromptP
   }
 }
 
+__device__ __forceinline__ void store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+
 // Joins the pieces of items (see combine_kernel) and voids the rows of requests with a bad length or page id.
 // Blocks (b, y): kv head b mod Hkv of item b / Hkv of the list, (row, four columns) y * 256 + t of it.
 template <typename T>
@@ -391,10 +397,7 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(PromptParams p) {
       const int pr = e.row0 + row, h = g * p.G + pr % p.G;
       const int64_t qrow = e.q0 + pr / p.G, at = (qrow * p.Hq + h) * p.D + dv * 4;
       const float inv = 1.f / lstar;
-      st_from_float(out, at + 0, acc.x * inv);
-      st_from_float(out, at + 1, acc.y * inv);
-      st_from_float(out, at + 2, acc.z * inv);
-      st_from_float(out, at + 3, acc.w * inv);
+      store4(out + at, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
       if (dv == 0 && p.lse) p.lse[qrow * p.Hq + h] = (mstar + log2f(lstar)) * kLn2;
     }
   }
@@ -414,6 +417,8 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(PromptParams p) {
 
 // Joins a request's partial results of its group's prefix with those of its own tokens.  Block (r, y): request r, items (position,
 // head, four columns) y * 256 + t.  a: the plan of the requests' own tokens; p: that of the prefixes.
+constexpr int kJoinHeads = 128;                              // kv heads whose chunks are kept in shared memory
+constexpr int kJoinItems = SPX_MAX_PACKED_ROWS / 64 + 2;     // items (of 64 rows at least) that a request's rows can lie in
 template <typename T>
 __global__ void __launch_bounds__(256) prefix_join_kernel(AttnParams a, PromptParams p) {
   SPX_TL_SCOPE(kTlCombine);
@@ -435,41 +440,35 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnParams a, PromptPa
     row0 = (int64_t)(q0 - p.q_indptr[max(p.group_indptr[u], 0)]) * G;
     bad = row0 < 0 || row0 + (int64_t)m * G > (int64_t)(p.unit_item0[u + 1] - item0) * p.unit_rows;
   }
-  struct Item { int dv, j, h, nch, base; int2 part; int64_t prow; };
-  auto open = [&](int item) -> Item {
-    Item x;
-    x.dv = item % vecs;
-    const int jh = item / vecs;
-    x.h = jh % a.Hq; x.j = jh / a.Hq;
-    const int g = x.h / G;
-    x.nch = a.pair_nchunks[r * a.Hkv + g]; x.base = a.pair_part_base[r * a.Hkv + g];
-    x.part = make_int2(0, 0);     // first slot, pieces
-    x.prow = 0;
-    if (tiles > 0 && !bad) {
-      const int64_t row = row0 + (int64_t)x.j * G + x.h % G;
-      x.part = p.item_part[item0 + row / p.unit_rows];
-      x.prow = row % p.unit_rows;
-    }
-    return x;
-  };
+  // chunks and first slots of the request's pairs, and of the few items that its rows lie in
+  __shared__ int2 s_pair[kJoinHeads], s_part[kJoinItems];
+  const int64_t first_item = row0 / p.unit_rows;
+  const int row_in = (int)(row0 - first_item * p.unit_rows);   // of the request's first packed row
+  for (int g = threadIdx.x; g < min(a.Hkv, kJoinHeads); g += blockDim.x) s_pair[g] = make_int2(a.pair_nchunks[r * a.Hkv + g], a.pair_part_base[r * a.Hkv + g]);
+  if (tiles > 0 && !bad && threadIdx.x < kJoinItems && item0 + first_item + threadIdx.x < p.unit_item0[u + 1]) s_part[threadIdx.x] = p.item_part[item0 + first_item + threadIdx.x];
+  __syncthreads();
   const int n_items = inside ? m * a.Hq * vecs : 0;
-  const int first = blockIdx.y * blockDim.x + threadIdx.x;
-  Item x{};
-  if (first < n_items) x = open(first);
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (first >= n_items) return;
   bad = bad || a.req_bad[r] || p.req_flag[r] || (u >= 0 && p.unit_bad[u]);
-  for (int item = first; item < n_items; item += gridDim.y * blockDim.x) {
-    if (item != first) x = open(item);
-    const int dv = x.dv, j = x.j, h = x.h, g = h / G, hg = h % G, nch = x.nch, base = x.base;
+#pragma unroll 2
+  for (int item = blockIdx.y * blockDim.x + threadIdx.x; item < n_items; item += gridDim.y * blockDim.x) {
+    const int dv = item % vecs, jh = item / vecs, h = jh % a.Hq, j = jh / a.Hq, g = h / G, hg = h % G;
+    const int2 own = g < kJoinHeads ? s_pair[g] : make_int2(a.pair_nchunks[r * a.Hkv + g], a.pair_part_base[r * a.Hkv + g]);
+    const int nch = own.x, base = own.y;
     const int64_t qh = (int64_t)(q0 + j) * a.Hq + h, at = qh * a.D + dv * 4;
     if (bad || nch == 0) {
-      for (int i = 0; i < 4; ++i) st_from_float(out, at + i, 0.f);
+      store4(out + at, make_float4(0.f, 0.f, 0.f, 0.f));
       if (dv == 0 && a.lse) a.lse[qh] = __int_as_float(0x7fc00000);
       continue;
     }
-    const int2 part = x.part;
-    const int64_t prow = x.prow;
+    int2 part = make_int2(0, 0);     // first slot, pieces
+    int64_t prow = 0;
+    if (tiles > 0) {
+      int row = row_in + j * G + hg, it = 0;
+      while (row >= p.unit_rows) { row -= p.unit_rows; ++it; }
+      part = s_part[it];
+      prow = row;
+    }
     float mstar = -INFINITY, lstar = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const int n = nch + part.y;
@@ -510,10 +509,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(AttnParams a, PromptPa
       }
     }
     const float inv = 1.f / lstar;
-    st_from_float(out, at + 0, acc.x * inv);
-    st_from_float(out, at + 1, acc.y * inv);
-    st_from_float(out, at + 2, acc.z * inv);
-    st_from_float(out, at + 3, acc.w * inv);
+    store4(out + at, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
     if (dv == 0 && a.lse) a.lse[qh] = (mstar + log2f(lstar)) * kLn2;
   }
 }

@@ -684,7 +684,7 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
   if (e != cudaSuccess) return SPX_ERR_CUDA;
   if (grouped) {
     const int64_t items = (int64_t)p.max_q_len * p.Hq * (p.D / 4);
-    const dim3 grid(p.batch, (unsigned)((items + 255) / 256));
+    const dim3 grid(p.batch, (unsigned)((items + 1023) / 1024));   // four items a thread
     e = a->kv_dtype == SPX_F32 ? launch_pdl(prefix_join_kernel<float>, grid, dim3(256), 0, stream, p, pre)
                                : launch_pdl(prefix_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, stream, p, pre);
     ++t_launches;
