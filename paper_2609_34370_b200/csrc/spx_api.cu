@@ -470,8 +470,8 @@ static PromptParams prompt_params(const spx_attn_args_t *a, const PromptWs &w, u
   p.workers = sms * (tc ? 1 : 2);
   // in eighths of a tile: of 128 tokens by 256 rows on the tensor cores (2 us; an entry's ends 4, the join 12), by 64 rows in fp32
   // arithmetic (10 us)
-  p.entry_cost = tc ? 16 : 8;
-  p.join_cost = tc ? 48 : 8;
+  p.entry_cost = tc ? 16 : 3;
+  p.join_cost = tc ? 48 : 4;
   p.min_piece = tc ? 4 : 1;
   p.hdr = reinterpret_cast<PromptHeader *>(ws + w.hdr);
   p.unit_item0 = reinterpret_cast<int32_t *>(ws + w.unit_item0);
@@ -545,7 +545,7 @@ static spx_status_t launch_prompts(const spx_attn_args_t *a, const PromptWs &w, 
   if (e != cudaSuccess) return SPX_ERR_CUDA;
   e = launch_prompt_main(a, p, stream, dev);
   if (e != cudaSuccess) return SPX_ERR_CUDA;
-  const dim3 grid(64, (p.unit_rows * (p.D / 4) + 255) / 256);
+  const dim3 grid(74, 8);   // most calls have nothing to join: no more blocks than run at once
   e = a->kv_dtype == SPX_F32 ? launch_pdl(prompt_join_kernel<float>, grid, dim3(256), 0, stream, p)
                              : launch_pdl(prompt_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, stream, p);
   ++t_launches;
