@@ -112,25 +112,43 @@ kv_append_kernel(const __grid_constant__ KvAppendParams p, const __grid_constant
   auto valid = [&](int q0, int q1, int L) -> bool {
     return q0 >= 0 && q1 > q0 && q1 <= p.total_q && L >= q1 - q0 && (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req;
   };
-  // the request of this block: each thread looks whether it is one of its own (in one memory round trip for up to 256 of
-  // them, whose bounds and length the block then has); block 0 looks at all lengths
   if (tid == 0) s_req = -1;
-  bool bad_len = false;
-  for (int c0 = 0; c0 < p.batch; c0 += kAppendThreads) {
-    const int c = c0 + tid;
+  if (p.batch <= kAppendThreads) {
+    // the request of this block: each thread looks whether it is its own, in one memory round trip
+    const int c = tid;
     int q0 = 0, q1 = 0, L = 0;
     if (c < p.batch) { q0 = p.q_indptr[c]; q1 = p.q_indptr[c + 1]; L = p.seq_lens[c]; }
-    if (c0 == 0) {
-      if (kRope)
-        for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
-      __syncthreads();
+    if (kRope)
+      for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
+    __syncthreads();
+    if (c < p.batch) {
+      const int64_t first = (int64_t)(q0 >> p.log2_rows) + c, next = (int64_t)(q1 >> p.log2_rows) + c + 1;
+      if (first <= (int64_t)blockIdx.x && (int64_t)blockIdx.x < next) { s_req = c; s_q0 = q0; s_m = valid(q0, q1, L) ? q1 - q0 : 0; s_L = L; }
+      if (blockIdx.x == 0 && !valid(q0, q1, L)) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
     }
-    if (c >= p.batch) continue;
-    const int64_t first = (int64_t)(q0 >> p.log2_rows) + c, next = (int64_t)(q1 >> p.log2_rows) + c + 1;
-    if (first <= (int64_t)blockIdx.x && (int64_t)blockIdx.x < next) { s_req = c; s_q0 = q0; s_m = valid(q0, q1, L) ? q1 - q0 : 0; s_L = L; }
-    bad_len |= !valid(q0, q1, L);
+  } else {
+    if (kRope)
+      for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
+    if (tid < 32) {
+      // 32 probes at a time
+      int lo = 0, hi = p.batch;   // base(lo) <= block, hi past the last candidate
+      while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, c = lo + tid * step;
+        const bool below = c < hi && (int64_t)(p.q_indptr[c] >> p.log2_rows) + c <= (int64_t)blockIdx.x;
+        const int n = __popc(__ballot_sync(0xffffffffu, below || tid == 0));   // the probes ascend
+        const int at = lo + (n - 1) * step;
+        hi = min(hi, at + step);
+        lo = at;
+      }
+      if (tid == 0) {
+        const int q0 = p.q_indptr[lo], q1 = p.q_indptr[lo + 1], L = p.seq_lens[lo];
+        s_req = lo; s_q0 = q0; s_m = valid(q0, q1, L) ? q1 - q0 : 0; s_L = L;
+      }
+    }
+    // lengths are looked at by the blocks together (a block of an invalid request may not come to it)
+    for (int c = blockIdx.x * kAppendThreads + tid; c < p.batch; c += gridDim.x * kAppendThreads)
+      if (!valid(p.q_indptr[c], p.q_indptr[c + 1], p.seq_lens[c])) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   }
-  if (blockIdx.x == 0 && bad_len) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   __syncthreads();
   const int r = s_req, q0 = s_q0, m = s_m, L = s_L;
   if (r < 0 || m == 0) return;

@@ -180,3 +180,35 @@ def test_prompts_with_images_enter_and_attend(kind, dtype):
     if scales:
         b.k_scales, b.v_scales = scales["k_scales"].cpu(), scales["v_scales"].cpu()
     b.check(out, lse)
+
+
+@pytest.mark.parametrize("rope", [False, True])
+def test_a_batch_of_many_requests(rope):
+    """More requests than a block looks at in one go, one of them invalid, prompts among single tokens."""
+    n = 700
+    m = [1 + (i % 3) for i in range(n)]
+    m[300], m[650] = 100, 37
+    lens = [x + i % 20 for i, x in enumerate(m)]
+    b = Batch(lens, m, 2, 1, 64, 16, dtype=F32, seed=13, poison=0.5)
+    g = torch.Generator().manual_seed(8)
+    new_k, new_v = (torch.randn(b.starts[-1], 1, 64, generator=g) for _ in range(2))
+    (_, k, v, strides, table, lens_d, starts, _, page, pages), _ = b.device()
+    lens_d[5] = 0
+    status = spx.kv_append(new_k.to(DEV), new_v.to(DEV), k, v, strides, table, lens_d, starts, page, pages, rope_base=10000.0 if rope else 0.0)
+    assert int(status.item()) == spx.DEV_BAD_LEN
+    t = torch.cat([torch.arange(a - c, a) for a, c in zip(lens, m)])
+    want_k = turned(new_k.double().numpy(), t[None].numpy().astype(np.float64), 10000.0, [32], False) if rope else new_k.double().numpy()
+    want = b.v.clone()
+    got_k = []
+    for r in range(n):
+        at = torch.arange(lens[r] - m[r], lens[r])
+        where = (b.table[r].long()[at // 16], at % 16)
+        if r != 5:
+            want.transpose(1, 2)[where] = new_v[b.starts[r]:b.starts[r + 1]]
+            got_k.append(k.cpu().transpose(1, 2)[where] if r % 50 == 0 or m[r] > 3 else None)
+        else:
+            got_k.append(None)
+    assert torch.equal(v.cpu(), want)
+    for r, x in enumerate(got_k):
+        if x is not None:
+            _check_rows(x, want_k[b.starts[r]:b.starts[r + 1]], F32)
