@@ -273,6 +273,33 @@ def time_extras(spx, binding, spec, b, attn_args, dev, iters: int = 200):
         if int(ws8.status.item()) != 0 or int(lws.status.item()) != 0:
             out["status_e4m3"] = [int(ws8.status.item()), int(lws.status.item())]
         del pools8, scales8, out8, lse8
+    # a prompt entering a cache of its own and attending, and the step with a prefix that every request shares
+    rows = 4096
+    npp = rows // spec.page_size
+    pk, pv = (torch.zeros((npp, spec.num_kv_heads, spec.page_size, b.q.shape[2]), dtype=b.q.dtype, device=dev) for _ in range(2))
+    prompt_q = torch.randn((rows,) + b.q.shape[1:], device=dev).to(b.q.dtype)
+    prompt_kv = torch.randn((rows, spec.num_kv_heads, b.q.shape[2]), device=dev).to(b.q.dtype)
+    table = torch.arange(npp, dtype=torch.int32, device=dev)[None]
+    length, start = (torch.tensor(x, dtype=torch.int32, device=dev) for x in ([rows], [0, rows]))
+    pargs = (pk, pv, pk.stride()[:3], table, length, start)
+    out["prompt_append_rope_us"] = timed(lambda: spx.kv_append(prompt_kv, prompt_kv, *pargs, spec.page_size, npp, status=status, rope_base=500000.0))
+    p_out, p_lse, pws = spx.prompt_attention(prompt_q, *pargs, spec.num_kv_heads, spec.page_size, npp)
+    out["prompt_attention_us"] = timed(lambda: spx.prompt_attention(prompt_q, *pargs, spec.num_kv_heads, spec.page_size, npp, out=p_out, lse=p_lse, ws=pws))
+    out["prompt_attention_tflops"] = 2 * b.q.shape[1] * b.q.shape[2] * rows * (rows + 1) / (out["prompt_attention_us"] * 1e-6) / 1e12
+    shared = (int(b.seq_lens.min()) - 16) // spx.PREFIX_TILE * spx.PREFIX_TILE
+    if shared > 0:
+        same = b.block_table.clone()
+        same[:, :shared // spec.page_size] = same[0, :shared // spec.page_size]
+        groups, prefix = (torch.tensor(x, dtype=torch.int32, device=dev) for x in ([0, b.batch], [shared]))
+        g_out, g_lse = torch.empty_like(b.q), torch.empty(b.q.shape[:2], dtype=torch.float32, device=dev)
+        ag = binding.make_attn_args(b.q, b.k_cache, b.v_cache, b.kv_strides, same, b.seq_lens, b.q_indptr, spec.num_kv_heads, spec.page_size,
+                                    b.num_pages, g_out, g_lse, max_q_len=max(b.k_host) + 1, group_indptr=groups, prefix_lens=prefix)
+        gws = spx.Workspace.allocate(spx.workspace_size(ag, base), dev)
+        out["shared_prefix_tokens"], out["step_shared_prefix_us"] = shared, timed(lambda: spx.verify_step(ag, base, gws, dev))
+        if int(gws.status.item()) != 0 or int(pws.status.item()) != 0:
+            out["status_prompts"] = [int(gws.status.item()), int(pws.status.item())]
+        del g_out, g_lse, gws
+    del pk, pv, prompt_q, prompt_kv, p_out, p_lse, pws
     # selective-speculation support and Algorithm 1
     cws = spx.Workspace.allocate(1 << 20, dev)
     out["draft_confidence_us"] = timed(lambda: spx.draft_confidence(b.draft_logits, b.draft_ids, b.q_indptr, ws=cws))
@@ -519,7 +546,7 @@ def main():
     ap.add_argument("--no-others", action="store_true", help="skip the table of the other four workloads (profiling runs)")
     ap.add_argument("--other-steps", type=int, default=300, help="timed steps per workload of the `workloads` table")
     ap.add_argument("--extras", action="store_true",
-                    help="also time the pieces around the step: KV append / rollback, verification variants, 8-bit pools, log-probabilities")
+                    help="also time the pieces around the step: KV append / rollback, verification variants, 8-bit pools, log-probabilities, prompts, shared prefixes")
     ap.add_argument("--extras-iters", type=int, default=200, help="timed calls per extras entry (profiling runs: a few)")
     ap.add_argument("--batch", type=int, default=0, help="override the workload's batch size (profiling captures of a smaller case)")
     ap.add_argument("--timeline", action="store_true",
