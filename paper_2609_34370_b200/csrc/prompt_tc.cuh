@@ -12,7 +12,7 @@
 //                   and warps 12-15 turn the codes into bf16 tiles.
 // Tensor memory is full: two score buffers of 128 columns and two outputs of D.
 //
-// The running maximum of a row is a reference that moves only when a weight under it would pass 2^8 (the output
+// The running maximum of a row is a reference that moves only when weights under it grow past 2^8 or so (the output
 // is then rescaled by the row's own thread).  Weights are rounded to bf16 (half a step of 2^-8 each, the type V has to be multiplied in); their sum is
 // taken in fp32 before that.
 //
@@ -573,8 +573,9 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
       const int limit = valid ? (causal ? e.vis0 + pr / p.G : e.vis0) : e.vis0 + (causal ? e.row0 / p.G : 0);   // last token the row sees
       const int whole = causal ? e.vis0 + (e.row0 + x * half_rows) / p.G : e.vis0;                               // ... and every row of the group
       // The warp of the other group on the same scheduler takes turns with this one at the exponentials: left alone the two fall into step, at the
-      // exponential unit together and away from it together.
-      const bool turns = e.rows > half_rows + quad * 32;
+      // exponential unit together and away from it together (the chunk of 500 rows behind 30,000 tokens 264 us, 249 with turns; a ragged
+      // batch 302, 283).  Where codes are converted beside them turns only wait (six prompts over 8-bit pools: 477 without, 533 with).
+      const bool turns = !kCodes && e.rows > half_rows + quad * 32;
       float m_ref = -INFINITY;
       bool fresh = true;          // some row of the warp has no reference yet
       uint64_t sum_a = pair(0.f, 0.f), sum_b = sum_a;
@@ -600,10 +601,11 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
           if (active) {
             const float4 *fk = factors + h * 16;
             const float2 *fv = reinterpret_cast<const float2 *>(factors + 32 + h * 16);
-            const uint64_t was_a = sum_a, was_b = sum_b;
             uint32_t pk[32];
-            // The weights are made under the reference as it is; only if one is past 2^8 (or a row has none yet) is the maximum
-            // taken, the reference moved and the weights made once more from the scores, which are still there.
+            uint64_t half_a, half_b;     // sums of the half's weights
+            // The weights are made under the reference as it is; only if their sum is past 64 * 2^8 (or a row has no reference yet) is
+            // the maximum taken, the reference moved and the weights made once more from the scores, which are still there.  (bf16
+            // has fp32's exponents: large weights lose nothing; looking for the largest weight instead took 5% more time.)
             bool look = fresh, held = false;
 #pragma unroll 1
             for (;;) {
@@ -661,7 +663,7 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
               const float ref = m_ref == -INFINITY ? 0.f : -m_ref;
               const uint64_t ref2 = pair(ref, ref);
               if (look) fresh = __any_sync(0xffffffffu, m_ref == -INFINITY);
-              float most = 0.f;
+              half_a = half_b = pair(0.f, 0.f);
               if (turns && !held) wait(&bars->turn[x][quad], x == 0 ? n_turn ^ 1 : n_turn, bars);
               auto weights = [&](auto scaled) {
                 constexpr int kBatch = 16, kHandOn = 48;
@@ -669,9 +671,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
 #pragma unroll
                   for (int i = 0; i < kBatch / 2; ++i) {
                     float a = s[at + 2 * i], b = s[at + 2 * i + 1];
-                    most = fmaxf(most, fmaxf(a, b));
-                    if (i & 1) sum_b = add2(sum_b, pair(a, b));
-                    else sum_a = add2(sum_a, pair(a, b));
+                    if (i & 1) half_b = add2(half_b, pair(a, b));
+                    else half_a = add2(half_a, pair(a, b));
                     if constexpr (decltype(scaled)::value) {
                       const float2 f = fv[at / 2 + i];
                       a *= factor(f.x);
@@ -694,11 +695,13 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
               };
               if (kCodes && general) weights(std::true_type());
               else weights(std::false_type());
-              if (look || !__any_sync(0xffffffffu, most > 256.f)) break;
+              float a, b;
+              unpair(add2(half_a, half_b), a, b);
+              if (look || !__any_sync(0xffffffffu, valid && !(a + b <= 16384.f))) break;   // (NaN too; rows that are none may hold anything)
               look = true;
-              sum_a = was_a;
-              sum_b = was_b;
             }
+            sum_a = add2(sum_a, half_a);
+            sum_b = add2(sum_b, half_b);
             tmem_st32(ts + h * 64, pk);
             wait_st();
           }
