@@ -119,7 +119,8 @@ typedef enum { SPX_CACHE_KV_DTYPE = 0, SPX_CACHE_E4M3 = 1 } spx_cache_format_t;
  * tokens in fp32.  Requests that no group holds, groups of one and prefixes shorter than a tile share nothing.  A request
  * whose block-table row differs from its group's first within those tiles sets SPX_DEV_BAD_PAGE, one with L_r - m_r below
  * them (the new positions belong to no prefix) SPX_DEV_BAD_LEN; both get the sentinel outputs, and so do all requests of a
- * group with a page id out of range in its prefix.  prefix_lens below zero count as zero.  The workspace is larger with groups: size it with num_groups set.
+ * group with a page id out of range in its prefix.  prefix_lens below zero count as zero.  (Two kernels and partial results for every request: worth their
+ * 25 to 30 us where a prefix of thousands of tokens has many requests behind it.)  The workspace is larger with groups: size it with num_groups set.
  */
 #define SPX_PREFIX_TILE 128
 typedef struct {
@@ -246,8 +247,9 @@ spx_status_t spx_verify_step(const spx_attn_args_t *attn, const spx_sample_args_
  * spx_prompt_workspace_size (0 = invalid arguments).  Errors in device data as for spx_verify_attention (L_r < m_r:
  * SPX_DEV_BAD_LEN).  Shared prefixes (num_groups > 0) are SPX_ERR_UNSUPPORTED here: a prompt's own rows
  * fill the tensor cores' tiles.
- * BF16 rows: fp32 accumulation, weights rounded to bfloat16 before they meet V (as in spx_verify_attention over 16-bit pools; also over 8-bit pools), their
- * sum before that rounding.  F32 rows, and pages of fewer than 8 tokens: fp32 products.
+ * BF16 rows: fp32 accumulation; weights are rounded to bfloat16 before they meet V (as in spx_verify_attention over 16-bit pools; over 8-bit pools times
+ * what a power of two leaves of their token's scale), their sum is taken before that.  8-bit values are exact but for those below 2^-126.  F32 rows,
+ * and pages of fewer than 8 tokens: fp32 products.
  */
 size_t spx_prompt_workspace_size(const spx_attn_args_t *args);
 spx_status_t spx_prompt_attention(const spx_attn_args_t *args, void *ws, size_t ws_bytes, int32_t *dev_status, void *cuda_stream);
