@@ -119,8 +119,8 @@ typedef enum { SPX_CACHE_KV_DTYPE = 0, SPX_CACHE_E4M3 = 1 } spx_cache_format_t;
  * tokens in fp32.  Requests that no group holds, groups of one and prefixes shorter than a tile share nothing.  A request
  * whose block-table row differs from its group's first within those tiles sets SPX_DEV_BAD_PAGE, one with L_r - m_r below
  * them (the new positions belong to no prefix) SPX_DEV_BAD_LEN; both get the sentinel outputs, and so do all requests of a
- * group with a page id out of range in its prefix.  prefix_lens below zero count as zero.  (Two kernels and partial results for every request: worth their
- * 25 to 30 us where a prefix of thousands of tokens has many requests behind it.)  The workspace is larger with groups: size it with num_groups set.
+ * group with a page id out of range in its prefix.  prefix_lens below zero count as zero.  (Two more kernels and partial results for
+ * every request: 64 requests of 6 rows, 32/8 heads of 128, gain from some 1300 shared tokens on and lose below.)  The workspace is larger with groups: size it with num_groups set.
  */
 #define SPX_PREFIX_TILE 128
 typedef struct {

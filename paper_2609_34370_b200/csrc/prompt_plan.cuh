@@ -10,7 +10,8 @@
 // prompt behind a long history: 64 entries of 238 tiles for 148 CTAs), long entries are cut into equal pieces along the tokens,
 // whose partial results a second kernel joins.  All items of a request are cut at the same tokens and are neighbours in the list,
 // so that the CTAs that read the same tokens do so together (a range of the tiles for each CTA, cut where it fell, balanced
-// better on paper and read the cache from HBM several times over: 250 to 420 us for that chunk, from board to board).
+// better on paper and read the cache from HBM several times over: 250 to 420 us for that chunk, from board to board).  A latency chain: 7 to 11 us a plan,
+// joins 1 us (24 prompts) to 23 (128 requests behind shared prefixes, 64 heads).
 #pragma once
 #include "common.cuh"
 #include "plan.cuh"
