@@ -106,27 +106,28 @@ __device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2
 template <bool kRope>
 __global__ void __launch_bounds__(kAppendThreads, 3)
 kv_append_kernel(const __grid_constant__ KvAppendParams p, const __grid_constant__ typename std::conditional<kRope, KvAppendAxes, KvNoAxes>::type ax) {
-  __shared__ int s_req, s_q0, s_m, s_L, s_page[kAppendRows];
+  __shared__ int s_page[kAppendRows], s_first;
+  __shared__ uint32_t s_claims[kAppendThreads / 32];   // bit i of word w: request s_first + 32 w + i has rows of this block
   __shared__ double s_inv_freq[kRope ? kRopeMaxHeadDim / 2 : 1];
   __shared__ __align__(16) double2 s_cs[kRope ? kAppendAngles : 1];
   const int tid = threadIdx.x;
   auto valid = [&](int q0, int q1, int L) -> bool {
     return q0 >= 0 && q1 > q0 && q1 <= p.total_q && L >= q1 - q0 && (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req;
   };
-  if (tid == 0) s_req = -1;
   if (p.batch <= kAppendThreads) {
-    // the request of this block: each thread looks whether it is its own, in one memory round trip
+    // the request of this block: each thread looks whether it is its own, in one memory round trip.  (Only where q_indptr descends
+    // somewhere can it be more than one, or another than the one whose rows these are by their number.)
     const int c = tid;
     int q0 = 0, q1 = 0, L = 0;
     if (c < p.batch) { q0 = p.q_indptr[c]; q1 = p.q_indptr[c + 1]; L = p.seq_lens[c]; }
     if (kRope)
       for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
-    __syncthreads();
-    if (c < p.batch) {
-      const int64_t first = (int64_t)(q0 >> p.log2_rows) + c, next = (int64_t)(q1 >> p.log2_rows) + c + 1;
-      if (first <= (int64_t)blockIdx.x && (int64_t)blockIdx.x < next) { s_req = c; s_q0 = q0; s_m = valid(q0, q1, L) ? q1 - q0 : 0; s_L = L; }
-      if (blockIdx.x == 0 && !valid(q0, q1, L)) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
-    }
+    const bool ok = c < p.batch && valid(q0, q1, L);
+    const int64_t first = (int64_t)(q0 >> p.log2_rows) + c, next = (int64_t)(q1 >> p.log2_rows) + c + 1;
+    const uint32_t claims = __ballot_sync(0xffffffffu, ok && first <= (int64_t)blockIdx.x && (int64_t)blockIdx.x < next);
+    if ((tid & 31) == 0) s_claims[tid >> 5] = claims;
+    if (tid == 0) s_first = 0;
+    if (blockIdx.x == 0 && c < p.batch && !ok) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   } else {
     if (kRope)
       for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
@@ -141,99 +142,106 @@ kv_append_kernel(const __grid_constant__ KvAppendParams p, const __grid_constant
         hi = min(hi, at + step);
         lo = at;
       }
-      if (tid == 0) {
-        const int q0 = p.q_indptr[lo], q1 = p.q_indptr[lo + 1], L = p.seq_lens[lo];
-        s_req = lo; s_q0 = q0; s_m = valid(q0, q1, L) ? q1 - q0 : 0; s_L = L;
-      }
+      if (tid < kAppendThreads / 32) s_claims[tid] = tid == 0;
+      if (tid == 0) s_first = lo;
     }
     // lengths are looked at by the blocks together (a block of an invalid request may not come to it)
     for (int c = blockIdx.x * kAppendThreads + tid; c < p.batch; c += gridDim.x * kAppendThreads)
       if (!valid(p.q_indptr[c], p.q_indptr[c + 1], p.seq_lens[c])) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   }
   __syncthreads();
-  const int r = s_req, q0 = s_q0, m = s_m, L = s_L;
-  if (r < 0 || m == 0) return;
-  const int64_t j0_64 = ((int64_t)blockIdx.x - ((q0 >> p.log2_rows) + (int64_t)r)) << p.log2_rows;
-  if (j0_64 < 0 || j0_64 >= m) return;
-  const int j0 = (int)j0_64, n = min(1 << p.log2_rows, m - j0), t0 = L - m + j0;
-  const int32_t *table = p.block_table + (int64_t)r * p.max_pages_per_req;
-  if (tid < n) s_page[tid] = table[(t0 + tid) >> p.log2P];
-  // a request with a bad page among its new positions is skipped as a whole: every one of its blocks looks at all of them
-  int bad = 0;
-  for (int i = ((L - m) >> p.log2P) + tid; i <= (L - 1) >> p.log2P; i += kAppendThreads) {
-    const int pg = table[i];
-    bad |= pg < 0 || pg >= p.num_pages;
-  }
-  if constexpr (kRope) {
-    const int half = p.D >> 1;
-    for (int i = tid; i < n * half; i += kAppendThreads) {
-      const int row = i / half, pair = i % half;
-      const int t = ax.axes ? ax.positions[(int64_t)ax.axis_of[pair] * ax.position_stride + q0 + j0 + row] : t0 + row;
-      double c, sn;
-      sincos((double)t * s_inv_freq[pair], &sn, &c);
-      if (p.elem_size == 4) {
-        s_cs[row * half + (pair & 3) * (half >> 2) + (pair >> 2)] = make_double2(c, sn);
-      } else {
-        float *at = reinterpret_cast<float *>(s_cs + row * half + (pair & 6) * (half >> 3) + (pair >> 3)) + (pair & 1);
-        const float ch = (float)c, sh = (float)sn;
-        at[0] = ch; at[2] = (float)(c - (double)ch);
-        at += (half >> 3) * 4;
-        at[0] = sh; at[2] = (float)(sn - (double)sh);
+  // the block's rows of request r, whose bounds are looked at here once more: no thread goes by another's
+  auto append = [&](int r) {
+    const int q0 = p.q_indptr[r], q1 = p.q_indptr[r + 1], L = p.seq_lens[r], m = q1 - q0;
+    if (!valid(q0, q1, L)) return;
+    const int64_t j0_64 = ((int64_t)blockIdx.x - ((q0 >> p.log2_rows) + (int64_t)r)) << p.log2_rows;
+    if (j0_64 < 0 || j0_64 >= m) return;
+    const int j0 = (int)j0_64, n = min(1 << p.log2_rows, m - j0), t0 = L - m + j0;
+    const int32_t *table = p.block_table + (int64_t)r * p.max_pages_per_req;
+    if (tid < n) s_page[tid] = table[(t0 + tid) >> p.log2P];
+    // a request with a bad page among its new positions is skipped as a whole: every one of its blocks looks at all of them
+    int bad = 0;
+    for (int i = ((L - m) >> p.log2P) + tid; i <= (L - 1) >> p.log2P; i += kAppendThreads) {
+      const int pg = table[i];
+      bad |= pg < 0 || pg >= p.num_pages;
+    }
+    if constexpr (kRope) {
+      const int half = p.D >> 1;
+      for (int i = tid; i < n * half; i += kAppendThreads) {
+        const int row = i / half, pair = i % half;
+        const int t = ax.axes ? ax.positions[(int64_t)ax.axis_of[pair] * ax.position_stride + q0 + j0 + row] : t0 + row;
+        double c, sn;
+        sincos((double)t * s_inv_freq[pair], &sn, &c);
+        if (p.elem_size == 4) {
+          s_cs[row * half + (pair & 3) * (half >> 2) + (pair >> 2)] = make_double2(c, sn);
+        } else {
+          float *at = reinterpret_cast<float *>(s_cs + row * half + (pair & 6) * (half >> 3) + (pair >> 3)) + (pair & 1);
+          const float ch = (float)c, sh = (float)sn;
+          at[0] = ch; at[2] = (float)(c - (double)ch);
+          at += (half >> 3) * 4;
+          at[0] = sh; at[2] = (float)(sn - (double)sh);
+        }
       }
     }
-  }
-  if (__syncthreads_or(bad)) {
-    if (tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
-    return;
-  }
-  const int row_bytes = p.D * p.elem_size, vecs = row_bytes >> 4;
-  auto cache_at = [&](int row, int g) -> int64_t {
-    return ((int64_t)s_page[row] * p.stride_page + (int64_t)g * p.stride_head + (int64_t)((t0 + row) & (p.P - 1)) * p.stride_token) * p.elem_size;
+    if (__syncthreads_or(bad)) {
+      if (tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
+      return;
+    }
+    const int row_bytes = p.D * p.elem_size, vecs = row_bytes >> 4;
+    auto cache_at = [&](int row, int g) -> int64_t {
+      return ((int64_t)s_page[row] * p.stride_page + (int64_t)g * p.stride_head + (int64_t)((t0 + row) & (p.P - 1)) * p.stride_token) * p.elem_size;
+    };
+    if constexpr (kRope) {
+      // a thread takes one vector of the first half of a head row and its partner in the second half: K's rows, then the
+      // query rows (two at a time, in 114 registers: 44 us for prompts with images, against 40)
+      const int half_vecs = vecs >> 1, half_bytes = row_bytes >> 1;
+      const int n_k = n * p.Hkv * half_vecs, n_all = n_k + (p.q_rows ? n * p.Hq * half_vecs : 0);
+      struct Task { const unsigned char *src; unsigned char *dst; int row, v; uint4 lo, hi; };
+      auto open = [&](int i) -> Task {
+        Task t;
+        if (i < n_k) {
+          t.v = i % half_vecs;
+          const int jg = i / half_vecs, g = jg % p.Hkv;
+          t.row = jg / p.Hkv;
+          t.src = p.new_k + ((int64_t)(q0 + j0 + t.row) * p.Hkv + g) * row_bytes + t.v * 16;
+          t.dst = p.k_cache + cache_at(t.row, g) + t.v * 16;
+        } else {
+          i -= n_k;
+          t.v = i % half_vecs;
+          const int jh = i / half_vecs, h = jh % p.Hq;
+          t.row = jh / p.Hq;
+          const int64_t at = ((int64_t)(q0 + j0 + t.row) * p.Hq + h) * row_bytes + t.v * 16;
+          t.src = p.q_rows + at;
+          t.dst = p.q_out + at;
+        }
+        t.lo = *reinterpret_cast<const uint4 *>(t.src);
+        t.hi = *reinterpret_cast<const uint4 *>(t.src + half_bytes);
+        return t;
+      };
+      auto close = [&](Task &t) {
+        const double2 *cs = s_cs + t.row * (p.D >> 1);
+        if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(t.lo, t.hi, cs, half_vecs, t.v);
+        else rope_vectors<float>(t.lo, t.hi, cs, half_vecs, t.v);
+        *reinterpret_cast<uint4 *>(t.dst) = t.lo;
+        *reinterpret_cast<uint4 *>(t.dst + half_bytes) = t.hi;
+      };
+      for (int i = tid; i < n_all; i += kAppendThreads) {
+        Task t = open(i);
+        close(t);
+      }
+    }
+    for (int i = tid; i < n * p.Hkv * vecs; i += kAppendThreads) {
+      const int v = i % vecs, jg = i / vecs, g = jg % p.Hkv, row = jg / p.Hkv;
+      const int64_t src = ((int64_t)(q0 + j0 + row) * p.Hkv + g) * row_bytes + v * 16, dst = cache_at(row, g) + v * 16;
+      if (!kRope) *reinterpret_cast<uint4 *>(p.k_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src));
+      *reinterpret_cast<uint4 *>(p.v_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_v + src));
+    }
   };
-  if constexpr (kRope) {
-    // a thread takes one vector of the first half of a head row and its partner in the second half: K's rows, then the
-    // query rows (two at a time, in 114 registers: 44 us for prompts with images, against 40)
-    const int half_vecs = vecs >> 1, half_bytes = row_bytes >> 1;
-    const int n_k = n * p.Hkv * half_vecs, n_all = n_k + (p.q_rows ? n * p.Hq * half_vecs : 0);
-    struct Task { const unsigned char *src; unsigned char *dst; int row, v; uint4 lo, hi; };
-    auto open = [&](int i) -> Task {
-      Task t;
-      if (i < n_k) {
-        t.v = i % half_vecs;
-        const int jg = i / half_vecs, g = jg % p.Hkv;
-        t.row = jg / p.Hkv;
-        t.src = p.new_k + ((int64_t)(q0 + j0 + t.row) * p.Hkv + g) * row_bytes + t.v * 16;
-        t.dst = p.k_cache + cache_at(t.row, g) + t.v * 16;
-      } else {
-        i -= n_k;
-        t.v = i % half_vecs;
-        const int jh = i / half_vecs, h = jh % p.Hq;
-        t.row = jh / p.Hq;
-        const int64_t at = ((int64_t)(q0 + j0 + t.row) * p.Hq + h) * row_bytes + t.v * 16;
-        t.src = p.q_rows + at;
-        t.dst = p.q_out + at;
-      }
-      t.lo = *reinterpret_cast<const uint4 *>(t.src);
-      t.hi = *reinterpret_cast<const uint4 *>(t.src + half_bytes);
-      return t;
-    };
-    auto close = [&](Task &t) {
-      const double2 *cs = s_cs + t.row * (p.D >> 1);
-      if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(t.lo, t.hi, cs, half_vecs, t.v);
-      else rope_vectors<float>(t.lo, t.hi, cs, half_vecs, t.v);
-      *reinterpret_cast<uint4 *>(t.dst) = t.lo;
-      *reinterpret_cast<uint4 *>(t.dst + half_bytes) = t.hi;
-    };
-    for (int i = tid; i < n_all; i += kAppendThreads) {
-      Task t = open(i);
-      close(t);
+  for (int w = 0; w < kAppendThreads / 32; ++w) {
+    for (uint32_t claims = s_claims[w]; claims; claims &= claims - 1) {
+      append(s_first + 32 * w + __ffs(claims) - 1);
+      __syncthreads();   // page ids and angles are read
     }
-  }
-  for (int i = tid; i < n * p.Hkv * vecs; i += kAppendThreads) {
-    const int v = i % vecs, jg = i / vecs, g = jg % p.Hkv, row = jg / p.Hkv;
-    const int64_t src = ((int64_t)(q0 + j0 + row) * p.Hkv + g) * row_bytes + v * 16, dst = cache_at(row, g) + v * 16;
-    if (!kRope) *reinterpret_cast<uint4 *>(p.k_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src));
-    *reinterpret_cast<uint4 *>(p.v_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_v + src));
   }
 }
 
