@@ -10,12 +10,14 @@ namespace spx {
 
 constexpr int kRopeMaxHeadDim = 512;
 constexpr int kAppendThreads = 256;
-constexpr int kAppendRows = 8;          // new rows of a block, at most
-constexpr int kAppendAngles = 1024;     // (row, pair) angles a block keeps: 8 rows of 256 elements, 4 of 512
+constexpr int kAppendRows = 8;          // new rows of a step, at most
+constexpr int kAppendVote = 1024;       // requests that the threads of a block look at in one go
+constexpr int kAppendAngles = 1024;     // (row, pair) angles a step keeps: 8 rows of 256 elements, 4 of 512
 
 struct KvAppendParams {
   int32_t batch, total_q, Hkv, D, P, log2P, num_pages, max_pages_per_req, elem_size;
-  int32_t log2_rows;       // new rows of a block
+  int32_t log2_rows;       // new rows of a step
+  int32_t log2_block;      // ... and of a block
   const unsigned char *new_k, *new_v;
   unsigned char *k_cache, *v_cache;
   int64_t stride_page, stride_head, stride_token;  // elements
@@ -26,9 +28,8 @@ struct KvAppendParams {
   unsigned char *q_out;
   int32_t Hq;
 };
-// Positions of several axes (axes = 0: a row's position is its place in the request).
+// Positions of several axes; without, a row's position is its place in the request.
 struct KvAppendAxes {
-  int32_t axes;
   const int32_t *positions;
   int64_t position_stride;
   unsigned char axis_of[kRopeMaxHeadDim / 2];
@@ -96,152 +97,205 @@ __device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2
   }
 }
 
-// A block takes up to kAppendRows new rows of a request, all heads of K, V and the query rows, 16 bytes a thread and step.
-// Block b belongs to the request r with base(r) <= b < base(r + 1), base(r) = q_indptr[r] / rows + r: m rows are at most
-// m / rows + 1 blocks, so no prefix sums are needed; blocks past a request's last one, and past the last request's, leave at once.  The angles are
-// worked out once a block and shared by its heads.
+// A block takes 1 << log2_block new rows of a request, up to kAppendRows a step, all heads of K, V and the query rows, 16 bytes a thread at a time.
+// Block r < batch takes the first rows of request r: in a verify step nearly all there are, with no search for whose rows they are
+// (64 requests of 6 rows, 8 heads of 128: 3.0 us with one, 2.6 without), and whatever the other requests' bounds are.  What a request has beyond is for the blocks behind:
+// its rows from j << log2_block on, j > 0, are those of block batch + (q_indptr[r] >> log2_block) + j - 1, which is below
+// batch + (q_indptr[r + 1] >> log2_block), so that no prefix sums are needed.  Blocks that are nobody's leave at once.  The angles are worked out once a
+// step and shared by its heads.
 // Pure copy and rotation: bound by launch latency at verify-step sizes (a few MB), by HBM beyond that.
-// kRope: with a rotary base (without, a kernel of fewer registers).  Eight rows a block, three blocks per SM: five prompts with images 40 us
-// (16 rows 49, two vectors a thread in flight 44, four blocks 41).
-template <bool kRope>
-__global__ void __launch_bounds__(kAppendThreads, 3)
-kv_append_kernel(const __grid_constant__ KvAppendParams p, const __grid_constant__ typename std::conditional<kRope, KvAppendAxes, KvNoAxes>::type ax) {
-  __shared__ int s_page[kAppendRows], s_first;
-  __shared__ uint32_t s_claims[kAppendThreads / 32];   // bit i of word w: request s_first + 32 w + i has rows of this block
+// kRope: with a rotary base (without, a kernel of fewer registers).  Eight rows a step, three blocks per SM: five prompts with images 38 us
+// (16 rows, two vectors a thread in flight, four blocks: slower each).
+template <bool kRope, typename Axes>
+__global__ void __launch_bounds__(kAppendThreads, kRope ? 3 : 4)
+kv_append_kernel(const __grid_constant__ KvAppendParams p, const __grid_constant__ Axes ax) {
+  __shared__ int s_page[kAppendRows];
+  __shared__ int4 s_whose;                 // a request and its bounds
   __shared__ double s_inv_freq[kRope ? kRopeMaxHeadDim / 2 : 1];
   __shared__ __align__(16) double2 s_cs[kRope ? kAppendAngles : 1];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, rows = 1 << p.log2_rows;
+  const bool head = blockIdx.x < (unsigned)p.batch;
+  const int chunk = (int)blockIdx.x - p.batch;
   auto valid = [&](int q0, int q1, int L) -> bool {
     return q0 >= 0 && q1 > q0 && q1 <= p.total_q && L >= q1 - q0 && (((int64_t)L + p.P - 1) >> p.log2P) <= (int64_t)p.max_pages_per_req;
   };
-  if (p.batch <= kAppendThreads) {
-    // the request of this block: each thread looks whether it is its own, in one memory round trip.  (Only where q_indptr descends
-    // somewhere can it be more than one, or another than the one whose rows these are by their number.)
-    const int c = tid;
-    int q0 = 0, q1 = 0, L = 0;
-    if (c < p.batch) { q0 = p.q_indptr[c]; q1 = p.q_indptr[c + 1]; L = p.seq_lens[c]; }
-    if (kRope)
-      for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
-    const bool ok = c < p.batch && valid(q0, q1, L);
-    const int64_t first = (int64_t)(q0 >> p.log2_rows) + c, next = (int64_t)(q1 >> p.log2_rows) + c + 1;
-    const uint32_t claims = __ballot_sync(0xffffffffu, ok && first <= (int64_t)blockIdx.x && (int64_t)blockIdx.x < next);
-    if ((tid & 31) == 0) s_claims[tid >> 5] = claims;
-    if (tid == 0) s_first = 0;
-    if (blockIdx.x == 0 && c < p.batch && !ok) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
-  } else {
-    if (kRope)
-      for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
-    if (tid < 32) {
-      // 32 probes at a time
-      int lo = 0, hi = p.batch;   // base(lo) <= block, hi past the last candidate
+  // first of the block's rows of a request
+  auto first_row = [&](int q0) -> int64_t { return head ? 0 : ((int64_t)chunk - (q0 >> p.log2_block) + 1) << p.log2_block; };
+  auto takes_part = [&](int q0, int q1, int L) -> bool {
+    const int64_t first = first_row(q0);
+    return valid(q0, q1, L) && (head || first > 0) && first < q1 - q0;
+  };
+  int r = blockIdx.x, q0 = 0, q1 = 0, L = 0;
+  if (head) { q0 = p.q_indptr[r]; q1 = p.q_indptr[r + 1]; L = p.seq_lens[r]; }
+  uint32_t mine = 0;      // bit u: request tid + u * kAppendThreads has rows of this block
+  if (!head) {
+    if (p.batch <= kAppendVote) {
+      // each thread looks whether the rows are its own requests', in one memory round trip
+      int a[kAppendVote / kAppendThreads][3];
+#pragma unroll
+      for (int u = 0; u < kAppendVote / kAppendThreads; ++u) {
+        const int c = tid + u * kAppendThreads;
+        a[u][0] = -1; a[u][1] = a[u][2] = 0;
+        if (c < p.batch) { a[u][0] = p.q_indptr[c]; a[u][1] = p.q_indptr[c + 1]; a[u][2] = p.seq_lens[c]; }
+      }
+#pragma unroll
+      for (int u = 0; u < kAppendVote / kAppendThreads; ++u)
+        if (takes_part(a[u][0], a[u][1], a[u][2])) {
+          s_whose = make_int4(mine ? -1 : tid + u * kAppendThreads, a[u][0], a[u][1], a[u][2]);
+          mine |= 1u << u;
+        }
+    } else if (tid < 32) {
+      // the last request that starts at or before the block's rows, 32 probes at a time.  (Where q_indptr descends somewhere this may
+      // miss a request, whose rows behind its first block's then stay out.)
+      int lo = 0, hi = p.batch;
       while (hi - lo > 1) {
         const int step = (hi - lo + 31) / 32, c = lo + tid * step;
-        const bool below = c < hi && (int64_t)(p.q_indptr[c] >> p.log2_rows) + c <= (int64_t)blockIdx.x;
+        const bool below = c < hi && (p.q_indptr[c] >> p.log2_block) <= chunk;
         const int n = __popc(__ballot_sync(0xffffffffu, below || tid == 0));   // the probes ascend
         const int at = lo + (n - 1) * step;
         hi = min(hi, at + step);
         lo = at;
       }
-      if (tid < kAppendThreads / 32) s_claims[tid] = tid == 0;
-      if (tid == 0) s_first = lo;
+      if (tid == 0) { s_whose = make_int4(lo, p.q_indptr[lo], p.q_indptr[lo + 1], p.seq_lens[lo]); mine = 1; }
     }
-    // lengths are looked at by the blocks together (a block of an invalid request may not come to it)
-    for (int c = blockIdx.x * kAppendThreads + tid; c < p.batch; c += gridDim.x * kAppendThreads)
-      if (!valid(p.q_indptr[c], p.q_indptr[c + 1], p.seq_lens[c])) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
   }
-  __syncthreads();
-  // the block's rows of request r, whose bounds are looked at here once more: no thread goes by another's
-  auto append = [&](int r) {
-    const int q0 = p.q_indptr[r], q1 = p.q_indptr[r + 1], L = p.seq_lens[r], m = q1 - q0;
-    if (!valid(q0, q1, L)) return;
-    const int64_t j0_64 = ((int64_t)blockIdx.x - ((q0 >> p.log2_rows) + (int64_t)r)) << p.log2_rows;
-    if (j0_64 < 0 || j0_64 >= m) return;
-    const int j0 = (int)j0_64, n = min(1 << p.log2_rows, m - j0), t0 = L - m + j0;
-    const int32_t *table = p.block_table + (int64_t)r * p.max_pages_per_req;
-    if (tid < n) s_page[tid] = table[(t0 + tid) >> p.log2P];
-    // a request with a bad page among its new positions is skipped as a whole: every one of its blocks looks at all of them
-    int bad = 0;
-    for (int i = ((L - m) >> p.log2P) + tid; i <= (L - 1) >> p.log2P; i += kAppendThreads) {
-      const int pg = table[i];
-      bad |= pg < 0 || pg >= p.num_pages;
+  if (kRope)
+    for (int i = tid; i < (p.D >> 1); i += kAppendThreads) s_inv_freq[i] = pow(p.rope_base, -2.0 * (double)i / (double)p.D);
+  bool many = false;
+  if (!head) {
+    const int n = __syncthreads_count(mine != 0);
+    if (n == 0) return;
+    const int4 w = s_whose;     // (one thread's, unless n > 1)
+    many = n > 1 || w.x < 0;
+    r = w.x; q0 = w.y; q1 = w.z; L = w.w;
+  } else if (kRope) {
+    __syncthreads();
+  }
+  for (;;) {
+    if (many) {
+      // q_indptr descends somewhere, and the rows are several requests': one after the other
+      __syncthreads();
+      if (mine) s_whose.x = tid + (__ffs(mine) - 1) * kAppendThreads;
+      __syncthreads();
+      r = s_whose.x;
+      q0 = p.q_indptr[r]; q1 = p.q_indptr[r + 1]; L = p.seq_lens[r];
     }
-    if constexpr (kRope) {
-      const int half = p.D >> 1;
-      for (int i = tid; i < n * half; i += kAppendThreads) {
-        const int row = i / half, pair = i % half;
-        const int t = ax.axes ? ax.positions[(int64_t)ax.axis_of[pair] * ax.position_stride + q0 + j0 + row] : t0 + row;
-        double c, sn;
-        sincos((double)t * s_inv_freq[pair], &sn, &c);
-        if (p.elem_size == 4) {
-          s_cs[row * half + (pair & 3) * (half >> 2) + (pair >> 2)] = make_double2(c, sn);
-        } else {
-          float *at = reinterpret_cast<float *>(s_cs + row * half + (pair & 6) * (half >> 3) + (pair >> 3)) + (pair & 1);
-          const float ch = (float)c, sh = (float)sn;
-          at[0] = ch; at[2] = (float)(c - (double)ch);
-          at += (half >> 3) * 4;
-          at[0] = sh; at[2] = (float)(sn - (double)sh);
-        }
-      }
-    }
-    if (__syncthreads_or(bad)) {
-      if (tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
+    if (!takes_part(q0, q1, L)) {
+      if (head && tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_LEN);
       return;
     }
-    const int row_bytes = p.D * p.elem_size, vecs = row_bytes >> 4;
-    auto cache_at = [&](int row, int g) -> int64_t {
-      return ((int64_t)s_page[row] * p.stride_page + (int64_t)g * p.stride_head + (int64_t)((t0 + row) & (p.P - 1)) * p.stride_token) * p.elem_size;
-    };
-    if constexpr (kRope) {
-      // a thread takes one vector of the first half of a head row and its partner in the second half: K's rows, then the
-      // query rows (two at a time, in 114 registers: 44 us for prompts with images, against 40)
-      const int half_vecs = vecs >> 1, half_bytes = row_bytes >> 1;
-      const int n_k = n * p.Hkv * half_vecs, n_all = n_k + (p.q_rows ? n * p.Hq * half_vecs : 0);
-      struct Task { const unsigned char *src; unsigned char *dst; int row, v; uint4 lo, hi; };
-      auto open = [&](int i) -> Task {
-        Task t;
-        if (i < n_k) {
-          t.v = i % half_vecs;
-          const int jg = i / half_vecs, g = jg % p.Hkv;
-          t.row = jg / p.Hkv;
-          t.src = p.new_k + ((int64_t)(q0 + j0 + t.row) * p.Hkv + g) * row_bytes + t.v * 16;
-          t.dst = p.k_cache + cache_at(t.row, g) + t.v * 16;
-        } else {
-          i -= n_k;
-          t.v = i % half_vecs;
-          const int jh = i / half_vecs, h = jh % p.Hq;
-          t.row = jh / p.Hq;
-          const int64_t at = ((int64_t)(q0 + j0 + t.row) * p.Hq + h) * row_bytes + t.v * 16;
-          t.src = p.q_rows + at;
-          t.dst = p.q_out + at;
-        }
-        t.lo = *reinterpret_cast<const uint4 *>(t.src);
-        t.hi = *reinterpret_cast<const uint4 *>(t.src + half_bytes);
-        return t;
-      };
-      auto close = [&](Task &t) {
-        const double2 *cs = s_cs + t.row * (p.D >> 1);
-        if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(t.lo, t.hi, cs, half_vecs, t.v);
-        else rope_vectors<float>(t.lo, t.hi, cs, half_vecs, t.v);
-        *reinterpret_cast<uint4 *>(t.dst) = t.lo;
-        *reinterpret_cast<uint4 *>(t.dst + half_bytes) = t.hi;
-      };
-      for (int i = tid; i < n_all; i += kAppendThreads) {
-        Task t = open(i);
-        close(t);
+    const int m = q1 - q0, first = (int)first_row(q0), end = (int)min((int64_t)m, (int64_t)first + (1 << p.log2_block));
+    const int32_t *table = p.block_table + (int64_t)r * p.max_pages_per_req;
+    // a request with a bad page among its new positions is skipped as a whole: every one of its blocks looks at all of them
+    int bad = 0;
+    if (m > rows) {
+      for (int i = ((L - m) >> p.log2P) + tid; i <= (L - 1) >> p.log2P; i += kAppendThreads) {
+        const int pg = table[i];
+        bad |= pg < 0 || pg >= p.num_pages;
       }
     }
-    for (int i = tid; i < n * p.Hkv * vecs; i += kAppendThreads) {
-      const int v = i % vecs, jg = i / vecs, g = jg % p.Hkv, row = jg / p.Hkv;
-      const int64_t src = ((int64_t)(q0 + j0 + row) * p.Hkv + g) * row_bytes + v * 16, dst = cache_at(row, g) + v * 16;
-      if (!kRope) *reinterpret_cast<uint4 *>(p.k_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_k + src));
-      *reinterpret_cast<uint4 *>(p.v_cache + dst) = __ldg(reinterpret_cast<const uint4 *>(p.new_v + src));
+    for (int j0 = first; j0 < end; j0 += rows) {
+      if (j0 > first) __syncthreads();   // the step before has read its page ids and angles
+      const int n = min(rows, end - j0), t0 = L - m + j0;
+      if (tid < n) {
+        const int pg = table[(t0 + tid) >> p.log2P];
+        s_page[tid] = pg;
+        bad |= pg < 0 || pg >= p.num_pages;
+      }
+      if constexpr (kRope) {
+        const int half = p.D >> 1;
+        for (int i = tid; i < n * half; i += kAppendThreads) {
+          const int row = i / half, pair = i % half;
+          int t = t0 + row;
+          if constexpr (std::is_same<Axes, KvAppendAxes>::value) t = ax.positions[(int64_t)ax.axis_of[pair] * ax.position_stride + q0 + j0 + row];
+          double c, sn;
+          sincos((double)t * s_inv_freq[pair], &sn, &c);
+          if (p.elem_size == 4) {
+            s_cs[row * half + (pair & 3) * (half >> 2) + (pair >> 2)] = make_double2(c, sn);
+          } else {
+            float *at = reinterpret_cast<float *>(s_cs + row * half + (pair & 6) * (half >> 3) + (pair >> 3)) + (pair & 1);
+            const float ch = (float)c, sh = (float)sn;
+            at[0] = ch; at[2] = (float)(c - (double)ch);
+            at += (half >> 3) * 4;
+            at[0] = sh; at[2] = (float)(sn - (double)sh);
+          }
+        }
+      }
+      if (j0 == first ? __syncthreads_or(bad) : (__syncthreads(), 0)) {
+        if (tid == 0) atomicOr(p.dev_status, SPX_DEV_BAD_PAGE);
+        break;
+      }
+      const int row_bytes = p.D * p.elem_size, vecs = row_bytes >> 4;
+      auto cache_at = [&](int row, int g) -> int64_t {
+        return ((int64_t)s_page[row] * p.stride_page + (int64_t)g * p.stride_head + (int64_t)((t0 + row) & (p.P - 1)) * p.stride_token) * p.elem_size;
+      };
+      if constexpr (kRope) {
+        // a thread takes one vector of the first half of a head row and its partner in the second half: K's rows, then the
+        // query rows (two at a time, in 114 registers: 44 us for prompts with images, where this took 40)
+        const int half_vecs = vecs >> 1, half_bytes = row_bytes >> 1;
+        const int n_k = n * p.Hkv * half_vecs, n_all = n_k + (p.q_rows ? n * p.Hq * half_vecs : 0);
+        struct Task { const unsigned char *src; unsigned char *dst; int row, v; uint4 lo, hi; };
+        auto open = [&](int i) -> Task {
+          Task t;
+          if (i < n_k) {
+            t.v = i % half_vecs;
+            const int jg = i / half_vecs, g = jg % p.Hkv;
+            t.row = jg / p.Hkv;
+            t.src = p.new_k + ((int64_t)(q0 + j0 + t.row) * p.Hkv + g) * row_bytes + t.v * 16;
+            t.dst = p.k_cache + cache_at(t.row, g) + t.v * 16;
+          } else {
+            i -= n_k;
+            t.v = i % half_vecs;
+            const int jh = i / half_vecs, h = jh % p.Hq;
+            t.row = jh / p.Hq;
+            const int64_t at = ((int64_t)(q0 + j0 + t.row) * p.Hq + h) * row_bytes + t.v * 16;
+            t.src = p.q_rows + at;
+            t.dst = p.q_out + at;
+          }
+          t.lo = *reinterpret_cast<const uint4 *>(t.src);
+          t.hi = *reinterpret_cast<const uint4 *>(t.src + half_bytes);
+          return t;
+        };
+        auto close = [&](Task &t) {
+          const double2 *cs = s_cs + t.row * (p.D >> 1);
+          if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(t.lo, t.hi, cs, half_vecs, t.v);
+          else rope_vectors<float>(t.lo, t.hi, cs, half_vecs, t.v);
+          *reinterpret_cast<uint4 *>(t.dst) = t.lo;
+          *reinterpret_cast<uint4 *>(t.dst + half_bytes) = t.hi;
+        };
+        for (int i = tid; i < n_all; i += kAppendThreads) {
+          Task t = open(i);
+          close(t);
+        }
+      }
+      // V, and K without a rotation: the step's rows lie one behind the other, so that loads need no division
+      const int n_copy = n * p.Hkv * vecs;
+      const uint4 *ks = reinterpret_cast<const uint4 *>(p.new_k + (int64_t)(q0 + j0) * p.Hkv * row_bytes);
+      const uint4 *vs = reinterpret_cast<const uint4 *>(p.new_v + (int64_t)(q0 + j0) * p.Hkv * row_bytes);
+      auto store = [&](int i, uint4 x, uint4 y) {
+        const int v = i % vecs, jg = i / vecs, g = jg % p.Hkv, row = jg / p.Hkv;
+        const int64_t dst = cache_at(row, g) + v * 16;
+        if (!kRope) *reinterpret_cast<uint4 *>(p.k_cache + dst) = x;
+        *reinterpret_cast<uint4 *>(p.v_cache + dst) = y;
+      };
+      constexpr int kAhead = 4;
+      int i = tid;
+      for (; i + (kAhead - 1) * kAppendThreads < n_copy; i += kAhead * kAppendThreads) {
+        uint4 x[kAhead], y[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          if (!kRope) x[u] = __ldg(ks + i + u * kAppendThreads);
+          y[u] = __ldg(vs + i + u * kAppendThreads);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) store(i + u * kAppendThreads, x[u], y[u]);
+      }
+#pragma unroll 1
+      for (; i < n_copy; i += kAppendThreads) store(i, kRope ? uint4() : __ldg(ks + i), __ldg(vs + i));
     }
-  };
-  for (int w = 0; w < kAppendThreads / 32; ++w) {
-    for (uint32_t claims = s_claims[w]; claims; claims &= claims - 1) {
-      append(s_first + 32 * w + __ffs(claims) - 1);
-      __syncthreads();   // page ids and angles are read
-    }
+    if (!many) return;
+    if (r % kAppendThreads == tid) mine &= mine - 1;
+    if (!__syncthreads_or(mine)) return;
   }
 }
 

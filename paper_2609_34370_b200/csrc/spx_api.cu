@@ -1167,18 +1167,20 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
   p.Hq = a->num_q_heads;
   p.log2_rows = log2_of(kAppendRows);
   while (rope && (a->head_dim / 2) << p.log2_rows > kAppendAngles) --p.log2_rows;
-  const int64_t blocks = ((int64_t)a->total_q >> p.log2_rows) + a->batch;
+  // a step a block; where blocks search for their request, all the rows that a verify step can bring, so that none of those hang on a search
+  p.log2_block = a->batch <= kAppendVote ? p.log2_rows : log2_of(SPX_MAX_K + 1);
+  const int64_t blocks = (int64_t)a->batch + (a->total_q <= 1 << p.log2_block ? 0 : a->total_q >> p.log2_block);
   if (blocks > 0x7fffffff) return SPX_ERR_UNSUPPORTED;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  if (rope) {
+  if (rope && a->rope_axes > 0) {
     KvAppendAxes ax{};
-    if (a->rope_axes > 0) {
-      ax.axes = a->rope_axes; ax.positions = a->positions; ax.position_stride = a->position_stride;
-      fill_axes(a, ax.axis_of);
-    }
-    kv_append_kernel<true><<<(unsigned)blocks, kAppendThreads, 0, stream>>>(p, ax);
+    ax.positions = a->positions; ax.position_stride = a->position_stride;
+    fill_axes(a, ax.axis_of);
+    kv_append_kernel<true, KvAppendAxes><<<(unsigned)blocks, kAppendThreads, 0, stream>>>(p, ax);
+  } else if (rope) {
+    kv_append_kernel<true, KvNoAxes><<<(unsigned)blocks, kAppendThreads, 0, stream>>>(p, KvNoAxes());
   } else {
-    kv_append_kernel<false><<<(unsigned)blocks, kAppendThreads, 0, stream>>>(p, KvNoAxes());
+    kv_append_kernel<false, KvNoAxes><<<(unsigned)blocks, kAppendThreads, 0, stream>>>(p, KvNoAxes());
   }
   ++t_launches;
   return cudaGetLastError() == cudaSuccess ? SPX_OK : SPX_ERR_CUDA;

@@ -89,3 +89,27 @@ def test_wrong_bounds_in_the_middle_of_a_batch(base):
         starts[at] = x
     lens = [max(1, min(b - a, total)) + i % 33 for i, (a, b) in enumerate(zip(starts, starts[1:]))]
     _run(starts, total, lens, BF16, base, False)
+
+
+@pytest.mark.parametrize("base", [0.0, 10000.0])
+@pytest.mark.parametrize("n", [256, 257, 700, 1024, 1025, 1400])
+def test_steps_of_many_requests_do_not_hang_on_each_others_bounds(n, base):
+    """Up to 16 rows a request, as a verify step brings them: the requests whose own bounds hold enter the cache, whatever the others' are."""
+    m = [1 + (5 * i) % 16 for i in range(n)]
+    starts = [0] + np.cumsum(m).tolist()
+    total = starts[-1]
+    for at, x in ((30, 100000), (70, -4), (110, total), (111, 3), (150, 0), (n - 1, total + 1)):
+        starts[at] = x
+    lens = [max(1, b - a) + i % 33 if b - a <= 16 else 2 for i, (a, b) in enumerate(zip(starts, starts[1:]))]
+    _run(starts, total, lens, BF16, base, False)
+
+
+@pytest.mark.parametrize("base", [0.0, 10000.0])
+@pytest.mark.parametrize("n,d_rows", [(3, 1), (255, 9), (300, 17), (300, 16), (1030, 33), (1030, 16)])
+def test_prompts_among_steps(n, d_rows, base):
+    """Ascending bounds: every row of prompts of many lengths enters, among requests of d_rows rows."""
+    m = [1 + (7 * i) % d_rows for i in range(n)]
+    for i, k in enumerate((8, 9, 16, 17, 24, 25, 31, 128, 129, 500)):
+        m[(i * 101) % n] = k
+    starts = [0] + np.cumsum(m).tolist()
+    _run(starts, starts[-1], [k + i % 50 for i, k in enumerate(m)], F32, base, True)
