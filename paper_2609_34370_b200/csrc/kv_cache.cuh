@@ -12,6 +12,7 @@ constexpr int kRopeMaxHeadDim = 512;
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 8;          // new rows of a step, at most
 constexpr int kAppendVote = 1024;       // requests that the threads of a block look at in one go
+constexpr int kAppendBlocks = 2048;     // blocks behind the requests' own that a call is cut into, at most
 constexpr int kAppendAngles = 1024;     // (row, pair) angles a step keeps: 8 rows of 256 elements, 4 of 512
 
 struct KvAppendParams {

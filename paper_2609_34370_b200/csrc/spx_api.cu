@@ -1171,6 +1171,10 @@ spx_status_t spx_kv_append(const spx_kv_append_args_t *a, int32_t *dev_status, v
   // and without a rotation where the requests' own blocks fill the SMs (500 requests of 16 rows 7.8 us, of 6 rows 4.4; with a step 9.4 and 4.6;
   // rotated, two steps of one block take their time one behind the other: 62 either way).
   p.log2_block = a->batch <= (rope ? kAppendVote : kAppendThreads) ? p.log2_rows : log2_of(SPX_MAX_K + 1);
+  // Twice the rows, and again, while they are more than kAppendBlocks blocks: each looks at all page ids of its request's new rows, work
+  // that grows with the square of a prompt (131072 rows, pages of one token: 586 us with a step a block, 212 so; pages of 16: 138 and 137,
+  // rotated 460 and 390; 32768 rows rotated 210 and 205, but 217 in half as many blocks).
+  while (a->total_q >> p.log2_block > kAppendBlocks) ++p.log2_block;
   const int64_t blocks = (int64_t)a->batch + (a->total_q <= 1 << p.log2_block ? 0 : a->total_q >> p.log2_block);
   if (blocks > 0x7fffffff) return SPX_ERR_UNSUPPORTED;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
