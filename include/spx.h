@@ -272,8 +272,7 @@ spx_status_t spx_prompt_attention(const spx_attn_args_t *args, void *ws, size_t 
  * the rotation of the Llama and Qwen families it evaluates): with rope_base > 0 every new K row is
  * rotated to its absolute position t before it is stored - for each head vector x and i < D/2,
  * with a = t * rope_base^(-2i/D):  y[i] = x[i] cos a - x[i+D/2] sin a,  y[i+D/2] = x[i+D/2] cos a +
- * x[i] sin a, computed in float64 and rounded float64 -> binary32 -> kv_dtype (nearest-even each; BF16 rows: angles in float64,
- * products and sum in pairs of binary32 to 2^-46, then the two roundings).
+ * x[i] sin a, computed in float64 and rounded float64 -> binary32 -> kv_dtype (nearest-even each).
  * V is copied as it is.  If q_rows is given ([TQ, num_q_heads, head_dim], kv_dtype, 16-byte
  * aligned), row q_indptr[r]+j is rotated IN PLACE to the same position, so that the attention that
  * follows sees rotated Q and K.  rope_base = 0: no rotation, q_rows ignored.  Needs head_dim/2 *

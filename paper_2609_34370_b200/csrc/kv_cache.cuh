@@ -37,16 +37,30 @@ struct KvAppendAxes {
 };
 struct KvNoAxes {};
 
-// Rotary embedding of the pairs (x[i], x[i + D/2]) of one head vector by angles whose cosine and sine are float64's; results
-// rounded to binary32 and then to the element type (nearest even each).  lo / hi are the 16-byte vectors that hold the
-// pairs' first and second elements.  cs: the angles of a row, 16 bytes a pair, laid out so that neighbouring vectors' lie side by
+// A pair (x0, x1) turned by an angle in float64: y0 and y1 rounded to binary32 and to bfloat16, in the low and the high half.
+// (Out of line: a few in a thousand vectors come here.)
+static __device__ __noinline__ uint32_t rope_pair_exact(float x0, float x1, double angle) {
+  double c, sn;
+  sincos(angle, &sn, &c);
+  const double a = (double)x0, b = (double)x1;
+  const __nv_bfloat16 y0 = __float2bfloat16_rn(__double2float_rn(a * c - b * sn)), y1 = __float2bfloat16_rn(__double2float_rn(b * c + a * sn));
+  return (uint32_t)*reinterpret_cast<const uint16_t *>(&y0) | (uint32_t)*reinterpret_cast<const uint16_t *>(&y1) << 16;
+}
+
+// Rotary embedding of the pairs (x[i], x[i + D/2]) of one head vector by angles whose cosine and sine are float64's; products and sum in
+// float64, results rounded to binary32 and then to the element type (nearest even each).  lo / hi are the 16-byte vectors that
+// hold the pairs' first and second elements.  cs: the angles of a row, 16 bytes a pair, laid out so that neighbouring vectors' lie side by
 // side, vecs vectors to half a row.
-//   float32 rows: products and sum in float64, (cos, sin) of vector v's pair u at [u * vecs + v].
-//   16-bit rows: products and sum in pairs of binary32 to 2^-46 of |x| (float64's arithmetic but for one in some millions of last
-//   bits of binary32, at a third of its time: conversions from and to float64 take 8 cycles each), (cos, cos', low parts) of pairs
-//   2u, 2u + 1 at [2u * vecs + v], the sines at [(2u + 1) * vecs + v].
-template <typename T>
-__device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2 *cs, int vecs, int v) {
+//   float32 rows: (cos, sin) of vector v's pair u at [u * vecs + v].
+//   16-bit rows: (cos, cos', low parts) of pairs 2u, 2u + 1 at [2u * vecs + v], the sines at [(2u + 1) * vecs + v].  Products and sum in
+//   pairs of binary32 (conversions from and to float64 take 8 cycles each).  With X = max(|x0|, |x1|), y is off by the roundings of x0 cos - x1 sin
+//   and of the last sum, half a last bit each, and by 2^-46 X beside them.  Where |y| > 2^-18 X that is 1.6 of y's last bits at most (a
+//   last bit of the first may be two of y's), so that float64's result rounded to binary32 is at most two away, and rounds to another
+//   bfloat16 only if y's lower half is within two of 0x8000.  Those pairs, the ones that cancel further, tiny ones and what is
+//   not finite (6 in 100 warps' vectors) are made again in float64, angle(i) being that of the vector's pair i: results are
+//   float64's, to the last bit and to the sign of a zero.
+template <typename T, typename Angle>
+__device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2 *cs, int vecs, int v, Angle angle) {
   if constexpr (sizeof(T) == 4) {
     union U { uint4 q; T e[4]; } a, b;
     a.q = lo; b.q = hi;
@@ -60,38 +74,40 @@ __device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2
     lo = a.q; hi = b.q;
   } else {
     const ulonglong2 *at = reinterpret_cast<const ulonglong2 *>(cs);
-    uint32_t a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
+    const uint32_t x[4] = {lo.x, lo.y, lo.z, lo.w}, y[4] = {hi.x, hi.y, hi.z, hi.w};
+    uint32_t a[4], b[4], again = 0;            // bit u: pairs 2u and 2u + 1
     uint64_t finite = e8::pair(0.f, 0.f);      // stays zero as long as results are finite
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const ulonglong2 c = at[2 * u * vecs + v], s = at[(2 * u + 1) * vecs + v];
       const CosSin k{c.x, c.y, s.x, s.y};
-      uint64_t y0, y1;
-      rotate2<true>(e8::pair(__uint_as_float(a[u] << 16), __uint_as_float(a[u] & 0xffff0000u)),
-                    e8::pair(__uint_as_float(b[u] << 16), __uint_as_float(b[u] & 0xffff0000u)), k, y0, y1);
-      finite = e8::fma2(y0, e8::pair(0.f, 0.f), e8::fma2(y1, e8::pair(0.f, 0.f), finite));
-      float p, q;
-      e8::unpair(y0, p, q);
-      const __nv_bfloat162 r0 = __floats2bfloat162_rn(p, q);
-      e8::unpair(y1, p, q);
-      const __nv_bfloat162 r1 = __floats2bfloat162_rn(p, q);
-      a[u] = *reinterpret_cast<const uint32_t *>(&r0); b[u] = *reinterpret_cast<const uint32_t *>(&r1);
+      const float x0 = __uint_as_float(x[u] << 16), x1 = __uint_as_float(x[u] & 0xffff0000u), y0 = __uint_as_float(y[u] << 16), y1 = __uint_as_float(y[u] & 0xffff0000u);
+      uint64_t r0, r1;
+      rotate2<false>(e8::pair(x0, x1), e8::pair(y0, y1), k, r0, r1);
+      finite = e8::fma2(r0, e8::pair(0.f, 0.f), e8::fma2(r1, e8::pair(0.f, 0.f), finite));
+      float p, q, r, t;
+      e8::unpair(r0, p, q);
+      e8::unpair(r1, r, t);
+      // the lower halves plus 0x8004, two in a word (a carry moves the upper one by one): below 8 if they were 0x7ffe .. 0x8002
+      const uint32_t half = __vminu2(__byte_perm(__float_as_uint(p), __float_as_uint(q), 0x5410) + 0x80048004u,
+                                     __byte_perm(__float_as_uint(r), __float_as_uint(t), 0x5410) + 0x80048004u);
+      const float least = fminf(fminf(fabsf(p), fabsf(q)), fminf(fabsf(r), fabsf(t)));
+      const float most = fmaxf(fmaxf(fmaxf(fabsf(x0), fabsf(x1)), fmaxf(fabsf(y0), fabsf(y1))), 0x1p-82f);
+      if ((half & 0xfff8u) == 0 || (half & 0xfff80000u) == 0 || !(least * 0x1p18f > most)) again |= 1u << u;
+      const __nv_bfloat162 h0 = __floats2bfloat162_rn(p, q), h1 = __floats2bfloat162_rn(r, t);
+      a[u] = *reinterpret_cast<const uint32_t *>(&h0); b[u] = *reinterpret_cast<const uint32_t *>(&h1);
     }
     float p, q;
     e8::unpair(finite, p, q);
-    if (p != 0.f || q != 0.f) {
-      // an infinity, a NaN or a result past binary32: the remainders above are none then, float64's arithmetic stands
-      const float *cs32 = reinterpret_cast<const float *>(cs);
-      const __nv_bfloat16 *x = reinterpret_cast<const __nv_bfloat16 *>(&lo), *y = reinterpret_cast<const __nv_bfloat16 *>(&hi);
+    if (p != 0.f || q != 0.f) again = 15;
+    if (again) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float *k = cs32 + ((i & 6) * vecs + v) * 4 + (i & 1);
-        const double c = (double)k[0] + (double)k[2], sn = (double)k[4 * vecs] + (double)k[4 * vecs + 2];
-        const double x0 = (double)__bfloat162float(x[i]), x1 = (double)__bfloat162float(y[i]);
-        const __nv_bfloat16 r0 = __float2bfloat16_rn(__double2float_rn(x0 * c - x1 * sn)), r1 = __float2bfloat16_rn(__double2float_rn(x1 * c + x0 * sn));
-        const uint32_t w0 = *reinterpret_cast<const uint16_t *>(&r0), w1 = *reinterpret_cast<const uint16_t *>(&r1);
-        a[i >> 1] = (i & 1) ? (a[i >> 1] & 0xffffu) | w0 << 16 : (a[i >> 1] & 0xffff0000u) | w0;
-        b[i >> 1] = (i & 1) ? (b[i >> 1] & 0xffffu) | w1 << 16 : (b[i >> 1] & 0xffff0000u) | w1;
+      for (int u = 0; u < 4; ++u) {
+        if (!(again >> u & 1)) continue;
+        const uint32_t even = rope_pair_exact(__uint_as_float(x[u] << 16), __uint_as_float(y[u] << 16), angle(2 * u));
+        const uint32_t odd = rope_pair_exact(__uint_as_float(x[u] & 0xffff0000u), __uint_as_float(y[u] & 0xffff0000u), angle(2 * u + 1));
+        a[u] = __byte_perm(even, odd, 0x5410);
+        b[u] = __byte_perm(even, odd, 0x7632);
       }
     }
     lo = make_uint4(a[0], a[1], a[2], a[3]); hi = make_uint4(b[0], b[1], b[2], b[3]);
@@ -203,14 +219,17 @@ kv_append_kernel(const __grid_constant__ KvAppendParams p, const __grid_constant
         s_page[tid] = pg;
         bad |= pg < 0 || pg >= p.num_pages;
       }
+      auto angle = [&](int row, int pair) -> double {
+        int t = t0 + row;
+        if constexpr (std::is_same<Axes, KvAppendAxes>::value) t = ax.positions[(int64_t)ax.axis_of[pair] * ax.position_stride + q0 + j0 + row];
+        return (double)t * s_inv_freq[pair];
+      };
       if constexpr (kRope) {
         const int half = p.D >> 1;
         for (int i = tid; i < n * half; i += kAppendThreads) {
           const int row = i / half, pair = i % half;
-          int t = t0 + row;
-          if constexpr (std::is_same<Axes, KvAppendAxes>::value) t = ax.positions[(int64_t)ax.axis_of[pair] * ax.position_stride + q0 + j0 + row];
           double c, sn;
-          sincos((double)t * s_inv_freq[pair], &sn, &c);
+          sincos(angle(row, pair), &sn, &c);
           if (p.elem_size == 4) {
             s_cs[row * half + (pair & 3) * (half >> 2) + (pair >> 2)] = make_double2(c, sn);
           } else {
@@ -259,8 +278,9 @@ kv_append_kernel(const __grid_constant__ KvAppendParams p, const __grid_constant
         };
         auto close = [&](Task &t) {
           const double2 *cs = s_cs + t.row * (p.D >> 1);
-          if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(t.lo, t.hi, cs, half_vecs, t.v);
-          else rope_vectors<float>(t.lo, t.hi, cs, half_vecs, t.v);
+          auto of_pair = [&](int i) -> double { return angle(t.row, t.v * 8 + i); };
+          if (p.elem_size == 2) rope_vectors<__nv_bfloat16>(t.lo, t.hi, cs, half_vecs, t.v, of_pair);
+          else rope_vectors<float>(t.lo, t.hi, cs, half_vecs, t.v, of_pair);
           *reinterpret_cast<uint4 *>(t.dst) = t.lo;
           *reinterpret_cast<uint4 *>(t.dst + half_bytes) = t.hi;
         };

@@ -95,3 +95,31 @@ def test_tiny_and_large_rows():
     room = 2.0 ** -51 * np.concatenate((np.hypot(x0, x1),) * 2, -1)
     sure = (_bits(want - room) == _bits(want + room))
     assert sure.mean() > 0.999 and (got == _bits(want))[sure].all()
+
+
+@pytest.mark.parametrize("base", [10000.0, 1e6])
+def test_millions_of_results(base):
+    """60,000 rows, eight million results a call: some hundreds lie within two binary32 steps of a border between two bfloat16 values."""
+    n = 60000
+    g = torch.Generator().manual_seed(4)
+    rows = torch.randn(n, 1, 128, generator=g).bfloat16()
+    pages = -(-n // 16)
+    pool = torch.zeros(pages, 1, 16, 128, dtype=torch.bfloat16, device=DEV)
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    x = rows.to(DEV)
+    status = spx.kv_append(x, x, pool, pool.clone(), pool.stride()[:3], ints([list(range(pages))]), ints([n]), ints([0, n]), 16, pages, rope_base=base)
+    assert int(status.item()) == 0
+    angle = torch.arange(n, dtype=torch.float64, device=DEV)[:, None] * torch.tensor([base ** (-2.0 * i / 128) for i in range(64)], dtype=torch.float64, device=DEV)
+    c, s = torch.cos(angle), torch.sin(angle)
+    x0, x1 = x[:, 0, :64].double(), x[:, 0, 64:].double()
+    got = pool.view(-1, 128)[:n]
+    near = 0
+    for y, have in ((x0 * c - x1 * s, got[:, :64]), (x1 * c + x0 * s, got[:, 64:])):
+        bits = lambda v: v.float().bfloat16().view(torch.int16)  # noqa: E731
+        # (frequency, angle, sine: off by 2^-52 of themselves each between libraries; angles below 2^16)
+        room = 2.0 ** -36 * torch.maximum(x0.abs(), x1.abs()) * (angle.abs() * 2.0 ** -16).clamp(min=2.0 ** -14)
+        sure = bits(y - room) == bits(y + room)
+        assert float(sure.double().mean()) > 0.9999
+        assert torch.equal(have.view(torch.int16)[sure], bits(y)[sure])
+        near += int((((y.float().view(torch.int32) & 0xFFFF) - 0x8000).abs() <= 2).sum())
+    assert near > 200
