@@ -121,7 +121,6 @@ struct PromptWs {
 struct AttnWs {
   size_t hdr, nchunks, part_base, combine_list, tile_prefix, valid_prefix, cost_prefix, cta_off, req_bad, work, part_ml, part_o, prefix, total;
   int32_t max_work, max_part_slots, rows_cap;
-  bool fits;
 };
 
 static int cache_elem_size(const spx_attn_args_t *a) {
@@ -144,6 +143,8 @@ static int log2_of(int x) {
   return n;
 }
 
+static PromptWs prompt_ws_layout(const spx_attn_args_t *a);
+
 // prompts: any number of rows a request
 static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs, bool prompts = false) {
   if (!a) return SPX_ERR_INVALID_ARG;
@@ -163,6 +164,7 @@ static spx_status_t check_attn(const spx_attn_args_t *a, bool need_ptrs, bool pr
   if (cf != SPX_OK) return cf;
   if (a->num_groups < 0) return SPX_ERR_INVALID_ARG;
   if (prompts && a->num_groups > 0) return SPX_ERR_UNSUPPORTED;
+  if ((prompts || a->num_groups > 0) && !prompt_ws_layout(a).fits) return SPX_ERR_UNSUPPORTED;   // before a call queues anything
   if (need_ptrs && a->batch > 0 && a->num_groups > 0 && (!a->group_indptr || !a->prefix_lens)) return SPX_ERR_INVALID_ARG;
   if (need_ptrs && prompts && a->total_q == 0) return SPX_OK;
   if (need_ptrs && a->batch > 0) {
@@ -213,7 +215,6 @@ static PromptWs prompt_ws_layout(const spx_attn_args_t *a) {
 
 static AttnWs attn_ws_layout(const spx_attn_args_t *a) {
   AttnWs w{};
-  w.fits = true;
   const int max_q = a->max_q_len == 0 ? SPX_MAX_K + 1 : a->max_q_len;
   const int G = a->num_q_heads / a->num_kv_heads;
   w.rows_cap = G * max_q;
@@ -237,9 +238,7 @@ static AttnWs attn_ws_layout(const spx_attn_args_t *a) {
   w.part_ml = off; off = align_up(off + sizeof(float2) * slots * w.rows_cap, 256);
   w.part_o = off; off = align_up(off + sizeof(float) * slots * w.rows_cap * a->head_dim, 256);
   if (a->num_groups > 0) {
-    const PromptWs pw = prompt_ws_layout(a);
-    w.fits = pw.fits;
-    w.prefix = off; off = align_up(off + pw.total, 256);
+    w.prefix = off; off = align_up(off + prompt_ws_layout(a).total, 256);
   }
   w.total = off;
   return w;
@@ -556,7 +555,6 @@ static spx_status_t launch_attention(const spx_attn_args_t *a, unsigned char *ws
                                      cudaStream_t stream, const DeviceInfo &dev, int phases = kPhaseAll) {
   if (a->batch == 0) return SPX_OK;
   const AttnWs w = attn_ws_layout(a);
-  if (!w.fits) return SPX_ERR_UNSUPPORTED;
   const bool grouped = a->num_groups > 0;
   PromptParams pre{};
   if (grouped) pre = prompt_params(a, prompt_ws_layout(a), ws + w.prefix, dev_status, dev);
@@ -825,9 +823,7 @@ size_t spx_workspace_size(const spx_attn_args_t *attn, const spx_sample_args_t *
   size_t total = 0;
   if (attn) {
     if (check_attn(attn, false) != SPX_OK) return 0;
-    const AttnWs w = attn_ws_layout(attn);
-    if (!w.fits) return 0;
-    total += w.total;
+    total += attn_ws_layout(attn).total;
   }
   if (sample) {
     if (check_sample(sample, false) != SPX_OK) return 0;
@@ -850,8 +846,7 @@ spx_status_t spx_verify_attention(const spx_attn_args_t *args, void *ws, size_t 
 
 size_t spx_prompt_workspace_size(const spx_attn_args_t *args) {
   if (check_attn(args, false, true) != SPX_OK) return 0;
-  const PromptWs w = prompt_ws_layout(args);
-  return w.fits ? w.total : 0;
+  return prompt_ws_layout(args).total;
 }
 
 spx_status_t spx_prompt_attention(const spx_attn_args_t *args, void *ws, size_t ws_bytes, int32_t *dev_status, void *cuda_stream) {
@@ -859,7 +854,6 @@ spx_status_t spx_prompt_attention(const spx_attn_args_t *args, void *ws, size_t 
   spx_status_t st = check_attn(args, true, true);
   if (st != SPX_OK) return st;
   const PromptWs w = prompt_ws_layout(args);
-  if (!w.fits) return SPX_ERR_UNSUPPORTED;
   st = check_ws(ws, ws_bytes, w.total, dev_status);
   if (st != SPX_OK) return st;
   DeviceInfo dev;
