@@ -3,8 +3,9 @@
 //
 // An item is 64 packed rows of one kv head; a step takes 64 tokens.  Threads hold 8 rows x 4 tokens of the scores and 8 rows x
 // D / 16 columns of the output, so that 24 shared-memory wavefronts feed 128 (256) FMAs of a warp.  The running maximum and
-// sum of a row live in the 16 lanes that share it; weights go through shared memory once.  112 KB and 128 threads a block:
-// two blocks per SM, one of which computes while the other loads.  Two prompts of 8192
+// sum of a row live in the 16 lanes that share it; weights go through shared memory once.  113 KB and 128 threads a block:
+// two blocks per SM, one of which computes while the other loads (8-bit pools, heads of 128, six prompts up to 1200 tokens: 354 us,
+// 474 with one).  Two prompts of 8192
 // tokens in bf16 take 33.8 ms here (32 of the 74 TFLOP/s that FMAs alone would allow); a 128-token piece of fp32 rows is a latency chain of 27 us.
 #pragma once
 #include "common.cuh"
@@ -15,6 +16,13 @@ namespace spx {
 constexpr int kPsThreads = 128;
 constexpr int kPsRows = 64, kPsTokens = 64;
 template <int D> constexpr int kPsSmem = (kPsRows * D + 2 * kPsTokens * D + kPsRows * kPsTokens) * 4;
+// What a block holds beside its tiles.  (The scales of 8-bit pools' tokens lie where the weights are to come: with 512 bytes more a second
+// block would not fit.)
+struct PsShared {
+  int64_t at[kPsTokens];     // element offset of a token's row in the pool, -1: none
+  int unit, infinite;
+};
+static_assert(2 * (kPsSmem<128> + sizeof(PsShared) + 1024) <= 228 * 1024, "two blocks per SM, and 1 KB of the system's for each");
 
 // 16-byte vectors of a row of D floats, spread so that eight rows' vectors of one column lie in eight different banks
 template <int D>
@@ -46,9 +54,8 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   extern __shared__ __align__(16) unsigned char smem_raw[];
   float *sQ = reinterpret_cast<float *>(smem_raw), *sK = sQ + kPsRows * D, *sV = sK + kPsTokens * D, *sP = sV + kPsTokens * D;
-  __shared__ int s_unit, s_infinite;
-  __shared__ int64_t s_at[kPsTokens];     // element offset of a token's row in the pool, -1: none
-  __shared__ float s_scale[2][kPsTokens];
+  __shared__ PsShared s;
+  float *sScale = sP;                     // [K, V][token], until the weights are written
   constexpr bool kCodes = sizeof(KV) == 1;
   constexpr int kVecs = D / 4;
   constexpr int kCols = D / 64;           // output columns of a thread, in vectors
@@ -57,12 +64,15 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
   T *out = reinterpret_cast<T *>(p.out);
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int n_units = p.hdr->n_units;
+  // where there is an SM for each unit, the SMs' second blocks leave them to the first (four prompts up to 200 tokens over 8-bit pools, heads
+  // of 128: 52 us, 61 with both)
+  if (n_units <= (int)gridDim.x / 2 && blockIdx.x >= gridDim.x / 2) return;
 
   for (;;) {
     __syncthreads();
-    if (tid == 0) s_unit = atomicAdd(&p.hdr->counter, 1);
+    if (tid == 0) s.unit = atomicAdd(&p.hdr->counter, 1);
     __syncthreads();
-    const int unit = s_unit;
+    const int unit = s.unit;
     if (unit >= n_units) break;
     {
       const PromptEntry e = p.entries[unit / p.Hkv];
@@ -112,14 +122,14 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
               at = (int64_t)page * p.stride_page + (int64_t)g * p.stride_head + (int64_t)in_page * p.stride_token;
               if constexpr (kCodes) {
                 const int64_t sc = (((int64_t)page * p.Hkv + g) << (p.log2P - p.log2SB)) + (in_page >> p.log2SB);
-                s_scale[0][tid] = p.k_scales[sc];
-                s_scale[1][tid] = p.v_scales[sc];
+                sScale[tid] = p.k_scales[sc];
+                sScale[kPsTokens + tid] = p.v_scales[sc];
               }
             }
           }
-          s_at[tid] = at;
+          s.at[tid] = at;
         }
-        if (tid == 0) s_infinite = 0;
+        if (tid == 0) s.infinite = 0;
         __syncthreads();
         const bool edge = t0 + kPsTokens - 1 > whole;
         bool infinite = false;
@@ -127,13 +137,13 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
 #pragma unroll 8
         for (int i = tid; i < kPsTokens * kVecs; i += kPsThreads) {
           const int tok = i / kVecs, v = i % kVecs;
-          const int64_t at = s_at[tok];
+          const int64_t at = s.at[tok];
           float4 k = make_float4(0.f, 0.f, 0.f, 0.f), w = k;
           if (at >= 0) {
             k = PsLoad<KV>::get(Kc + at + v * 4);
             w = PsLoad<KV>::get(Vc + at + v * 4);
             if constexpr (kCodes) {
-              const float a = s_scale[0][tok], b = s_scale[1][tok];
+              const float a = sScale[tok], b = sScale[kPsTokens + tok];
               k.x *= a; k.y *= a; k.z *= a; k.w *= a;
               w.x *= b; w.y *= b; w.z *= b; w.w *= b;
             }
@@ -145,14 +155,14 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
           *ps_vec<D>(sK, tok, v) = k;
           *ps_vec<D>(sV, tok, v) = w;
         }
-        if (edge && infinite) s_infinite = 1;
+        if (edge && infinite) s.infinite = 1;
         __syncthreads();
         // scores of rows ty * 8 + i, tokens tx + 16 j
-        float s[8][4];
+        float x[8][4];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+          for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
 #pragma unroll 2
         for (int v = 0; v < kVecs; ++v) {
           float4 k[4];
@@ -163,8 +173,8 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
             const float4 a = *ps_vec<D>(sQ, ty * 8 + i, v);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              s[i][j] = fmaf(a.x, k[j].x, s[i][j]); s[i][j] = fmaf(a.y, k[j].y, s[i][j]);
-              s[i][j] = fmaf(a.z, k[j].z, s[i][j]); s[i][j] = fmaf(a.w, k[j].w, s[i][j]);
+              x[i][j] = fmaf(a.x, k[j].x, x[i][j]); x[i][j] = fmaf(a.y, k[j].y, x[i][j]);
+              x[i][j] = fmaf(a.z, k[j].z, x[i][j]); x[i][j] = fmaf(a.w, k[j].w, x[i][j]);
             }
           }
         }
@@ -174,8 +184,8 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int t = t0 + tx + 16 * j;
-            if (edge && !(t < t_end && t <= limit[i])) s[i][j] = -INFINITY;
-            top = fmaxf(top, s[i][j]);
+            if (edge && !(t < t_end && t <= limit[i])) x[i][j] = -INFINITY;
+            top = fmaxf(top, x[i][j]);
           }
 #pragma unroll
           for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -184,7 +194,7 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
           float sum = 0.f;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float w = fast_exp2(s[i][j] - ref);
+            const float w = fast_exp2(x[i][j] - ref);
             sum += w;
             sP[(ty * 8 + i) * kPsTokens + tx + 16 * j] = w;
           }
@@ -194,7 +204,7 @@ __global__ void __launch_bounds__(kPsThreads) prompt_simt_kernel(PromptParams p)
           for (int c = 0; c < kCols; ++c) { o[i][c].x *= alpha; o[i][c].y *= alpha; o[i][c].z *= alpha; o[i][c].w *= alpha; }
         }
         __syncwarp();   // (a row's weights are written and read by one half warp)
-        const bool guard = edge && s_infinite;
+        const bool guard = edge && s.infinite;
 #pragma unroll 2
         for (int tv = 0; tv < kPsTokens / 4; ++tv) {
           float4 w[4][kCols];
