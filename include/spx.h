@@ -590,6 +590,9 @@ spx_status_t spx_debug_wait_expiry(int32_t *report, int32_t *dev_status, void *c
  */
 spx_status_t spx_debug_warp_wait_expiry(int32_t *report, int32_t *dev_status, void *cuda_stream);
 
+/* The same for the wait of the attention of prompts and shared prefixes. */
+spx_status_t spx_debug_prompt_wait_expiry(int32_t *report, int32_t *dev_status, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

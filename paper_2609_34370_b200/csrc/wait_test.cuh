@@ -6,6 +6,7 @@
 #include "attn_e4m3.cuh"
 #include "attn_tc.cuh"
 #include "lm_head.cuh"
+#include "prompt_tc.cuh"
 #include "sampler.cuh"
 
 namespace spx {
@@ -49,13 +50,13 @@ __global__ void __launch_bounds__(128) wait_expiry_kernel(int32_t *report, int32
   }
 }
 
-// The warp-wide wait of the kernel over 8-bit pools, which hands no outcome back: two warps wait on a barrier each, then
-// each on another one.  report[w], report[2 + w]: clock cycles warp w spent in its first and second wait; report[4]: the CTA's
+// The warp-wide waits that hand no outcome back: two warps wait on a barrier each, then each on another one.
+// report[w], report[2 + w]: clock cycles warp w spent in its first and second wait; report[4]: the CTA's
 // abort flag; report[5]: how many of the four waits were satisfied (must be none).
-__global__ void __launch_bounds__(64) warp_wait_expiry_kernel(int32_t *report, int32_t *dev_status) {
-  __shared__ E8Barriers bars;
+template <typename Bars, typename Wait>
+__device__ __forceinline__ void two_warps_wait(Bars &bars, uint64_t *barriers, Wait wait, int32_t *report, int32_t *dev_status) {
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 4; ++i) tc::mbar_init(&bars.s_full[i], 1);
+    for (int i = 0; i < 4; ++i) tc::mbar_init(&barriers[i], 1);
     bars.abort = 0;
     bars.dev_status = dev_status;
     report[5] = 0;
@@ -64,17 +65,29 @@ __global__ void __launch_bounds__(64) warp_wait_expiry_kernel(int32_t *report, i
   __syncthreads();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = 0; i < 2; ++i) {
-    const uint32_t bar = tc::smem_u32(&bars.s_full[2 * i + warp]);
+    uint64_t *bar = &barriers[2 * i + warp];
     const long long t0 = clock64();
-    e8::warp_wait(bar, 0, &bars);
+    wait(bar);
     if (lane == 0) {
       report[2 * i + warp] = (int32_t)min(clock64() - t0, (long long)0x7fffffff);
-      if (e8::try_wait(bar, 0)) atomicAdd(report + 5, 1);
+      if (e8::try_wait(tc::smem_u32(bar), 0)) atomicAdd(report + 5, 1);
     }
     __syncwarp();
   }
   __syncthreads();
   if (threadIdx.x == 0) report[4] = bars.abort;
+}
+
+// that of the attention over 8-bit pools
+__global__ void __launch_bounds__(64) warp_wait_expiry_kernel(int32_t *report, int32_t *dev_status) {
+  __shared__ E8Barriers bars;
+  two_warps_wait(bars, bars.s_full, [&](uint64_t *bar) { e8::warp_wait(tc::smem_u32(bar), 0, &bars); }, report, dev_status);
+}
+
+// that of the attention of prompts and shared prefixes
+__global__ void __launch_bounds__(64) prompt_wait_expiry_kernel(int32_t *report, int32_t *dev_status) {
+  __shared__ PtBars bars;
+  two_warps_wait(bars, &bars.s_full[0][0], [&](uint64_t *bar) { pt::wait(bar, 0, &bars); }, report, dev_status);
 }
 
 }  // namespace spx
