@@ -503,7 +503,8 @@ prompt_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
         for (int v = 0; v < 2; ++v) {
           const uint32_t at = 2 * n_tile + v, rs = at % Cfg::kRawSlots, slot = at % Cfg::kSlots;
           const uint32_t bits = __float_as_uint(v ? vs : ks);
-          const float mul = __uint_as_float((bits & 0x7f800000u) ? bits & 0xff800000u : bits);
+          const uint32_t exponent = bits & 0x7f800000u;    // (a scale below the smallest normal, or not finite, is taken as it is)
+          const float mul = __uint_as_float(exponent != 0 && exponent != 0x7f800000u ? bits & 0xff800000u : bits);
           const uint64_t mul2_ = pair(mul, mul);
           wait(&bars->raw_full[rs], at / Cfg::kRawSlots, bars);
           wait(&bars->kv_empty[slot], at / Cfg::kSlots ^ 1, bars);
