@@ -23,7 +23,7 @@ constexpr int kPromptBuckets = 1024;       // lengths the entries are sorted by 
 struct PromptHeader {
   int32_t n_units;       // units of work: entries times kv heads
   int32_t counter;       // next unit of work
-  int32_t n_join;        // items in pieces (of plans whose whole items go to the output)
+  int32_t n_join;        // items in pieces (prompts)
   int32_t any_bad;       // some request's rows are to be voided
 };
 
@@ -82,7 +82,7 @@ struct PromptParams {
   int32_t *unit_bad;                  // [units]
   int32_t *item_tiles;                // [max_items]
   PromptEntry *entries;               // [max_items + max_pieces]
-  PromptJoin *join;                   // [max_pieces]
+  PromptJoin *join;                   // prompts: [max_pieces]
   int2 *item_part;                    // prefixes: [max_items] (first slot, pieces)
   int32_t max_items;
   int32_t max_pieces;                 // pieces that items are cut into; times Hkv slots, in front of those of a prefix plan's whole items
@@ -265,8 +265,11 @@ __device__ __forceinline__ void prompt_plan_block(const PromptParams &p) {
     const int tiles = i < NI ? p.item_tiles[i] : 0, k = i < NI ? pieces_of(tiles, piece_of_all) : 0;
     const int64_t slot = scan_1024(k > 1 ? k : 0, s_scratch, total) + slots;
     slots += total;
-    const int64_t at_join = scan_1024(k > 1 ? 1 : 0, s_scratch, total) + joins;
-    joins += total;
+    int64_t at_join = 0;
+    if (!p.groups) {   // (those of a prefix are joined with the requests' own tokens, item by item)
+      at_join = scan_1024(k > 1 ? 1 : 0, s_scratch, total) + joins;
+      joins += total;
+    }
     if (i >= NI) continue;
     PromptEntry e;
     const int u = last_at_most(p.unit_item0, p.units, i);
@@ -285,8 +288,9 @@ __device__ __forceinline__ void prompt_plan_block(const PromptParams &p) {
       e.slot = k > 1 || p.groups ? first + c * p.Hkv : -1;
       p.entries[at] = e;
     }
-    if (p.groups) p.item_part[i] = make_int2(first, k);
-    if (k > 1) {
+    if (p.groups) {
+      p.item_part[i] = make_int2(first, k);
+    } else if (k > 1) {
       PromptJoin j;
       j.unit = u; j.q0 = e.q0; j.row0 = e.row0; j.rows = e.rows; j.first = first; j.pieces = k; j.pad[0] = j.pad[1] = 0;
       p.join[at_join] = j;

@@ -201,8 +201,9 @@ static PromptWs prompt_ws_layout(const spx_attn_args_t *a) {
   w.unit_item0 = take(4 * ((size_t)w.units + 1)); w.unit_bad = take(4 * (size_t)w.units);
   w.item_tiles = take(4 * (size_t)items);
   w.entries = take(sizeof(PromptEntry) * (size_t)(items + w.max_pieces));
-  w.join = take(sizeof(PromptJoin) * (size_t)w.max_pieces);
-  if (prefixes) {
+  if (!prefixes) {
+    w.join = take(sizeof(PromptJoin) * (size_t)w.max_pieces);
+  } else {
     w.item_part = take(sizeof(int2) * (size_t)items);
     w.req_group = take(4 * (size_t)a->batch); w.group_tiles = take(4 * (size_t)w.units); w.req_flag = take(4 * (size_t)a->batch);
   }
