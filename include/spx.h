@@ -120,7 +120,10 @@ typedef enum { SPX_CACHE_KV_DTYPE = 0, SPX_CACHE_E4M3 = 1 } spx_cache_format_t;
  * whose block-table row differs from its group's first within those tiles sets SPX_DEV_BAD_PAGE, one with L_r - m_r below
  * them (the new positions belong to no prefix) SPX_DEV_BAD_LEN; both get the sentinel outputs, and so do all requests of a
  * group with a page id out of range in its prefix.  prefix_lens below zero count as zero.  (Two more kernels and partial results for
- * every request: 64 requests of 6 rows, 32/8 heads of 128, gain from some 1300 shared tokens on and lose below.)  The workspace is larger with groups: size it with num_groups set.
+ * every request.  64 requests of 6 rows, 32/8 heads of 128, gain from some 1300 shared tokens on and lose below: attention 70 us without
+ * groups, 94 with, behind 512 tokens, 203 and 111 behind 4096; over 8-bit pools from some 2900; the whole step from some 1600.)  The workspace
+ * is larger with groups, by partial results of 256 rows of fp32 for each group and kv head, however few rows the group has (128 KB at head_dim
+ * 128; in fp32 arithmetic 64 rows): size it with num_groups set.
  */
 #define SPX_PREFIX_TILE 128
 typedef struct {
@@ -265,7 +268,9 @@ spx_status_t spx_prompt_attention(const spx_attn_args_t *args, void *ws, size_t 
  * block_table[r][t/page_size], slot t%page_size (seq_lens already counts the new positions).  A request may bring any number
  * >= 1 of rows (a prompt as well as a step).
  * Values are copied bit for bit; no other slot is touched.  Requests with an invalid length or
- * page id set SPX_DEV_BAD_LEN / SPX_DEV_BAD_PAGE and are skipped.  Pools and strides as in
+ * page id set SPX_DEV_BAD_LEN / SPX_DEV_BAD_PAGE and are skipped, the others enter the cache.  (Where q_indptr
+ * descends somewhere rows of valid requests may stay out: beside 8-bit pools any, else, of more than 1024 requests, those past a
+ * request's 16th.)  Pools and strides as in
  * spx_attn_args_t; head_dim * element size must be a multiple of 16 bytes.
  *
  * Optional rotary embedding on the way (the paper does not discuss positional encoding; this is
@@ -324,7 +329,7 @@ typedef struct {
   int64_t kv_stride_page, kv_stride_head, kv_stride_token;
   const int32_t *block_table;         /* [B, max_pages_per_req]                               */
   const int32_t *seq_lens;            /* [B], counts the new positions                        */
-  const int32_t *q_indptr;            /* [B+1]                                                */
+  const int32_t *q_indptr;            /* [B+1], q_indptr[0] = 0, non-decreasing               */
   float rope_base;                    /* 0: plain copy; > 0: rotary base (e.g. 10000, 500000) */
   int32_t num_q_heads;                /* heads of q_rows (ignored when q_rows is NULL)        */
   void *q_rows;                       /* optional, rotated in place; NULL: none               */

@@ -12,8 +12,8 @@
 //                   and warps 12-15 turn the codes into bf16 tiles.
 // Tensor memory is full: two score buffers of 128 columns and two outputs of D.
 //
-// Two prompts of 8192 tokens, 32/8 heads of 128: 907 us (1.21 PFLOP/s), 1057 where the clock falls under the load; 24 of up to 2000 tokens 283;
-// six of up to 4000 over 8-bit pools 480.  No unit alone bounds it (MMA pipe 53 % busy, exponentials 50 %), but the chain between them.
+// Two prompts of 8192 tokens, 32/8 heads of 128: 907 us (1.21 PFLOP/s), 1064 on boards whose clock falls under the load; 24 of up to 2000 tokens 283
+// to 325; six of up to 4000 over 8-bit pools 480 to 500.  No unit alone bounds it (MMA pipe 53 % busy, exponentials 50 %), but the chain between them.
 //
 // The running maximum of a row is a reference that moves only when weights under it grow past 2^8 or so (the output
 // is then rescaled by the row's own thread).  Weights are rounded to bf16 (half a step of 2^-8 each, the type V has to be multiplied in); their sum is
