@@ -121,7 +121,7 @@ __device__ __forceinline__ void rope_vectors(uint4 &lo, uint4 &hi, const double2
 // batch + (q_indptr[r + 1] >> log2_block), so that no prefix sums are needed.  Blocks that are nobody's leave at once.  The angles are worked out once a
 // step and shared by its heads.
 // Pure copy and rotation: bound by launch latency at verify-step sizes (a few MB), by HBM beyond that.
-// kRope: with a rotary base (without, a kernel of fewer registers).  Eight rows a step, three blocks per SM: five prompts with images 38 us
+// kRope: with a rotary base (without, a kernel of fewer registers).  Eight rows a step, three blocks per SM: five prompts with images 39 us
 // (16 rows, two vectors a thread in flight, four blocks: slower each).
 template <bool kRope, typename Axes>
 __global__ void __launch_bounds__(kAppendThreads, kRope ? 3 : 4)

@@ -186,7 +186,7 @@ __device__ __forceinline__ void prompt_plan_block(const PromptParams &p) {
     n_items += total;
     if (u < p.units) p.unit_item0[u] = (int)min(off, (int64_t)p.max_items);
   }
-  if (n_items > p.max_items) n_items = p.max_items;   // (cannot be: the units' rows do not overlap)
+  if (n_items > p.max_items) n_items = p.max_items;   // (only where q_indptr, or the bounds of groups, descend somewhere)
   if (tid == 0) p.unit_item0[p.units] = (int)n_items;
   __syncthreads();
   const int NI = (int)n_items;
